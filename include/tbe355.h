@@ -285,6 +285,31 @@ tbe_status tbe_calibration_gather(tbe_handle* h, void* buf, size_t buf_bytes, si
                                   int32_t slice_bytes, int64_t gathers, int32_t write_back, void* sink,
                                   size_t sink_bytes, void* hip_stream);
 
+/* Layer norm over the columns of a matrix, and its gradients (what the rows of a non-pooled lookup go through before a model uses them;
+ * the paper leaves the model above the lookup open).
+ *   mean[r] = 1/cols sum_j x[r,j];  rstd[r] = 1 / sqrt(1/cols sum_j (x[r,j] - mean[r])^2 + eps);
+ *   y[r,j] = (x[r,j] - mean[r]) * rstd[r] * weight[j] + bias[j]
+ * and, with h = (x - mean) * rstd and g = dy * weight,
+ *   dx[r,j] = rstd[r] * (g[r,j] - 1/cols sum_i g[r,i] - h[r,j] * 1/cols sum_i g[r,i] h[r,i]),
+ *   dweight[j] = sum_r dy[r,j] h[r,j],  dbias[j] = sum_r dy[r,j].
+ *   x, y, dy, dx   DEVICE, `rows` rows of `cols` elements of `dtype`, consecutive rows *_stride elements apart (>= cols); any base
+ *                  address that is a multiple of the element's size.  y may be x, dx may be dy or x, with equal strides; otherwise
+ *                  they share no byte with an input
+ *   weight, bias   DEVICE, cols elements of param_dtype, or NULL (1 and 0);  dweight, dbias likewise, each or both NULL: not wanted
+ *   mean, rstd     DEVICE float [rows]; the forward writes them unless NULL, the backward reads them
+ *   workspace      DEVICE, 256-byte aligned, >= tbe_layer_norm_workspace_bytes(h, rows, cols); may be NULL where neither dweight nor
+ *                  dbias is wanted
+ * 0 <= rows < 2^31 (no row: dweight and dbias become zero), 1 <= cols <= 8192, eps finite and >= 0.  Sums are in fp32, each result is
+ * rounded once, to nearest even; the order of the additions is fixed (no atomics).  The handle gives the timing record. */
+tbe_status tbe_layer_norm(const tbe_handle* h, const void* x, int64_t x_stride, tbe_io_dtype dtype, int64_t rows, int32_t cols,
+                          const void* weight, const void* bias, tbe_io_dtype param_dtype, float eps, void* y, int64_t y_stride,
+                          float* mean, float* rstd, void* hip_stream);
+tbe_status tbe_layer_norm_workspace_bytes(const tbe_handle* h, int64_t rows, int32_t cols, size_t* bytes);
+tbe_status tbe_layer_norm_backward(const tbe_handle* h, const void* dy, int64_t dy_stride, const void* x, int64_t x_stride,
+                                   tbe_io_dtype dtype, int64_t rows, int32_t cols, const void* weight, tbe_io_dtype param_dtype,
+                                   const float* mean, const float* rstd, void* dx, int64_t dx_stride, void* dweight, void* dbias,
+                                   void* workspace, size_t workspace_bytes, void* hip_stream);
+
 const char* tbe_status_string(tbe_status s);
 
 /* "tbe355 gfx950 <digest>": the digest names the sources and build settings this library was compiled from (twelve

@@ -30,7 +30,8 @@ EXPORTS = ["tbe_create", "tbe_destroy", "tbe_workspace_bytes", "tbe_forward", "t
            "tbe_forward_ex", "tbe_backward_rowwise_adagrad_ex", "tbe_backward_rowwise_adagrad_static", "tbe_backward_prepare",
            "tbe_backward_apply_rowwise_adagrad", "tbe_backward_apply_sgd", "tbe_backward_sgd", "tbe_replica_mean", "tbe_lookup_seq",
            "tbe_backward_seq_rowwise_adagrad", "tbe_debug_sorted", "tbe_debug_hot_rows", "tbe_debug_forward_kernels", "tbe_poll_index_error", "tbe_set_tunable", "tbe_timing_enable",
-           "tbe_timing_count", "tbe_timing_read", "tbe_calibration_copy", "tbe_calibration_gather", "tbe_status_string", "tbe_build_info"]
+           "tbe_timing_count", "tbe_timing_read", "tbe_calibration_copy", "tbe_calibration_gather", "tbe_status_string", "tbe_build_info",
+           "tbe_layer_norm", "tbe_layer_norm_workspace_bytes", "tbe_layer_norm_backward"]
 
 
 class TbeError(RuntimeError):
@@ -113,6 +114,13 @@ def load_library():
     L.tbe_calibration_gather.restype = ctypes.c_int
     L.tbe_calibration_gather.argtypes = [vp, vp, ctypes.c_size_t, ctypes.c_size_t, i32, i32, i64, i32, vp,
                                          ctypes.c_size_t, vp]
+    L.tbe_layer_norm.restype = ctypes.c_int
+    L.tbe_layer_norm.argtypes = [vp, vp, i64, ctypes.c_int, i64, i32, vp, vp, ctypes.c_int, f32, vp, i64, vp, vp, vp]
+    L.tbe_layer_norm_workspace_bytes.restype = ctypes.c_int
+    L.tbe_layer_norm_workspace_bytes.argtypes = [vp, i64, i32, ctypes.POINTER(ctypes.c_size_t)]
+    L.tbe_layer_norm_backward.restype = ctypes.c_int
+    L.tbe_layer_norm_backward.argtypes = [vp, vp, i64, vp, i64, ctypes.c_int, i64, i32, vp, ctypes.c_int, vp, vp, vp, i64, vp, vp, vp,
+                                          ctypes.c_size_t, vp]
     L.tbe_build_info.restype = ctypes.c_char_p
     L.tbe_build_info.argtypes = []
     L.tbe_status_string.restype = ctypes.c_char_p
@@ -148,6 +156,30 @@ def _dev_ptr(t: Optional[torch.Tensor], dtype: torch.dtype, what: str) -> Option
     if not t.is_contiguous():
         raise ValueError(f"{what} must be contiguous")
     return t.data_ptr()
+
+
+def _rows_ptr(t: torch.Tensor, like: Optional[torch.Tensor], what: str) -> int:
+    """A device matrix whose last axis is contiguous; same type and shape as `like`."""
+    if not t.is_cuda:
+        raise ValueError(f"{what} must be a device tensor")
+    if t.dtype not in _IO:
+        raise TypeError(f"{what} must be float32, float16 or bfloat16, got {t.dtype}")
+    if like is not None and (t.dtype != like.dtype or t.shape != like.shape):
+        raise ValueError(f"{what} must be {like.dtype} {tuple(like.shape)}, got {t.dtype} {tuple(t.shape)}")
+    if t.shape[-1] > 1 and t.numel() and t.stride(-1) != 1:
+        raise ValueError(f"the last axis of {what} must be contiguous")
+    return t.data_ptr()
+
+
+def _param_ptr(t: Optional[torch.Tensor], n: int, dtype: Optional[torch.dtype], what: str) -> Optional[int]:
+    """A parameter vector or table of n elements, or None."""
+    if t is None:
+        return None
+    if t.dtype not in _IO:
+        raise TypeError(f"{what} must be float32, float16 or bfloat16, got {t.dtype}")
+    if t.numel() != n:
+        raise ValueError(f"{what} must have {n} elements, got {t.numel()}")
+    return _dev_ptr(t, dtype or t.dtype, what)
 
 
 def _index_dtype(indices: torch.Tensor, offsets: torch.Tensor) -> int:
@@ -423,6 +455,70 @@ class TBE:
         st = self._lib.tbe_replica_mean(self._h, ptrs, len(replicas), first.numel(),
                                         F32 if first.dtype == torch.float32 else F16, _stream_ptr(stream))
         _check(st, "tbe_replica_mean")
+
+    # ---- tbe_layer_norm
+    def layer_norm(self, x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, *,
+                   eps: float = 1e-5, out: Optional[torch.Tensor] = None, mean: Optional[torch.Tensor] = None,
+                   rstd: Optional[torch.Tensor] = None, stats: bool = True, stream: Optional[torch.cuda.Stream] = None
+                   ) -> Tuple[torch.Tensor, Optional[torch.Tensor], Optional[torch.Tensor]]:
+        """x: [rows, cols] (float32, float16 or bfloat16; rows may be apart); weight, bias: [cols] of one type.  Returns (out, mean,
+        rstd); mean and rstd, float32 [rows], are what the backward needs - stats=False leaves out those that are not given."""
+        if x.dim() != 2:
+            raise ValueError("x must have two axes")
+        rows, cols = x.shape
+        params = weight if weight is not None else bias
+        if weight is not None and bias is not None and weight.dtype != bias.dtype:
+            raise TypeError(f"weight and bias must be of one type, got {weight.dtype} / {bias.dtype}")
+        out = torch.empty(rows, cols, dtype=x.dtype, device=x.device) if out is None else out
+        if stats and mean is None:
+            mean = torch.empty(rows, dtype=torch.float32, device=x.device)
+        if stats and rstd is None:
+            rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
+        st = self._lib.tbe_layer_norm(self._h, _rows_ptr(x, None, "x"), x.stride(0), _IO[x.dtype], rows, cols,
+                                      _param_ptr(weight, cols, None, "weight"), _param_ptr(bias, cols, None, "bias"),
+                                      IO_F32 if params is None else _IO[params.dtype], float(eps), _rows_ptr(out, x, "out"), out.stride(0),
+                                      _param_ptr(mean, rows, torch.float32, "mean"), _param_ptr(rstd, rows, torch.float32, "rstd"),
+                                      _stream_ptr(stream))
+        _check(st, "tbe_layer_norm")
+        return out, mean, rstd
+
+    # ---- tbe_layer_norm_workspace_bytes
+    def layer_norm_workspace_bytes(self, rows: int, cols: int) -> int:
+        n = ctypes.c_size_t()
+        _check(self._lib.tbe_layer_norm_workspace_bytes(self._h, int(rows), int(cols), ctypes.byref(n)), "tbe_layer_norm_workspace_bytes")
+        return int(n.value)
+
+    def alloc_layer_norm_workspace(self, rows: int, cols: int, device="cuda") -> torch.Tensor:
+        return torch.empty(self.layer_norm_workspace_bytes(rows, cols), dtype=torch.uint8, device=device)
+
+    # ---- tbe_layer_norm_backward
+    def layer_norm_backward(self, grad_out: torch.Tensor, x: torch.Tensor, weight: Optional[torch.Tensor], mean: torch.Tensor,
+                            rstd: torch.Tensor, workspace: Optional[torch.Tensor], *, grad_x: Optional[torch.Tensor] = None,
+                            grad_weight: Optional[torch.Tensor] = None, grad_bias: Optional[torch.Tensor] = None, params: bool = True,
+                            param_dtype: Optional[torch.dtype] = None, stream: Optional[torch.cuda.Stream] = None
+                            ) -> Tuple[torch.Tensor, Optional[torch.Tensor], Optional[torch.Tensor]]:
+        """Returns (grad_x, grad_weight, grad_bias); the last two, of the weight's type (param_dtype, or float32, where there is no
+        weight), are made unless params=False leaves out those that are not given."""
+        if x.dim() != 2:
+            raise ValueError("x must have two axes")
+        rows, cols = x.shape
+        given = [t.dtype for t in (weight, grad_weight, grad_bias) if t is not None]
+        pt = given[0] if given else (param_dtype or torch.float32)
+        if pt not in _IO or any(t != pt for t in given) or (param_dtype or pt) != pt:
+            raise TypeError(f"weight and its gradients must be of one type, got {given}")
+        grad_x = torch.empty(rows, cols, dtype=x.dtype, device=x.device) if grad_x is None else grad_x
+        if params and grad_weight is None:
+            grad_weight = torch.empty(cols, dtype=pt, device=x.device)
+        if params and grad_bias is None:
+            grad_bias = torch.empty(cols, dtype=pt, device=x.device)
+        st = self._lib.tbe_layer_norm_backward(
+            self._h, _rows_ptr(grad_out, x, "grad_out"), grad_out.stride(0), _rows_ptr(x, None, "x"), x.stride(0), _IO[x.dtype], rows, cols,
+            _param_ptr(weight, cols, None, "weight"), _IO[pt], _param_ptr(mean, rows, torch.float32, "mean"),
+            _param_ptr(rstd, rows, torch.float32, "rstd"), _rows_ptr(grad_x, x, "grad_x"), grad_x.stride(0),
+            _param_ptr(grad_weight, cols, pt, "grad_weight"), _param_ptr(grad_bias, cols, pt, "grad_bias"),
+            _dev_ptr(workspace, torch.uint8, "workspace"), 0 if workspace is None else int(workspace.numel()), _stream_ptr(stream))
+        _check(st, "tbe_layer_norm_backward")
+        return grad_x, grad_weight, grad_bias
 
     # ---- tbe_debug_sorted
     def debug_sorted(self, workspace: torch.Tensor, B: int, nnz: int) -> Dict[str, torch.Tensor]:

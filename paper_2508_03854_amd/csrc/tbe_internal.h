@@ -156,4 +156,13 @@ hipError_t launch_segment_update(const tbe_handle* h, const Workspace& w, char* 
 hipError_t launch_lookup_seq(const tbe_handle* h, const void* tables, const void* indices, const void* offsets, int idx32,
                              int64_t nnz, void* out, int out_io, int64_t out_elems, hipStream_t s);
 
+// layer norm over rows of n elements (tbe_norm.hip); io, param_io: 0 float, 1 binary16, 2 bfloat16
+constexpr int kNormMaxCols = 8192;
+size_t layer_norm_workspace(int64_t rows, int n);
+hipError_t launch_layer_norm(const tbe_handle* h, const void* x, int64_t x_stride, int io, int64_t rows, int n, const void* weight,
+                             const void* bias, int param_io, float eps, void* y, int64_t y_stride, float* mean, float* rstd, hipStream_t s);
+hipError_t launch_layer_norm_backward(const tbe_handle* h, const void* dy, int64_t dy_stride, const void* x, int64_t x_stride, int io,
+                                      int64_t rows, int n, const void* weight, int param_io, const float* mean, const float* rstd,
+                                      void* dx, int64_t dx_stride, void* dw, void* db, void* workspace, hipStream_t s);
+
 }  // namespace tbe
