@@ -310,6 +310,59 @@ tbe_status tbe_layer_norm_backward(const tbe_handle* h, const void* dy, int64_t 
                                    const float* mean, const float* rstd, void* dx, int64_t dx_stride, void* dweight, void* dbias,
                                    void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/* Attention over packed sequences (what a model does with the events of a sequence; the paper leaves it open).  Sequence s has queries
+ * q_offsets[s] .. q_offsets[s+1]-1 and keys k_offsets[s] .. (its first k_lengths[s] ones where k_lengths is given: a cache with room left).
+ * Its last query stands where its last key stands: query i of nq has place p_i = nk - nq + i among the keys.
+ *   x_ij = scale * q_i . k_j + bias[head, bucket_map[max_distance + clamp(p_i - j, -max_distance, max_distance)]],
+ *   over all keys j of the sequence, or with `causal` those with j <= p_i;
+ *   lse_i = log sum_j exp x_ij;  out_i = sum_j exp(x_ij - lse_i) v_j;
+ * a query that sees no key gets zeros, and lse -infinity.  So training and whole prompts have q_offsets == k_offsets, a new event per user
+ * has one query per sequence, and a cache is extended by a few.  Head h reads key head h / (heads / kv_heads).  Gradients, from dout:
+ *   P = exp(x - lse), dS_ij = P_ij (dout_i . v_j - dout_i . out_i),  dq_i = scale sum_j dS_ij k_j,
+ *   dk_j = scale sum_i dS_ij q_i,  dv_j = sum_i P_ij dout_i  (over all heads that read the key head),
+ *   dbias[head, b] = sum of dS over the pairs of bucket b.
+ * Rows of dk and dv that no query saw, or that are a cache's room, become zero.
+ *   q, k, v, out and gradients   DEVICE, [rows][heads or kv_heads][head_dim] of dtype: consecutive rows row_stride, consecutive heads
+ *             head_stride elements apart, so that they may be column blocks of one matrix.  16-byte aligned, strides multiples of 16
+ *             bytes, 0 <= row_stride < 2^22 (a result's at least head_dim); head_dim <= 128, a multiple of 8 (4 for TBE_IO_F32).  Results
+ *             share no byte with each other or with what is read
+ *   q_offsets, k_offsets   DEVICE, sequences + 1 of index_dtype, ascending from 0 to q_rows resp. k_rows;  k_lengths  DEVICE,
+ *             `sequences` of the same type, or NULL.  A sequence whose numbers do not fit is left out - rows of the results that no
+ *             other sequence claims keep their contents; offsets that do not ascend may cost other sequences, too - and is reported
+ *             by tbe_poll_index_error; nothing outside the buffers is touched
+ *   bias      DEVICE, [heads][buckets] of bias_dtype, or NULL: none.  -infinity hides a bucket; finite values beyond +-1e30 count as that
+ *   bucket_map  DEVICE int32 [2 max_distance + 1], 0 <= max_distance <= 1024; a number outside [0, buckets) counts as no bias and is
+ *             reported likewise
+ *   lse       DEVICE float [heads][q_rows]; the forward writes it unless NULL, the backward reads it
+ * 0 <= q_rows, k_rows < 2^31, 1 <= sequences < 2^24, 1 <= kv_heads <= heads <= 1024 with heads a multiple of kv_heads,
+ * 1 <= buckets <= 1024.  Scores, softmax and sums are in fp32; probabilities and dS are rounded once to dtype where they are multiplied by
+ * v, k, q or dout (fp32: not at all), results once when stored.  The order of all additions is fixed: results do not depend on
+ * timing.  A value that is not finite reaches those results of the forward that see it, and
+ * of the backward results of its sequence.  The handle
+ * gives the timing record and the error flag. */
+typedef struct {
+    void* data;
+    int64_t row_stride, head_stride; /* in elements */
+} tbe_rows;
+typedef struct {
+    int32_t sequences, heads, kv_heads, head_dim;
+    int64_t q_rows, k_rows;
+    tbe_io_dtype dtype;
+    tbe_index_dtype index_dtype;
+    tbe_rows q, k, v;
+    const void *q_offsets, *k_offsets, *k_lengths;
+    int32_t causal;
+    float scale; /* finite */
+    const void* bias;
+    const int32_t* bucket_map;
+    tbe_io_dtype bias_dtype;
+    int32_t buckets, max_distance;
+} tbe_attention_args;
+/* Workspace for calls with these sizes (sequences .. k_rows; buckets 0: without bias; no pointer is read). */
+tbe_status tbe_attention_workspace_bytes(const tbe_handle* h, const tbe_attention_args* args, int backward, size_t* bytes);
+tbe_status tbe_attention(const tbe_handle* h, const tbe_attention_args* args, tbe_rows out, float* lse, void* workspace,
+                         size_t workspace_bytes, void* hip_stream);
+
 const char* tbe_status_string(tbe_status s);
 
 /* "tbe355 gfx950 <digest>": the digest names the sources and build settings this library was compiled from (twelve

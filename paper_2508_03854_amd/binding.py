@@ -31,13 +31,27 @@ EXPORTS = ["tbe_create", "tbe_destroy", "tbe_workspace_bytes", "tbe_forward", "t
            "tbe_backward_apply_rowwise_adagrad", "tbe_backward_apply_sgd", "tbe_backward_sgd", "tbe_replica_mean", "tbe_lookup_seq",
            "tbe_backward_seq_rowwise_adagrad", "tbe_debug_sorted", "tbe_debug_hot_rows", "tbe_debug_forward_kernels", "tbe_poll_index_error", "tbe_set_tunable", "tbe_timing_enable",
            "tbe_timing_count", "tbe_timing_read", "tbe_calibration_copy", "tbe_calibration_gather", "tbe_status_string", "tbe_build_info",
-           "tbe_layer_norm", "tbe_layer_norm_workspace_bytes", "tbe_layer_norm_backward"]
+           "tbe_layer_norm", "tbe_layer_norm_workspace_bytes", "tbe_layer_norm_backward", "tbe_attention_workspace_bytes", "tbe_attention"]
 
 
 class TbeError(RuntimeError):
     def __init__(self, status: int, what: str):
         super().__init__(f"{what}: status {status} ({_status_string(status)})")
         self.status = status
+
+
+class Rows(ctypes.Structure):
+    """tbe_rows"""
+    _fields_ = [("data", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class AttentionArgs(ctypes.Structure):
+    """tbe_attention_args"""
+    _fields_ = [("sequences", ctypes.c_int32), ("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("q_rows", ctypes.c_int64), ("k_rows", ctypes.c_int64), ("dtype", ctypes.c_int), ("index_dtype", ctypes.c_int),
+                ("q", Rows), ("k", Rows), ("v", Rows), ("q_offsets", ctypes.c_void_p), ("k_offsets", ctypes.c_void_p),
+                ("k_lengths", ctypes.c_void_p), ("causal", ctypes.c_int32), ("scale", ctypes.c_float), ("bias", ctypes.c_void_p),
+                ("bucket_map", ctypes.c_void_p), ("bias_dtype", ctypes.c_int), ("buckets", ctypes.c_int32), ("max_distance", ctypes.c_int32)]
 
 
 _lib = None
@@ -121,6 +135,10 @@ def load_library():
     L.tbe_layer_norm_backward.restype = ctypes.c_int
     L.tbe_layer_norm_backward.argtypes = [vp, vp, i64, vp, i64, ctypes.c_int, i64, i32, vp, ctypes.c_int, vp, vp, vp, i64, vp, vp, vp,
                                           ctypes.c_size_t, vp]
+    L.tbe_attention_workspace_bytes.restype = ctypes.c_int
+    L.tbe_attention_workspace_bytes.argtypes = [vp, ctypes.POINTER(AttentionArgs), ctypes.c_int, ctypes.POINTER(ctypes.c_size_t)]
+    L.tbe_attention.restype = ctypes.c_int
+    L.tbe_attention.argtypes = [vp, ctypes.POINTER(AttentionArgs), Rows, vp, vp, ctypes.c_size_t, vp]
     L.tbe_build_info.restype = ctypes.c_char_p
     L.tbe_build_info.argtypes = []
     L.tbe_status_string.restype = ctypes.c_char_p
@@ -169,6 +187,13 @@ def _rows_ptr(t: torch.Tensor, like: Optional[torch.Tensor], what: str) -> int:
     if t.shape[-1] > 1 and t.numel() and t.stride(-1) != 1:
         raise ValueError(f"the last axis of {what} must be contiguous")
     return t.data_ptr()
+
+
+def _heads(t: torch.Tensor, like: Optional[torch.Tensor], what: str) -> Rows:
+    """A device matrix [rows, heads, head_dim] whose last axis is contiguous; same type and shape as `like`."""
+    if t.dim() != 3:
+        raise ValueError(f"{what} must have three axes: rows, heads, head_dim")
+    return Rows(_rows_ptr(t, like, what), t.stride(0), t.stride(1))
 
 
 def _param_ptr(t: Optional[torch.Tensor], n: int, dtype: Optional[torch.dtype], what: str) -> Optional[int]:
@@ -519,6 +544,66 @@ class TBE:
             _dev_ptr(workspace, torch.uint8, "workspace"), 0 if workspace is None else int(workspace.numel()), _stream_ptr(stream))
         _check(st, "tbe_layer_norm_backward")
         return grad_x, grad_weight, grad_bias
+
+    # ---- tbe_attention_workspace_bytes
+    def attention_workspace_bytes(self, sequences: int, q_rows: int, k_rows: int, heads: int, kv_heads: int, head_dim: int, *,
+                                  buckets: int = 0, backward: bool = False) -> int:
+        """For calls of these sizes, with a bias of `buckets` buckets (0: without), of any element type."""
+        dtype = IO_F32 if head_dim % 8 else IO_BF16
+        a = AttentionArgs(sequences=int(sequences), heads=int(heads), kv_heads=int(kv_heads), head_dim=int(head_dim), q_rows=int(q_rows),
+                          k_rows=int(k_rows), dtype=dtype, buckets=int(buckets))
+        n = ctypes.c_size_t()
+        _check(self._lib.tbe_attention_workspace_bytes(self._h, ctypes.byref(a), int(backward), ctypes.byref(n)),
+               "tbe_attention_workspace_bytes")
+        return int(n.value)
+
+    def alloc_attention_workspace(self, sequences: int, q_rows: int, k_rows: int, heads: int, kv_heads: int, head_dim: int, *,
+                                  buckets: int = 0, backward: bool = False, device="cuda") -> torch.Tensor:
+        return torch.empty(self.attention_workspace_bytes(sequences, q_rows, k_rows, heads, kv_heads, head_dim, buckets=buckets,
+                                                          backward=backward), dtype=torch.uint8, device=device)
+
+    def _attention_args(self, q, k, v, q_offsets, k_offsets, k_lengths, causal, scale, bias, bucket_map) -> AttentionArgs:
+        rows = [_heads(q, None, "q"), _heads(k, None, "k"), _heads(v, None, "v")]
+        if k.dtype != q.dtype or v.dtype != q.dtype or v.shape != k.shape or k.shape[2] != q.shape[2]:
+            raise ValueError("q, k and v must agree in type and head_dim, k and v in shape")
+        n = q_offsets.numel() - 1
+        if k_offsets.numel() != n + 1 or (k_lengths is not None and k_lengths.numel() != n):
+            raise ValueError("q_offsets and k_offsets must have one entry more than k_lengths")
+        idt = _index_dtype(q_offsets, k_offsets)
+        a = AttentionArgs(sequences=n, heads=q.shape[1], kv_heads=k.shape[1], head_dim=q.shape[2], q_rows=q.shape[0], k_rows=k.shape[0],
+                          dtype=_IO[q.dtype], index_dtype=idt, q=rows[0], k=rows[1], v=rows[2],
+                          q_offsets=_dev_ptr(q_offsets, q_offsets.dtype, "q_offsets"), k_offsets=_dev_ptr(k_offsets, q_offsets.dtype, "k_offsets"),
+                          k_lengths=_dev_ptr(k_lengths, q_offsets.dtype, "k_lengths"), causal=int(causal),
+                          scale=q.shape[2] ** -0.5 if scale is None else float(scale))
+        if (bias is None) != (bucket_map is None):
+            raise ValueError("bias and bucket_map belong together")
+        if bias is not None:
+            if bias.dim() != 2 or bias.shape[0] != q.shape[1] or bucket_map.dim() != 1 or bucket_map.numel() % 2 != 1:
+                raise ValueError("bias must be [heads, buckets] and bucket_map [2 * max_distance + 1]")
+            a.bias, a.bias_dtype = _param_ptr(bias, bias.numel(), None, "bias"), _IO[bias.dtype]
+            a.bucket_map, a.buckets, a.max_distance = _dev_ptr(bucket_map, torch.int32, "bucket_map"), bias.shape[1], bucket_map.numel() // 2
+        return a
+
+    # ---- tbe_attention
+    def attention(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_offsets: torch.Tensor, k_offsets: torch.Tensor,
+                  workspace: Optional[torch.Tensor], *, causal: bool = True, scale: Optional[float] = None,
+                  k_lengths: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, bucket_map: Optional[torch.Tensor] = None,
+                  out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, stats: bool = True,
+                  stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+        """q: [q_rows, heads, head_dim], k and v: [k_rows, kv_heads, head_dim] (float32, float16 or bfloat16; last axis contiguous,
+        column blocks of one matrix are fine); offsets: [sequences + 1], k_lengths: [sequences], int64 or int32; scale: head_dim ** -0.5
+        unless given; bias: [heads, buckets], bucket_map: int32 [2 * max_distance + 1].  Returns (out, lse), lse float32
+        [heads, q_rows]; stats=False: no lse unless it is given."""
+        a = self._attention_args(q, k, v, q_offsets, k_offsets, k_lengths, causal, scale, bias, bucket_map)
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
+        if stats and lse is None:
+            lse = torch.empty(q.shape[1], q.shape[0], dtype=torch.float32, device=q.device)
+        st = self._lib.tbe_attention(self._h, ctypes.byref(a), _heads(out, q, "out"),
+                                     _param_ptr(lse, q.shape[0] * q.shape[1], torch.float32, "lse"),
+                                     _dev_ptr(workspace, torch.uint8, "workspace"), 0 if workspace is None else int(workspace.numel()),
+                                     _stream_ptr(stream))
+        _check(st, "tbe_attention")
+        return out, lse
 
     # ---- tbe_debug_sorted
     def debug_sorted(self, workspace: torch.Tensor, B: int, nnz: int) -> Dict[str, torch.Tensor]:

@@ -1,0 +1,228 @@
+// What the attention kernels share: the sequences' places, tiles of rows in LDS, matrix products of 32 x 32 tiles.
+//
+// Lanes and tiles.  A product of the matrix cores leaves a 32 x 32 tile with one column per lane: lane l holds column l % 32 and, of the
+// 32 rows, those 8 i + 4 (l / 32) + e  (i, e < 4) in register 4 i + e.  The kernels put what a softmax runs over into the rows and what
+// it is one of into the columns, so that row maxima and sums are a lane's own, but for one exchange between the wavefront's halves,
+// and the tile of probabilities is, as it lies in the registers, an operand of the next product (fragment m: registers 8 m .. 8 m + 7
+// of a 16-bit type, 4 m .. 4 m + 3 of fp32).  The other operand's fragments then take their rows in the same order.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include "tbe_elems.h"
+#include "tbe_internal.h"
+
+namespace tbe {
+
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+
+// a value that all lanes hold, as a scalar
+__device__ __forceinline__ int uniform(const int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+constexpr int kTabMargin = 64;         // a tile that reaches into the table of distances reaches at most 63 beyond its ends
+constexpr int kTabBytes = 24 << 10;    // LDS for such tables
+
+// Sixteen zero bytes: what stands behind a sequence's end, or behind a row's, is read from here.
+extern __device__ const uint4 attn_zeros;
+
+template <typename T>
+struct Mma {   // 16-bit types: fragments of 8 elements a lane, 16 of the summed axis at a time
+    static constexpr int kE = 8, kK = 16;
+    static __device__ __forceinline__ f32x16_t mma(const uint4 a, const uint4 b, const f32x16_t c) {
+        if constexpr (__is_same(T, bf16_t))
+            return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+        else
+            return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
+    }
+    // registers 8 m .. 8 m + 7 of a tile as an operand; each is rounded once
+    static __device__ __forceinline__ uint4 pack(const f32x16_t& s, const int m) {
+        const T* const t = nullptr;
+        return make_uint4(pack2(t, s[8 * m], s[8 * m + 1]), pack2(t, s[8 * m + 2], s[8 * m + 3]), pack2(t, s[8 * m + 4], s[8 * m + 5]),
+                          pack2(t, s[8 * m + 6], s[8 * m + 7]));
+    }
+};
+template <>
+struct Mma<float> {   // four products of two of the summed axis each
+    static constexpr int kE = 4, kK = 8;
+    static __device__ __forceinline__ f32x16_t mma(const uint4 a, const uint4 b, f32x16_t c) {
+        c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.x), __uint_as_float(b.x), c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.y), __uint_as_float(b.y), c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.z), __uint_as_float(b.z), c, 0, 0, 0);
+        return __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.w), __uint_as_float(b.w), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ uint4 pack(const f32x16_t& s, const int m) {
+        return make_uint4(__float_as_uint(s[4 * m]), __float_as_uint(s[4 * m + 1]), __float_as_uint(s[4 * m + 2]), __float_as_uint(s[4 * m + 3]));
+    }
+};
+
+// A tile of rows of D elements in LDS, sixteen-byte chunks: chunk c of row r lies at place c ^ swizzle(r) of its row, so that neither
+// reading a column of chunks nor reading down the rows piles up on a few banks.  Rows arrive straight from memory; a wavefront's 64 chunks
+// land one behind the other, so it is the source that is permuted.
+template <typename T, int D>
+struct Tile {
+    static constexpr int kChunks = D * (int)sizeof(T) / 16;   // of a row: 4 to 32
+    static __device__ __forceinline__ int swizzle(const int r) { return kChunks == 4 ? (r >> 1) & 3 : r & (kChunks < 16 ? kChunks - 1 : 15); }
+    // fragment c of the tile's row r, along the row (the lanes' halves take alternate chunks)
+    static __device__ __forceinline__ uint4 along(const char* lds, const int r, const int c, const int half) {
+        return *reinterpret_cast<const uint4*>(lds + (r * kChunks + ((2 * c + half) ^ swizzle(r))) * 16);
+    }
+    // fragment m down the rows first + ..., column 32 t + l % 32: the rows that registers of fragment m stand for
+    static __device__ __forceinline__ uint4 down(const char* lds, const int first, const int m, const int t) {
+        const int l = lane_id(), half = l >> 5;
+        if constexpr (sizeof(T) == 2) {
+            // sixteen lanes read four rows of sixteen columns, and get a column of four rows each
+            typedef __attribute__((address_space(3))) s16x4_t* lds_ptr;
+            const int j = l & 15, c = 4 * t + 2 * ((l >> 4) & 1) + ((j & 3) >> 1), r = first + 16 * m + 4 * half + (j >> 2);
+            const char* const p = lds + (r * kChunks + (c ^ swizzle(r))) * 16 + (j & 1) * 8;
+            const char* const q = lds + ((r + 8) * kChunks + (c ^ swizzle(r + 8))) * 16 + (j & 1) * 8;
+            const uint2 a = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)p));
+            const uint2 b = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)q));
+            return make_uint4(a.x, a.y, b.x, b.y);
+        } else {
+            const int e = 32 * t + (l & 31), r = first + 8 * m + 4 * half;
+            uint32_t w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                w[i] = *reinterpret_cast<const uint32_t*>(lds + ((r + i) * kChunks + ((e >> 2) ^ swizzle(r + i))) * 16 + (e & 3) * 4);
+            return make_uint4(w[0], w[1], w[2], w[3]);
+        }
+    }
+    static __device__ __forceinline__ float element(const char* lds, const int r, const int e) {
+        constexpr int kE = 16 / (int)sizeof(T);
+        return elem_float(*reinterpret_cast<const T*>(lds + (r * kChunks + ((e / kE) ^ swizzle(r))) * 16 + (e % kE) * (int)sizeof(T)));
+    }
+    // ROWS rows from row j0 of a sequence on, of which there are `rows`, by WAVES wavefronts (this one is number w); complete after
+    // loads_done().  `stride`: bytes from row to row
+    template <int ROWS, int WAVES>
+    static __device__ __forceinline__ void fetch(char* lds, const char* base, const int64_t stride, const int j0, const int rows, const int dim, const int w) {
+        constexpr int kLoads = ROWS * kChunks / 64 / WAVES;
+        static_assert(kLoads * 64 * WAVES == ROWS * kChunks, "whole loads");
+        const bool inside = j0 + ROWS <= rows && dim == D;
+        const char* const from = base + (int64_t)j0 * stride;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int n = (w * kLoads + i) * 64 + lane_id(), r = n / kChunks, c = (n % kChunks) ^ swizzle(r);
+            const char* src = from + (uint32_t)(r * (uint32_t)stride + c * 16);
+            if (!inside && (j0 + r >= rows || c * 16 >= dim * (int)sizeof(T))) src = reinterpret_cast<const char*>(&attn_zeros);
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
+                                             (__attribute__((address_space(3))) void*)(lds + (w * kLoads + i) * 1024), 16, 0, 0);
+        }
+    }
+};
+// waits for this wavefront's loads (vmcnt 0, the other counters as they are); as a builtin, so that the compiler knows of it
+__device__ __forceinline__ void loads_done() {
+    __builtin_amdgcn_s_waitcnt(0x0F70);
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// x's value in the lane 32 further on (or back), combined with this lane's
+__device__ __forceinline__ float halves_max(const float x) {
+    const unsigned u = __float_as_uint(x);
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+// A matrix [rows][heads][dim]: bytes from row to row and from head to head.
+struct RowsView {
+    const char* p;
+    int64_t row, head;
+    __device__ __forceinline__ const char* at(const int64_t r, const int h) const { return p + r * row + h * head; }
+};
+
+struct AttnArgs {
+    RowsView q, k, v, o, dout, dq, dk, dv;
+    float* lse;               // [H][q_rows]
+    const float* delta;       // [H][q_rows]: the backward's row sums of dout * out
+    IdxView q_off, k_off, k_len;   // k_len.p may be null
+    int N, H, kv, group, dim, causal;
+    int64_t q_rows, k_rows;
+    float scale, scale2;      // scale2: |scale| log2(e); negative: scale < 0
+    int negative;
+    const void* bias;         // [H][buckets]
+    int bias_io, buckets, far;
+    const int32_t* map;
+    int32_t* err;
+    // how queries are shared out: a unit has `pack` heads of a group side by side and qpt queries of each per 32 columns
+    int pack, qpt, block, V, splits;   // block: queries of a unit; V: units of a head that the sequences may need; splits of the keys
+    float *part_o, *part_ml;
+    float* part_bias;
+};
+
+// Sequence of unit v of V = q_rows / block + N: sequence s owns units offsets[s] / block + s on, as many as it needs, and there is
+// always room (a sequence never needs more than its rows / block, rounded down, and one).  All lanes of a wavefront together, 64 offsets
+// at a time.
+__device__ __forceinline__ int find_sequence(const IdxView off, const int N, const uint32_t v, const uint32_t block) {
+    int lo = 0, hi = N;
+    while (hi - lo > 1) {
+        const int step = (hi - lo + 63) / 64, s = lo + lane_id() * step;
+        const bool before = s < hi && (uint32_t)off[s] / block + (uint32_t)s <= v;
+        const uint64_t m = __ballot(before);
+        const int k = m ? 63 - __builtin_clzll(m) : 0;
+        lo += k * step;
+        hi = hi < lo + step ? hi : lo + step;
+    }
+    return uniform(lo);
+}
+
+struct Sequence {
+    int64_t q0, k0;   // first rows
+    int nq, nk;       // queries, keys
+    int cap;          // rows of k and v that are the sequence's, filled or not
+};
+// The five numbers of a sequence, one in each of the first lanes: one trip to memory.
+__device__ __forceinline__ int64_t sequence_numbers(const AttnArgs& a, const int s) {
+    const int l = lane_id();
+    const IdxView& from = l < 2 ? a.q_off : (l < 4 || !a.k_len.p ? a.k_off : a.k_len);
+    return l < 5 ? from[s + (l < 4 ? l & 1 : 0)] : 0;
+}
+// false: they are not what they have to be (reported)
+__device__ __forceinline__ bool take_sequence(const AttnArgs& a, const int s, const int64_t mine, Sequence& q) {
+    const int64_t q0 = lane_i64(mine, 0), q1 = lane_i64(mine, 1), k0 = lane_i64(mine, 2), k1 = lane_i64(mine, 3);
+    const int64_t n = a.k_len.p ? lane_i64(mine, 4) : k1 - k0;
+    bool ok = q0 >= 0 && q0 <= q1 && q1 <= a.q_rows && k0 >= 0 && k0 <= k1 && k1 <= a.k_rows && n >= 0 && n <= k1 - k0;
+    if (s == 0) ok = ok && q0 == 0 && k0 == 0;
+    if (s == a.N - 1) ok = ok && q1 == a.q_rows && k1 == a.k_rows;
+    q.q0 = q0; q.k0 = k0;
+    q.nq = uniform((int)(q1 - q0)); q.nk = uniform((int)n); q.cap = uniform((int)(k1 - k0));
+    if (!ok && lane_id() == 0) *a.err = 1;
+    return ok;
+}
+// Offsets that do not ascend may keep the search from ever meeting the sequence that is wrong, so that unit n of the first head (there are
+// at least as many as sequences) looks at sequence n besides: `peek` is loaded early and judged when the unit is done.
+__device__ __forceinline__ void judge(const AttnArgs& a, const bool looks, const int n, const int64_t peek) {
+    Sequence q;
+    if (looks) (void)take_sequence(a, n, peek, q);
+}
+
+// The bias of a head by (key's place - query's place), as an exponent of 2: entry far + kTabMargin + (key - query), distances beyond
+// `far` like `far` itself.  A finite bias beyond +-1e30 counts as that (so that it stays finite here); a bucket outside the table
+// counts as no bias and is reported.
+__device__ __forceinline__ int tab_size(const int far) { return 2 * far + 1 + 2 * kTabMargin; }
+__device__ __forceinline__ void fill_bias(float* tab, const AttnArgs& a, const int head0, const int heads, const int threads) {
+    const int size = tab_size(a.far), used = a.causal ? a.far + kTabMargin + 1 : size;
+    for (int n = threadIdx.x; n < heads * used; n += threads) {
+        const int g = n / used, t = n - g * used;
+        int d = a.far + kTabMargin - t;   // query - key
+        d = d > a.far ? a.far : (d < -a.far ? -a.far : d);
+        const int b = a.map[d + a.far];
+        float x = 0.f;
+        if ((uint32_t)b < (uint32_t)a.buckets) {
+            x = param_load(a.bias, a.bias_io, (int64_t)(head0 + g) * a.buckets + b);
+            if (x > 1e30f && x < __builtin_inff()) x = 1e30f;
+            if (x < -1e30f && x > -__builtin_inff()) x = -1e30f;
+            x *= kLog2e;
+        } else {
+            *a.err = 1;
+        }
+        tab[g * size + t] = x;
+    }
+}
+
+// Workgroups are dealt to the 8 dies one by one; each die takes a run of neighbours, so that those that read the same keys share its
+// level-2 cache.  The grid has 8 * ceil(n / 8) workgroups.
+__device__ __forceinline__ uint32_t die_order(const uint32_t n) { return (blockIdx.x & 7u) * ((n + 7u) / 8u) + (blockIdx.x >> 3); }
+
+}  // namespace tbe

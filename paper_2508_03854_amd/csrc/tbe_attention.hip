@@ -1,0 +1,385 @@
+// Attention over packed sequences, forward (see tbe355.h for what it computes): one pass over the keys with the running maximum and sum
+// of the softmax; no score leaves the registers.
+//   S^T = K Q^T  (a tile: 32 keys x 32 columns)    p = 2^(x - m)    O^T += V^T P
+// Bound: long sequences by the vector unit's work on every score (the exponential, the sums) next to the matrix cores, single tokens by
+// reading the keys and values once.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "tbe_attention.h"
+
+namespace tbe {
+
+__device__ const uint4 attn_zeros = {0u, 0u, 0u, 0u};
+
+// SHARE = 4: the four wavefronts of a workgroup take neighbouring queries of one head and share the tiles of keys and values.
+// SHARE = 1: every wavefront is on its own, with `pack` heads of a group side by side in its columns and, with splits > 1, one of several
+// parts of the keys; the parts are joined by attn_join_kernel.
+template <typename T, int D, int SHARE>
+constexpr int kv_rows() { return SHARE == 4 && D * (int)sizeof(T) <= 256 ? 64 : 32; }
+template <typename T, int D, int SHARE>
+constexpr int attn_waves() { return SHARE == 1 && D * (int)sizeof(T) > 256 ? 2 : 4; }
+
+template <typename T, int D>   // wavefronts of a SIMD that the registers are to leave room for
+constexpr int attn_occupancy() { return sizeof(T) == 2 ? (D == 32 ? 3 : (D == 64 ? 2 : 1)) : (D == 32 ? 2 : 1); }
+
+template <typename T, int D, int SHARE, bool BIAS>
+__global__ __launch_bounds__((64 * attn_waves<T, D, SHARE>()), (attn_occupancy<T, D>())) void attn_kernel(const AttnArgs a) {
+    constexpr int kWaves = attn_waves<T, D, SHARE>(), BK = kv_rows<T, D, SHARE>(), kT = BK / 32, kD = D / 32;
+    constexpr int kE = Mma<T>::kE, kK = Mma<T>::kK, kC = D / kK, kM = 32 / kK;
+    constexpr int kTile = BK * D * (int)sizeof(T);
+    // two buffers each, as arrays of their own: loads into one of them are seen not to concern what is read from another
+    constexpr int kLds = SHARE == 4 ? kTile : kWaves * kTile;
+    __shared__ __align__(16) char keys0[kLds], keys1[kLds], values0[kLds], values1[kLds];
+    extern __shared__ float tab[];
+    const int wave = uniform(threadIdx.x >> 6), lane = lane_id(), col = lane & 31, half = lane >> 5;
+    const uint32_t per_head = SHARE == 4 ? (uint32_t)a.V : ((uint32_t)a.V * a.splits + kWaves - 1) / kWaves;
+    const uint32_t groups = per_head * (uint32_t)(a.H / a.pack), wg = die_order(groups);
+    if (wg >= groups) return;
+    const int hh = wg / per_head, head0 = hh * a.pack;
+    const uint32_t item = wg - hh * per_head;
+    if (BIAS) {
+        fill_bias(tab, a, head0, a.pack, 64 * kWaves);
+        __syncthreads();
+    }
+    const uint32_t unit = SHARE == 4 ? item : item * kWaves + wave;
+    if (unit >= (uint32_t)a.V * a.splits) return;
+    const uint32_t v = SHARE == 4 ? unit : unit / a.splits;
+    const int split = SHARE == 4 ? 0 : unit - v * a.splits;
+    const bool looks = hh == 0 && split == 0 && (SHARE == 1 || wave == 0) && v < (uint32_t)a.N;
+    const int64_t peek = looks ? sequence_numbers(a, v) : 0;
+    const int s = find_sequence(a.q_off, a.N, v, a.block);
+    Sequence q;
+    const bool fits = take_sequence(a, s, sequence_numbers(a, s), q);
+    const uint32_t start = (uint32_t)q.q0 / a.block + s, blocks = ((uint32_t)q.nq + a.block - 1) / a.block;
+    if (!fits || v < start || v - start >= blocks) return judge(a, looks, v, peek);
+    // the last queries, which see the most keys, first
+    const int i0 = uniform((int)(blocks - 1 - (v - start)) * a.block), iw = i0 + (SHARE == 4 ? wave * 32 : 0);
+    const int ci = SHARE == 4 ? col : col / a.pack, cg = SHARE == 4 ? 0 : col - ci * a.pack, i = iw + ci, head = head0 + cg;
+    const bool is = ci < a.qpt && i < q.nq;
+    const int first = q.nk - q.nq + iw, pos = first + ci;   // places among the keys: of the wavefront's first query, of this column's
+
+    uint4 fq[kC];
+    {
+        const char* const row = a.q.at(q.q0 + (is ? i : 0), head);
+#pragma unroll
+        for (int c = 0; c < kC; ++c) {
+            const int e = kK * c + kE * half;
+            fq[c] = make_uint4(0u, 0u, 0u, 0u);
+            if (is && e < a.dim) fq[c] = *reinterpret_cast<const uint4*>(row + e * sizeof(T));
+            if (a.negative) {   // the sign of the scale
+                constexpr uint32_t sign = sizeof(T) == 2 ? 0x80008000u : 0x80000000u;
+                fq[c] = make_uint4(fq[c].x ^ sign, fq[c].y ^ sign, fq[c].z ^ sign, fq[c].w ^ sign);
+            }
+        }
+    }
+    // keys of this unit: all that its last query sees, or a part of them
+    int jend = q.nk;
+    if (a.causal) {
+        const int last = q.nk - q.nq + (i0 + a.block < q.nq ? i0 + a.block : q.nq);
+        jend = jend < last ? jend : last;
+    }
+    const int tiles = jend > 0 ? (jend + BK - 1) / BK : 0;
+    const int part = SHARE == 4 ? tiles : (tiles + a.splits - 1) / a.splits;
+    const int t0 = uniform(split * part), t1 = uniform(t0 + part < tiles ? t0 + part : tiles);
+    const int wave_last = first + a.qpt - 1;   // the last place that a query of this wavefront may have
+
+    const int kvh = head0 / a.group;
+    const char* const kb = a.k.at(q.k0, kvh);
+    const char* const vb = a.v.at(q.k0, kvh);
+    const int own = SHARE == 4 ? 0 : wave * kTile, fw = SHARE == 4 ? wave : 0;
+    auto fetch = [&](const int t, char* const kt, char* const vt) __attribute__((always_inline)) {
+        Tile<T, D>::template fetch<BK, SHARE>(kt + own, kb, a.k.row, t * BK, q.nk, a.dim, fw);
+        Tile<T, D>::template fetch<BK, SHARE>(vt + own, vb, a.v.row, t * BK, q.nk, a.dim, fw);
+    };
+
+    f32x16_t o[kD];
+#pragma unroll
+    for (int d = 0; d < kD; ++d) o[d] = f32x16_t{};
+    float m = -__builtin_inff(), sum = 0.f;
+    float beyond = 0.f, ahead = 0.f;
+    const float* const ht = tab + cg * tab_size(a.far);
+    if (BIAS) {
+        beyond = ht[kTabMargin];
+        ahead = a.causal ? 0.f : ht[2 * a.far + kTabMargin];
+    }
+
+    auto step = [&](const int t, const char* const kt_, const char* const vt_, char* const kn, char* const vn) __attribute__((always_inline)) {
+        loads_done();
+        if (SHARE == 4) __syncthreads();
+        if (t + 1 < t1) fetch(t + 1, kn, vn);
+        const int j0 = t * BK;
+        const char* const kt = kt_ + own;
+        const char* const vt = vt_ + own;
+        if (SHARE == 4 && ((a.causal && j0 > wave_last) || iw >= q.nq)) return;
+        f32x16_t x[kT];
+#pragma unroll
+        for (int k = 0; k < kT; ++k) {
+            x[k] = f32x16_t{};
+#pragma unroll
+            for (int c = 0; c < kC; ++c) x[k] = Mma<T>::mma(Tile<T, D>::along(kt, 32 * k + col, c, half), fq[c], x[k]);
+        }
+        if (BIAS) {
+#pragma unroll
+            for (int k = 0; k < kT; ++k) {
+                const int j = j0 + 32 * k;
+                if (first - (j + 31) >= a.far || wave_last - j <= -a.far) {
+                    const float b = first - (j + 31) >= a.far ? beyond : ahead;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) x[k][r] = fmaf(x[k][r], a.scale2, b);
+                } else {
+                    const float* const from = ht + (j + 4 * half - pos + a.far + kTabMargin);
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) x[k][r] = fmaf(x[k][r], a.scale2, from[8 * (r / 4) + r % 4]);
+                }
+            }
+        }
+        const bool masked = j0 + BK > q.nk || (a.causal && j0 + BK - 1 > first);
+        if (masked) {
+            const int end = a.causal && pos + 1 < q.nk ? pos + 1 : q.nk;   // the keys that this column sees end here
+#pragma unroll
+            for (int k = 0; k < kT; ++k)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (j0 + 32 * k + 8 * (r / 4) + 4 * half + r % 4 >= end) x[k][r] = -__builtin_inff();
+        }
+        float top = x[0][0];
+#pragma unroll
+        for (int k = 0; k < kT; ++k)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) top = fmaxf(top, x[k][r]);
+        top = halves_max(top);
+        if (!BIAS) top *= a.scale2;
+        // A maximum that grows by less than 2^8 is left as it is: the probabilities stay below 2^8, and what they are divided by
+        // in the end is added up from them.
+        if (__any(top > m + 8.f || (m == -__builtin_inff() && top != m))) {
+            const float grown = fmaxf(m, top);
+            const float shrink = grown == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(m - grown);
+            m = grown;
+            sum *= shrink;
+#pragma unroll
+            for (int d = 0; d < kD; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[d][r] *= shrink;
+        }
+        const float at = m == -__builtin_inff() ? 0.f : m;   // (nothing seen so far: every probability is 2^-inf = 0)
+#pragma unroll
+        for (int k = 0; k < kT; ++k)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                x[k][r] = __builtin_amdgcn_exp2f(BIAS ? x[k][r] - at : fmaf(x[k][r], a.scale2, -at));
+                sum += x[k][r];
+            }
+        uint4 p[kT][kM];   // (rounded to the values' type: the sum they are divided by is not)
+#pragma unroll
+        for (int k = 0; k < kT; ++k)
+#pragma unroll
+            for (int c = 0; c < kM; ++c) p[k][c] = Mma<T>::pack(x[k], c);
+        if (!masked) {
+#pragma unroll
+            for (int k = 0; k < kT; ++k)
+#pragma unroll
+                for (int c = 0; c < kM; ++c)
+#pragma unroll
+                    for (int d = 0; d < kD; ++d) o[d] = Mma<T>::mma(Tile<T, D>::down(vt, 32 * k, c, d), p[k][c], o[d]);
+            return;
+        }
+        // Some probabilities are 0 because their keys are hidden, and 0 times a value that is not finite is not 0: where this tile's
+        // share of a result is not finite, it is added up once more key by key, without the hidden ones.
+#pragma unroll
+        for (int d = 0; d < kD; ++d) {
+            f32x16_t more = f32x16_t{};
+#pragma unroll
+            for (int k = 0; k < kT; ++k)
+#pragma unroll
+                for (int c = 0; c < kM; ++c) more = Mma<T>::mma(Tile<T, D>::down(vt, 32 * k, c, d), p[k][c], more);
+            float test = 0.f;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) test = fmaf(more[r], 0.f, test);   // 0, or NaN
+            if (__any(test != 0.f)) {
+                f32x16_t sure = f32x16_t{};
+#pragma unroll
+                for (int k = 0; k < kT; ++k)
+#pragma unroll 1
+                    for (int j = 0; j < 32; ++j) {
+                        int h = half;
+                        asm volatile("" : "+v"(h));   // (keeps what follows from it inside the loop, where it costs no registers)
+                        float one = 0.f;
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) one = j - 4 * h == 8 * (r / 4) + r % 4 ? x[k][r] : one;
+                        one = elem_float(elem_round<T>(__shfl(one, col + 8 * (j & 4))));
+                        if (one != 0.f)
+#pragma unroll
+                            for (int r = 0; r < 16; ++r) sure[r] = fmaf(one, Tile<T, D>::element(vt, 32 * k + j, 32 * d + 8 * (r / 4) + 4 * h + r % 4), sure[r]);
+                    }
+                if (test != 0.f) more = sure;   // (a column that was finite keeps its bits)
+            }
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[d][r] += more[r];
+        }
+    };
+    if (t0 < t1) fetch(t0, keys0, values0);
+    for (int t = t0; t < t1; t += 2) {
+        step(t, keys0, values0, keys1, values1);
+        if (t + 1 < t1) step(t + 1, keys1, values1, keys0, values0);
+    }
+    judge(a, looks, v, peek);
+    sum = pair_sum<32>(sum);
+    if (!is) return;
+    if (SHARE == 1 && a.splits > 1) {
+        const int64_t at = (((int64_t)hh * a.V + v) * a.splits + split) * 32 + col;
+        if (half == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * at) = make_float2(m, sum);
+        float* const to = a.part_o + at * D;
+#pragma unroll
+        for (int d = 0; d < kD; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4)
+                *reinterpret_cast<float4*>(to + 32 * d + 2 * r + 4 * half) = make_float4(o[d][r], o[d][r + 1], o[d][r + 2], o[d][r + 3]);
+        return;
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;   // (no key seen: zeros)
+    char* const to = const_cast<char*>(a.o.at(q.q0 + i, head));
+#pragma unroll
+    for (int d = 0; d < kD; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+            const int e = 32 * d + 2 * r + 4 * half;
+            if (e < a.dim) {
+                if constexpr (sizeof(T) == 2)
+                    *reinterpret_cast<uint2*>(to + 2 * e) = make_uint2(pack2((const T*)nullptr, o[d][r] * inv, o[d][r + 1] * inv),
+                                                                       pack2((const T*)nullptr, o[d][r + 2] * inv, o[d][r + 3] * inv));
+                else *reinterpret_cast<float4*>(to + 4 * e) = make_float4(o[d][r] * inv, o[d][r + 1] * inv, o[d][r + 2] * inv, o[d][r + 3] * inv);
+            }
+        }
+    if (a.lse && half == 0) a.lse[(int64_t)head * a.q_rows + q.q0 + i] = sum == 0.f ? -__builtin_inff() : fmaf(m, kLn2, logf(sum));
+}
+
+// Joins the parts of the keys: one wavefront per query and head, in the order of the parts.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void attn_join_kernel(const AttnArgs a) {
+    const int lane = lane_id();
+    const int64_t n = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col = (int)(n & 31);
+    const int64_t hv = n >> 5;
+    const int hh = (int)(hv / a.V), ci = col / a.pack, head = hh * a.pack + col - ci * a.pack;
+    const uint32_t v = (uint32_t)(hv - (int64_t)hh * a.V);
+    if (hh >= a.H / a.pack || ci >= a.qpt) return;
+    const int s = find_sequence(a.q_off, a.N, v, a.block);
+    Sequence q;
+    if (!take_sequence(a, s, sequence_numbers(a, s), q)) return;
+    const uint32_t start = (uint32_t)q.q0 / a.block + s, blocks = ((uint32_t)q.nq + a.block - 1) / a.block;
+    if (v < start || v - start >= blocks) return;
+    const int i = (int)(blocks - 1 - (v - start)) * a.block + ci;
+    if (i >= q.nq) return;
+    float m = -__builtin_inff();
+    for (int k = lane; k < a.splits; k += 64) m = fmaxf(m, a.part_ml[2 * ((hv * a.splits + k) * 32 + col)]);
+#pragma unroll
+    for (int w = 32; w; w >>= 1) m = fmaxf(m, __shfl_xor(m, w));
+    const float at = m == -__builtin_inff() ? 0.f : m;
+    constexpr int kPer = D >= 64 ? D / 64 : 1;
+    float o[kPer], sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) o[e] = 0.f;
+    const int e0 = (lane * kPer) & (D - 1);   // (rows of 32 elements: the upper half of the wavefront does the same again)
+    for (int k = 0; k < a.splits; ++k) {
+        const int64_t p = (hv * a.splits + k) * 32 + col;
+        const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + 2 * p);
+        const float w = __builtin_amdgcn_exp2f(ml.x - at);
+        sum = fmaf(ml.y, w, sum);
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) o[e] = fmaf(a.part_o[p * D + e0 + e], w, o[e]);
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    T* const to = reinterpret_cast<T*>(const_cast<char*>(a.o.at(q.q0 + i, head)));
+#pragma unroll
+    for (int e = 0; e < kPer; ++e)
+        if (e0 + e < a.dim) to[e0 + e] = elem_round<T>(o[e] * inv);
+    if (a.lse && lane == 0) a.lse[(int64_t)head * a.q_rows + q.q0 + i] = sum == 0.f ? -__builtin_inff() : fmaf(m, kLn2, logf(sum));
+}
+
+// How the forward shares out its work.  Sequences of many queries: 128 neighbours share the keys' tiles.  Few queries per sequence:
+// wavefronts on their own, heads of a group side by side where one query would leave its columns empty, and the keys in parts where
+// there would be too few wavefronts to keep the memory busy.
+AttnPlan attn_plan(const AttnShape& sh, const int max_pack) {
+    AttnPlan p;
+    const int64_t mean_q = sh.N > 0 ? (sh.q_rows + sh.N - 1) / sh.N : 0, mean_k = sh.N > 0 ? (sh.k_rows + sh.N - 1) / sh.N : 0;
+    p.D = sh.dim <= 32 ? 32 : (sh.dim <= 64 ? 64 : 128);
+    p.pack = 1;
+    p.splits = 1;
+    p.shared = mean_q > 64;
+    if (p.shared) {
+        p.qpt = 32;
+        p.block = 128;
+    } else {
+        const int group = sh.H / sh.kv;
+        const int64_t table = sh.buckets ? (2 * (int64_t)sh.far + 1 + 2 * kTabMargin) * 4 : 0;
+        for (int g = 2; g <= group && g <= max_pack; ++g)   // more heads side by side as long as a sequence's queries of all of them fit
+            if (group % g == 0 && mean_q * g <= 32 && g * table <= kTabBytes) p.pack = g;
+        p.qpt = p.block = 32 / p.pack;
+    }
+    p.V = sh.q_rows / p.block + sh.N;
+    if (!p.shared) {
+        const int64_t units = (sh.q_rows / p.block < sh.N ? sh.N : sh.q_rows / p.block + sh.N / 2) * (sh.H / p.pack);
+        int64_t want = units > 0 ? 2048 / units : 1;
+        const int64_t most = mean_k / 256;
+        want = want < most ? want : most;
+        p.splits = (int)(want < 1 ? 1 : (want > 128 ? 128 : want));
+    }
+    const int64_t cells = (int64_t)(sh.H / p.pack) * p.V * p.splits * 32;
+    p.part_ml = p.splits > 1 ? ((size_t)cells * 8 + 255) & ~(size_t)255 : 0;
+    p.part_o = p.splits > 1 ? ((size_t)cells * p.D * 4 + 255) & ~(size_t)255 : 0;
+    return p;
+}
+
+bool attn_grid_ok(const AttnShape& sh, const AttnPlan& p) {
+    return (int64_t)(sh.H / p.pack) * p.V * (p.splits > 1 ? 8 * (int64_t)p.splits : 1) < ((int64_t)1 << 31) - 64;
+}
+size_t attn_workspace(const AttnShape& sh, const bool backward) {
+    size_t most = 0;
+    for (int pack = 1; pack <= 32; ++pack) {   // (how many heads go side by side depends on the bias)
+        AttnShape any = sh;
+        any.far = 0;
+        const AttnPlan p = attn_plan(any, pack);
+        most = std::max(most, p.part_ml + p.part_o);
+    }
+    return most;
+}
+
+template <typename T, int D, int SHARE, bool BIAS>
+static hipError_t launch_one(const AttnArgs& a, hipStream_t s) {
+    constexpr int kWaves = attn_waves<T, D, SHARE>();
+    const size_t table = BIAS ? (size_t)a.pack * (2 * a.far + 1 + 2 * kTabMargin) * 4 : 0;
+    const uint64_t per_head = SHARE == 4 ? (uint64_t)a.V : ((uint64_t)a.V * a.splits + kWaves - 1) / kWaves;
+    const uint64_t groups = per_head * (uint64_t)(a.H / a.pack);
+    attn_kernel<T, D, SHARE, BIAS><<<(unsigned)((groups + 7) / 8 * 8), 64 * kWaves, table, s>>>(a);
+    return hipGetLastError();
+}
+template <typename T, int D>
+static hipError_t launch_dim(const tbe_handle* h, const AttnArgs& a, const AttnPlan& p, hipStream_t s) {
+    hipError_t e;
+    {
+        LaunchTimer tm(h, s, "attention");
+        if (p.shared) e = a.bias ? launch_one<T, D, 4, true>(a, s) : launch_one<T, D, 4, false>(a, s);
+        else e = a.bias ? launch_one<T, D, 1, true>(a, s) : launch_one<T, D, 1, false>(a, s);
+        tm.done();
+    }
+    if (e != hipSuccess || p.splits == 1) return e;
+    LaunchTimer tm(h, s, "attention_join");
+    attn_join_kernel<T, D><<<(unsigned)((int64_t)(a.H / a.pack) * a.V * 8), 256, 0, s>>>(a);
+    tm.done();
+    return hipGetLastError();
+}
+template <typename T>
+static hipError_t launch_type(const tbe_handle* h, const AttnArgs& a, const AttnPlan& p, hipStream_t s) {
+    return p.D == 32 ? launch_dim<T, 32>(h, a, p, s) : (p.D == 64 ? launch_dim<T, 64>(h, a, p, s) : launch_dim<T, 128>(h, a, p, s));
+}
+
+hipError_t launch_attention(const tbe_handle* h, AttnArgs a, const AttnPlan& p, int io, void* workspace, hipStream_t s) {
+    a.pack = p.pack; a.qpt = p.qpt; a.block = p.block; a.V = (int)p.V; a.splits = p.splits;
+    a.part_ml = static_cast<float*>(workspace);
+    a.part_o = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.part_ml);
+    return io == 0 ? launch_type<float>(h, a, p, s) : (io == 1 ? launch_type<__half>(h, a, p, s) : launch_type<bf16_t>(h, a, p, s));
+}
+
+}  // namespace tbe

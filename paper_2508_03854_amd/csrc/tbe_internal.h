@@ -165,4 +165,24 @@ hipError_t launch_layer_norm_backward(const tbe_handle* h, const void* dy, int64
                                       int64_t rows, int n, const void* weight, int param_io, const float* mean, const float* rstd,
                                       void* dx, int64_t dx_stride, void* dw, void* db, void* workspace, hipStream_t s);
 
+// attention over packed sequences (tbe_attention.hip, tbe_attention_backward.hip)
+constexpr int kAttnMaxDim = 128, kAttnMaxFar = 1024;
+struct AttnShape {
+    int64_t q_rows, k_rows;
+    int N, H, kv, dim, buckets, far;   // buckets 0: no bias
+};
+struct AttnPlan {
+    int D;        // elements of a row as the kernels have it
+    bool shared;  // wavefronts of a workgroup share tiles
+    int pack, qpt, block, splits;
+    int64_t V;
+    size_t part_ml, part_o;   // bytes
+};
+// max_pack: heads side by side at most
+AttnPlan attn_plan(const AttnShape& sh, int max_pack = 32);
+bool attn_grid_ok(const AttnShape& sh, const AttnPlan& p);   // the launches stay below 2^31 workgroups
+size_t attn_workspace(const AttnShape& sh, bool backward);   // for any max_distance
+struct AttnArgs;
+hipError_t launch_attention(const tbe_handle* h, AttnArgs a, const AttnPlan& p, int io, void* workspace, hipStream_t s);
+
 }  // namespace tbe
