@@ -327,8 +327,8 @@ tbe_status tbe_layer_norm_backward(const tbe_handle* h, const void* dy, int64_t 
  *             bytes, 0 <= row_stride < 2^22 (a result's at least head_dim); head_dim <= 128, a multiple of 8 (4 for TBE_IO_F32).  Results
  *             share no byte with each other or with what is read
  *   q_offsets, k_offsets   DEVICE, sequences + 1 of index_dtype, ascending from 0 to q_rows resp. k_rows;  k_lengths  DEVICE,
- *             `sequences` of the same type, or NULL.  A sequence whose numbers do not fit is left out - rows of the results that no
- *             other sequence claims keep their contents; offsets that do not ascend may cost other sequences, too - and is reported
+ *             `sequences` of the same type, or NULL.  A sequence whose numbers do not fit, and with
+ *             offsets that do not ascend others too, is left out: what its rows of the results then hold is not specified.  It is reported
  *             by tbe_poll_index_error; nothing outside the buffers is touched
  *   bias      DEVICE, [heads][buckets] of bias_dtype, or NULL: none.  -infinity hides a bucket; finite values beyond +-1e30 count as that
  *   bucket_map  DEVICE int32 [2 max_distance + 1], 0 <= max_distance <= 1024; a number outside [0, buckets) counts as no bias and is
@@ -362,6 +362,12 @@ typedef struct {
 tbe_status tbe_attention_workspace_bytes(const tbe_handle* h, const tbe_attention_args* args, int backward, size_t* bytes);
 tbe_status tbe_attention(const tbe_handle* h, const tbe_attention_args* args, tbe_rows out, float* lse, void* workspace,
                          size_t workspace_bytes, void* hip_stream);
+
+/* Gradients, from the same args, the forward's out and lse, and dout.  All of dq, dk and dv are written; dbias ([heads][buckets] of
+ * bias_dtype) may be NULL.  Workspace: backward != 0. */
+tbe_status tbe_attention_backward(const tbe_handle* h, const tbe_attention_args* args, tbe_rows out, const float* lse, tbe_rows dout,
+                                  tbe_rows dq, tbe_rows dk, tbe_rows dv, void* dbias, void* workspace, size_t workspace_bytes,
+                                  void* hip_stream);
 
 const char* tbe_status_string(tbe_status s);
 

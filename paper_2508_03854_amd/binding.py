@@ -31,7 +31,7 @@ EXPORTS = ["tbe_create", "tbe_destroy", "tbe_workspace_bytes", "tbe_forward", "t
            "tbe_backward_apply_rowwise_adagrad", "tbe_backward_apply_sgd", "tbe_backward_sgd", "tbe_replica_mean", "tbe_lookup_seq",
            "tbe_backward_seq_rowwise_adagrad", "tbe_debug_sorted", "tbe_debug_hot_rows", "tbe_debug_forward_kernels", "tbe_poll_index_error", "tbe_set_tunable", "tbe_timing_enable",
            "tbe_timing_count", "tbe_timing_read", "tbe_calibration_copy", "tbe_calibration_gather", "tbe_status_string", "tbe_build_info",
-           "tbe_layer_norm", "tbe_layer_norm_workspace_bytes", "tbe_layer_norm_backward", "tbe_attention_workspace_bytes", "tbe_attention"]
+           "tbe_layer_norm", "tbe_layer_norm_workspace_bytes", "tbe_layer_norm_backward", "tbe_attention_workspace_bytes", "tbe_attention", "tbe_attention_backward"]
 
 
 class TbeError(RuntimeError):
@@ -139,6 +139,8 @@ def load_library():
     L.tbe_attention_workspace_bytes.argtypes = [vp, ctypes.POINTER(AttentionArgs), ctypes.c_int, ctypes.POINTER(ctypes.c_size_t)]
     L.tbe_attention.restype = ctypes.c_int
     L.tbe_attention.argtypes = [vp, ctypes.POINTER(AttentionArgs), Rows, vp, vp, ctypes.c_size_t, vp]
+    L.tbe_attention_backward.restype = ctypes.c_int
+    L.tbe_attention_backward.argtypes = [vp, ctypes.POINTER(AttentionArgs), Rows, vp, Rows, Rows, Rows, Rows, vp, vp, ctypes.c_size_t, vp]
     L.tbe_build_info.restype = ctypes.c_char_p
     L.tbe_build_info.argtypes = []
     L.tbe_status_string.restype = ctypes.c_char_p
@@ -604,6 +606,32 @@ class TBE:
                                      _stream_ptr(stream))
         _check(st, "tbe_attention")
         return out, lse
+
+    # ---- tbe_attention_backward
+    def attention_backward(self, grad_out: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor,
+                           lse: torch.Tensor, q_offsets: torch.Tensor, k_offsets: torch.Tensor, workspace: torch.Tensor, *,
+                           causal: bool = True, scale: Optional[float] = None, k_lengths: Optional[torch.Tensor] = None,
+                           bias: Optional[torch.Tensor] = None, bucket_map: Optional[torch.Tensor] = None,
+                           grad_q: Optional[torch.Tensor] = None, grad_k: Optional[torch.Tensor] = None,
+                           grad_v: Optional[torch.Tensor] = None, grad_bias: Optional[torch.Tensor] = None,
+                           stream: Optional[torch.cuda.Stream] = None
+                           ) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor, Optional[torch.Tensor]]:
+        """Arguments as of attention(), its out and lse, and the upstream gradient.  Returns (grad_q, grad_k, grad_v, grad_bias)."""
+        a = self._attention_args(q, k, v, q_offsets, k_offsets, k_lengths, causal, scale, bias, bucket_map)
+        grad_q = torch.empty(q.shape, dtype=q.dtype, device=q.device) if grad_q is None else grad_q
+        grad_k = torch.empty(k.shape, dtype=q.dtype, device=q.device) if grad_k is None else grad_k
+        grad_v = torch.empty(v.shape, dtype=q.dtype, device=q.device) if grad_v is None else grad_v
+        if bias is None and grad_bias is not None:
+            raise ValueError("grad_bias without bias")
+        if bias is not None and grad_bias is None:
+            grad_bias = torch.empty_like(bias)
+        st = self._lib.tbe_attention_backward(
+            self._h, ctypes.byref(a), _heads(out, q, "out"), _param_ptr(lse, q.shape[0] * q.shape[1], torch.float32, "lse"),
+            _heads(grad_out, q, "grad_out"), _heads(grad_q, q, "grad_q"), _heads(grad_k, k, "grad_k"), _heads(grad_v, v, "grad_v"),
+            None if bias is None else _param_ptr(grad_bias, bias.numel(), bias.dtype, "grad_bias"),
+            _dev_ptr(workspace, torch.uint8, "workspace"), 0 if workspace is None else int(workspace.numel()), _stream_ptr(stream))
+        _check(st, "tbe_attention_backward")
+        return grad_q, grad_k, grad_v, grad_bias
 
     # ---- tbe_debug_sorted
     def debug_sorted(self, workspace: torch.Tensor, B: int, nnz: int) -> Dict[str, torch.Tensor]:

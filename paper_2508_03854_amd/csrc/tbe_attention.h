@@ -26,7 +26,7 @@ constexpr int kTabMargin = 64;         // a tile that reaches into the table of 
 constexpr int kTabBytes = 24 << 10;    // LDS for such tables
 
 // Sixteen zero bytes: what stands behind a sequence's end, or behind a row's, is read from here.
-extern __device__ const uint4 attn_zeros;
+static __device__ const uint4 attn_zeros = {0u, 0u, 0u, 0u};
 
 template <typename T>
 struct Mma {   // 16-bit types: fragments of 8 elements a lane, 16 of the summed axis at a time

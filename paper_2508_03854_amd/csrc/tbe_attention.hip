@@ -11,8 +11,6 @@
 
 namespace tbe {
 
-__device__ const uint4 attn_zeros = {0u, 0u, 0u, 0u};
-
 // SHARE = 4: the four wavefronts of a workgroup take neighbouring queries of one head and share the tiles of keys and values.
 // SHARE = 1: every wavefront is on its own, with `pack` heads of a group side by side in its columns and, with splits > 1, one of several
 // parts of the keys; the parts are joined by attn_join_kernel.
@@ -336,6 +334,7 @@ bool attn_grid_ok(const AttnShape& sh, const AttnPlan& p) {
     return (int64_t)(sh.H / p.pack) * p.V * (p.splits > 1 ? 8 * (int64_t)p.splits : 1) < ((int64_t)1 << 31) - 64;
 }
 size_t attn_workspace(const AttnShape& sh, const bool backward) {
+    if (backward) return attn_backward_workspace(sh);
     size_t most = 0;
     for (int pack = 1; pack <= 32; ++pack) {   // (how many heads go side by side depends on the bias)
         AttnShape any = sh;

@@ -1,0 +1,552 @@
+// Gradients of attention over packed sequences (see tbe355.h).  The scores are computed again from q and k, the probabilities from them and
+// the forward's lse; two kernels, so that every sum has one owner and a fixed order:
+//   attn_dq_kernel    columns are queries:  S^T = K Q^T, dP^T = V dO^T, dS;  dQ^T += K^T dS;  also D = rowsum(dO O), and dbias
+//   attn_dkv_kernel   columns are keys:     S = Q K^T,   dP = dO V^T,   dS;  dV^T += dO^T P,  dK^T += Q^T dS
+// Seven products of a tile instead of five: sums of dQ from one kernel over key blocks would need atomics or a pass over partial sums.
+// Bound: the matrix cores and the vector unit's work on every score, twice; short sequences by the trips to memory of a wavefront.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "tbe_attention.h"
+
+namespace tbe {
+
+static __device__ const float attn_inf = __builtin_inff();
+
+// SHARE = 4: the wavefronts of a workgroup take neighbouring columns of one sequence and share tiles.  SHARE = 1: each is on its own.
+template <typename T, int D, int SHARE>
+constexpr int bwd_rows() { return SHARE == 4 && D * (int)sizeof(T) <= 128 ? 64 : 32; }
+template <typename T, int D, int SHARE>
+constexpr int bwd_waves() { return SHARE == 4 ? 4 : (D * (int)sizeof(T) <= 128 ? 4 : (D * (int)sizeof(T) <= 256 ? 2 : 1)); }
+template <typename T, int D>
+constexpr int bwd_occupancy() { return sizeof(T) == 2 && D <= 64 ? 2 : 1; }
+
+// The fragments of one column's row of D elements, dim of them there; nothing: zeros
+template <typename T, int D>
+__device__ __forceinline__ void column_row(uint4 (&f)[D / Mma<T>::kK], const char* row, const bool is, const int half, const int dim) {
+    constexpr int kE = Mma<T>::kE, kK = Mma<T>::kK;
+#pragma unroll
+    for (int c = 0; c < D / kK; ++c) {
+        const int e = kK * c + kE * half;
+        f[c] = make_uint4(0u, 0u, 0u, 0u);
+        if (is && e < dim) f[c] = *reinterpret_cast<const uint4*>(row + e * sizeof(T));
+    }
+}
+template <typename T, int N>
+__device__ __forceinline__ void flip_signs(uint4 (&f)[N]) {
+    constexpr uint32_t sign = sizeof(T) == 2 ? 0x80008000u : 0x80000000u;
+#pragma unroll
+    for (int c = 0; c < N; ++c) f[c] = make_uint4(f[c].x ^ sign, f[c].y ^ sign, f[c].z ^ sign, f[c].w ^ sign);
+}
+// a column's share of a transposed result, times `by`, to its row
+template <typename T, int D>
+__device__ __forceinline__ void store_column(char* row, const f32x16_t (&o)[D / 32], const float by, const int half, const int dim) {
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+            const int e = 32 * d + 2 * r + 4 * half;
+            if (e < dim) {
+                if constexpr (sizeof(T) == 2)
+                    *reinterpret_cast<uint2*>(row + 2 * e) = make_uint2(pack2((const T*)nullptr, o[d][r] * by, o[d][r + 1] * by),
+                                                                        pack2((const T*)nullptr, o[d][r + 2] * by, o[d][r + 3] * by));
+                else *reinterpret_cast<float4*>(row + 4 * e) = make_float4(o[d][r] * by, o[d][r + 1] * by, o[d][r + 2] * by, o[d][r + 3] * by);
+            }
+        }
+}
+
+// dbias of a unit: its sums by distance, [from, to) of a table, added up by bucket; `lane` of `lanes` does every lanes-th bucket.
+__device__ __forceinline__ void bucket_sums(const AttnArgs& a, float* out, const float* sums, const int from, const int to, const float beyond,
+                                            const float ahead, const int lane, const int lanes) {
+    const int b_beyond = a.map[2 * a.far], b_ahead = a.map[0];
+    for (int b = lane; b < a.buckets; b += lanes) {
+        float s = (b == b_beyond ? beyond : 0.f) + (b == b_ahead ? ahead : 0.f);
+        for (int t = from; t < to; ++t) {
+            int d = a.far + kTabMargin - t;
+            d = d > a.far ? a.far : (d < -a.far ? -a.far : d);
+            if (a.map[d + a.far] == b) s += sums[t];
+        }
+        out[b] = s;
+    }
+}
+
+template <typename T, int D, int SHARE, bool BIAS>
+__global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (bwd_occupancy<T, D>())) void attn_dq_kernel(const AttnArgs a) {
+    constexpr int kWaves = bwd_waves<T, D, SHARE>(), BK = bwd_rows<T, D, SHARE>(), kT = BK / 32, kD = D / 32;
+    constexpr int kE = Mma<T>::kE, kK = Mma<T>::kK, kC = D / kK, kM = 32 / kK;
+    constexpr int kTile = BK * D * (int)sizeof(T), kLds = SHARE == 4 ? kTile : kWaves * kTile;
+    __shared__ __align__(16) char keys0[kLds], keys1[kLds], values0[kLds], values1[kLds];
+    extern __shared__ float tab[];   // the bias by distance, then sums by distance: two arrays of that size for each wavefront
+    const int wave = uniform(threadIdx.x >> 6), lane = lane_id(), col = lane & 31, half = lane >> 5;
+    const uint32_t per_head = SHARE == 4 ? (uint32_t)a.V : ((uint32_t)a.V + kWaves - 1) / kWaves;
+    const uint32_t groups = per_head * (uint32_t)a.H, wg = die_order(groups);
+    if (wg >= groups) return;
+    const int head = wg / per_head, size = tab_size(a.far);
+    const uint32_t v = SHARE == 4 ? wg - head * per_head : (wg - head * per_head) * kWaves + wave;
+    if (BIAS) {
+        fill_bias(tab, a, head, 1, 64 * kWaves);
+        for (int n = threadIdx.x; n < 2 * kWaves * size; n += 64 * kWaves) tab[size + n] = 0.f;
+        __syncthreads();
+    }
+    if (v >= (uint32_t)a.V) return;
+    float* const part = BIAS ? a.part_bias + ((int64_t)head * a.V + v) * a.buckets : nullptr;
+    const int me = SHARE == 4 ? threadIdx.x : lane, of = SHARE == 4 ? 64 * kWaves : 64;   // of the unit's lanes
+    const bool looks = head == 0 && (SHARE == 1 || wave == 0) && v < (uint32_t)a.N;
+    const int64_t peek = looks ? sequence_numbers(a, v) : 0;
+    const int s = find_sequence(a.q_off, a.N, v, a.block);
+    Sequence q;
+    const bool fits = take_sequence(a, s, sequence_numbers(a, s), q);
+    const uint32_t start = (uint32_t)q.q0 / a.block + s, blocks = ((uint32_t)q.nq + a.block - 1) / a.block;
+    if (!fits || v < start || v - start >= blocks) {
+        if (BIAS)
+            for (int b = me; b < a.buckets; b += of) part[b] = 0.f;
+        return judge(a, looks, v, peek);
+    }
+    const int i0 = uniform((int)(blocks - 1 - (v - start)) * a.block), iw = i0 + (SHARE == 4 ? wave * 32 : 0), i = iw + col;
+    const bool is = i < q.nq;
+    const int first = q.nk - q.nq + iw, pos = first + col, wave_last = first + 31;
+    const int64_t row = q.q0 + (is ? i : 0);
+
+    uint4 fq[kC], fy[kC];
+    column_row<T, D>(fq, a.q.at(row, head), is, half, a.dim);
+    column_row<T, D>(fy, a.dout.at(row, head), is, half, a.dim);
+    float delta = 0.f;
+    {
+        uint4 fo[kC];
+        column_row<T, D>(fo, a.o.at(row, head), is, half, a.dim);
+#pragma unroll
+        for (int c = 0; c < kC; ++c) {
+            float x[kE], y[kE];
+            Frag<T>::unpack(fo[c], x);
+            Frag<T>::unpack(fy[c], y);
+#pragma unroll
+            for (int e = 0; e < kE; ++e) delta = fmaf(x[e], y[e], delta);
+        }
+        delta = pair_sum<32>(delta);
+    }
+    if (a.negative) flip_signs<T, kC>(fq);
+    float lse = is ? a.lse[(int64_t)head * a.q_rows + row] : 0.f;
+    lse = lse == -__builtin_inff() ? __builtin_inff() : lse * kLog2e;   // (a row that saw nothing: all its probabilities 2^-inf)
+    if (is && half == 0) const_cast<float*>(a.delta)[(int64_t)head * a.q_rows + row] = delta;
+
+    int jend = q.nk;
+    if (a.causal) {
+        const int last = q.nk - q.nq + (i0 + a.block < q.nq ? i0 + a.block : q.nq);
+        jend = jend < last ? jend : last;
+    }
+    const int tiles = uniform(jend > 0 ? (jend + BK - 1) / BK : 0);
+    const int kvh = head / a.group;
+    const char* const kb = a.k.at(q.k0, kvh);
+    const char* const vb = a.v.at(q.k0, kvh);
+    const int own = SHARE == 4 ? 0 : wave * kTile, fw = SHARE == 4 ? wave : 0;
+    auto fetch = [&](const int t, char* const kt, char* const vt) __attribute__((always_inline)) {
+        Tile<T, D>::template fetch<BK, SHARE>(kt + own, kb, a.k.row, t * BK, q.nk, a.dim, fw);
+        Tile<T, D>::template fetch<BK, SHARE>(vt + own, vb, a.v.row, t * BK, q.nk, a.dim, fw);
+    };
+    f32x16_t dq[kD];
+#pragma unroll
+    for (int d = 0; d < kD; ++d) dq[d] = f32x16_t{};
+    float beyond = 0.f, ahead = 0.f, sum_beyond = 0.f, sum_ahead = 0.f;
+    float* const sums = tab + size * (1 + 2 * (BIAS ? wave : 0));
+    if (BIAS) {
+        beyond = tab[kTabMargin];
+        ahead = a.causal ? 0.f : tab[2 * a.far + kTabMargin];
+    }
+    auto step = [&](const int t, const char* const kt_, const char* const vt_, char* const kn, char* const vn) __attribute__((always_inline)) {
+        loads_done();
+        if (SHARE == 4) __syncthreads();
+        if (t + 1 < tiles) fetch(t + 1, kn, vn);
+        const char* const kt = kt_ + own;
+        const char* const vt = vt_ + own;
+#pragma unroll
+        for (int k = 0; k < kT; ++k) {
+            const int j0 = t * BK + 32 * k;
+            if (j0 >= q.nk || (a.causal && j0 > wave_last) || iw >= q.nq) return;
+            f32x16_t x = f32x16_t{}, g = f32x16_t{};
+#pragma unroll
+            for (int c = 0; c < kC; ++c) x = Mma<T>::mma(Tile<T, D>::along(kt, 32 * k + col, c, half), fq[c], x);
+#pragma unroll
+            for (int c = 0; c < kC; ++c) g = Mma<T>::mma(Tile<T, D>::along(vt, 32 * k + col, c, half), fy[c], g);
+            const bool all_beyond = first - (j0 + 31) >= a.far, all_ahead = wave_last - j0 <= -a.far;
+            const int at = j0 + 4 * half - pos + a.far + kTabMargin;   // of this lane's first key among the distances
+            if (!BIAS) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) x[r] = __builtin_amdgcn_exp2f(fmaf(x[r], a.scale2, -lse));
+            } else if (all_beyond || all_ahead) {
+                const float b = all_beyond ? beyond : ahead;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) x[r] = __builtin_amdgcn_exp2f(fmaf(x[r], a.scale2, b) - lse);
+            } else {
+                const float* const from = tab + at;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) x[r] = __builtin_amdgcn_exp2f(fmaf(x[r], a.scale2, from[8 * (r / 4) + r % 4]) - lse);
+            }
+#pragma unroll
+            for (int r = 0; r < 16; ++r) g[r] = x[r] * (g[r] - delta);
+            if (j0 + 32 > q.nk || (a.causal && j0 + 31 > first)) {
+                const int end = a.causal && pos + 1 < q.nk ? pos + 1 : q.nk;
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (j0 + 8 * (r / 4) + 4 * half + r % 4 >= end) g[r] = 0.f;
+            }
+            if (BIAS && is) {
+                if (all_beyond || all_ahead) {
+                    float sum = 0.f;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) sum += g[r];
+                    if (all_beyond) sum_beyond += sum;
+                    else sum_ahead += sum;
+                } else {
+                    // 32 neighbouring distances a register, one for each lane of a half; the halves, which overlap, have an array each.  An
+                    // LDS addition is done in program order and no other wavefront adds here, so the order of the sums is fixed.
+                    float* const to = sums + half * size + at;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) __hip_atomic_fetch_add(to + 8 * (r / 4) + r % 4, g[r], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+                }
+            }
+#pragma unroll
+            for (int c = 0; c < kM; ++c) {
+                const uint4 p = Mma<T>::pack(g, c);
+#pragma unroll
+                for (int d = 0; d < kD; ++d) dq[d] = Mma<T>::mma(Tile<T, D>::down(kt, 32 * k, c, d), p, dq[d]);
+            }
+        }
+    };
+    if (tiles > 0) fetch(0, keys0, values0);
+    for (int t = 0; t < tiles; t += 2) {
+        step(t, keys0, values0, keys1, values1);
+        if (t + 1 < tiles) step(t + 1, keys1, values1, keys0, values0);
+    }
+    judge(a, looks, v, peek);
+    if (is) store_column<T, D>(const_cast<char*>(a.dq.at(row, head)), dq, a.scale, half, a.dim);
+    if (!BIAS) return;
+    // the distances that this unit has met
+    const int unit_first = q.nk - q.nq + i0, unit_last = unit_first + a.block - 1;
+    int from = a.far + kTabMargin - (unit_last < a.far + kTabMargin ? unit_last : a.far + kTabMargin);
+    int to = a.far + kTabMargin + (a.causal ? 0 : (q.nk - 1 - unit_first < a.far + kTabMargin ? q.nk - 1 - unit_first : a.far + kTabMargin)) + 1;
+    from = from < 0 ? 0 : (from > size ? size : from);
+    to = to > size ? size : to;
+    sum_beyond = group_sum(sum_beyond, 64);
+    sum_ahead = group_sum(sum_ahead, 64);
+    if (SHARE == 4) {
+        __syncthreads();
+        if (lane == 0) {   // the bias itself is not needed any more
+            tab[2 * wave] = sum_beyond;
+            tab[2 * wave + 1] = sum_ahead;
+        }
+        for (int t = from + (int)threadIdx.x; t < to; t += 64 * kWaves) {
+            float x = 0.f;
+#pragma unroll
+            for (int w = 0; w < 2 * kWaves; ++w) x += tab[size * (1 + w) + t];
+            tab[size + t] = x;
+        }
+        __syncthreads();
+        sum_beyond = tab[0] + tab[2] + tab[4] + tab[6];
+        sum_ahead = tab[1] + tab[3] + tab[5] + tab[7];
+    } else {
+        for (int t = from + lane; t < to; t += 64) sums[t] += sums[size + t];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+    bucket_sums(a, part, SHARE == 4 ? tab + size : sums, from, to, sum_beyond, sum_ahead, me, of);
+}
+
+// Sums the units' shares of dbias, in their order: 8 buckets of a head a workgroup, 32 slices of the units beside each other.
+__global__ __launch_bounds__(256) void attn_dbias_kernel(const AttnArgs a, void* dbias) {
+    __shared__ float part[32][9];
+    const int c = threadIdx.x % 8, k = threadIdx.x / 8, b = blockIdx.x * 8 + c, head = blockIdx.y;
+    float s = 0.f;
+    if (b < a.buckets)
+        for (int64_t v = k; v < a.V; v += 32) s += a.part_bias[((int64_t)head * a.V + v) * a.buckets + b];
+    part[k][c] = s;
+    __syncthreads();
+    if (k == 0 && b < a.buckets) {
+        float t = 0.f;
+        for (int i = 0; i < 32; ++i) t += part[i][c];
+        param_store(dbias, a.bias_io, (int64_t)head * a.buckets + b, t);
+    }
+}
+
+// A unit: `block` keys of a sequence and a key head, hp of the heads that read it one after the other.  Where a group is cut into several
+// such parts, each leaves fp32 sums (part_o: [2][parts][k_rows][kv][D]), which attn_dkv_join_kernel adds up.
+template <typename T, int D, int SHARE, bool BIAS>
+__global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (bwd_occupancy<T, D>())) void attn_dkv_kernel(const AttnArgs a) {
+    constexpr int kWaves = bwd_waves<T, D, SHARE>(), BQ = bwd_rows<T, D, SHARE>(), kT = BQ / 32, kD = D / 32;
+    constexpr int kK = Mma<T>::kK, kC = D / kK, kM = 32 / kK;
+    constexpr int kTile = BQ * D * (int)sizeof(T), kSets = SHARE == 4 ? 1 : kWaves, kLds = kSets * kTile;
+    __shared__ __align__(16) char rows0[kLds], rows1[kLds], grads0[kLds], grads1[kLds];
+    __shared__ __align__(16) float stats0[kSets * 128], stats1[kSets * 128];   // lse and delta of 64 rows
+    extern __shared__ float tab[];
+    const int wave = uniform(threadIdx.x >> 6), lane = lane_id(), col = lane & 31, half = lane >> 5;
+    const int parts = a.splits, hp = a.pack;
+    const uint32_t per_head = SHARE == 4 ? (uint32_t)a.V : ((uint32_t)a.V + kWaves - 1) / kWaves;
+    const uint32_t groups = per_head * (uint32_t)(a.kv * parts), wg = die_order(groups);
+    if (wg >= groups) return;
+    const int hh = wg / per_head, kvh = hh / parts, part = hh - kvh * parts, head0 = kvh * a.group + part * hp, size = tab_size(a.far);
+    const uint32_t v = SHARE == 4 ? wg - hh * per_head : (wg - hh * per_head) * kWaves + wave;
+    if (BIAS && SHARE == 1) {
+        fill_bias(tab, a, head0, hp, 64 * kWaves);
+        __syncthreads();
+    }
+    if (v >= (uint32_t)a.V) return;
+    const int s = find_sequence(a.k_off, a.N, v, a.block);
+    Sequence q;
+    if (!take_sequence(a, s, sequence_numbers(a, s), q)) return;
+    const uint32_t start = (uint32_t)q.k0 / a.block + s, blocks = ((uint32_t)q.cap + a.block - 1) / a.block;
+    if (v < start || v - start >= blocks) return;
+    const int j0 = uniform((int)(v - start) * a.block), jw = j0 + (SHARE == 4 ? wave * 32 : 0), j = jw + col;
+    const bool is = j < q.nk;
+
+    uint4 fk[kC], fv[kC];
+    column_row<T, D>(fk, a.k.at(q.k0 + (is ? j : 0), kvh), is, half, a.dim);
+    column_row<T, D>(fv, a.v.at(q.k0 + (is ? j : 0), kvh), is, half, a.dim);
+    if (a.negative) flip_signs<T, kC>(fk);
+
+    // the queries that see these keys: all, or from the one in the first key's place on
+    const int lead = q.nk - q.nq;   // the first query's place
+    int t0 = 0;
+    if (a.causal && j0 > lead) t0 = (j0 - lead) / BQ;
+    const int all = j0 < q.nk ? (q.nq + BQ - 1) / BQ : 0;
+    t0 = uniform(t0 < all ? t0 : all);
+    const int tiles = uniform(all - t0), steps = tiles * hp;
+    const int own = SHARE == 4 ? 0 : wave * kTile, own_stats = SHARE == 4 ? 0 : wave * 128, fw = SHARE == 4 ? wave : 0;
+    auto fetch = [&](const int g, const int t, char* const qt, char* const yt, float* const st) __attribute__((always_inline)) {
+        const int head = head0 + g;
+        Tile<T, D>::template fetch<BQ, SHARE>(qt + own, a.q.at(q.q0, head), a.q.row, t * BQ, q.nq, a.dim, fw);
+        Tile<T, D>::template fetch<BQ, SHARE>(yt + own, a.dout.at(q.q0, head), a.dout.row, t * BQ, q.nq, a.dim, fw);
+        if (SHARE == 1 || wave < 2) {
+            const int i = t * BQ + lane;
+            const bool there = lane < BQ && i < q.nq;
+            const int64_t at = (int64_t)head * a.q_rows + q.q0 + i;
+            const float* const l = there ? a.lse + at : &attn_inf;
+            const float* const d = there ? a.delta + at : reinterpret_cast<const float*>(&attn_zeros);
+            if (SHARE == 1 || wave == 0)
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)l, (__attribute__((address_space(3))) void*)(st + own_stats), 4, 0, 0);
+            if (SHARE == 1 || wave == 1)
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)d, (__attribute__((address_space(3))) void*)(st + own_stats + 64), 4, 0, 0);
+        }
+    };
+    f32x16_t dk[kD], dv[kD];
+#pragma unroll
+    for (int d = 0; d < kD; ++d) dk[d] = dv[d] = f32x16_t{};
+    // the step after (g, t) is (g, t + 1) or the next head's first
+    auto step = [&](const int g, const int t, const bool more, const char* const qt_, const char* const yt_, const float* const st_, char* const qn,
+                    char* const yn, float* const sn) __attribute__((always_inline)) {
+        loads_done();
+        if (SHARE == 4) __syncthreads();
+        if (more) {
+            const bool next = t + 1 == t0 + tiles;
+            fetch(next ? g + 1 : g, next ? t0 : t + 1, qn, yn, sn);
+        }
+        if (BIAS && SHARE == 4 && t == t0) {
+            fill_bias(tab, a, head0 + g, 1, 64 * kWaves);
+            __syncthreads();
+        }
+        const char* const qt = qt_ + own;
+        const char* const yt = yt_ + own;
+        const float* const ht = SHARE == 4 ? tab : tab + g * size;
+#pragma unroll
+        for (int k = 0; k < kT; ++k) {
+            const int i0 = t * BQ + 32 * k, first = lead + i0;   // the first query and its place
+            if (i0 >= q.nq || jw >= q.nk) return;
+            if (a.causal && first + 31 < jw) continue;
+            f32x16_t x = f32x16_t{}, g_ = f32x16_t{};
+#pragma unroll
+            for (int c = 0; c < kC; ++c) x = Mma<T>::mma(Tile<T, D>::along(qt, 32 * k + col, c, half), fk[c], x);
+#pragma unroll
+            for (int c = 0; c < kC; ++c) g_ = Mma<T>::mma(Tile<T, D>::along(yt, 32 * k + col, c, half), fv[c], g_);
+            const float* const lse = st_ + own_stats + 32 * k + 4 * half;
+            const bool all_beyond = first - (jw + 31) >= a.far, all_ahead = first + 31 - jw <= -a.far;
+            float flat = 0.f;
+            if (BIAS && (all_beyond || all_ahead)) flat = all_beyond ? ht[kTabMargin] : (a.causal ? 0.f : ht[2 * a.far + kTabMargin]);
+            const bool by_distance = BIAS && !all_beyond && !all_ahead;
+            const float* const from = by_distance ? ht + (j - first - 4 * half + a.far + kTabMargin) - 27 : nullptr;
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+                const float4 l4 = *reinterpret_cast<const float4*>(lse + 8 * n), d4 = *reinterpret_cast<const float4*>(lse + 64 + 8 * n);
+                const float l[4] = {l4.x, l4.y, l4.z, l4.w}, d[4] = {d4.x, d4.y, d4.z, d4.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int r = 4 * n + e;
+                    const float at = l[e] == -__builtin_inff() ? __builtin_inff() : l[e] * kLog2e;
+                    if (!BIAS) x[r] = __builtin_amdgcn_exp2f(fmaf(x[r], a.scale2, -at));
+                    else x[r] = __builtin_amdgcn_exp2f(fmaf(x[r], a.scale2, by_distance ? from[27 - 8 * n - e] : flat) - at);
+                    g_[r] = x[r] * (g_[r] - d[e]);
+                }
+            }
+            if (a.causal && first < jw + 31) {   // hidden: queries before the key's place
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (first + 8 * (r / 4) + 4 * half + r % 4 < j) x[r] = g_[r] = 0.f;
+            }
+#pragma unroll
+            for (int c = 0; c < kM; ++c) {
+                const uint4 p = Mma<T>::pack(x, c), ds = Mma<T>::pack(g_, c);
+#pragma unroll
+                for (int d = 0; d < kD; ++d) {
+                    dv[d] = Mma<T>::mma(Tile<T, D>::down(yt, 32 * k, c, d), p, dv[d]);
+                    dk[d] = Mma<T>::mma(Tile<T, D>::down(qt, 32 * k, c, d), ds, dk[d]);
+                }
+            }
+        }
+    };
+    if (steps > 0) fetch(0, t0, rows0, grads0, stats0);
+    int g = 0, t = t0;
+    for (int n = 0; n < steps; n += 2) {
+        step(g, t, n + 1 < steps, rows0, grads0, stats0, rows1, grads1, stats1);
+        if (++t == t0 + tiles) { t = t0; ++g; }
+        if (n + 1 >= steps) break;
+        step(g, t, n + 2 < steps, rows1, grads1, stats1, rows0, grads0, stats0);
+        if (++t == t0 + tiles) { t = t0; ++g; }
+    }
+    if (j >= q.cap) return;
+    const float by = is ? 1.f : 0.f;   // (a cache's room: zeros)
+    if (!is) {
+#pragma unroll
+        for (int d = 0; d < kD; ++d) dk[d] = dv[d] = f32x16_t{};
+    }
+    const int64_t row = q.k0 + j;
+    if (parts > 1) {
+        char* const to = reinterpret_cast<char*>(a.part_o + (((int64_t)part * a.k_rows + row) * a.kv + kvh) * D);
+        store_column<float, D>(to, dk, by, half, D);
+        store_column<float, D>(to + (int64_t)parts * a.k_rows * a.kv * D * 4, dv, by, half, D);
+    } else {
+        store_column<T, D>(const_cast<char*>(a.dk.at(row, kvh)), dk, a.scale, half, a.dim);
+        store_column<T, D>(const_cast<char*>(a.dv.at(row, kvh)), dv, 1.f, half, a.dim);
+    }
+}
+
+// Adds up the parts of a group's heads, in their order: four elements a lane.  Rows that are no sequence's are left as they are, which is
+// decided by the rows' places between the first and the last offset alone: the offsets ascend, or the call has been reported.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void attn_dkv_join_kernel(const AttnArgs a) {
+    const int64_t per = (int64_t)a.kv * (D / 4), n = a.k_rows * per;
+    const int64_t plane = a.k_rows * a.kv * D;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+        const int64_t row = i / per;
+        const int rest = (int)(i - row * per), kvh = rest / (D / 4), e = (rest - kvh * (D / 4)) * 4;
+        if (e >= a.dim) continue;
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+            float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int p = 0; p < a.splits; ++p) {
+                const float4 x = *reinterpret_cast<const float4*>(a.part_o + (which * a.splits + p) * plane + (row * a.kv + kvh) * D + e);
+                sum.x += x.x; sum.y += x.y; sum.z += x.z; sum.w += x.w;
+            }
+            const float by = which == 0 ? a.scale : 1.f;
+            char* const to = const_cast<char*>((which == 0 ? a.dk : a.dv).at(row, kvh));
+            if constexpr (sizeof(T) == 2)
+                *reinterpret_cast<uint2*>(to + 2 * e) = make_uint2(pack2((const T*)nullptr, sum.x * by, sum.y * by), pack2((const T*)nullptr, sum.z * by, sum.w * by));
+            else *reinterpret_cast<float4*>(to + 4 * e) = make_float4(sum.x * by, sum.y * by, sum.z * by, sum.w * by);
+        }
+    }
+}
+
+// How the backward shares out its work: queries and keys of long sequences by 128, of short ones by 32; the heads of a group in
+// parts where there would be too few workgroups of keys to fill the chip.
+AttnBackwardPlan attn_backward_plan(const AttnShape& sh) {
+    AttnBackwardPlan p;
+    const int64_t mean_q = (sh.q_rows + sh.N - 1) / sh.N, mean_k = (sh.k_rows + sh.N - 1) / sh.N;
+    const int group = sh.H / sh.kv;
+    p.D = sh.dim <= 32 ? 32 : (sh.dim <= 64 ? 64 : 128);
+    p.shared_q = mean_q > 64;
+    p.block_q = p.shared_q ? 128 : 32;
+    p.V_q = sh.q_rows / p.block_q + sh.N;
+    const int64_t tables = sh.buckets ? (int64_t)group * (2 * sh.far + 1 + 2 * kTabMargin) * 4 : 0;
+    p.shared_k = mean_k > 64 || tables > kTabBytes;
+    p.block_k = p.shared_k ? 128 : 32;
+    p.V_k = sh.k_rows / p.block_k + sh.N;
+    const int64_t units = (sh.k_rows / p.block_k + 1) * sh.kv, enough = p.shared_k ? 768 : 4096;
+    p.parts = 1;
+    while (p.parts < group && units * p.parts < enough) {
+        int next = p.parts + 1;
+        while (group % next != 0) ++next;
+        p.parts = next;
+    }
+    p.delta = ((size_t)sh.H * (size_t)sh.q_rows * 4 + 255) & ~(size_t)255;
+    p.part_bias = sh.buckets ? ((size_t)sh.H * (size_t)p.V_q * (size_t)sh.buckets * 4 + 255) & ~(size_t)255 : 0;
+    p.part_kv = p.parts > 1 ? 2 * (size_t)p.parts * (size_t)sh.k_rows * (size_t)sh.kv * (size_t)p.D * 4 : 0;
+    p.grid_ok = (int64_t)sh.H * p.V_q < ((int64_t)1 << 31) - 64 && (int64_t)sh.kv * p.parts * p.V_k < ((int64_t)1 << 31) - 64;
+    return p;
+}
+size_t attn_backward_workspace(const AttnShape& sh) {   // (large tables of distances make the keys' units large)
+    AttnShape near = sh, far = sh;
+    near.far = 0;
+    far.far = kAttnMaxFar;
+    size_t most = 0;
+    for (const AttnShape& x : {near, far}) {
+        const AttnBackwardPlan p = attn_backward_plan(x);
+        most = std::max(most, p.delta + p.part_bias + p.part_kv);
+    }
+    return most;
+}
+
+static hipError_t room_for(const void* kernel, const size_t bytes) {
+    return bytes > (32 << 10) ? hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) : hipSuccess;
+}
+template <typename T, int D, int SHARE, bool BIAS>
+static hipError_t launch_dq(const AttnArgs& a, hipStream_t s) {
+    constexpr int kWaves = bwd_waves<T, D, SHARE>();
+    const size_t table = BIAS ? (size_t)(1 + 2 * kWaves) * (2 * a.far + 1 + 2 * kTabMargin) * 4 : 0;
+    const uint64_t per_head = SHARE == 4 ? (uint64_t)a.V : ((uint64_t)a.V + kWaves - 1) / kWaves;
+    const hipError_t e = room_for(reinterpret_cast<const void*>(attn_dq_kernel<T, D, SHARE, BIAS>), table);
+    if (e != hipSuccess) return e;
+    attn_dq_kernel<T, D, SHARE, BIAS><<<(unsigned)((per_head * a.H + 7) / 8 * 8), 64 * kWaves, table, s>>>(a);
+    return hipGetLastError();
+}
+template <typename T, int D, int SHARE, bool BIAS>
+static hipError_t launch_dkv(const AttnArgs& a, hipStream_t s) {
+    constexpr int kWaves = bwd_waves<T, D, SHARE>();
+    const size_t table = BIAS ? (size_t)(SHARE == 4 ? 1 : a.pack) * (2 * a.far + 1 + 2 * kTabMargin) * 4 : 0;
+    const uint64_t per_head = SHARE == 4 ? (uint64_t)a.V : ((uint64_t)a.V + kWaves - 1) / kWaves;
+    attn_dkv_kernel<T, D, SHARE, BIAS><<<(unsigned)((per_head * a.kv * a.splits + 7) / 8 * 8), 64 * kWaves, table, s>>>(a);
+    return hipGetLastError();
+}
+template <typename T, int D>
+static hipError_t launch_dim(const tbe_handle* h, AttnArgs a, const AttnBackwardPlan& p, void* dbias, hipStream_t s) {
+    hipError_t e = hipSuccess;
+    if (a.q_rows > 0) {
+        a.V = (int)p.V_q; a.block = p.block_q;
+        LaunchTimer tm(h, s, "attention_dq");
+        if (p.shared_q) e = a.bias ? launch_dq<T, D, 4, true>(a, s) : launch_dq<T, D, 4, false>(a, s);
+        else e = a.bias ? launch_dq<T, D, 1, true>(a, s) : launch_dq<T, D, 1, false>(a, s);
+        tm.done();
+        if (e != hipSuccess) return e;
+    }
+    if (dbias) {
+        a.V = a.q_rows > 0 ? (int)p.V_q : 0;
+        LaunchTimer tm(h, s, "attention_dbias");
+        attn_dbias_kernel<<<dim3((a.buckets + 7) / 8, a.H), 256, 0, s>>>(a, dbias);
+        tm.done();
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    if (a.k_rows == 0) return e;
+    a.V = (int)p.V_k; a.block = p.block_k; a.splits = p.parts; a.pack = a.group / p.parts;
+    {
+        LaunchTimer tm(h, s, "attention_dkv");
+        if (p.shared_k) e = a.bias ? launch_dkv<T, D, 4, true>(a, s) : launch_dkv<T, D, 4, false>(a, s);
+        else e = a.bias ? launch_dkv<T, D, 1, true>(a, s) : launch_dkv<T, D, 1, false>(a, s);
+        tm.done();
+    }
+    if (e != hipSuccess || p.parts == 1) return e;
+    LaunchTimer tm(h, s, "attention_dkv_join");
+    const int64_t lanes = a.k_rows * a.kv * (D / 4), want = (lanes + 255) / 256;
+    attn_dkv_join_kernel<T, D><<<(unsigned)(want < 8192 ? want : 8192), 256, 0, s>>>(a);
+    tm.done();
+    return hipGetLastError();
+}
+template <typename T>
+static hipError_t launch_type(const tbe_handle* h, const AttnArgs& a, const AttnBackwardPlan& p, void* dbias, hipStream_t s) {
+    return p.D == 32 ? launch_dim<T, 32>(h, a, p, dbias, s) : (p.D == 64 ? launch_dim<T, 64>(h, a, p, dbias, s) : launch_dim<T, 128>(h, a, p, dbias, s));
+}
+
+hipError_t launch_attention_backward(const tbe_handle* h, AttnArgs a, const AttnBackwardPlan& p, int io, void* dbias, void* workspace, hipStream_t s) {
+    char* const ws = static_cast<char*>(workspace);
+    a.delta = reinterpret_cast<float*>(ws);
+    a.part_bias = reinterpret_cast<float*>(ws + p.delta);
+    a.part_o = reinterpret_cast<float*>(ws + p.delta + p.part_bias);
+    return io == 0 ? launch_type<float>(h, a, p, dbias, s) : (io == 1 ? launch_type<__half>(h, a, p, dbias, s) : launch_type<bf16_t>(h, a, p, dbias, s));
+}
+
+}  // namespace tbe

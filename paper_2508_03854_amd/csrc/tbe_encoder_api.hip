@@ -148,4 +148,25 @@ tbe_status tbe_attention(const tbe_handle* h, const tbe_attention_args* args, tb
     return done(launch_attention(h, k, p, (int)args->dtype, workspace, static_cast<hipStream_t>(hip_stream)));
 }
 
+tbe_status tbe_attention_backward(const tbe_handle* h, const tbe_attention_args* args, tbe_rows out, const float* lse, tbe_rows dout,
+                                  tbe_rows dq, tbe_rows dk, tbe_rows dv, void* dbias, void* workspace, size_t workspace_bytes,
+                                  void* hip_stream) {
+    AttnArgs k;
+    const tbe_status st = attention_args(h, args, k);
+    if (st != TBE_OK) return st;
+    if (!rows_view(out, args->q_rows, args, false, k.o) || !rows_view(dout, args->q_rows, args, false, k.dout)) return TBE_EINVAL;
+    if (!rows_view(dq, args->q_rows, args, true, k.dq) || !rows_view(dk, args->k_rows, args, true, k.dk) || !rows_view(dv, args->k_rows, args, true, k.dv)) return TBE_EINVAL;
+    if ((!lse && args->q_rows > 0) || !multiple_of(lse, 4)) return TBE_EINVAL;
+    if (dbias && (!args->bias || !multiple_of(dbias, io_size(args->bias_dtype)))) return TBE_EINVAL;
+    k.lse = const_cast<float*>(lse);
+    const AttnBackwardPlan p = attn_backward_plan(attention_shape(args));
+    const size_t need = p.delta + p.part_bias + p.part_kv;
+    if (need > 0) {
+        if (!workspace || !multiple_of(workspace, 256)) return TBE_EINVAL;
+        if (workspace_bytes < need) return TBE_EWORKSPACE;
+    }
+    if (!p.grid_ok) return TBE_ESHAPE;
+    return done(launch_attention_backward(h, k, p, (int)args->dtype, dbias, workspace, static_cast<hipStream_t>(hip_stream)));
+}
+
 }  // extern "C"

@@ -184,5 +184,14 @@ bool attn_grid_ok(const AttnShape& sh, const AttnPlan& p);   // the launches sta
 size_t attn_workspace(const AttnShape& sh, bool backward);   // for any max_distance
 struct AttnArgs;
 hipError_t launch_attention(const tbe_handle* h, AttnArgs a, const AttnPlan& p, int io, void* workspace, hipStream_t s);
+struct AttnBackwardPlan {
+    int D, block_q, block_k, parts;   // parts: of the heads of a group
+    bool shared_q, shared_k, grid_ok;
+    int64_t V_q, V_k;
+    size_t delta, part_bias, part_kv;   // bytes
+};
+AttnBackwardPlan attn_backward_plan(const AttnShape& sh);
+size_t attn_backward_workspace(const AttnShape& sh);
+hipError_t launch_attention_backward(const tbe_handle* h, AttnArgs a, const AttnBackwardPlan& p, int io, void* dbias, void* workspace, hipStream_t s);
 
 }  // namespace tbe
