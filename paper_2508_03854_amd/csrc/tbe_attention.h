@@ -58,6 +58,15 @@ struct Mma<float> {   // four products of two of the summed axis each
     }
 };
 
+// every lane's BYTES bytes to LDS, one lane's behind the other's
+template <int BYTES>
+__device__ __forceinline__ void load_lds(const void* from, void* to) {
+    const auto src = (const __attribute__((address_space(1))) void*)from;
+    const auto dst = (__attribute__((address_space(3))) void*)to;
+    if constexpr (BYTES == 16) __builtin_amdgcn_global_load_lds(src, dst, 16, 0, 0);
+    else __builtin_amdgcn_global_load_lds(src, dst, 4, 0, 0);
+}
+
 // A tile of rows of D elements in LDS, sixteen-byte chunks: chunk c of row r lies at place c ^ swizzle(r) of its row, so that neither
 // reading a column of chunks nor reading down the rows piles up on a few banks.  Rows arrive straight from memory; a wavefront's 64 chunks
 // land one behind the other, so it is the source that is permuted.
@@ -100,15 +109,20 @@ struct Tile {
     static __device__ __forceinline__ void fetch(char* lds, const char* base, const int64_t stride, const int j0, const int rows, const int dim, const int w) {
         constexpr int kLoads = ROWS * kChunks / 64 / WAVES;
         static_assert(kLoads * 64 * WAVES == ROWS * kChunks, "whole loads");
-        const bool inside = j0 + ROWS <= rows && dim == D;
         const char* const from = base + (int64_t)j0 * stride;
+        if (j0 + ROWS <= rows && dim == D) {   // (offsets that stay the same from tile to tile)
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const int n = (w * kLoads + i) * 64 + lane_id(), r = n / kChunks, c = (n % kChunks) ^ swizzle(r);
-            const char* src = from + (uint32_t)(r * (uint32_t)stride + c * 16);
-            if (!inside && (j0 + r >= rows || c * 16 >= dim * (int)sizeof(T))) src = reinterpret_cast<const char*>(&attn_zeros);
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
-                                             (__attribute__((address_space(3))) void*)(lds + (w * kLoads + i) * 1024), 16, 0, 0);
+            for (int i = 0; i < kLoads; ++i) {
+                const int n = (w * kLoads + i) * 64 + lane_id(), r = n / kChunks, c = (n % kChunks) ^ swizzle(r);
+                load_lds<16>(from + (uint32_t)(r * (uint32_t)stride + c * 16), lds + (w * kLoads + i) * 1024);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const int n = (w * kLoads + i) * 64 + lane_id(), r = n / kChunks, c = (n % kChunks) ^ swizzle(r);
+                const bool there = j0 + r < rows && c * 16 < dim * (int)sizeof(T);
+                load_lds<16>(there ? from + (uint32_t)(r * (uint32_t)stride + c * 16) : reinterpret_cast<const char*>(&attn_zeros), lds + (w * kLoads + i) * 1024);
+            }
         }
     }
 };
@@ -201,7 +215,8 @@ __device__ __forceinline__ void judge(const AttnArgs& a, const bool looks, const
 // `far` like `far` itself.  A finite bias beyond +-1e30 counts as that (so that it stays finite here); a bucket outside the table
 // counts as no bias and is reported.
 __device__ __forceinline__ int tab_size(const int far) { return 2 * far + 1 + 2 * kTabMargin; }
-__device__ __forceinline__ void fill_bias(float* tab, const AttnArgs& a, const int head0, const int heads, const int threads) {
+__device__ __forceinline__ void fill_bias(float* tab, const AttnArgs& a, const int head0, const int heads, const int threads,
+                                          uint16_t* bucket = nullptr) {
     const int size = tab_size(a.far), used = a.causal ? a.far + kTabMargin + 1 : size;
     for (int n = threadIdx.x; n < heads * used; n += threads) {
         const int g = n / used, t = n - g * used;
@@ -218,6 +233,7 @@ __device__ __forceinline__ void fill_bias(float* tab, const AttnArgs& a, const i
             *a.err = 1;
         }
         tab[g * size + t] = x;
+        if (bucket) bucket[t] = (uint16_t)((uint32_t)b < (uint32_t)a.buckets ? b : 0xFFFF);
     }
 }
 

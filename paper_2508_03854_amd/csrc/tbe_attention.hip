@@ -20,7 +20,7 @@ template <typename T, int D, int SHARE>
 constexpr int attn_waves() { return SHARE == 1 && D * (int)sizeof(T) > 256 ? 2 : 4; }
 
 template <typename T, int D>   // wavefronts of a SIMD that the registers are to leave room for
-constexpr int attn_occupancy() { return sizeof(T) == 2 ? (D == 32 ? 3 : (D == 64 ? 2 : 1)) : (D == 32 ? 2 : 1); }
+constexpr int attn_occupancy() { return sizeof(T) == 2 ? (D == 32 ? 4 : (D == 64 ? 3 : 2)) : (D == 32 ? 2 : 1); }
 
 template <typename T, int D, int SHARE, bool BIAS>
 __global__ __launch_bounds__((64 * attn_waves<T, D, SHARE>()), (attn_occupancy<T, D>())) void attn_kernel(const AttnArgs a) {
@@ -103,6 +103,16 @@ __global__ __launch_bounds__((64 * attn_waves<T, D, SHARE>()), (attn_occupancy<T
         ahead = a.causal ? 0.f : ht[2 * a.far + kTabMargin];
     }
 
+    bool met = false;      // a tile some of whose keys are hidden from some columns
+    uint64_t before = 0;   // lanes whose results were not finite before the first of them
+    auto not_finite = [&]() __attribute__((always_inline)) {
+        float test = 0.f;
+#pragma unroll
+        for (int d = 0; d < kD; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) test = fmaf(o[d][r], 0.f, test);   // 0, or NaN
+        return test != 0.f;
+    };
     auto step = [&](const int t, const char* const kt_, const char* const vt_, char* const kn, char* const vn) __attribute__((always_inline)) {
         loads_done();
         if (SHARE == 4) __syncthreads();
@@ -174,48 +184,16 @@ __global__ __launch_bounds__((64 * attn_waves<T, D, SHARE>()), (attn_occupancy<T
         for (int k = 0; k < kT; ++k)
 #pragma unroll
             for (int c = 0; c < kM; ++c) p[k][c] = Mma<T>::pack(x[k], c);
-        if (!masked) {
-#pragma unroll
-            for (int k = 0; k < kT; ++k)
-#pragma unroll
-                for (int c = 0; c < kM; ++c)
-#pragma unroll
-                    for (int d = 0; d < kD; ++d) o[d] = Mma<T>::mma(Tile<T, D>::down(vt, 32 * k, c, d), p[k][c], o[d]);
-            return;
+        if (masked && !met) {
+            met = true;
+            before = __ballot(not_finite());
         }
-        // Some probabilities are 0 because their keys are hidden, and 0 times a value that is not finite is not 0: where this tile's
-        // share of a result is not finite, it is added up once more key by key, without the hidden ones.
 #pragma unroll
-        for (int d = 0; d < kD; ++d) {
-            f32x16_t more = f32x16_t{};
+        for (int k = 0; k < kT; ++k)
 #pragma unroll
-            for (int k = 0; k < kT; ++k)
+            for (int c = 0; c < kM; ++c)
 #pragma unroll
-                for (int c = 0; c < kM; ++c) more = Mma<T>::mma(Tile<T, D>::down(vt, 32 * k, c, d), p[k][c], more);
-            float test = 0.f;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) test = fmaf(more[r], 0.f, test);   // 0, or NaN
-            if (__any(test != 0.f)) {
-                f32x16_t sure = f32x16_t{};
-#pragma unroll
-                for (int k = 0; k < kT; ++k)
-#pragma unroll 1
-                    for (int j = 0; j < 32; ++j) {
-                        int h = half;
-                        asm volatile("" : "+v"(h));   // (keeps what follows from it inside the loop, where it costs no registers)
-                        float one = 0.f;
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) one = j - 4 * h == 8 * (r / 4) + r % 4 ? x[k][r] : one;
-                        one = elem_float(elem_round<T>(__shfl(one, col + 8 * (j & 4))));
-                        if (one != 0.f)
-#pragma unroll
-                            for (int r = 0; r < 16; ++r) sure[r] = fmaf(one, Tile<T, D>::element(vt, 32 * k + j, 32 * d + 8 * (r / 4) + 4 * h + r % 4), sure[r]);
-                    }
-                if (test != 0.f) more = sure;   // (a column that was finite keeps its bits)
-            }
-#pragma unroll
-            for (int r = 0; r < 16; ++r) o[d][r] += more[r];
-        }
+                for (int d = 0; d < kD; ++d) o[d] = Mma<T>::mma(Tile<T, D>::down(vt, 32 * k, c, d), p[k][c], o[d]);
     };
     if (t0 < t1) fetch(t0, keys0, values0);
     for (int t = t0; t < t1; t += 2) {
@@ -224,6 +202,60 @@ __global__ __launch_bounds__((64 * attn_waves<T, D, SHARE>()), (attn_occupancy<T
     }
     judge(a, looks, v, peek);
     sum = pair_sum<32>(sum);
+    // The probability of a hidden key is 0, but 0 times a value that is not finite is not.  Columns whose results stopped being finite in a
+    // tile with hidden keys are computed once more, key by key, without these.
+    if (met) {
+        uint64_t bad = __ballot(not_finite()) & ~before;
+        bad |= bad >> 32 | bad << 32;
+        if (bad) {
+            const int last = t1 * BK < jend ? t1 * BK : jend, end = a.causal && pos + 1 < last ? pos + 1 : last;
+            float sm, ss;
+#pragma unroll
+            for (int d = 0; d < kD; ++d) {   // (32 elements of the result at a time: it is registers that are short)
+                f32x16_t so = f32x16_t{};
+                sm = -__builtin_inff();
+                ss = 0.f;
+#pragma unroll 1
+                for (int j = t0 * BK; j < last; ++j) {
+                    const T* const kr = reinterpret_cast<const T*>(kb + j * a.k.row);
+                    float x = 0.f;
+#pragma unroll
+                    for (int c = 0; c < kC; ++c) {
+                        const int e = kK * c + kE * half;
+                        if (e < a.dim) {
+                            float qe[kE], ke[kE];
+                            Frag<T>::unpack(fq[c], qe);
+                            Frag<T>::unpack(*reinterpret_cast<const uint4*>(kr + e), ke);
+#pragma unroll
+                            for (int n = 0; n < kE; ++n) x = fmaf(qe[n], ke[n], x);
+                        }
+                    }
+                    x = pair_sum<32>(x) * a.scale2;
+                    if (BIAS) {
+                        const int apart = pos - j;
+                        x += ht[a.far + kTabMargin - (apart > a.far ? a.far : (apart < -a.far ? -a.far : apart))];
+                    }
+                    if (j >= end || (x == -__builtin_inff() && sm == x)) continue;
+                    const float grown = fmaxf(sm, x), shrink = __builtin_amdgcn_exp2f(sm - grown);
+                    float p = __builtin_amdgcn_exp2f(x - grown);
+                    sm = grown;
+                    ss = fmaf(ss, shrink, p);
+                    p = elem_float(elem_round<T>(p));
+                    const T* const vr = reinterpret_cast<const T*>(vb + j * a.v.row);
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const int e = 32 * d + 8 * (r / 4) + 4 * half + r % 4;
+                        so[r] = fmaf(so[r], shrink, e < a.dim ? p * elem_float(vr[e]) : 0.f);
+                    }
+                }
+                if (bad >> lane & 1) o[d] = so;
+            }
+            if (bad >> lane & 1) {
+                m = sm;
+                sum = ss;
+            }
+        }
+    }
     if (!is) return;
     if (SHARE == 1 && a.splits > 1) {
         const int64_t at = (((int64_t)hh * a.V + v) * a.splits + split) * 32 + col;
@@ -270,29 +302,35 @@ __global__ __launch_bounds__(256) void attn_join_kernel(const AttnArgs a) {
     if (v < start || v - start >= blocks) return;
     const int i = (int)(blocks - 1 - (v - start)) * a.block + ci;
     if (i >= q.nq) return;
-    float m = -__builtin_inff();
-    for (int k = lane; k < a.splits; k += 64) m = fmaxf(m, a.part_ml[2 * ((hv * a.splits + k) * 32 + col)]);
+    // lane k: the maximum, sum and weight of parts k and k + 64 (there are at most 128)
+    const int64_t p0 = hv * a.splits * 32 + col;
+    const float2 none = make_float2(-__builtin_inff(), 0.f);
+    const float2 ml0 = lane < a.splits ? *reinterpret_cast<const float2*>(a.part_ml + 2 * (p0 + 32 * lane)) : none;
+    const float2 ml1 = lane + 64 < a.splits ? *reinterpret_cast<const float2*>(a.part_ml + 2 * (p0 + 32 * (lane + 64))) : none;
+    float m = fmaxf(ml0.x, ml1.x);
 #pragma unroll
     for (int w = 32; w; w >>= 1) m = fmaxf(m, __shfl_xor(m, w));
     const float at = m == -__builtin_inff() ? 0.f : m;
-    constexpr int kPer = D >= 64 ? D / 64 : 1;
-    float o[kPer], sum = 0.f;
-#pragma unroll
-    for (int e = 0; e < kPer; ++e) o[e] = 0.f;
+    const float w0 = __builtin_amdgcn_exp2f(ml0.x - at), w1 = __builtin_amdgcn_exp2f(ml1.x - at);
+    const float sum = group_sum(fmaf(ml0.y, w0, ml1.y * w1), 64);
+    constexpr int kPer = D >= 64 ? D / 64 : 1, kAhead = 8;   // elements a lane; parts under way together
+    typedef float out_t __attribute__((ext_vector_type(kPer)));
+    out_t o = {};
     const int e0 = (lane * kPer) & (D - 1);   // (rows of 32 elements: the upper half of the wavefront does the same again)
-    for (int k = 0; k < a.splits; ++k) {
-        const int64_t p = (hv * a.splits + k) * 32 + col;
-        const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + 2 * p);
-        const float w = __builtin_amdgcn_exp2f(ml.x - at);
-        sum = fmaf(ml.y, w, sum);
+    const float* const from = a.part_o + p0 * D + e0;
+    for (int k = 0; k < a.splits; k += kAhead) {
+        out_t x[kAhead];
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) o[e] = fmaf(a.part_o[p * D + e0 + e], w, o[e]);
+        for (int n = 0; n < kAhead; ++n) x[n] = *reinterpret_cast<const out_t*>(from + (int64_t)(k + n < a.splits ? k + n : k) * 32 * D);
+#pragma unroll
+        for (int n = 0; n < kAhead; ++n)
+            if (k + n < a.splits) o += bcast_lane(k + n < 64 ? w0 : w1, (k + n) & 63) * x[n];
     }
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
     T* const to = reinterpret_cast<T*>(const_cast<char*>(a.o.at(q.q0 + i, head)));
 #pragma unroll
     for (int e = 0; e < kPer; ++e)
-        if (e0 + e < a.dim) to[e0 + e] = elem_round<T>(o[e] * inv);
+        if (e0 + e < a.dim) to[e0 + e] = elem_round<T>((kPer == 1 ? o[0] : o[e]) * inv);
     if (a.lse && lane == 0) a.lse[(int64_t)head * a.q_rows + q.q0 + i] = sum == 0.f ? -__builtin_inff() : fmaf(m, kLn2, logf(sum));
 }
 

@@ -57,16 +57,14 @@ __device__ __forceinline__ void store_column(char* row, const f32x16_t (&o)[D / 
 }
 
 // dbias of a unit: its sums by distance, [from, to) of a table, added up by bucket; `lane` of `lanes` does every lanes-th bucket.
-__device__ __forceinline__ void bucket_sums(const AttnArgs& a, float* out, const float* sums, const int from, const int to, const float beyond,
-                                            const float ahead, const int lane, const int lanes) {
-    const int b_beyond = a.map[2 * a.far], b_ahead = a.map[0];
+// bucket: the bucket of every entry of the table.
+__device__ __forceinline__ void bucket_sums(const AttnArgs& a, float* out, const float* sums, const uint16_t* bucket, const int from, const int to,
+                                            const float beyond, const float ahead, const int lane, const int lanes) {
+    const int b_beyond = bucket[kTabMargin], b_ahead = bucket[2 * a.far + kTabMargin];
     for (int b = lane; b < a.buckets; b += lanes) {
-        float s = (b == b_beyond ? beyond : 0.f) + (b == b_ahead ? ahead : 0.f);
-        for (int t = from; t < to; ++t) {
-            int d = a.far + kTabMargin - t;
-            d = d > a.far ? a.far : (d < -a.far ? -a.far : d);
-            if (a.map[d + a.far] == b) s += sums[t];
-        }
+        float s = (b == b_beyond ? beyond : 0.f) + (!a.causal && b == b_ahead ? ahead : 0.f);
+#pragma unroll 8
+        for (int t = from; t < to; ++t) s += bucket[t] == b ? sums[t] : 0.f;
         out[b] = s;
     }
 }
@@ -77,15 +75,16 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (bwd_occupancy<T, 
     constexpr int kE = Mma<T>::kE, kK = Mma<T>::kK, kC = D / kK, kM = 32 / kK;
     constexpr int kTile = BK * D * (int)sizeof(T), kLds = SHARE == 4 ? kTile : kWaves * kTile;
     __shared__ __align__(16) char keys0[kLds], keys1[kLds], values0[kLds], values1[kLds];
-    extern __shared__ float tab[];   // the bias by distance, then sums by distance: two arrays of that size for each wavefront
+    extern __shared__ float tab[];   // the bias by distance, sums by distance - two arrays of that size for each wavefront -, the buckets
     const int wave = uniform(threadIdx.x >> 6), lane = lane_id(), col = lane & 31, half = lane >> 5;
     const uint32_t per_head = SHARE == 4 ? (uint32_t)a.V : ((uint32_t)a.V + kWaves - 1) / kWaves;
     const uint32_t groups = per_head * (uint32_t)a.H, wg = die_order(groups);
     if (wg >= groups) return;
     const int head = wg / per_head, size = tab_size(a.far);
     const uint32_t v = SHARE == 4 ? wg - head * per_head : (wg - head * per_head) * kWaves + wave;
+    uint16_t* const bucket = reinterpret_cast<uint16_t*>(tab + size * (1 + 2 * kWaves));
     if (BIAS) {
-        fill_bias(tab, a, head, 1, 64 * kWaves);
+        fill_bias(tab, a, head, 1, 64 * kWaves, bucket);
         for (int n = threadIdx.x; n < 2 * kWaves * size; n += 64 * kWaves) tab[size + n] = 0.f;
         __syncthreads();
     }
@@ -248,17 +247,14 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (bwd_occupancy<T, 
         for (int t = from + lane; t < to; t += 64) sums[t] += sums[size + t];
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
-    bucket_sums(a, part, SHARE == 4 ? tab + size : sums, from, to, sum_beyond, sum_ahead, me, of);
+    bucket_sums(a, part, SHARE == 4 ? tab + size : sums, bucket, from, to, sum_beyond, sum_ahead, me, of);
 }
 
 // Sums the units' shares of dbias, in their order: 8 buckets of a head a workgroup, 32 slices of the units beside each other.
 __global__ __launch_bounds__(256) void attn_dbias_kernel(const AttnArgs a, void* dbias) {
     __shared__ float part[32][9];
     const int c = threadIdx.x % 8, k = threadIdx.x / 8, b = blockIdx.x * 8 + c, head = blockIdx.y;
-    float s = 0.f;
-    if (b < a.buckets)
-        for (int64_t v = k; v < a.V; v += 32) s += a.part_bias[((int64_t)head * a.V + v) * a.buckets + b];
-    part[k][c] = s;
+    part[k][c] = b < a.buckets ? strided_sum(a.part_bias + (int64_t)head * a.V * a.buckets + b, a.buckets, k, a.V, 32) : 0.f;
     __syncthreads();
     if (k == 0 && b < a.buckets) {
         float t = 0.f;
@@ -321,9 +317,9 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (bwd_occupancy<T, 
             const float* const l = there ? a.lse + at : &attn_inf;
             const float* const d = there ? a.delta + at : reinterpret_cast<const float*>(&attn_zeros);
             if (SHARE == 1 || wave == 0)
-                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)l, (__attribute__((address_space(3))) void*)(st + own_stats), 4, 0, 0);
+                load_lds<4>(l, st + own_stats);
             if (SHARE == 1 || wave == 1)
-                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)d, (__attribute__((address_space(3))) void*)(st + own_stats + 64), 4, 0, 0);
+                load_lds<4>(d, st + own_stats + 64);
         }
     };
     f32x16_t dk[kD], dv[kD];
@@ -487,7 +483,7 @@ static hipError_t room_for(const void* kernel, const size_t bytes) {
 template <typename T, int D, int SHARE, bool BIAS>
 static hipError_t launch_dq(const AttnArgs& a, hipStream_t s) {
     constexpr int kWaves = bwd_waves<T, D, SHARE>();
-    const size_t table = BIAS ? (size_t)(1 + 2 * kWaves) * (2 * a.far + 1 + 2 * kTabMargin) * 4 : 0;
+    const size_t table = BIAS ? (size_t)(2 * a.far + 1 + 2 * kTabMargin) * ((1 + 2 * kWaves) * 4 + 2) : 0;
     const uint64_t per_head = SHARE == 4 ? (uint64_t)a.V : ((uint64_t)a.V + kWaves - 1) / kWaves;
     const hipError_t e = room_for(reinterpret_cast<const void*>(attn_dq_kernel<T, D, SHARE, BIAS>), table);
     if (e != hipSuccess) return e;

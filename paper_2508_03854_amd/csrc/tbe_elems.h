@@ -97,4 +97,18 @@ struct Frag<float> {
     }
 };
 
+// Sum of p[i * stride] for i = first, first + step, ... below n: eight loads under way together, added in their order.
+__device__ __forceinline__ float strided_sum(const float* __restrict__ p, const int64_t stride, int64_t first, const int64_t n, const int64_t step) {
+    float s = 0.f;
+    for (; first + 7 * step < n; first += 8 * step) {
+        float x[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = p[(first + k * step) * stride];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s += x[k];
+    }
+    for (; first < n; first += step) s += p[first * stride];
+    return s;
+}
+
 }  // namespace tbe

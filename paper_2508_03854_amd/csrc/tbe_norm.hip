@@ -218,19 +218,16 @@ __global__ __launch_bounds__(kNormThreads) void layer_norm_backward_kernel(const
     }
 }
 
-// Columns of the weight's and the bias's gradient: 16 columns a workgroup, 16 slices of the workgroups' sums beside each other.
+// Columns of the weight's and the bias's gradient: 8 columns a workgroup, 32 slices of the workgroups' sums beside each other.
 __global__ __launch_bounds__(256) void norm_params_kernel(const float* __restrict__ partial, const int blocks, const int n, void* dw, void* db, const int io) {
-    __shared__ float part[16][17];
-    const int c = threadIdx.x % 16, k = threadIdx.x / 16, e = blockIdx.x * 16 + c;
-    float s = 0.f;
-    if (e < 2 * n)
-        for (int i = k; i < blocks; i += 16) s += partial[(int64_t)i * 2 * n + e];
-    part[k][c] = s;
+    __shared__ float part[32][9];
+    const int c = threadIdx.x % 8, k = threadIdx.x / 8, e = blockIdx.x * 8 + c;
+    part[k][c] = e < 2 * n ? strided_sum(partial + e, 2 * n, k, blocks, 32) : 0.f;
     __syncthreads();
     if (k == 0 && e < 2 * n) {
         float t = 0.f;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) t += part[i][c];
+        for (int i = 0; i < 32; ++i) t += part[i][c];
         void* const to = e < n ? dw : db;
         if (to) param_store(to, io, e < n ? e : e - n, t);
     }
@@ -323,7 +320,7 @@ hipError_t launch_layer_norm_backward(const tbe_handle* h, const void* dy, int64
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !a.partial) return e;
     LaunchTimer tp(h, s, "layer_norm_params");
-    norm_params_kernel<<<(2 * n + 15) / 16, 256, 0, s>>>(a.partial, norm_backward_blocks(rows, n, io == 0 ? 4 : 8), n, dw, db, param_io);
+    norm_params_kernel<<<(2 * n + 7) / 8, 256, 0, s>>>(a.partial, norm_backward_blocks(rows, n, io == 0 ? 4 : 8), n, dw, db, param_io);
     tp.done();
     return hipGetLastError();
 }
