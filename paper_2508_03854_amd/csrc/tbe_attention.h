@@ -67,6 +67,18 @@ __device__ __forceinline__ void load_lds(const void* from, void* to) {
     else __builtin_amdgcn_global_load_lds(src, dst, 4, 0, 0);
 }
 
+// Ends a run of matrix products whose results are next read on the other side of a branch.  A result may be read by a vector instruction only
+// 11 (16-bit types) or 18 (fp32) issue slots after its product; the hardware does not wait, and the compiler, which has to fill in
+// the slots, was seen to count them along one of the branch's two ways only (7 slots on the other, and results of the last product but
+// partly there).
+template <typename T>
+__device__ __forceinline__ void settle() {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_nop 15");
+    if constexpr (sizeof(T) == 4) asm volatile("s_nop 3");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
 // A tile of rows of D elements in LDS, sixteen-byte chunks: chunk c of row r lies at place c ^ swizzle(r) of its row, so that neither
 // reading a column of chunks nor reading down the rows piles up on a few banks.  Rows arrive straight from memory; a wavefront's 64 chunks
 // land one behind the other, so it is the source that is permuted.
@@ -161,6 +173,7 @@ struct AttnArgs {
     int32_t* err;
     // how queries are shared out: a unit has `pack` heads of a group side by side and qpt queries of each per 32 columns
     int pack, qpt, block, V, splits;   // block: queries of a unit; V: units of a head that the sequences may need; splits of the keys
+    int together;             // the wavefronts of a workgroup take parts of one split's keys and join them
     float *part_o, *part_ml;
     float* part_bias;
 };

@@ -12,8 +12,9 @@
 namespace tbe {
 
 // SHARE = 4: the four wavefronts of a workgroup take neighbouring queries of one head and share the tiles of keys and values.
-// SHARE = 1: every wavefront is on its own, with `pack` heads of a group side by side in its columns and, with splits > 1, one of several
-// parts of the keys; the parts are joined by attn_join_kernel.
+// SHARE = 1: every wavefront is on its own, with `pack` heads of a group side by side in its columns; or (together) the wavefronts of a
+// workgroup have the same columns and a part of the keys each, joined in LDS, and with splits > 1 several workgroups do, joined by
+// attn_join_kernel.
 template <typename T, int D, int SHARE>
 constexpr int kv_rows() { return SHARE == 4 && D * (int)sizeof(T) <= 256 ? 64 : 32; }
 template <typename T, int D, int SHARE>
@@ -32,7 +33,8 @@ __global__ __launch_bounds__((64 * attn_waves<T, D, SHARE>()), (attn_occupancy<T
     __shared__ __align__(16) char keys0[kLds], keys1[kLds], values0[kLds], values1[kLds];
     extern __shared__ float tab[];
     const int wave = uniform(threadIdx.x >> 6), lane = lane_id(), col = lane & 31, half = lane >> 5;
-    const uint32_t per_head = SHARE == 4 ? (uint32_t)a.V : ((uint32_t)a.V * a.splits + kWaves - 1) / kWaves;
+    const bool together = SHARE == 1 && a.together;
+    const uint32_t per_head = SHARE == 4 || together ? (uint32_t)a.V * a.splits : ((uint32_t)a.V + kWaves - 1) / kWaves;
     const uint32_t groups = per_head * (uint32_t)(a.H / a.pack), wg = die_order(groups);
     if (wg >= groups) return;
     const int hh = wg / per_head, head0 = hh * a.pack;
@@ -41,11 +43,11 @@ __global__ __launch_bounds__((64 * attn_waves<T, D, SHARE>()), (attn_occupancy<T
         fill_bias(tab, a, head0, a.pack, 64 * kWaves);
         __syncthreads();
     }
-    const uint32_t unit = SHARE == 4 ? item : item * kWaves + wave;
+    const uint32_t unit = SHARE == 4 || together ? item : item * kWaves + wave;
     if (unit >= (uint32_t)a.V * a.splits) return;
     const uint32_t v = SHARE == 4 ? unit : unit / a.splits;
     const int split = SHARE == 4 ? 0 : unit - v * a.splits;
-    const bool looks = hh == 0 && split == 0 && (SHARE == 1 || wave == 0) && v < (uint32_t)a.N;
+    const bool looks = hh == 0 && split == 0 && ((SHARE == 1 && !together) || wave == 0) && v < (uint32_t)a.N;
     const int64_t peek = looks ? sequence_numbers(a, v) : 0;
     const int s = find_sequence(a.q_off, a.N, v, a.block);
     Sequence q;
@@ -79,8 +81,8 @@ __global__ __launch_bounds__((64 * attn_waves<T, D, SHARE>()), (attn_occupancy<T
         jend = jend < last ? jend : last;
     }
     const int tiles = jend > 0 ? (jend + BK - 1) / BK : 0;
-    const int part = SHARE == 4 ? tiles : (tiles + a.splits - 1) / a.splits;
-    const int t0 = uniform(split * part), t1 = uniform(t0 + part < tiles ? t0 + part : tiles);
+    const int parts = SHARE == 4 ? 1 : (together ? a.splits * kWaves : 1), part = (tiles + parts - 1) / parts;
+    const int t0 = uniform(SHARE == 4 || !together ? 0 : (split * kWaves + wave) * part), t1 = uniform(t0 + part < tiles ? t0 + part : tiles);
     const int wave_last = first + a.qpt - 1;   // the last place that a query of this wavefront may have
 
     const int kvh = head0 / a.group;
@@ -128,6 +130,7 @@ __global__ __launch_bounds__((64 * attn_waves<T, D, SHARE>()), (attn_occupancy<T
 #pragma unroll
             for (int c = 0; c < kC; ++c) x[k] = Mma<T>::mma(Tile<T, D>::along(kt, 32 * k + col, c, half), fq[c], x[k]);
         }
+        settle<T>();
         if (BIAS) {
 #pragma unroll
             for (int k = 0; k < kT; ++k) {
@@ -194,6 +197,7 @@ __global__ __launch_bounds__((64 * attn_waves<T, D, SHARE>()), (attn_occupancy<T
             for (int c = 0; c < kM; ++c)
 #pragma unroll
                 for (int d = 0; d < kD; ++d) o[d] = Mma<T>::mma(Tile<T, D>::down(vt, 32 * k, c, d), p[k][c], o[d]);
+        settle<T>();
     };
     if (t0 < t1) fetch(t0, keys0, values0);
     for (int t = t0; t < t1; t += 2) {
@@ -256,18 +260,59 @@ __global__ __launch_bounds__((64 * attn_waves<T, D, SHARE>()), (attn_occupancy<T
             }
         }
     }
-    if (!is) return;
-    if (SHARE == 1 && a.splits > 1) {
-        const int64_t at = (((int64_t)hh * a.V + v) * a.splits + split) * 32 + col;
-        if (half == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * at) = make_float2(m, sum);
-        float* const to = a.part_o + at * D;
+    if (SHARE == 1 && together) {
+        // The parts' results meet where the tiles were, as fp32 rows of D elements, sixteen bytes of a row at place c ^ column: a column's
+        // lanes do not all fall on the same banks.
+        constexpr int kRow = D / 4;
+        auto piece = [&](const int w) __attribute__((always_inline)) {
+            return sizeof(T) == 2 ? (w < 2 ? keys0 : keys1) + (w & 1) * 128 * D : keys0 + w * 128 * D;
+        };
+        __shared__ float2 stats[kWaves * 32];
+        __syncthreads();
+        {
+            char* const to = piece(wave);
 #pragma unroll
-        for (int d = 0; d < kD; ++d)
+            for (int d = 0; d < kD; ++d)
 #pragma unroll
-            for (int r = 0; r < 16; r += 4)
-                *reinterpret_cast<float4*>(to + 32 * d + 2 * r + 4 * half) = make_float4(o[d][r], o[d][r + 1], o[d][r + 2], o[d][r + 3]);
+                for (int r = 0; r < 16; r += 4)
+                    *reinterpret_cast<float4*>(to + (col * kRow + ((8 * d + r / 2 + half) ^ (col % kRow))) * 16) = make_float4(o[d][r], o[d][r + 1], o[d][r + 2], o[d][r + 3]);
+            if (half == 0) stats[wave * 32 + col] = make_float2(m, sum);
+        }
+        __syncthreads();
+        for (int n = threadIdx.x; n < 32 * kRow; n += 64 * kWaves) {
+            const int c = n / kRow, e = n % kRow, cc = c / a.pack, ii = iw + cc, hd = head0 + c - cc * a.pack;
+            if (cc >= a.qpt || ii >= q.nq) continue;
+            float top = -__builtin_inff(), total = 0.f;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) top = fmaxf(top, stats[w * 32 + c].x);
+            const float at = top == -__builtin_inff() ? 0.f : top;
+            float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                const float2 ms = stats[w * 32 + c];
+                const float by = __builtin_amdgcn_exp2f(ms.x - at);
+                const float4 y = *reinterpret_cast<const float4*>(piece(w) + (c * kRow + (e ^ (c % kRow))) * 16);
+                total = fmaf(ms.y, by, total);
+                x.x = fmaf(y.x, by, x.x); x.y = fmaf(y.y, by, x.y);
+                x.z = fmaf(y.z, by, x.z); x.w = fmaf(y.w, by, x.w);
+            }
+            if (a.splits > 1) {
+                const int64_t cell = (((int64_t)hh * a.V + v) * a.splits + split) * 32 + c;
+                if (e == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * cell) = make_float2(top, total);
+                *reinterpret_cast<float4*>(a.part_o + cell * D + 4 * e) = x;
+                continue;
+            }
+            const float inv = total == 0.f ? 0.f : 1.f / total;
+            if (4 * e < a.dim) {
+                char* const to = const_cast<char*>(a.o.at(q.q0 + ii, hd)) + 4 * e * sizeof(T);
+                if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(to) = make_uint2(pack2((const T*)nullptr, x.x * inv, x.y * inv), pack2((const T*)nullptr, x.z * inv, x.w * inv));
+                else *reinterpret_cast<float4*>(to) = make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv);
+            }
+            if (a.lse && e == 0) a.lse[(int64_t)hd * a.q_rows + q.q0 + ii] = total == 0.f ? -__builtin_inff() : fmaf(top, kLn2, logf(total));
+        }
         return;
     }
+    if (!is) return;
     const float inv = sum == 0.f ? 0.f : 1.f / sum;   // (no key seen: zeros)
     char* const to = const_cast<char*>(a.o.at(q.q0 + i, head));
 #pragma unroll
@@ -355,12 +400,12 @@ AttnPlan attn_plan(const AttnShape& sh, const int max_pack) {
         p.qpt = p.block = 32 / p.pack;
     }
     p.V = sh.q_rows / p.block + sh.N;
+    p.together = false;
     if (!p.shared) {
         const int64_t units = (sh.q_rows / p.block < sh.N ? sh.N : sh.q_rows / p.block + sh.N / 2) * (sh.H / p.pack);
-        int64_t want = units > 0 ? 2048 / units : 1;
-        const int64_t most = mean_k / 256;
-        want = want < most ? want : most;
-        p.splits = (int)(want < 1 ? 1 : (want > 128 ? 128 : want));
+        const int64_t want = std::min(units > 0 ? 2048 / units : 1, mean_k / 128);
+        p.together = want > 1;
+        p.splits = (int)std::min<int64_t>(128, std::max<int64_t>(1, (want + 3) / 4));
     }
     const int64_t cells = (int64_t)(sh.H / p.pack) * p.V * p.splits * 32;
     p.part_ml = p.splits > 1 ? ((size_t)cells * 8 + 255) & ~(size_t)255 : 0;
@@ -387,7 +432,7 @@ template <typename T, int D, int SHARE, bool BIAS>
 static hipError_t launch_one(const AttnArgs& a, hipStream_t s) {
     constexpr int kWaves = attn_waves<T, D, SHARE>();
     const size_t table = BIAS ? (size_t)a.pack * (2 * a.far + 1 + 2 * kTabMargin) * 4 : 0;
-    const uint64_t per_head = SHARE == 4 ? (uint64_t)a.V : ((uint64_t)a.V * a.splits + kWaves - 1) / kWaves;
+    const uint64_t per_head = SHARE == 4 || a.together ? (uint64_t)a.V * a.splits : ((uint64_t)a.V + kWaves - 1) / kWaves;
     const uint64_t groups = per_head * (uint64_t)(a.H / a.pack);
     attn_kernel<T, D, SHARE, BIAS><<<(unsigned)((groups + 7) / 8 * 8), 64 * kWaves, table, s>>>(a);
     return hipGetLastError();
@@ -413,7 +458,7 @@ static hipError_t launch_type(const tbe_handle* h, const AttnArgs& a, const Attn
 }
 
 hipError_t launch_attention(const tbe_handle* h, AttnArgs a, const AttnPlan& p, int io, void* workspace, hipStream_t s) {
-    a.pack = p.pack; a.qpt = p.qpt; a.block = p.block; a.V = (int)p.V; a.splits = p.splits;
+    a.pack = p.pack; a.qpt = p.qpt; a.block = p.block; a.V = (int)p.V; a.splits = p.splits; a.together = p.together;
     a.part_ml = static_cast<float*>(workspace);
     a.part_o = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.part_ml);
     return io == 0 ? launch_type<float>(h, a, p, s) : (io == 1 ? launch_type<__half>(h, a, p, s) : launch_type<bf16_t>(h, a, p, s));

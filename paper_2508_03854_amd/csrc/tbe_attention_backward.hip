@@ -110,8 +110,23 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (bwd_occupancy<T, 
     uint4 fq[kC], fy[kC];
     column_row<T, D>(fq, a.q.at(row, head), is, half, a.dim);
     column_row<T, D>(fy, a.dout.at(row, head), is, half, a.dim);
+    if (a.negative) flip_signs<T, kC>(fq);
+    float lse = is ? a.lse[(int64_t)head * a.q_rows + row] : 0.f;
+    lse = lse == -__builtin_inff() ? __builtin_inff() : lse * kLog2e;   // (a row that saw nothing: all its probabilities 2^-inf)
+
+    int jend = q.nk;
+    if (a.causal) {
+        const int last = q.nk - q.nq + (i0 + a.block < q.nq ? i0 + a.block : q.nq);
+        jend = jend < last ? jend : last;
+    }
+    const int tiles = uniform(jend > 0 ? (jend + BK - 1) / BK : 0);
+    // D of a row from its few keys' P and dP, or else from the forward's result.  That was rounded, which against the sum over few keys is
+    // as much as the rounding of dS and of the gradient: 4096 bfloat16 sequences of 12 events on average have dq 1.6 times as far from
+    // 64 bits as a single rounding with the latter alone, 1.4 times with the former up to kFew tiles.
+    constexpr int kFew = 4;
+    const bool few = tiles <= kFew, one = kT == 1 && tiles == 1;
     float delta = 0.f;
-    {
+    if (!few) {
         uint4 fo[kC];
         column_row<T, D>(fo, a.o.at(row, head), is, half, a.dim);
 #pragma unroll
@@ -124,17 +139,6 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (bwd_occupancy<T, 
         }
         delta = pair_sum<32>(delta);
     }
-    if (a.negative) flip_signs<T, kC>(fq);
-    float lse = is ? a.lse[(int64_t)head * a.q_rows + row] : 0.f;
-    lse = lse == -__builtin_inff() ? __builtin_inff() : lse * kLog2e;   // (a row that saw nothing: all its probabilities 2^-inf)
-    if (is && half == 0) const_cast<float*>(a.delta)[(int64_t)head * a.q_rows + row] = delta;
-
-    int jend = q.nk;
-    if (a.causal) {
-        const int last = q.nk - q.nq + (i0 + a.block < q.nq ? i0 + a.block : q.nq);
-        jend = jend < last ? jend : last;
-    }
-    const int tiles = uniform(jend > 0 ? (jend + BK - 1) / BK : 0);
     const int kvh = head / a.group;
     const char* const kb = a.k.at(q.k0, kvh);
     const char* const vb = a.v.at(q.k0, kvh);
@@ -152,6 +156,7 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (bwd_occupancy<T, 
         beyond = tab[kTabMargin];
         ahead = a.causal ? 0.f : tab[2 * a.far + kTabMargin];
     }
+    bool sums_only = few && !one;   // a first run over the keys for D alone
     auto step = [&](const int t, const char* const kt_, const char* const vt_, char* const kn, char* const vn) __attribute__((always_inline)) {
         loads_done();
         if (SHARE == 4) __syncthreads();
@@ -167,6 +172,7 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (bwd_occupancy<T, 
             for (int c = 0; c < kC; ++c) x = Mma<T>::mma(Tile<T, D>::along(kt, 32 * k + col, c, half), fq[c], x);
 #pragma unroll
             for (int c = 0; c < kC; ++c) g = Mma<T>::mma(Tile<T, D>::along(vt, 32 * k + col, c, half), fy[c], g);
+            settle<T>();
             const bool all_beyond = first - (j0 + 31) >= a.far, all_ahead = wave_last - j0 <= -a.far;
             const int at = j0 + 4 * half - pos + a.far + kTabMargin;   // of this lane's first key among the distances
             if (!BIAS) {
@@ -181,14 +187,22 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (bwd_occupancy<T, 
 #pragma unroll
                 for (int r = 0; r < 16; ++r) x[r] = __builtin_amdgcn_exp2f(fmaf(x[r], a.scale2, from[8 * (r / 4) + r % 4]) - lse);
             }
-#pragma unroll
-            for (int r = 0; r < 16; ++r) g[r] = x[r] * (g[r] - delta);
             if (j0 + 32 > q.nk || (a.causal && j0 + 31 > first)) {
                 const int end = a.causal && pos + 1 < q.nk ? pos + 1 : q.nk;
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
-                    if (j0 + 8 * (r / 4) + 4 * half + r % 4 >= end) g[r] = 0.f;
+                    if (j0 + 8 * (r / 4) + 4 * half + r % 4 >= end) x[r] = g[r] = 0.f;
             }
+            if (sums_only || one) {
+                float sum = 0.f;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) sum = fmaf(x[r], g[r], sum);
+                delta += sum;
+                if (sums_only) continue;
+                delta = pair_sum<32>(delta);
+            }
+#pragma unroll
+            for (int r = 0; r < 16; ++r) g[r] = x[r] * (g[r] - delta);
             if (BIAS && is) {
                 if (all_beyond || all_ahead) {
                     float sum = 0.f;
@@ -210,14 +224,22 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (bwd_occupancy<T, 
 #pragma unroll
                 for (int d = 0; d < kD; ++d) dq[d] = Mma<T>::mma(Tile<T, D>::down(kt, 32 * k, c, d), p, dq[d]);
             }
+            settle<T>();
         }
     };
-    if (tiles > 0) fetch(0, keys0, values0);
-    for (int t = 0; t < tiles; t += 2) {
-        step(t, keys0, values0, keys1, values1);
-        if (t + 1 < tiles) step(t + 1, keys1, values1, keys0, values0);
+    for (;;) {
+        if (tiles > 0) fetch(0, keys0, values0);
+        for (int t = 0; t < tiles; t += 2) {
+            step(t, keys0, values0, keys1, values1);
+            if (t + 1 < tiles) step(t + 1, keys1, values1, keys0, values0);
+        }
+        if (!sums_only) break;
+        sums_only = false;
+        delta = pair_sum<32>(delta);
+        if (SHARE == 4) __syncthreads();   // (the first tile's place may still be read)
     }
     judge(a, looks, v, peek);
+    if (is && half == 0) const_cast<float*>(a.delta)[(int64_t)head * a.q_rows + row] = delta;
     if (is) store_column<T, D>(const_cast<char*>(a.dq.at(row, head)), dq, a.scale, half, a.dim);
     if (!BIAS) return;
     // the distances that this unit has met
@@ -351,6 +373,7 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (bwd_occupancy<T, 
             for (int c = 0; c < kC; ++c) x = Mma<T>::mma(Tile<T, D>::along(qt, 32 * k + col, c, half), fk[c], x);
 #pragma unroll
             for (int c = 0; c < kC; ++c) g_ = Mma<T>::mma(Tile<T, D>::along(yt, 32 * k + col, c, half), fv[c], g_);
+            settle<T>();
             const float* const lse = st_ + own_stats + 32 * k + 4 * half;
             const bool all_beyond = first - (jw + 31) >= a.far, all_ahead = first + 31 - jw <= -a.far;
             float flat = 0.f;
@@ -384,6 +407,7 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (bwd_occupancy<T, 
                     dk[d] = Mma<T>::mma(Tile<T, D>::down(qt, 32 * k, c, d), ds, dk[d]);
                 }
             }
+            settle<T>();
         }
     };
     if (steps > 0) fetch(0, t0, rows0, grads0, stats0);

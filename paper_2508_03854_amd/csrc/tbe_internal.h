@@ -174,6 +174,7 @@ struct AttnShape {
 struct AttnPlan {
     int D;        // elements of a row as the kernels have it
     bool shared;  // wavefronts of a workgroup share tiles
+    bool together;   // ... or take parts of the same keys
     int pack, qpt, block, splits;
     int64_t V;
     size_t part_ml, part_o;   // bytes
