@@ -22,7 +22,7 @@ typedef short s16x4_t __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ int uniform(const int x) { return __builtin_amdgcn_readfirstlane(x); }
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
-constexpr int kTabMargin = 64;         // a tile that reaches into the table of distances reaches at most 63 beyond its ends
+constexpr int kTabMargin = 68;         // a tile that reaches into the table of distances reaches at most 66 beyond its ends
 constexpr int kTabBytes = 24 << 10;    // LDS for such tables
 
 // Sixteen zero bytes: what stands behind a sequence's end, or behind a row's, is read from here.
@@ -30,7 +30,7 @@ static __device__ const uint4 attn_zeros = {0u, 0u, 0u, 0u};
 
 template <typename T>
 struct Mma {   // 16-bit types: fragments of 8 elements a lane, 16 of the summed axis at a time
-    static constexpr int kE = 8, kK = 16;
+    static constexpr int kE = 8, kK = 16, kDown = 2, kMfmas = 1;   // kDown: LDS reads of a fragment down the rows; kMfmas: of its product
     static __device__ __forceinline__ f32x16_t mma(const uint4 a, const uint4 b, const f32x16_t c) {
         if constexpr (__is_same(T, bf16_t))
             return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
@@ -46,7 +46,7 @@ struct Mma {   // 16-bit types: fragments of 8 elements a lane, 16 of the summed
 };
 template <>
 struct Mma<float> {   // four products of two of the summed axis each
-    static constexpr int kE = 4, kK = 8;
+    static constexpr int kE = 4, kK = 8, kDown = 4, kMfmas = 4;
     static __device__ __forceinline__ f32x16_t mma(const uint4 a, const uint4 b, f32x16_t c) {
         c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.x), __uint_as_float(b.x), c, 0, 0, 0);
         c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.y), __uint_as_float(b.y), c, 0, 0, 0);
@@ -77,6 +77,22 @@ __device__ __forceinline__ void settle() {
     asm volatile("s_nop 15");
     if constexpr (sizeof(T) == 4) asm volatile("s_nop 3");
     __builtin_amdgcn_sched_barrier(0);
+}
+
+// How a run of N products of fragments from LDS is to be put in order: the reads of AHEAD fragments under way before the first product, then
+// a product for every further fragment.  READS, MFMAS: instructions of a fragment.
+template <int N, int READS, int MFMAS, int AHEAD>
+__device__ __forceinline__ void reads_ahead() {
+    constexpr int kAhead = AHEAD < N ? AHEAD : N;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+#pragma unroll
+    for (int i = 0; i < N - kAhead; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, MFMAS, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) __builtin_amdgcn_sched_group_barrier(0x008, MFMAS, 0);
 }
 
 // A tile of rows of D elements in LDS, sixteen-byte chunks: chunk c of row r lies at place c ^ swizzle(r) of its row, so that neither
@@ -161,7 +177,7 @@ struct RowsView {
 struct AttnArgs {
     RowsView q, k, v, o, dout, dq, dk, dv;
     float* lse;               // [H][q_rows]
-    const float* delta;       // [H][q_rows]: the backward's row sums of dout * out
+    float *delta, *lse2;      // [H][q_rows] of the backward: row sums of P dP; lse as an exponent of 2, +infinity for rows that saw nothing
     IdxView q_off, k_off, k_len;   // k_len.p may be null
     int N, H, kv, group, dim, causal;
     int64_t q_rows, k_rows;

@@ -20,11 +20,11 @@ constexpr int kv_rows() { return SHARE == 4 && D * (int)sizeof(T) <= 256 ? 64 : 
 template <typename T, int D, int SHARE>
 constexpr int attn_waves() { return SHARE == 1 && D * (int)sizeof(T) > 256 ? 2 : 4; }
 
-template <typename T, int D>   // wavefronts of a SIMD that the registers are to leave room for
-constexpr int attn_occupancy() { return sizeof(T) == 2 ? (D == 32 ? 4 : (D == 64 ? 3 : 2)) : (D == 32 ? 2 : 1); }
+template <typename T, int D, int SHARE>   // wavefronts of a SIMD that the registers are to leave room for (and the LDS does)
+constexpr int attn_occupancy() { return sizeof(T) == 4 ? (D == 32 ? 2 : 1) : (D == 32 ? 4 : (D == 64 ? (SHARE == 4 ? 3 : 2) : (SHARE == 4 ? 2 : 1))); }
 
 template <typename T, int D, int SHARE, bool BIAS>
-__global__ __launch_bounds__((64 * attn_waves<T, D, SHARE>()), (attn_occupancy<T, D>())) void attn_kernel(const AttnArgs a) {
+__global__ __launch_bounds__((64 * attn_waves<T, D, SHARE>()), (attn_occupancy<T, D, SHARE>())) void attn_kernel(const AttnArgs a) {
     constexpr int kWaves = attn_waves<T, D, SHARE>(), BK = kv_rows<T, D, SHARE>(), kT = BK / 32, kD = D / 32;
     constexpr int kE = Mma<T>::kE, kK = Mma<T>::kK, kC = D / kK, kM = 32 / kK;
     constexpr int kTile = BK * D * (int)sizeof(T);
@@ -130,6 +130,7 @@ __global__ __launch_bounds__((64 * attn_waves<T, D, SHARE>()), (attn_occupancy<T
 #pragma unroll
             for (int c = 0; c < kC; ++c) x[k] = Mma<T>::mma(Tile<T, D>::along(kt, 32 * k + col, c, half), fq[c], x[k]);
         }
+        reads_ahead<kT * kC, 1, Mma<T>::kMfmas, 4>();
         settle<T>();
         if (BIAS) {
 #pragma unroll
@@ -197,6 +198,7 @@ __global__ __launch_bounds__((64 * attn_waves<T, D, SHARE>()), (attn_occupancy<T
             for (int c = 0; c < kM; ++c)
 #pragma unroll
                 for (int d = 0; d < kD; ++d) o[d] = Mma<T>::mma(Tile<T, D>::down(vt, 32 * k, c, d), p[k][c], o[d]);
+        reads_ahead<kT * kM * kD, Mma<T>::kDown, Mma<T>::kMfmas, 4>();
         settle<T>();
     };
     if (t0 < t1) fetch(t0, keys0, values0);

@@ -19,8 +19,10 @@ template <typename T, int D, int SHARE>
 constexpr int bwd_rows() { return SHARE == 4 && D * (int)sizeof(T) <= 128 ? 64 : 32; }
 template <typename T, int D, int SHARE>
 constexpr int bwd_waves() { return SHARE == 4 ? 4 : (D * (int)sizeof(T) <= 128 ? 4 : (D * (int)sizeof(T) <= 256 ? 2 : 1)); }
+template <typename T, int D, int SHARE>   // wavefronts of a SIMD that the registers are to leave room for
+constexpr int dq_occupancy() { return sizeof(T) == 2 && (D <= 64 || SHARE == 4) ? 2 : 1; }
 template <typename T, int D>
-constexpr int bwd_occupancy() { return sizeof(T) == 2 && D <= 64 ? 2 : 1; }
+constexpr int dkv_occupancy() { return sizeof(T) == 2 && D <= 64 ? 2 : 1; }
 
 // The fragments of one column's row of D elements, dim of them there; nothing: zeros
 template <typename T, int D>
@@ -56,6 +58,33 @@ __device__ __forceinline__ void store_column(char* row, const f32x16_t (&o)[D / 
         }
 }
 
+// Sums along the diagonals of a tile of 32 keys (rows: registers) by 32 queries (columns: lanes): lane `col` of a half gets, for that half's
+// rows, which begin at 4 * half, the sums for key - query = 4 half - col (first) and 32 + 4 half - col (second).
+// Row 16 c + n of the tile moved n lanes down its 16-lane row has one diagonal per lane, but for the lanes that it leaves, which are the
+// ends of the next diagonals 16 away: a shift one way and the other, each part of an addition.  No trip through the LDS: one
+// addition to an LDS word per value took 215 clocks for a wavefront's 64.
+template <int R>
+__device__ __forceinline__ void diagonal_row(const f32x16_t& g, float (&d)[3]) {
+    constexpr int n = 8 * ((R / 4) % 2) + R % 4, c = R / 8;
+    if constexpr (n == 0) {
+        d[c] += g[R];
+    } else {
+        d[c] += dpp_lane<0x100 + n>(g[R]);            // row_shl:n, zeros from beyond
+        d[c + 1] += dpp_lane<0x110 + 16 - n>(g[R]);   // row_shr:16-n
+    }
+}
+__device__ __forceinline__ float2 diagonal_sums(const f32x16_t& g) {
+    float d[3] = {0.f, 0.f, 0.f};   // key - query = 4 half + 16 (i - lane row) - lane in row
+    diagonal_row<0>(g, d); diagonal_row<1>(g, d); diagonal_row<2>(g, d); diagonal_row<3>(g, d);
+    diagonal_row<4>(g, d); diagonal_row<5>(g, d); diagonal_row<6>(g, d); diagonal_row<7>(g, d);
+    diagonal_row<8>(g, d); diagonal_row<9>(g, d); diagonal_row<10>(g, d); diagonal_row<11>(g, d);
+    diagonal_row<12>(g, d); diagonal_row<13>(g, d); diagonal_row<14>(g, d); diagonal_row<15>(g, d);
+    const unsigned u = __float_as_uint(d[1]);
+    const auto rows = __builtin_amdgcn_permlane16_swap(u, u, false, false);   // the even and the odd row's d[1], each in both
+    const bool odd = lane_id() & 16;
+    return make_float2(d[0] + (odd ? 0.f : __uint_as_float(rows[1])), d[2] + (odd ? __uint_as_float(rows[0]) : 0.f));
+}
+
 // dbias of a unit: its sums by distance, [from, to) of a table, added up by bucket; `lane` of `lanes` does every lanes-th bucket.
 // bucket: the bucket of every entry of the table.
 __device__ __forceinline__ void bucket_sums(const AttnArgs& a, float* out, const float* sums, const uint16_t* bucket, const int from, const int to,
@@ -70,7 +99,7 @@ __device__ __forceinline__ void bucket_sums(const AttnArgs& a, float* out, const
 }
 
 template <typename T, int D, int SHARE, bool BIAS>
-__global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (bwd_occupancy<T, D>())) void attn_dq_kernel(const AttnArgs a) {
+__global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dq_occupancy<T, D, SHARE>())) void attn_dq_kernel(const AttnArgs a) {
     constexpr int kWaves = bwd_waves<T, D, SHARE>(), BK = bwd_rows<T, D, SHARE>(), kT = BK / 32, kD = D / 32;
     constexpr int kE = Mma<T>::kE, kK = Mma<T>::kK, kC = D / kK, kM = 32 / kK;
     constexpr int kTile = BK * D * (int)sizeof(T), kLds = SHARE == 4 ? kTile : kWaves * kTile;
@@ -111,7 +140,7 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (bwd_occupancy<T, 
     column_row<T, D>(fq, a.q.at(row, head), is, half, a.dim);
     column_row<T, D>(fy, a.dout.at(row, head), is, half, a.dim);
     if (a.negative) flip_signs<T, kC>(fq);
-    float lse = is ? a.lse[(int64_t)head * a.q_rows + row] : 0.f;
+    float lse = is ? a.lse[(int64_t)head * a.q_rows + row] : __builtin_inff();   // (columns without a query: probabilities 0)
     lse = lse == -__builtin_inff() ? __builtin_inff() : lse * kLog2e;   // (a row that saw nothing: all its probabilities 2^-inf)
 
     int jend = q.nk;
@@ -150,7 +179,8 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (bwd_occupancy<T, 
     f32x16_t dq[kD];
 #pragma unroll
     for (int d = 0; d < kD; ++d) dq[d] = f32x16_t{};
-    float beyond = 0.f, ahead = 0.f, sum_beyond = 0.f, sum_ahead = 0.f;
+    float beyond = 0.f, ahead = 0.f, sum_beyond = 0.f, sum_ahead = 0.f, carry = 0.f;
+    int carry_at = -1;   // the first key of the tile whose store the carry waits for
     float* const sums = tab + size * (1 + 2 * (BIAS ? wave : 0));
     if (BIAS) {
         beyond = tab[kTabMargin];
@@ -172,6 +202,7 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (bwd_occupancy<T, 
             for (int c = 0; c < kC; ++c) x = Mma<T>::mma(Tile<T, D>::along(kt, 32 * k + col, c, half), fq[c], x);
 #pragma unroll
             for (int c = 0; c < kC; ++c) g = Mma<T>::mma(Tile<T, D>::along(vt, 32 * k + col, c, half), fy[c], g);
+            reads_ahead<2 * kC, 1, Mma<T>::kMfmas, 4>();
             settle<T>();
             const bool all_beyond = first - (j0 + 31) >= a.far, all_ahead = wave_last - j0 <= -a.far;
             const int at = j0 + 4 * half - pos + a.far + kTabMargin;   // of this lane's first key among the distances
@@ -179,9 +210,9 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (bwd_occupancy<T, 
 #pragma unroll
                 for (int r = 0; r < 16; ++r) x[r] = __builtin_amdgcn_exp2f(fmaf(x[r], a.scale2, -lse));
             } else if (all_beyond || all_ahead) {
-                const float b = all_beyond ? beyond : ahead;
+                const float b = (all_beyond ? beyond : ahead) - lse;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) x[r] = __builtin_amdgcn_exp2f(fmaf(x[r], a.scale2, b) - lse);
+                for (int r = 0; r < 16; ++r) x[r] = __builtin_amdgcn_exp2f(fmaf(x[r], a.scale2, b));
             } else {
                 const float* const from = tab + at;
 #pragma unroll
@@ -203,7 +234,7 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (bwd_occupancy<T, 
             }
 #pragma unroll
             for (int r = 0; r < 16; ++r) g[r] = x[r] * (g[r] - delta);
-            if (BIAS && is) {
+            if (BIAS) {
                 if (all_beyond || all_ahead) {
                     float sum = 0.f;
 #pragma unroll
@@ -211,11 +242,12 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (bwd_occupancy<T, 
                     if (all_beyond) sum_beyond += sum;
                     else sum_ahead += sum;
                 } else {
-                    // 32 neighbouring distances a register, one for each lane of a half; the halves, which overlap, have an array each.  An
-                    // LDS addition is done in program order and no other wavefront adds here, so the order of the sums is fixed.
-                    float* const to = sums + half * size + at;
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) __hip_atomic_fetch_add(to + 8 * (r / 4) + r % 4, g[r], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+                    // What a tile has of one distance lies on a diagonal; see diagonal_sums.  A distance of a half's array is met by two
+                    // neighbouring tiles and stored once, with the second.
+                    const float2 now = diagonal_sums(g);
+                    sums[half * size + j0 - first + a.far + kTabMargin + 4 * half - col] = now.x + carry;
+                    carry = now.y;
+                    carry_at = j0 + 32;
                 }
             }
 #pragma unroll
@@ -224,6 +256,7 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (bwd_occupancy<T, 
 #pragma unroll
                 for (int d = 0; d < kD; ++d) dq[d] = Mma<T>::mma(Tile<T, D>::down(kt, 32 * k, c, d), p, dq[d]);
             }
+            reads_ahead<kM * kD, Mma<T>::kDown, Mma<T>::kMfmas, 4>();
             settle<T>();
         }
     };
@@ -239,9 +272,13 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (bwd_occupancy<T, 
         if (SHARE == 4) __syncthreads();   // (the first tile's place may still be read)
     }
     judge(a, looks, v, peek);
-    if (is && half == 0) const_cast<float*>(a.delta)[(int64_t)head * a.q_rows + row] = delta;
+    if (is && half == 0) {   // for attn_dkv_kernel
+        a.delta[(int64_t)head * a.q_rows + row] = delta;
+        a.lse2[(int64_t)head * a.q_rows + row] = lse;
+    }
     if (is) store_column<T, D>(const_cast<char*>(a.dq.at(row, head)), dq, a.scale, half, a.dim);
     if (!BIAS) return;
+    if (carry_at >= 0) sums[half * size + carry_at - first + a.far + kTabMargin + 4 * half - col] = carry;
     // the distances that this unit has met
     const int unit_first = q.nk - q.nq + i0, unit_last = unit_first + a.block - 1;
     int from = a.far + kTabMargin - (unit_last < a.far + kTabMargin ? unit_last : a.far + kTabMargin);
@@ -288,7 +325,7 @@ __global__ __launch_bounds__(256) void attn_dbias_kernel(const AttnArgs a, void*
 // A unit: `block` keys of a sequence and a key head, hp of the heads that read it one after the other.  Where a group is cut into several
 // such parts, each leaves fp32 sums (part_o: [2][parts][k_rows][kv][D]), which attn_dkv_join_kernel adds up.
 template <typename T, int D, int SHARE, bool BIAS>
-__global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (bwd_occupancy<T, D>())) void attn_dkv_kernel(const AttnArgs a) {
+__global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dkv_occupancy<T, D>())) void attn_dkv_kernel(const AttnArgs a) {
     constexpr int kWaves = bwd_waves<T, D, SHARE>(), BQ = bwd_rows<T, D, SHARE>(), kT = BQ / 32, kD = D / 32;
     constexpr int kK = Mma<T>::kK, kC = D / kK, kM = 32 / kK;
     constexpr int kTile = BQ * D * (int)sizeof(T), kSets = SHARE == 4 ? 1 : kWaves, kLds = kSets * kTile;
@@ -336,7 +373,7 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (bwd_occupancy<T, 
             const int i = t * BQ + lane;
             const bool there = lane < BQ && i < q.nq;
             const int64_t at = (int64_t)head * a.q_rows + q.q0 + i;
-            const float* const l = there ? a.lse + at : &attn_inf;
+            const float* const l = there ? a.lse2 + at : &attn_inf;
             const float* const d = there ? a.delta + at : reinterpret_cast<const float*>(&attn_zeros);
             if (SHARE == 1 || wave == 0)
                 load_lds<4>(l, st + own_stats);
@@ -373,6 +410,7 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (bwd_occupancy<T, 
             for (int c = 0; c < kC; ++c) x = Mma<T>::mma(Tile<T, D>::along(qt, 32 * k + col, c, half), fk[c], x);
 #pragma unroll
             for (int c = 0; c < kC; ++c) g_ = Mma<T>::mma(Tile<T, D>::along(yt, 32 * k + col, c, half), fv[c], g_);
+            reads_ahead<2 * kC, 1, Mma<T>::kMfmas, 4>();
             settle<T>();
             const float* const lse = st_ + own_stats + 32 * k + 4 * half;
             const bool all_beyond = first - (jw + 31) >= a.far, all_ahead = first + 31 - jw <= -a.far;
@@ -387,9 +425,8 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (bwd_occupancy<T, 
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int r = 4 * n + e;
-                    const float at = l[e] == -__builtin_inff() ? __builtin_inff() : l[e] * kLog2e;
-                    if (!BIAS) x[r] = __builtin_amdgcn_exp2f(fmaf(x[r], a.scale2, -at));
-                    else x[r] = __builtin_amdgcn_exp2f(fmaf(x[r], a.scale2, by_distance ? from[27 - 8 * n - e] : flat) - at);
+                    if (!BIAS) x[r] = __builtin_amdgcn_exp2f(fmaf(x[r], a.scale2, -l[e]));
+                    else x[r] = __builtin_amdgcn_exp2f(fmaf(x[r], a.scale2, by_distance ? from[27 - 8 * n - e] : flat) - l[e]);
                     g_[r] = x[r] * (g_[r] - d[e]);
                 }
             }
@@ -407,6 +444,7 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (bwd_occupancy<T, 
                     dk[d] = Mma<T>::mma(Tile<T, D>::down(qt, 32 * k, c, d), ds, dk[d]);
                 }
             }
+            reads_ahead<2 * kM * kD, Mma<T>::kDown, Mma<T>::kMfmas, 4>();
             settle<T>();
         }
     };
@@ -483,7 +521,7 @@ AttnBackwardPlan attn_backward_plan(const AttnShape& sh) {
         while (group % next != 0) ++next;
         p.parts = next;
     }
-    p.delta = ((size_t)sh.H * (size_t)sh.q_rows * 4 + 255) & ~(size_t)255;
+    p.delta = 2 * (((size_t)sh.H * (size_t)sh.q_rows * 4 + 255) & ~(size_t)255);   // with lse, as an exponent of 2
     p.part_bias = sh.buckets ? ((size_t)sh.H * (size_t)p.V_q * (size_t)sh.buckets * 4 + 255) & ~(size_t)255 : 0;
     p.part_kv = p.parts > 1 ? 2 * (size_t)p.parts * (size_t)sh.k_rows * (size_t)sh.kv * (size_t)p.D * 4 : 0;
     p.grid_ok = (int64_t)sh.H * p.V_q < ((int64_t)1 << 31) - 64 && (int64_t)sh.kv * p.parts * p.V_k < ((int64_t)1 << 31) - 64;
@@ -564,6 +602,7 @@ static hipError_t launch_type(const tbe_handle* h, const AttnArgs& a, const Attn
 hipError_t launch_attention_backward(const tbe_handle* h, AttnArgs a, const AttnBackwardPlan& p, int io, void* dbias, void* workspace, hipStream_t s) {
     char* const ws = static_cast<char*>(workspace);
     a.delta = reinterpret_cast<float*>(ws);
+    a.lse2 = reinterpret_cast<float*>(ws + p.delta / 2);
     a.part_bias = reinterpret_cast<float*>(ws + p.delta);
     a.part_o = reinterpret_cast<float*>(ws + p.delta + p.part_bias);
     return io == 0 ? launch_type<float>(h, a, p, dbias, s) : (io == 1 ? launch_type<__half>(h, a, p, dbias, s) : launch_type<bf16_t>(h, a, p, dbias, s));
