@@ -350,4 +350,4 @@ def test_refusals(tbe):
     assert L.tbe_attention(tbe._h, None, binding.Rows(), None, None, 0, None) == binding.EINVAL
     a = binding.AttentionArgs(sequences=1, heads=1, kv_heads=1, head_dim=8, dtype=5)
     import ctypes
-    assert L.tbe_attention(tbe._h, ctypes.byref(a), binding.Rows(), None, None, 0, None) == binding.EDTYPE
+    assert L.tbe_attention(tbe._h, ctypes.addressof(a), binding.Rows(), None, None, 0, None) == binding.EDTYPE
