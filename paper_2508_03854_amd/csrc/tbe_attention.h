@@ -23,6 +23,10 @@ __device__ __forceinline__ int uniform(const int x) { return __builtin_amdgcn_re
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr int kTabMargin = 68;         // a tile that reaches into the table of distances reaches at most 66 beyond its ends
+// So many wavefronts, were there one for every 32 rows of a sequence and head, and short sequences share wavefronts.  A wavefront of one sequence /
+// shared ones, 8 heads of 64 bfloat16, lengths lognormal (7 in the middle, 12 on average), us: 64 sequences (704 wavefronts) forward 11.2 / 10.7,
+// dq 20.2 / 20.9; 256 (2816) 18.2 / 13.2, 32.0 / 26.5; 1024 (11264) 44.5 / 23.3, 73.8 / 50.7; 4096 149 / 65, 251 / 161.
+constexpr int64_t kManyUnits = 2048;
 constexpr int kTabBytes = 24 << 10;    // LDS for such tables
 
 // Sixteen zero bytes: what stands behind a sequence's end, or behind a row's, is read from here.
@@ -127,9 +131,29 @@ struct Tile {
             return make_uint4(w[0], w[1], w[2], w[3]);
         }
     }
-    static __device__ __forceinline__ float element(const char* lds, const int r, const int e) {
-        constexpr int kE = 16 / (int)sizeof(T);
-        return elem_float(*reinterpret_cast<const T*>(lds + (r * kChunks + ((e / kE) ^ swizzle(r))) * 16 + (e % kE) * (int)sizeof(T)));
+    // what is not finite in the tile's first 32 rows becomes 0; the rows that had such, a bit each
+    static __device__ __forceinline__ uint32_t clean(char* lds) {
+        constexpr uint32_t lower = sizeof(T) == 4 ? 0x7F800000u : (__is_same(T, bf16_t) ? 0x7F80u : 0x7C00u);
+        uint32_t rows = 0;
+#pragma unroll 1
+        for (int n = lane_id(); n < 32 * kChunks; n += 64) {
+            uint4* const p = reinterpret_cast<uint4*>(lds + n * 16);
+            const uint4 v = *p;
+            uint32_t w[4] = {v.x, v.y, v.z, v.w};
+            bool bad = false;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if ((w[i] & lower) == lower) { w[i] &= sizeof(T) == 4 ? 0u : 0xFFFF0000u; bad = true; }
+                if (sizeof(T) == 2 && (w[i] >> 16 & lower) == lower) { w[i] &= 0xFFFFu; bad = true; }
+            }
+            if (bad) {
+                *p = make_uint4(w[0], w[1], w[2], w[3]);
+                rows |= 1u << (n / kChunks);
+            }
+        }
+#pragma unroll
+        for (int i = 32; i; i >>= 1) rows |= __shfl_xor(rows, i);
+        return rows;
     }
     // ROWS rows from row j0 of a sequence on, of which there are `rows`, by WAVES wavefronts (this one is number w); complete after
     // loads_done().  `stride`: bytes from row to row
@@ -210,6 +234,40 @@ __device__ __forceinline__ int find_sequence(const IdxView off, const int N, con
     return uniform(lo);
 }
 
+// The largest s below N with offsets[s] <= row: the sequence of a row, if offsets[s + 1] > row.
+__device__ __forceinline__ int find_row(const IdxView off, const int N, const int64_t row) {
+    int lo = 0, hi = N;
+    while (hi - lo > 1) {
+        const int step = (hi - lo + 63) / 64, s = lo + lane_id() * step;
+        const uint64_t m = __ballot(s < hi && off[s] <= row);
+        const int k = m ? 63 - __builtin_clzll(m) : 0;
+        lo += k * step;
+        hi = hi < lo + step ? hi : lo + step;
+    }
+    return uniform(lo);
+}
+// ... of each of 32 neighbouring rows, for the lane l % 32 that has it (rows: there are so many in all).  The ends of the next 64 sequences are
+// loaded together, and every lane counts those that lie before its row; where many sequences are empty, 64 more.
+__device__ __forceinline__ int lane_sequence(const IdxView off, const int N, const int64_t row0, const int64_t rows) {
+    const int64_t row = row0 + (lane_id() & 31);
+    int base = find_row(off, N, row0), mine = base;
+    bool open = row < rows;
+    while (__any(open)) {
+        const int s = base + 1 + lane_id();
+        const int64_t e = s <= N ? off[s] : INT64_MAX;
+        const int end = e > row0 + 32 ? 32 : (int)(e - row0 < 0 ? 0 : e - row0);   // rows of the 32 before it
+        int n = 0;   // ends at or before this lane's row; they ascend
+#pragma unroll
+        for (int step = 32; step; step >>= 1)
+            if (__shfl(end, n + step - 1) <= (int)(row - row0)) n += step;
+        n += n == 63 && __shfl(end, 63) <= (int)(row - row0);
+        if (open) mine = base + n;
+        open = open && n == 64 && base + 64 < N;
+        base += 64;
+    }
+    return mine < N ? mine : N - 1;
+}
+
 struct Sequence {
     int64_t q0, k0;   // first rows
     int nq, nk;       // queries, keys
@@ -233,6 +291,31 @@ __device__ __forceinline__ bool take_sequence(const AttnArgs& a, const int s, co
     if (!ok && lane_id() == 0) *a.err = 1;
     return ok;
 }
+// A lane's own sequence, where the rows of several share a tile.
+struct LaneSequence {
+    int64_t q0, q1, k0, k1;
+    bool fits;
+};
+__device__ __forceinline__ LaneSequence lane_numbers(const AttnArgs& a, const int s) {
+    LaneSequence q;
+    q.q0 = a.q_off[s]; q.q1 = a.q_off[s + 1]; q.k0 = a.k_off[s]; q.k1 = a.k_off[s + 1];
+    q.fits = q.q0 >= 0 && q.q0 <= q.q1 && q.q1 <= a.q_rows && q.k0 >= 0 && q.k0 <= q.k1 && q.k1 <= a.k_rows;
+    if (s == 0) q.fits = q.fits && q.q0 == 0 && q.k0 == 0;
+    if (s == a.N - 1) q.fits = q.fits && q.q1 == a.q_rows && q.k1 == a.k_rows;
+    if (!q.fits) *a.err = 1;
+    return q;
+}
+// All sequences looked over by `units` wavefronts, 64 at a time.
+__device__ __forceinline__ void judge_all(const AttnArgs& a, const uint32_t unit, const uint32_t units) {
+    for (int64_t s = (int64_t)unit * 64 + lane_id(); s < a.N; s += (int64_t)units * 64) (void)lane_numbers(a, (int)s);
+}
+// whether any of the 32 rows from j0 on that `rows` names lies in [lo, end)
+__device__ __forceinline__ bool meets(const uint32_t rows, const int j0, const int lo, const int end) {
+    const int from = lo - j0 < 0 ? 0 : lo - j0, to = end - j0 > 32 ? 32 : end - j0;
+    return from < to && (rows >> from & (to - from >= 32 ? 0xFFFFFFFFu : (1u << (to - from)) - 1u)) != 0;
+}
+__device__ __forceinline__ int wave_min_i32(const int x) { return -wave_max_i32(-x); }
+
 // Offsets that do not ascend may keep the search from ever meeting the sequence that is wrong, so that unit n of the first head (there are
 // at least as many as sequences) looks at sequence n besides: `peek` is loaded early and judged when the unit is done.
 __device__ __forceinline__ void judge(const AttnArgs& a, const bool looks, const int n, const int64_t peek) {

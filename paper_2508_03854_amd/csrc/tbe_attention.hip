@@ -15,10 +15,12 @@ namespace tbe {
 // SHARE = 1: every wavefront is on its own, with `pack` heads of a group side by side in its columns; or (together) the wavefronts of a
 // workgroup have the same columns and a part of the keys each, joined in LDS, and with splits > 1 several workgroups do, joined by
 // attn_join_kernel.
+// SHARE = 0: short sequences: a wavefront takes 32 neighbouring rows of q, whosesoever they are, and the keys of all their sequences; a column
+// hides what is not its own sequence's (see kManyUnits).
 template <typename T, int D, int SHARE>
 constexpr int kv_rows() { return SHARE == 4 && D * (int)sizeof(T) <= 256 ? 64 : 32; }
 template <typename T, int D, int SHARE>
-constexpr int attn_waves() { return SHARE == 1 && D * (int)sizeof(T) > 256 ? 2 : 4; }
+constexpr int attn_waves() { return SHARE != 4 && D * (int)sizeof(T) > 256 ? 2 : 4; }
 
 template <typename T, int D, int SHARE>   // wavefronts of a SIMD that the registers are to leave room for (and the LDS does)
 constexpr int attn_occupancy() { return sizeof(T) == 4 ? (D == 32 ? 2 : 1) : (D == 32 ? 4 : (D == 64 ? (SHARE == 4 ? 3 : 2) : (SHARE == 4 ? 2 : 1))); }
@@ -27,7 +29,8 @@ template <typename T, int D, int SHARE, bool BIAS>
 __global__ __launch_bounds__((64 * attn_waves<T, D, SHARE>()), (attn_occupancy<T, D, SHARE>())) void attn_kernel(const AttnArgs a) {
     constexpr int kWaves = attn_waves<T, D, SHARE>(), BK = kv_rows<T, D, SHARE>(), kT = BK / 32, kD = D / 32;
     constexpr int kE = Mma<T>::kE, kK = Mma<T>::kK, kC = D / kK, kM = 32 / kK;
-    constexpr int kTile = BK * D * (int)sizeof(T);
+    constexpr int kTile = BK * D * (int)sizeof(T), kSharers = SHARE == 4 ? 4 : 1;
+    constexpr bool kRows = SHARE == 0;
     // two buffers each, as arrays of their own: loads into one of them are seen not to concern what is read from another
     constexpr int kLds = SHARE == 4 ? kTile : kWaves * kTile;
     __shared__ __align__(16) char keys0[kLds], keys1[kLds], values0[kLds], values1[kLds];
@@ -45,20 +48,55 @@ __global__ __launch_bounds__((64 * attn_waves<T, D, SHARE>()), (attn_occupancy<T
     }
     const uint32_t unit = SHARE == 4 || together ? item : item * kWaves + wave;
     if (unit >= (uint32_t)a.V * a.splits) return;
-    const uint32_t v = SHARE == 4 ? unit : unit / a.splits;
-    const int split = SHARE == 4 ? 0 : unit - v * a.splits;
-    const bool looks = hh == 0 && split == 0 && ((SHARE == 1 && !together) || wave == 0) && v < (uint32_t)a.N;
+    const uint32_t v = SHARE != 1 ? unit : unit / a.splits;
+    const int split = SHARE != 1 ? 0 : unit - v * a.splits;
+    const bool looks = !kRows && hh == 0 && split == 0 && ((SHARE == 1 && !together) || wave == 0) && v < (uint32_t)a.N;
     const int64_t peek = looks ? sequence_numbers(a, v) : 0;
-    const int s = find_sequence(a.q_off, a.N, v, a.block);
     Sequence q;
-    const bool fits = take_sequence(a, s, sequence_numbers(a, s), q);
-    const uint32_t start = (uint32_t)q.q0 / a.block + s, blocks = ((uint32_t)q.nq + a.block - 1) / a.block;
-    if (!fits || v < start || v - start >= blocks) return judge(a, looks, v, peek);
-    // the last queries, which see the most keys, first
-    const int i0 = uniform((int)(blocks - 1 - (v - start)) * a.block), iw = i0 + (SHARE == 4 ? wave * 32 : 0);
-    const int ci = SHARE == 4 ? col : col / a.pack, cg = SHARE == 4 ? 0 : col - ci * a.pack, i = iw + ci, head = head0 + cg;
-    const bool is = ci < a.qpt && i < q.nq;
-    const int first = q.nk - q.nq + iw, pos = first + ci;   // places among the keys: of the wavefront's first query, of this column's
+    int i0, iw, i, cg = 0, head = head0, first, pos, jend;
+    bool is;
+    // SHARE = 0: this column's own keys and its place among all rows of k
+    int own_lo = 0, own_end = 0, own_pos = 0;
+    if constexpr (kRows) {
+        if (hh == 0) judge_all(a, v, a.V);
+        q.q0 = (int64_t)v * 32;
+        q.k0 = 0;
+        q.nk = (int)a.k_rows;
+        q.nq = 32;
+        const LaneSequence mine = lane_numbers(a, lane_sequence(a.q_off, a.N, q.q0, a.q_rows));
+        const int64_t row = q.q0 + col;
+        is = mine.fits && row >= mine.q0 && row < mine.q1;
+        own_pos = (int)(mine.k1 - mine.q1 + row);
+        own_lo = is ? (int)mine.k0 : 0;
+        own_end = is ? (int)mine.k1 : 0;
+        if (a.causal && own_pos + 1 < own_end) own_end = own_pos + 1;
+        if (own_end < own_lo) own_end = own_lo;
+        i0 = iw = 0;
+        i = col;
+        first = pos = jend = 0;
+        if (!__any(is)) return;
+    } else {
+        const int s = find_sequence(a.q_off, a.N, v, a.block);
+        const bool fits = take_sequence(a, s, sequence_numbers(a, s), q);
+        const uint32_t start = (uint32_t)q.q0 / a.block + s, blocks = ((uint32_t)q.nq + a.block - 1) / a.block;
+        if (!fits || v < start || v - start >= blocks) return judge(a, looks, v, peek);
+        // the last queries, which see the most keys, first
+        i0 = uniform((int)(blocks - 1 - (v - start)) * a.block);
+        iw = i0 + (SHARE == 4 ? wave * 32 : 0);
+        const int ci = SHARE == 4 ? col : col / a.pack;
+        cg = SHARE == 4 ? 0 : col - ci * a.pack;
+        i = iw + ci;
+        head = head0 + cg;
+        is = ci < a.qpt && i < q.nq;
+        first = q.nk - q.nq + iw;   // place among the keys of the wavefront's first query ...
+        pos = first + ci;           // ... and of this column's
+        // keys of this unit: all that its last query sees
+        jend = q.nk;
+        if (a.causal) {
+            const int last = q.nk - q.nq + (i0 + a.block < q.nq ? i0 + a.block : q.nq);
+            jend = jend < last ? jend : last;
+        }
+    }
 
     uint4 fq[kC];
     {
@@ -74,24 +112,23 @@ __global__ __launch_bounds__((64 * attn_waves<T, D, SHARE>()), (attn_occupancy<T
             }
         }
     }
-    // keys of this unit: all that its last query sees, or a part of them
-    int jend = q.nk;
-    if (a.causal) {
-        const int last = q.nk - q.nq + (i0 + a.block < q.nq ? i0 + a.block : q.nq);
-        jend = jend < last ? jend : last;
+    // ... or a part of them
+    int t0 = 0, t1, jbase = 0, lo = 0, end = 0;
+    {
+        const int tiles = jend > 0 ? (jend + BK - 1) / BK : 0;
+        const int parts = together ? a.splits * kWaves : 1, part = (tiles + parts - 1) / parts;
+        if (together) t0 = uniform((split * kWaves + wave) * part);
+        t1 = uniform(t0 + part < tiles ? t0 + part : tiles);
     }
-    const int tiles = jend > 0 ? (jend + BK - 1) / BK : 0;
-    const int parts = SHARE == 4 ? 1 : (together ? a.splits * kWaves : 1), part = (tiles + parts - 1) / parts;
-    const int t0 = uniform(SHARE == 4 || !together ? 0 : (split * kWaves + wave) * part), t1 = uniform(t0 + part < tiles ? t0 + part : tiles);
-    const int wave_last = first + a.qpt - 1;   // the last place that a query of this wavefront may have
+    int wave_last = first + a.qpt - 1;   // the last place that a query of this wavefront may have
 
     const int kvh = head0 / a.group;
     const char* const kb = a.k.at(q.k0, kvh);
     const char* const vb = a.v.at(q.k0, kvh);
     const int own = SHARE == 4 ? 0 : wave * kTile, fw = SHARE == 4 ? wave : 0;
     auto fetch = [&](const int t, char* const kt, char* const vt) __attribute__((always_inline)) {
-        Tile<T, D>::template fetch<BK, SHARE>(kt + own, kb, a.k.row, t * BK, q.nk, a.dim, fw);
-        Tile<T, D>::template fetch<BK, SHARE>(vt + own, vb, a.v.row, t * BK, q.nk, a.dim, fw);
+        Tile<T, D>::template fetch<BK, kSharers>(kt + own, kb, a.k.row, jbase + t * BK, q.nk, a.dim, fw);
+        Tile<T, D>::template fetch<BK, kSharers>(vt + own, vb, a.v.row, jbase + t * BK, q.nk, a.dim, fw);
     };
 
     f32x16_t o[kD];
@@ -105,6 +142,7 @@ __global__ __launch_bounds__((64 * attn_waves<T, D, SHARE>()), (attn_occupancy<T
         ahead = a.causal ? 0.f : ht[2 * a.far + kTabMargin];
     }
 
+    bool clean = false, poisoned = false;   // SHARE = 0, see below
     bool met = false;      // a tile some of whose keys are hidden from some columns
     uint64_t before = 0;   // lanes whose results were not finite before the first of them
     auto not_finite = [&]() __attribute__((always_inline)) {
@@ -119,10 +157,11 @@ __global__ __launch_bounds__((64 * attn_waves<T, D, SHARE>()), (attn_occupancy<T
         loads_done();
         if (SHARE == 4) __syncthreads();
         if (t + 1 < t1) fetch(t + 1, kn, vn);
-        const int j0 = t * BK;
+        const int j0 = jbase + t * BK;
         const char* const kt = kt_ + own;
         const char* const vt = vt_ + own;
         if (SHARE == 4 && ((a.causal && j0 > wave_last) || iw >= q.nq)) return;
+        if (kRows && clean) poisoned |= meets(Tile<T, D>::clean(const_cast<char*>(vt)), j0, lo, end);
         f32x16_t x[kT];
 #pragma unroll
         for (int k = 0; k < kT; ++k) {
@@ -147,8 +186,14 @@ __global__ __launch_bounds__((64 * attn_waves<T, D, SHARE>()), (attn_occupancy<T
                 }
             }
         }
-        const bool masked = j0 + BK > q.nk || (a.causal && j0 + BK - 1 > first);
-        if (masked) {
+        const bool masked = kRows || j0 + BK > q.nk || (a.causal && j0 + BK - 1 > first);
+        if constexpr (kRows) {
+#pragma unroll
+            for (int k = 0; k < kT; ++k)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if ((uint32_t)(j0 + 32 * k + 8 * (r / 4) + 4 * half + r % 4 - lo) >= (uint32_t)(end - lo)) x[k][r] = -__builtin_inff();
+        } else if (masked) {
             const int end = a.causal && pos + 1 < q.nk ? pos + 1 : q.nk;   // the keys that this column sees end here
 #pragma unroll
             for (int k = 0; k < kT; ++k)
@@ -188,7 +233,7 @@ __global__ __launch_bounds__((64 * attn_waves<T, D, SHARE>()), (attn_occupancy<T
         for (int k = 0; k < kT; ++k)
 #pragma unroll
             for (int c = 0; c < kM; ++c) p[k][c] = Mma<T>::pack(x[k], c);
-        if (masked && !met) {
+        if (!kRows && masked && !met) {
             met = true;
             before = __ballot(not_finite());
         }
@@ -201,20 +246,56 @@ __global__ __launch_bounds__((64 * attn_waves<T, D, SHARE>()), (attn_occupancy<T
         reads_ahead<kT * kM * kD, Mma<T>::kDown, Mma<T>::kMfmas, 4>();
         settle<T>();
     };
-    if (t0 < t1) fetch(t0, keys0, values0);
-    for (int t = t0; t < t1; t += 2) {
-        step(t, keys0, values0, keys1, values1);
-        if (t + 1 < t1) step(t + 1, keys1, values1, keys0, values0);
+again:
+    uint64_t todo = kRows ? __ballot(is) : 1;
+    while (todo) {
+        if constexpr (kRows) {
+            // Columns whose places lie as their rows do go together: all of them where queries and keys are the same rows.
+            const int shift = uniform(bcast_lane(own_pos - col, __ffsll((unsigned long long)todo) - 1));
+            const bool mine = is && own_pos - col == shift;
+            todo &= ~__ballot(mine);
+            first = shift;
+            pos = first + col;
+            wave_last = first + 31;
+            lo = mine ? own_lo : 0;
+            end = mine ? own_end : 0;
+            jbase = wave_min_i32(lo < end ? lo : 0x7FFFFFFF);
+            const int last = wave_max_i32(lo < end ? end : 0);
+            t1 = jbase < last ? (last - jbase + BK - 1) / BK : 0;
+        } else {
+            todo = 0;
+        }
+        if (t0 < t1) fetch(t0, keys0, values0);
+        for (int t = t0; t < t1; t += 2) {
+            step(t, keys0, values0, keys1, values1);
+            if (t + 1 < t1) step(t + 1, keys1, values1, keys0, values0);
+        }
     }
-    judge(a, looks, v, peek);
-    sum = pair_sum<32>(sum);
     // The probability of a hidden key is 0, but 0 times a value that is not finite is not.  Columns whose results stopped being finite in a
-    // tile with hidden keys are computed once more, key by key, without these.
-    if (met) {
-        uint64_t bad = __ballot(not_finite()) & ~before;
+    // tile with hidden keys are computed once more, key by key, without these.  With SHARE = 0, where they may be another sequence's, all
+    // is first done again on tiles in which such values are 0, which is right, bit by bit, for the columns that see none of them.
+    if (kRows && !clean && __any(not_finite())) {
+#pragma unroll
+        for (int d = 0; d < kD; ++d) o[d] = f32x16_t{};
+        m = -__builtin_inff();
+        sum = 0.f;
+        clean = true;
+        goto again;
+    }
+    if (!kRows) judge(a, looks, v, peek);
+    sum = pair_sum<32>(sum);
+    if (kRows ? clean : met) {
+        uint64_t bad = kRows ? __ballot(poisoned) : __ballot(not_finite()) & ~before;
         bad |= bad >> 32 | bad << 32;
         if (bad) {
-            const int last = t1 * BK < jend ? t1 * BK : jend, end = a.causal && pos + 1 < last ? pos + 1 : last;
+            int from = t0 * BK, last = t1 * BK < jend ? t1 * BK : jend;
+            if constexpr (kRows) {
+                from = wave_min_i32(own_lo < own_end ? own_lo : 0x7FFFFFFF);
+                last = wave_max_i32(own_lo < own_end ? own_end : 0);
+            } else {
+                own_end = a.causal && pos + 1 < last ? pos + 1 : last;
+                own_pos = pos;
+            }
             float sm, ss;
 #pragma unroll
             for (int d = 0; d < kD; ++d) {   // (32 elements of the result at a time: it is registers that are short)
@@ -222,7 +303,7 @@ __global__ __launch_bounds__((64 * attn_waves<T, D, SHARE>()), (attn_occupancy<T
                 sm = -__builtin_inff();
                 ss = 0.f;
 #pragma unroll 1
-                for (int j = t0 * BK; j < last; ++j) {
+                for (int j = from; j < last; ++j) {
                     const T* const kr = reinterpret_cast<const T*>(kb + j * a.k.row);
                     float x = 0.f;
 #pragma unroll
@@ -238,10 +319,10 @@ __global__ __launch_bounds__((64 * attn_waves<T, D, SHARE>()), (attn_occupancy<T
                     }
                     x = pair_sum<32>(x) * a.scale2;
                     if (BIAS) {
-                        const int apart = pos - j;
+                        const int apart = own_pos - j;
                         x += ht[a.far + kTabMargin - (apart > a.far ? a.far : (apart < -a.far ? -a.far : apart))];
                     }
-                    if (j >= end || (x == -__builtin_inff() && sm == x)) continue;
+                    if (j < own_lo || j >= own_end || (x == -__builtin_inff() && sm == x)) continue;
                     const float grown = fmaxf(sm, x), shrink = __builtin_amdgcn_exp2f(sm - grown);
                     float p = __builtin_amdgcn_exp2f(x - grown);
                     sm = grown;
@@ -401,11 +482,12 @@ AttnPlan attn_plan(const AttnShape& sh, const int max_pack) {
             if (group % g == 0 && mean_q * g <= 32 && g * table <= kTabBytes) p.pack = g;
         p.qpt = p.block = 32 / p.pack;
     }
-    p.V = sh.q_rows / p.block + sh.N;
+    p.rows = !p.shared && p.pack == 1 && !sh.caches && mean_k <= 2 * mean_q && (sh.q_rows / 32 + sh.N) * sh.H >= kManyUnits;
+    p.V = p.rows ? (sh.q_rows + 31) / 32 : sh.q_rows / p.block + sh.N;
     p.together = false;
     if (!p.shared) {
         const int64_t units = (sh.q_rows / p.block < sh.N ? sh.N : sh.q_rows / p.block + sh.N / 2) * (sh.H / p.pack);
-        const int64_t want = std::min(units > 0 ? 2048 / units : 1, mean_k / 128);
+        const int64_t want = p.rows ? 1 : std::min(units > 0 ? 2048 / units : 1, mean_k / 128);
         p.together = want > 1;
         p.splits = (int)std::min<int64_t>(128, std::max<int64_t>(1, (want + 3) / 4));
     }
@@ -424,6 +506,7 @@ size_t attn_workspace(const AttnShape& sh, const bool backward) {
     for (int pack = 1; pack <= 32; ++pack) {   // (how many heads go side by side depends on the bias)
         AttnShape any = sh;
         any.far = 0;
+        any.caches = true;
         const AttnPlan p = attn_plan(any, pack);
         most = std::max(most, p.part_ml + p.part_o);
     }
@@ -445,6 +528,7 @@ static hipError_t launch_dim(const tbe_handle* h, const AttnArgs& a, const AttnP
     {
         LaunchTimer tm(h, s, "attention");
         if (p.shared) e = a.bias ? launch_one<T, D, 4, true>(a, s) : launch_one<T, D, 4, false>(a, s);
+        else if (p.rows) e = a.bias ? launch_one<T, D, 0, true>(a, s) : launch_one<T, D, 0, false>(a, s);
         else e = a.bias ? launch_one<T, D, 1, true>(a, s) : launch_one<T, D, 1, false>(a, s);
         tm.done();
     }

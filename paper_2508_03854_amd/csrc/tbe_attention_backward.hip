@@ -15,6 +15,8 @@ namespace tbe {
 static __device__ const float attn_inf = __builtin_inff();
 
 // SHARE = 4: the wavefronts of a workgroup take neighbouring columns of one sequence and share tiles.  SHARE = 1: each is on its own.
+// SHARE = 0: each is on its own and takes 32 neighbouring rows, whosesoever they are, with all that their sequences have on the other
+// side; a column hides what is not its own sequence's (see kManyUnits).
 template <typename T, int D, int SHARE>
 constexpr int bwd_rows() { return SHARE == 4 && D * (int)sizeof(T) <= 128 ? 64 : 32; }
 template <typename T, int D, int SHARE>
@@ -102,7 +104,8 @@ template <typename T, int D, int SHARE, bool BIAS>
 __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dq_occupancy<T, D, SHARE>())) void attn_dq_kernel(const AttnArgs a) {
     constexpr int kWaves = bwd_waves<T, D, SHARE>(), BK = bwd_rows<T, D, SHARE>(), kT = BK / 32, kD = D / 32;
     constexpr int kE = Mma<T>::kE, kK = Mma<T>::kK, kC = D / kK, kM = 32 / kK;
-    constexpr int kTile = BK * D * (int)sizeof(T), kLds = SHARE == 4 ? kTile : kWaves * kTile;
+    constexpr int kTile = BK * D * (int)sizeof(T), kLds = SHARE == 4 ? kTile : kWaves * kTile, kSharers = SHARE == 4 ? 4 : 1;
+    constexpr bool kRows = SHARE == 0;
     __shared__ __align__(16) char keys0[kLds], keys1[kLds], values0[kLds], values1[kLds];
     extern __shared__ float tab[];   // the bias by distance, sums by distance - two arrays of that size for each wavefront -, the buckets
     const int wave = uniform(threadIdx.x >> 6), lane = lane_id(), col = lane & 31, half = lane >> 5;
@@ -120,21 +123,58 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dq_occupancy<T, D
     if (v >= (uint32_t)a.V) return;
     float* const part = BIAS ? a.part_bias + ((int64_t)head * a.V + v) * a.buckets : nullptr;
     const int me = SHARE == 4 ? threadIdx.x : lane, of = SHARE == 4 ? 64 * kWaves : 64;   // of the unit's lanes
-    const bool looks = head == 0 && (SHARE == 1 || wave == 0) && v < (uint32_t)a.N;
+    const bool looks = !kRows && head == 0 && (SHARE == 1 || wave == 0) && v < (uint32_t)a.N;
     const int64_t peek = looks ? sequence_numbers(a, v) : 0;
-    const int s = find_sequence(a.q_off, a.N, v, a.block);
     Sequence q;
-    const bool fits = take_sequence(a, s, sequence_numbers(a, s), q);
-    const uint32_t start = (uint32_t)q.q0 / a.block + s, blocks = ((uint32_t)q.nq + a.block - 1) / a.block;
-    if (!fits || v < start || v - start >= blocks) {
-        if (BIAS)
-            for (int b = me; b < a.buckets; b += of) part[b] = 0.f;
-        return judge(a, looks, v, peek);
+    int iw, first, pos, wave_last, tiles, jbase = 0, lo = 0, end = 0;
+    int own_lo = 0, own_end = 0, own_pos = 0;   // SHARE = 0: this column's own keys, and its place among all rows of k
+    int back, on;                               // the furthest that a key lies behind and ahead of a query here
+    bool is;
+    int64_t row;
+    if constexpr (kRows) {
+        if (head == 0) judge_all(a, v, a.V);
+        q.q0 = (int64_t)v * 32;
+        q.k0 = 0;
+        q.nk = (int)a.k_rows;
+        q.nq = 32;
+        const LaneSequence mine = lane_numbers(a, lane_sequence(a.q_off, a.N, q.q0, a.q_rows));
+        row = q.q0 + col;
+        is = mine.fits && row >= mine.q0 && row < mine.q1;
+        own_pos = (int)(mine.k1 - mine.q1 + row);
+        own_lo = is ? (int)mine.k0 : 0;
+        own_end = is ? (int)mine.k1 : 0;
+        if (a.causal && own_pos + 1 < own_end) own_end = own_pos + 1;
+        if (own_end < own_lo) own_end = own_lo;
+        const bool sees = own_lo < own_end;
+        back = wave_max_i32(sees ? own_pos - own_lo : -0x40000000);
+        on = wave_max_i32(sees ? own_end - 1 - own_pos : -0x40000000);
+        row = is ? row : 0;
+        iw = first = pos = wave_last = tiles = 0;
+    } else {
+        const int s = find_sequence(a.q_off, a.N, v, a.block);
+        const bool fits = take_sequence(a, s, sequence_numbers(a, s), q);
+        const uint32_t start = (uint32_t)q.q0 / a.block + s, blocks = ((uint32_t)q.nq + a.block - 1) / a.block;
+        if (!fits || v < start || v - start >= blocks) {
+            if (BIAS)
+                for (int b = me; b < a.buckets; b += of) part[b] = 0.f;
+            return judge(a, looks, v, peek);
+        }
+        const int i0 = uniform((int)(blocks - 1 - (v - start)) * a.block), i = i0 + (SHARE == 4 ? wave * 32 : 0) + col;
+        iw = i0 + (SHARE == 4 ? wave * 32 : 0);
+        is = i < q.nq;
+        first = q.nk - q.nq + iw;
+        pos = first + col;
+        wave_last = first + 31;
+        row = q.q0 + (is ? i : 0);
+        int jend = q.nk;
+        if (a.causal) {
+            const int last = q.nk - q.nq + (i0 + a.block < q.nq ? i0 + a.block : q.nq);
+            jend = jend < last ? jend : last;
+        }
+        tiles = uniform(jend > 0 ? (jend + BK - 1) / BK : 0);
+        back = q.nk - q.nq + i0 + a.block - 1;
+        on = q.nk - 1 - (q.nk - q.nq + i0);
     }
-    const int i0 = uniform((int)(blocks - 1 - (v - start)) * a.block), iw = i0 + (SHARE == 4 ? wave * 32 : 0), i = iw + col;
-    const bool is = i < q.nq;
-    const int first = q.nk - q.nq + iw, pos = first + col, wave_last = first + 31;
-    const int64_t row = q.q0 + (is ? i : 0);
 
     uint4 fq[kC], fy[kC];
     column_row<T, D>(fq, a.q.at(row, head), is, half, a.dim);
@@ -143,38 +183,19 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dq_occupancy<T, D
     float lse = is ? a.lse[(int64_t)head * a.q_rows + row] : __builtin_inff();   // (columns without a query: probabilities 0)
     lse = lse == -__builtin_inff() ? __builtin_inff() : lse * kLog2e;   // (a row that saw nothing: all its probabilities 2^-inf)
 
-    int jend = q.nk;
-    if (a.causal) {
-        const int last = q.nk - q.nq + (i0 + a.block < q.nq ? i0 + a.block : q.nq);
-        jend = jend < last ? jend : last;
-    }
-    const int tiles = uniform(jend > 0 ? (jend + BK - 1) / BK : 0);
     // D of a row from its few keys' P and dP, or else from the forward's result.  That was rounded, which against the sum over few keys is
     // as much as the rounding of dS and of the gradient: 4096 bfloat16 sequences of 12 events on average have dq 1.6 times as far from
     // 64 bits as a single rounding with the latter alone, 1.4 times with the former up to kFew tiles.
     constexpr int kFew = 4;
-    const bool few = tiles <= kFew, one = kT == 1 && tiles == 1;
-    float delta = 0.f;
-    if (!few) {
-        uint4 fo[kC];
-        column_row<T, D>(fo, a.o.at(row, head), is, half, a.dim);
-#pragma unroll
-        for (int c = 0; c < kC; ++c) {
-            float x[kE], y[kE];
-            Frag<T>::unpack(fo[c], x);
-            Frag<T>::unpack(fy[c], y);
-#pragma unroll
-            for (int e = 0; e < kE; ++e) delta = fmaf(x[e], y[e], delta);
-        }
-        delta = pair_sum<32>(delta);
-    }
+    float delta = 0.f, dsum;
+    bool one, sums_only;   // all keys in one tile of 32; a first run over the keys for D alone
     const int kvh = head / a.group;
     const char* const kb = a.k.at(q.k0, kvh);
     const char* const vb = a.v.at(q.k0, kvh);
     const int own = SHARE == 4 ? 0 : wave * kTile, fw = SHARE == 4 ? wave : 0;
     auto fetch = [&](const int t, char* const kt, char* const vt) __attribute__((always_inline)) {
-        Tile<T, D>::template fetch<BK, SHARE>(kt + own, kb, a.k.row, t * BK, q.nk, a.dim, fw);
-        Tile<T, D>::template fetch<BK, SHARE>(vt + own, vb, a.v.row, t * BK, q.nk, a.dim, fw);
+        Tile<T, D>::template fetch<BK, kSharers>(kt + own, kb, a.k.row, jbase + t * BK, q.nk, a.dim, fw);
+        Tile<T, D>::template fetch<BK, kSharers>(vt + own, vb, a.v.row, jbase + t * BK, q.nk, a.dim, fw);
     };
     f32x16_t dq[kD];
 #pragma unroll
@@ -186,17 +207,21 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dq_occupancy<T, D
         beyond = tab[kTabMargin];
         ahead = a.causal ? 0.f : tab[2 * a.far + kTabMargin];
     }
-    bool sums_only = few && !one;   // a first run over the keys for D alone
+    bool clean = false, poisoned = false;   // see below
     auto step = [&](const int t, const char* const kt_, const char* const vt_, char* const kn, char* const vn) __attribute__((always_inline)) {
         loads_done();
         if (SHARE == 4) __syncthreads();
         if (t + 1 < tiles) fetch(t + 1, kn, vn);
         const char* const kt = kt_ + own;
         const char* const vt = vt_ + own;
+        if (kRows && clean) {
+            const uint32_t rows = Tile<T, D>::clean(const_cast<char*>(kt)) | Tile<T, D>::clean(const_cast<char*>(vt));
+            poisoned |= meets(rows, jbase + t * BK, lo, end);
+        }
 #pragma unroll
         for (int k = 0; k < kT; ++k) {
-            const int j0 = t * BK + 32 * k;
-            if (j0 >= q.nk || (a.causal && j0 > wave_last) || iw >= q.nq) return;
+            const int j0 = jbase + t * BK + 32 * k;
+            if (!kRows && (j0 >= q.nk || (a.causal && j0 > wave_last) || iw >= q.nq)) return;
             f32x16_t x = f32x16_t{}, g = f32x16_t{};
 #pragma unroll
             for (int c = 0; c < kC; ++c) x = Mma<T>::mma(Tile<T, D>::along(kt, 32 * k + col, c, half), fq[c], x);
@@ -218,7 +243,11 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dq_occupancy<T, D
 #pragma unroll
                 for (int r = 0; r < 16; ++r) x[r] = __builtin_amdgcn_exp2f(fmaf(x[r], a.scale2, from[8 * (r / 4) + r % 4]) - lse);
             }
-            if (j0 + 32 > q.nk || (a.causal && j0 + 31 > first)) {
+            if constexpr (kRows) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if ((uint32_t)(j0 + 8 * (r / 4) + 4 * half + r % 4 - lo) >= (uint32_t)(end - lo)) x[r] = g[r] = 0.f;
+            } else if (j0 + 32 > q.nk || (a.causal && j0 + 31 > first)) {
                 const int end = a.causal && pos + 1 < q.nk ? pos + 1 : q.nk;
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
@@ -228,13 +257,14 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dq_occupancy<T, D
                 float sum = 0.f;
 #pragma unroll
                 for (int r = 0; r < 16; ++r) sum = fmaf(x[r], g[r], sum);
-                delta += sum;
+                dsum += sum;
                 if (sums_only) continue;
-                delta = pair_sum<32>(delta);
+                const float d = pair_sum<32>(dsum);
+                delta = !kRows || lo < end ? d : delta;
             }
 #pragma unroll
             for (int r = 0; r < 16; ++r) g[r] = x[r] * (g[r] - delta);
-            if (BIAS) {
+            if (BIAS && !(kRows && clean)) {
                 if (all_beyond || all_ahead) {
                     float sum = 0.f;
 #pragma unroll
@@ -245,7 +275,8 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dq_occupancy<T, D
                     // What a tile has of one distance lies on a diagonal; see diagonal_sums.  A distance of a half's array is met by two
                     // neighbouring tiles and stored once, with the second.
                     const float2 now = diagonal_sums(g);
-                    sums[half * size + j0 - first + a.far + kTabMargin + 4 * half - col] = now.x + carry;
+                    float* const to = sums + half * size + j0 - first + a.far + kTabMargin + 4 * half - col;
+                    *to = now.x + carry + (kRows ? *to : 0.f);   // (other columns' places may have met these distances before)
                     carry = now.y;
                     carry_at = j0 + 32;
                 }
@@ -260,29 +291,92 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dq_occupancy<T, D
             settle<T>();
         }
     };
-    for (;;) {
-        if (tiles > 0) fetch(0, keys0, values0);
-        for (int t = 0; t < tiles; t += 2) {
-            step(t, keys0, values0, keys1, values1);
-            if (t + 1 < tiles) step(t + 1, keys1, values1, keys0, values0);
+    // SHARE = 0: what is hidden has dS = 0, but 0 times a key that is not finite is not 0.  Where a result is not finite, all is done once
+    // more on tiles in which such elements are 0, and columns of whose own keys some are not finite become NaN.
+again:
+    uint64_t todo = kRows ? __ballot(is) : 1;
+    while (todo) {
+        if constexpr (kRows) {   // columns whose places lie as their rows do go together
+            const int shift = uniform(bcast_lane(own_pos - col, __ffsll((unsigned long long)todo) - 1));
+            const bool mine = is && own_pos - col == shift;
+            todo &= ~__ballot(mine);
+            first = shift;
+            pos = first + col;
+            wave_last = first + 31;
+            lo = mine ? own_lo : 0;
+            end = mine ? own_end : 0;
+            jbase = wave_min_i32(lo < end ? lo : 0x7FFFFFFF);
+            const int last = wave_max_i32(lo < end ? end : 0);
+            tiles = jbase < last ? (last - jbase + BK - 1) / BK : 0;
+        } else {
+            todo = 0;
         }
-        if (!sums_only) break;
-        sums_only = false;
-        delta = pair_sum<32>(delta);
-        if (SHARE == 4) __syncthreads();   // (the first tile's place may still be read)
+        one = kT == 1 && tiles == 1;
+        sums_only = tiles <= kFew && !one;
+        dsum = 0.f;
+        if (tiles > kFew) {
+            uint4 fo[kC];
+            column_row<T, D>(fo, a.o.at(row, head), is, half, a.dim);
+            float d = 0.f;
+#pragma unroll
+            for (int c = 0; c < kC; ++c) {
+                float x[kE], y[kE];
+                Frag<T>::unpack(fo[c], x);
+                Frag<T>::unpack(fy[c], y);
+#pragma unroll
+                for (int e = 0; e < kE; ++e) d = fmaf(x[e], y[e], d);
+            }
+            d = pair_sum<32>(d);
+            delta = !kRows || lo < end ? d : delta;
+        }
+        for (;;) {
+            if (tiles > 0) fetch(0, keys0, values0);
+            for (int t = 0; t < tiles; t += 2) {
+                step(t, keys0, values0, keys1, values1);
+                if (t + 1 < tiles) step(t + 1, keys1, values1, keys0, values0);
+            }
+            if (!sums_only) break;
+            sums_only = false;
+            const float d = pair_sum<32>(dsum);
+            delta = !kRows || lo < end ? d : delta;
+            if (SHARE == 4) __syncthreads();   // (the first tile's place may still be read)
+        }
+        if (BIAS && carry_at >= 0) {
+            float* const to = sums + half * size + carry_at - first + a.far + kTabMargin + 4 * half - col;
+            *to = carry + (kRows ? *to : 0.f);
+            carry = 0.f;
+            carry_at = -1;
+        }
     }
-    judge(a, looks, v, peek);
+    if (!kRows) judge(a, looks, v, peek);
+    if (kRows && !clean) {
+        float test = 0.f;
+#pragma unroll
+        for (int d = 0; d < kD; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) test = fmaf(dq[d][r], 0.f, test);
+        if (__any(test != 0.f)) {
+#pragma unroll
+            for (int d = 0; d < kD; ++d) dq[d] = f32x16_t{};
+            clean = true;
+            goto again;
+        }
+    }
+    if (kRows && poisoned) {
+#pragma unroll
+        for (int d = 0; d < kD; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) dq[d][r] = __builtin_nanf("");
+    }
     if (is && half == 0) {   // for attn_dkv_kernel
         a.delta[(int64_t)head * a.q_rows + row] = delta;
         a.lse2[(int64_t)head * a.q_rows + row] = lse;
     }
     if (is) store_column<T, D>(const_cast<char*>(a.dq.at(row, head)), dq, a.scale, half, a.dim);
     if (!BIAS) return;
-    if (carry_at >= 0) sums[half * size + carry_at - first + a.far + kTabMargin + 4 * half - col] = carry;
     // the distances that this unit has met
-    const int unit_first = q.nk - q.nq + i0, unit_last = unit_first + a.block - 1;
-    int from = a.far + kTabMargin - (unit_last < a.far + kTabMargin ? unit_last : a.far + kTabMargin);
-    int to = a.far + kTabMargin + (a.causal ? 0 : (q.nk - 1 - unit_first < a.far + kTabMargin ? q.nk - 1 - unit_first : a.far + kTabMargin)) + 1;
+    const int reach = a.far + kTabMargin;
+    int from = reach - (back < reach ? back : reach), to = reach + (a.causal || on < 0 ? 0 : (on < reach ? on : reach)) + 1;
     from = from < 0 ? 0 : (from > size ? size : from);
     to = to > size ? size : to;
     sum_beyond = group_sum(sum_beyond, 64);
@@ -328,7 +422,8 @@ template <typename T, int D, int SHARE, bool BIAS>
 __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dkv_occupancy<T, D>())) void attn_dkv_kernel(const AttnArgs a) {
     constexpr int kWaves = bwd_waves<T, D, SHARE>(), BQ = bwd_rows<T, D, SHARE>(), kT = BQ / 32, kD = D / 32;
     constexpr int kK = Mma<T>::kK, kC = D / kK, kM = 32 / kK;
-    constexpr int kTile = BQ * D * (int)sizeof(T), kSets = SHARE == 4 ? 1 : kWaves, kLds = kSets * kTile;
+    constexpr int kTile = BQ * D * (int)sizeof(T), kSets = SHARE == 4 ? 1 : kWaves, kLds = kSets * kTile, kSharers = SHARE == 4 ? 4 : 1;
+    constexpr bool kRows = SHARE == 0;
     __shared__ __align__(16) char rows0[kLds], rows1[kLds], grads0[kLds], grads1[kLds];
     __shared__ __align__(16) float stats0[kSets * 128], stats1[kSets * 128];   // lse and delta of 64 rows
     extern __shared__ float tab[];
@@ -339,51 +434,77 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dkv_occupancy<T, 
     if (wg >= groups) return;
     const int hh = wg / per_head, kvh = hh / parts, part = hh - kvh * parts, head0 = kvh * a.group + part * hp, size = tab_size(a.far);
     const uint32_t v = SHARE == 4 ? wg - hh * per_head : (wg - hh * per_head) * kWaves + wave;
-    if (BIAS && SHARE == 1) {
+    if (BIAS && SHARE != 4) {
         fill_bias(tab, a, head0, hp, 64 * kWaves);
         __syncthreads();
     }
     if (v >= (uint32_t)a.V) return;
-    const int s = find_sequence(a.k_off, a.N, v, a.block);
     Sequence q;
-    if (!take_sequence(a, s, sequence_numbers(a, s), q)) return;
-    const uint32_t start = (uint32_t)q.k0 / a.block + s, blocks = ((uint32_t)q.cap + a.block - 1) / a.block;
-    if (v < start || v - start >= blocks) return;
-    const int j0 = uniform((int)(v - start) * a.block), jw = j0 + (SHARE == 4 ? wave * 32 : 0), j = jw + col;
-    const bool is = j < q.nk;
+    int j0, jw, j, lead, t0 = 0, tiles, ibase = 0, lo = 0, end = 0;
+    int own_lo = 0, own_end = 0, own_lead = 0;   // SHARE = 0: the rows of q that see this column's key, and how far their places lie from their rows
+    bool is, writes;
+    if constexpr (kRows) {
+        if (hh == 0) judge_all(a, v, a.V);
+        q.k0 = (int64_t)v * 32;
+        q.q0 = 0;
+        q.nq = (int)a.q_rows;
+        q.nk = q.cap = 32;
+        const LaneSequence mine = lane_numbers(a, lane_sequence(a.k_off, a.N, q.k0, a.k_rows));
+        const int64_t row = q.k0 + col;
+        is = writes = mine.fits && row >= mine.k0 && row < mine.k1;
+        own_lead = (int)(mine.k1 - mine.q1);
+        own_lo = is ? (int)mine.q0 : 0;
+        own_end = is ? (int)mine.q1 : 0;
+        if (is && a.causal && (int)row - own_lead > own_lo) own_lo = (int)row - own_lead;
+        if (own_end < own_lo) own_end = own_lo;
+        j0 = jw = 0;
+        j = col;
+        lead = tiles = 0;
+        if (!__any(is)) return;
+    } else {
+        const int s = find_sequence(a.k_off, a.N, v, a.block);
+        if (!take_sequence(a, s, sequence_numbers(a, s), q)) return;
+        const uint32_t start = (uint32_t)q.k0 / a.block + s, blocks = ((uint32_t)q.cap + a.block - 1) / a.block;
+        if (v < start || v - start >= blocks) return;
+        j0 = uniform((int)(v - start) * a.block);
+        jw = j0 + (SHARE == 4 ? wave * 32 : 0);
+        j = jw + col;
+        is = j < q.nk;
+        writes = j < q.cap;
+        // the queries that see these keys: all, or from the one in the first key's place on
+        lead = q.nk - q.nq;   // the first query's place
+        if (a.causal && j0 > lead) t0 = (j0 - lead) / BQ;
+        const int all = j0 < q.nk ? (q.nq + BQ - 1) / BQ : 0;
+        t0 = uniform(t0 < all ? t0 : all);
+        tiles = uniform(all - t0);
+    }
 
     uint4 fk[kC], fv[kC];
     column_row<T, D>(fk, a.k.at(q.k0 + (is ? j : 0), kvh), is, half, a.dim);
     column_row<T, D>(fv, a.v.at(q.k0 + (is ? j : 0), kvh), is, half, a.dim);
     if (a.negative) flip_signs<T, kC>(fk);
 
-    // the queries that see these keys: all, or from the one in the first key's place on
-    const int lead = q.nk - q.nq;   // the first query's place
-    int t0 = 0;
-    if (a.causal && j0 > lead) t0 = (j0 - lead) / BQ;
-    const int all = j0 < q.nk ? (q.nq + BQ - 1) / BQ : 0;
-    t0 = uniform(t0 < all ? t0 : all);
-    const int tiles = uniform(all - t0), steps = tiles * hp;
     const int own = SHARE == 4 ? 0 : wave * kTile, own_stats = SHARE == 4 ? 0 : wave * 128, fw = SHARE == 4 ? wave : 0;
     auto fetch = [&](const int g, const int t, char* const qt, char* const yt, float* const st) __attribute__((always_inline)) {
         const int head = head0 + g;
-        Tile<T, D>::template fetch<BQ, SHARE>(qt + own, a.q.at(q.q0, head), a.q.row, t * BQ, q.nq, a.dim, fw);
-        Tile<T, D>::template fetch<BQ, SHARE>(yt + own, a.dout.at(q.q0, head), a.dout.row, t * BQ, q.nq, a.dim, fw);
-        if (SHARE == 1 || wave < 2) {
-            const int i = t * BQ + lane;
+        Tile<T, D>::template fetch<BQ, kSharers>(qt + own, a.q.at(q.q0, head), a.q.row, ibase + t * BQ, q.nq, a.dim, fw);
+        Tile<T, D>::template fetch<BQ, kSharers>(yt + own, a.dout.at(q.q0, head), a.dout.row, ibase + t * BQ, q.nq, a.dim, fw);
+        if (SHARE != 4 || wave < 2) {
+            const int i = ibase + t * BQ + lane;
             const bool there = lane < BQ && i < q.nq;
             const int64_t at = (int64_t)head * a.q_rows + q.q0 + i;
             const float* const l = there ? a.lse2 + at : &attn_inf;
             const float* const d = there ? a.delta + at : reinterpret_cast<const float*>(&attn_zeros);
-            if (SHARE == 1 || wave == 0)
+            if (SHARE != 4 || wave == 0)
                 load_lds<4>(l, st + own_stats);
-            if (SHARE == 1 || wave == 1)
+            if (SHARE != 4 || wave == 1)
                 load_lds<4>(d, st + own_stats + 64);
         }
     };
     f32x16_t dk[kD], dv[kD];
 #pragma unroll
     for (int d = 0; d < kD; ++d) dk[d] = dv[d] = f32x16_t{};
+    bool clean = false, poisoned = false;   // as in attn_dq_kernel
     // the step after (g, t) is (g, t + 1) or the next head's first
     auto step = [&](const int g, const int t, const bool more, const char* const qt_, const char* const yt_, const float* const st_, char* const qn,
                     char* const yn, float* const sn) __attribute__((always_inline)) {
@@ -400,11 +521,15 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dkv_occupancy<T, 
         const char* const qt = qt_ + own;
         const char* const yt = yt_ + own;
         const float* const ht = SHARE == 4 ? tab : tab + g * size;
+        if (kRows && clean) {
+            const uint32_t rows = Tile<T, D>::clean(const_cast<char*>(qt)) | Tile<T, D>::clean(const_cast<char*>(yt));
+            poisoned |= meets(rows, ibase + t * BQ, lo, end);
+        }
 #pragma unroll
         for (int k = 0; k < kT; ++k) {
-            const int i0 = t * BQ + 32 * k, first = lead + i0;   // the first query and its place
-            if (i0 >= q.nq || jw >= q.nk) return;
-            if (a.causal && first + 31 < jw) continue;
+            const int i0 = ibase + t * BQ + 32 * k, first = lead + i0;   // the first query and its place
+            if (!kRows && (i0 >= q.nq || jw >= q.nk)) return;
+            if (!kRows && a.causal && first + 31 < jw) continue;
             f32x16_t x = f32x16_t{}, g_ = f32x16_t{};
 #pragma unroll
             for (int c = 0; c < kC; ++c) x = Mma<T>::mma(Tile<T, D>::along(qt, 32 * k + col, c, half), fk[c], x);
@@ -430,7 +555,11 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dkv_occupancy<T, 
                     g_[r] = x[r] * (g_[r] - d[e]);
                 }
             }
-            if (a.causal && first < jw + 31) {   // hidden: queries before the key's place
+            if constexpr (kRows) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if ((uint32_t)(i0 + 8 * (r / 4) + 4 * half + r % 4 - lo) >= (uint32_t)(end - lo)) x[r] = g_[r] = 0.f;
+            } else if (a.causal && first < jw + 31) {   // hidden: queries before the key's place
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
                     if (first + 8 * (r / 4) + 4 * half + r % 4 < j) x[r] = g_[r] = 0.f;
@@ -448,16 +577,52 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dkv_occupancy<T, 
             settle<T>();
         }
     };
-    if (steps > 0) fetch(0, t0, rows0, grads0, stats0);
-    int g = 0, t = t0;
-    for (int n = 0; n < steps; n += 2) {
-        step(g, t, n + 1 < steps, rows0, grads0, stats0, rows1, grads1, stats1);
-        if (++t == t0 + tiles) { t = t0; ++g; }
-        if (n + 1 >= steps) break;
-        step(g, t, n + 2 < steps, rows1, grads1, stats1, rows0, grads0, stats0);
-        if (++t == t0 + tiles) { t = t0; ++g; }
+again:
+    uint64_t todo = kRows ? __ballot(is) : 1;
+    while (todo) {
+        if constexpr (kRows) {   // keys whose queries' places lie alike go together
+            lead = uniform(bcast_lane(own_lead, __ffsll((unsigned long long)todo) - 1)) - (int)q.k0;
+            const bool mine = is && own_lead - (int)q.k0 == lead;
+            todo &= ~__ballot(mine);
+            lo = mine ? own_lo : 0;
+            end = mine ? own_end : 0;
+            ibase = wave_min_i32(lo < end ? lo : 0x7FFFFFFF);
+            const int last = wave_max_i32(lo < end ? end : 0);
+            tiles = ibase < last ? (last - ibase + BQ - 1) / BQ : 0;
+        } else {
+            todo = 0;
+        }
+        const int steps = tiles * hp;
+        if (steps > 0) fetch(0, t0, rows0, grads0, stats0);
+        int g = 0, t = t0;
+        for (int n = 0; n < steps; n += 2) {
+            step(g, t, n + 1 < steps, rows0, grads0, stats0, rows1, grads1, stats1);
+            if (++t == t0 + tiles) { t = t0; ++g; }
+            if (n + 1 >= steps) break;
+            step(g, t, n + 2 < steps, rows1, grads1, stats1, rows0, grads0, stats0);
+            if (++t == t0 + tiles) { t = t0; ++g; }
+        }
     }
-    if (j >= q.cap) return;
+    if (kRows && !clean) {
+        float test = 0.f;
+#pragma unroll
+        for (int d = 0; d < kD; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) test = fmaf(dk[d][r], 0.f, fmaf(dv[d][r], 0.f, test));
+        if (__any(test != 0.f)) {   // as in attn_dq_kernel
+#pragma unroll
+            for (int d = 0; d < kD; ++d) dk[d] = dv[d] = f32x16_t{};
+            clean = true;
+            goto again;
+        }
+    }
+    if (kRows && poisoned) {
+#pragma unroll
+        for (int d = 0; d < kD; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) dk[d][r] = dv[d][r] = __builtin_nanf("");
+    }
+    if (!writes) return;
     const float by = is ? 1.f : 0.f;   // (a cache's room: zeros)
     if (!is) {
 #pragma unroll
@@ -501,19 +666,23 @@ __global__ __launch_bounds__(256) void attn_dkv_join_kernel(const AttnArgs a) {
 }
 
 // How the backward shares out its work: queries and keys of long sequences by 128, of short ones by 32; the heads of a group in
-// parts where there would be too few workgroups of keys to fill the chip.
+// parts where there would be too few workgroups of keys to fill the chip.  Short sequences share wavefronts where there are many (see
+// kManyUnits); of dk and dv only those of narrow heads gain: wavefronts of one sequence / shared ones, 4096 sequences of 12 events on average,
+// 4 heads of 32 55 / 50, 8 of 64 173 / 161, 2 of 128 99 / 103, all of 40 events 8 of 64 452 / 501, 2 of 128 213 / 257 us.
 AttnBackwardPlan attn_backward_plan(const AttnShape& sh) {
     AttnBackwardPlan p;
     const int64_t mean_q = (sh.q_rows + sh.N - 1) / sh.N, mean_k = (sh.k_rows + sh.N - 1) / sh.N;
     const int group = sh.H / sh.kv;
     p.D = sh.dim <= 32 ? 32 : (sh.dim <= 64 ? 64 : 128);
     p.shared_q = mean_q > 64;
+    p.rows_q = !p.shared_q && !sh.caches && mean_k <= 2 * mean_q && (sh.q_rows / 32 + sh.N) * sh.H >= kManyUnits;
     p.block_q = p.shared_q ? 128 : 32;
-    p.V_q = sh.q_rows / p.block_q + sh.N;
+    p.V_q = p.rows_q ? (sh.q_rows + 31) / 32 : sh.q_rows / p.block_q + sh.N;
     const int64_t tables = sh.buckets ? (int64_t)group * (2 * sh.far + 1 + 2 * kTabMargin) * 4 : 0;
     p.shared_k = mean_k > 64 || tables > kTabBytes;
+    p.rows_k = p.D == 32 && !p.shared_k && !sh.caches && mean_q <= 2 * mean_k && (sh.k_rows / 32 + sh.N) * sh.kv >= kManyUnits;
     p.block_k = p.shared_k ? 128 : 32;
-    p.V_k = sh.k_rows / p.block_k + sh.N;
+    p.V_k = p.rows_k ? (sh.k_rows + 31) / 32 : sh.k_rows / p.block_k + sh.N;
     const int64_t units = (sh.k_rows / p.block_k + 1) * sh.kv, enough = p.shared_k ? 768 : 4096;
     p.parts = 1;
     while (p.parts < group && units * p.parts < enough) {
@@ -529,6 +698,7 @@ AttnBackwardPlan attn_backward_plan(const AttnShape& sh) {
 }
 size_t attn_backward_workspace(const AttnShape& sh) {   // (large tables of distances make the keys' units large)
     AttnShape near = sh, far = sh;
+    near.caches = far.caches = true;   // (which has the most units)
     near.far = 0;
     far.far = kAttnMaxFar;
     size_t most = 0;
@@ -567,6 +737,7 @@ static hipError_t launch_dim(const tbe_handle* h, AttnArgs a, const AttnBackward
         a.V = (int)p.V_q; a.block = p.block_q;
         LaunchTimer tm(h, s, "attention_dq");
         if (p.shared_q) e = a.bias ? launch_dq<T, D, 4, true>(a, s) : launch_dq<T, D, 4, false>(a, s);
+        else if (p.rows_q) e = a.bias ? launch_dq<T, D, 0, true>(a, s) : launch_dq<T, D, 0, false>(a, s);
         else e = a.bias ? launch_dq<T, D, 1, true>(a, s) : launch_dq<T, D, 1, false>(a, s);
         tm.done();
         if (e != hipSuccess) return e;
@@ -584,6 +755,7 @@ static hipError_t launch_dim(const tbe_handle* h, AttnArgs a, const AttnBackward
     {
         LaunchTimer tm(h, s, "attention_dkv");
         if (p.shared_k) e = a.bias ? launch_dkv<T, D, 4, true>(a, s) : launch_dkv<T, D, 4, false>(a, s);
+        else if (p.rows_k) e = a.bias ? launch_dkv<T, D, 0, true>(a, s) : launch_dkv<T, D, 0, false>(a, s);
         else e = a.bias ? launch_dkv<T, D, 1, true>(a, s) : launch_dkv<T, D, 1, false>(a, s);
         tm.done();
     }

@@ -170,11 +170,13 @@ constexpr int kAttnMaxDim = 128, kAttnMaxFar = 1024;
 struct AttnShape {
     int64_t q_rows, k_rows;
     int N, H, kv, dim, buckets, far;   // buckets 0: no bias
+    bool caches;                       // k_lengths is given
 };
 struct AttnPlan {
     int D;        // elements of a row as the kernels have it
     bool shared;  // wavefronts of a workgroup share tiles
     bool together;   // ... or take parts of the same keys
+    bool rows;       // a wavefront takes 32 rows, whosesoever they are
     int pack, qpt, block, splits;
     int64_t V;
     size_t part_ml, part_o;   // bytes
@@ -187,7 +189,7 @@ struct AttnArgs;
 hipError_t launch_attention(const tbe_handle* h, AttnArgs a, const AttnPlan& p, int io, void* workspace, hipStream_t s);
 struct AttnBackwardPlan {
     int D, block_q, block_k, parts;   // parts: of the heads of a group
-    bool shared_q, shared_k, grid_ok;
+    bool shared_q, shared_k, rows_q, rows_k, grid_ok;
     int64_t V_q, V_k;
     size_t delta, part_bias, part_kv;   // bytes
 };
