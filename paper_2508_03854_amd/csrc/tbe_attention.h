@@ -99,13 +99,17 @@ __device__ __forceinline__ void reads_ahead() {
     for (int i = 0; i < kAhead; ++i) __builtin_amdgcn_sched_group_barrier(0x008, MFMAS, 0);
 }
 
-// A tile of rows of D elements in LDS, sixteen-byte chunks: chunk c of row r lies at place c ^ swizzle(r) of its row, so that neither
-// reading a column of chunks nor reading down the rows piles up on a few banks.  Rows arrive straight from memory; a wavefront's 64 chunks
-// land one behind the other, so it is the source that is permuted.
+// A tile of rows of D elements in LDS, sixteen-byte chunks: chunk c of row r lies at place c ^ swizzle(r) of its row.  The LDS serves 256
+// bytes a clock: of 16-byte reads along the rows those of 16 rows, which therefore lie in 16 different chunks of the 64 banks; of 8-byte
+// reads down the rows those of 4 rows by 4 chunks, which therefore lie in different quarters.  (The row's number alone as the swizzle
+// left the latter four to a quarter, 60 % of the LDS's clocks.)  Rows arrive straight from memory; a wavefront's 64 chunks land one
+// behind the other, so it is the source that is permuted.
 template <typename T, int D>
 struct Tile {
     static constexpr int kChunks = D * (int)sizeof(T) / 16;   // of a row: 4 to 32
-    static __device__ __forceinline__ int swizzle(const int r) { return kChunks == 4 ? (r >> 1) & 3 : r & (kChunks < 16 ? kChunks - 1 : 15); }
+    static __device__ __forceinline__ int swizzle(const int r) {
+        return kChunks == 4 ? (r >> 2) & 3 : (kChunks == 8 ? ((r >> 1) & 1) << 2 | ((r >> 2) & 3) : (r & 3) << 2 | ((r >> 2) & 3));
+    }
     // fragment c of the tile's row r, along the row (the lanes' halves take alternate chunks)
     static __device__ __forceinline__ uint4 along(const char* lds, const int r, const int c, const int half) {
         return *reinterpret_cast<const uint4*>(lds + (r * kChunks + ((2 * c + half) ^ swizzle(r))) * 16);
