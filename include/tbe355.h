@@ -334,7 +334,7 @@ tbe_status tbe_layer_norm_backward(const tbe_handle* h, const void* dy, int64_t 
  *   bucket_map  DEVICE int32 [2 max_distance + 1], 0 <= max_distance <= 1024; a number outside [0, buckets) counts as no bias and is
  *             reported likewise
  *   lse       DEVICE float [heads][q_rows]; the forward writes it unless NULL, the backward reads it
- * 0 <= q_rows, k_rows < 2^31, 1 <= sequences < 2^24, 1 <= kv_heads <= heads <= 1024 with heads a multiple of kv_heads,
+ * 0 <= q_rows, k_rows <= 2^31 - 4096, 1 <= sequences < 2^24, 1 <= kv_heads <= heads <= 1024 with heads a multiple of kv_heads,
  * 1 <= buckets <= 1024.  Scores, softmax and sums are in fp32; probabilities and dS are rounded once to dtype where they are multiplied by
  * v, k, q or dout (fp32: not at all), results once when stored.  The order of all additions is fixed: results do not depend on
  * timing.  A value that is not finite reaches those results of the forward that see it, and

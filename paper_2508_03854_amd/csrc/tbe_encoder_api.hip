@@ -68,8 +68,8 @@ tbe_status tbe_layer_norm_backward(const tbe_handle* h, const void* dy, int64_t 
 static tbe_status check_attention_sizes(const tbe_handle* h, const tbe_attention_args* a) {
     if (!h || !a) return TBE_EINVAL;
     if (!io_known(a->dtype) || (a->index_dtype != TBE_I64 && a->index_dtype != TBE_I32)) return TBE_EDTYPE;
-    const int64_t most = (int64_t)1 << 31;
-    if (a->sequences < 1 || a->sequences >= 1 << 24 || a->q_rows < 0 || a->q_rows >= most || a->k_rows < 0 || a->k_rows >= most) return TBE_ESHAPE;
+    const int64_t most = ((int64_t)1 << 31) - 4096;   // (a tile beyond the last row has a number still)
+    if (a->sequences < 1 || a->sequences >= 1 << 24 || a->q_rows < 0 || a->q_rows > most || a->k_rows < 0 || a->k_rows > most) return TBE_ESHAPE;
     if (a->kv_heads < 1 || a->heads < a->kv_heads || a->heads > 1024 || a->heads % a->kv_heads != 0) return TBE_ESHAPE;
     if (a->head_dim < 1 || a->head_dim > kAttnMaxDim || a->head_dim % (16 / (int)io_size(a->dtype)) != 0) return TBE_ESHAPE;
     if (a->buckets < 0 || a->buckets > 1024) return TBE_ESHAPE;
