@@ -29,6 +29,22 @@ constexpr int kTabMargin = 68;         // a tile that reaches into the table of 
 constexpr int64_t kManyUnits = 2048;
 constexpr int kTabBytes = 24 << 10;    // LDS for such tables
 
+// Sequences of few rows have a wavefront for every 32 of them, longer ones a workgroup for every 128, which share the tiles of the other side: up
+// to 64 rows on average, and as long as neither side has more than `most`.  Shared / on their own, us, as many sequences as named of that
+// length, with bias, causal:
+//   forward  32 bfloat16: 512 of 128 44 / 28, of 180 54 / 44, 256 of 150 with 300 keys 39 / 44, 64 of 400 23 / 26
+//            64 bfloat16: 512 of 80 83 / 50, of 128 178 / 83, of 180 234 / 161, 64 of 256 38 / 32, of 600 101 / 101;  fp32: 64 of 256 63 / 61
+//            128 bfloat16: 64 of 80 15.6 / 14.8, of 128 17.6 / 25.3;  fp32: 64 of 128 33 / 46
+//   dq       32 bfloat16: 512 of 128 102 / 88, of 180 136 / 141;  fp32: 512 of 128 296 / 235, of 200 410 / 431
+//            64 bfloat16: 512 of 128 371 / 250, of 180 452 / 400, 64 of 256 76 / 77, 256 of 245 372 / 424;  fp32: 512 of 128 639 / 344,
+//            64 of 400 255 / 209, of 600 378 / 375
+//            128 bfloat16: 64 of 128 33 / 45;  fp32: 67 / 82
+//   dk, dv   32 bfloat16: 512 of 128 64 / 51, of 180 70 / 86
+//            64 bfloat16: 512 of 128 256 / 171, 64 of 180 41 / 35, of 256 46 / 49;  fp32: 64 of 400 289 / 199, of 600 385 / 366
+//            128 bfloat16: 64 of 128 35 / 27, of 400 129 / 91, 16 of 2000 335 / 313, 4 of 4000 451 / 248 (the shared kernel has one
+//            wavefront a SIMD, which waits at its barriers);  fp32: 64 of 80 41 / 45, of 200 121 / 148
+inline bool attn_few(const int64_t mean, const int64_t other, const int64_t most) { return mean <= 64 || (mean <= most && other <= most); }
+
 // Sixteen zero bytes: what stands behind a sequence's end, or behind a row's, is read from here.
 static __device__ const uint4 attn_zeros = {0u, 0u, 0u, 0u};
 

@@ -462,16 +462,19 @@ __global__ __launch_bounds__(256) void attn_join_kernel(const AttnArgs a) {
     if (a.lse && lane == 0) a.lse[(int64_t)head * a.q_rows + q.q0 + i] = sum == 0.f ? -__builtin_inff() : fmaf(m, kLn2, logf(sum));
 }
 
-// How the forward shares out its work.  Sequences of many queries: 128 neighbours share the keys' tiles.  Few queries per sequence:
-// wavefronts on their own, heads of a group side by side where one query would leave its columns empty, and the keys in parts where
-// there would be too few wavefronts to keep the memory busy.
+// How the forward shares out its work.  Sequences of many queries: 128 neighbours share the keys' tiles (see attn_few).  Few queries per
+// sequence: wavefronts on their own, heads of a group side by side where one query would leave its columns empty (24 caches of 34,000 keys, one
+// query, 16 heads of 2: 173 us; one head each: 943), and the keys in parts of 128 or more where there would be fewer than 2048 wavefronts.  Parts
+// for one query of 16 heads of 2 of 128 elements, none / this, us with the join: one cache of 256 keys 17 / 11, of 16,384 514 / 23.5; 64 of them 639 /
+// 195; for half as many wavefronts 191 (but 61 queries each of 8 heads of 64 117 / 62), for twice as many 200; parts of 64 or more keys, one cache
+// of 256, 1024, 16,384 keys: 18 / 11, 18 / 20, 26 / 23.5; of 256 or more 17 / 11, 21 / 20, 26 / 23.5.
 AttnPlan attn_plan(const AttnShape& sh, const int max_pack) {
     AttnPlan p;
     const int64_t mean_q = sh.N > 0 ? (sh.q_rows + sh.N - 1) / sh.N : 0, mean_k = sh.N > 0 ? (sh.k_rows + sh.N - 1) / sh.N : 0;
     p.D = sh.dim <= 32 ? 32 : (sh.dim <= 64 ? 64 : 128);
     p.pack = 1;
     p.splits = 1;
-    p.shared = mean_q > 64;
+    p.shared = !attn_few(mean_q, mean_k, p.D == 32 ? 128 : (p.D == 64 ? 256 : 64));
     if (p.shared) {
         p.qpt = 32;
         p.block = 128;

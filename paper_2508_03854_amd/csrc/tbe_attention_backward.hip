@@ -674,12 +674,13 @@ AttnBackwardPlan attn_backward_plan(const AttnShape& sh) {
     const int64_t mean_q = (sh.q_rows + sh.N - 1) / sh.N, mean_k = (sh.k_rows + sh.N - 1) / sh.N;
     const int group = sh.H / sh.kv;
     p.D = sh.dim <= 32 ? 32 : (sh.dim <= 64 ? 64 : 128);
-    p.shared_q = mean_q > 64;
+    const int64_t few = p.D == 32 ? 128 : (p.D == 64 ? (sh.narrow ? 192 : 384) : 64);
+    p.shared_q = !attn_few(mean_q, mean_k, few);
     p.rows_q = !p.shared_q && !sh.caches && mean_k <= 2 * mean_q && (sh.q_rows / 32 + sh.N) * sh.H >= kManyUnits;
     p.block_q = p.shared_q ? 128 : 32;
     p.V_q = p.rows_q ? (sh.q_rows + 31) / 32 : sh.q_rows / p.block_q + sh.N;
     const int64_t tables = sh.buckets ? (int64_t)group * (2 * sh.far + 1 + 2 * kTabMargin) * 4 : 0;
-    p.shared_k = mean_k > 64 || tables > kTabBytes;
+    p.shared_k = tables > kTabBytes || !attn_few(mean_k, mean_q, p.D == 128 && sh.narrow ? INT64_MAX : few);
     p.rows_k = p.D == 32 && !p.shared_k && !sh.caches && mean_q <= 2 * mean_k && (sh.k_rows / 32 + sh.N) * sh.kv >= kManyUnits;
     p.block_k = p.shared_k ? 128 : 32;
     p.V_k = p.rows_k ? (sh.k_rows + 31) / 32 : sh.k_rows / p.block_k + sh.N;
@@ -697,15 +698,16 @@ AttnBackwardPlan attn_backward_plan(const AttnShape& sh) {
     return p;
 }
 size_t attn_backward_workspace(const AttnShape& sh) {   // (large tables of distances make the keys' units large)
-    AttnShape near = sh, far = sh;
-    near.caches = far.caches = true;   // (which has the most units)
-    near.far = 0;
-    far.far = kAttnMaxFar;
+    AttnShape any = sh;
+    any.caches = true;   // (which has the most units)
     size_t most = 0;
-    for (const AttnShape& x : {near, far}) {
-        const AttnBackwardPlan p = attn_backward_plan(x);
-        most = std::max(most, p.delta + p.part_bias + p.part_kv);
-    }
+    for (const int far : {0, kAttnMaxFar})
+        for (const bool narrow : {false, true}) {
+            any.far = far;
+            any.narrow = narrow;
+            const AttnBackwardPlan p = attn_backward_plan(any);
+            most = std::max(most, p.delta + p.part_bias + p.part_kv);
+        }
     return most;
 }
 

@@ -80,6 +80,7 @@ static AttnShape attention_shape(const tbe_attention_args* a) {
     sh.q_rows = a->q_rows; sh.k_rows = a->k_rows;
     sh.N = a->sequences; sh.H = a->heads; sh.kv = a->kv_heads; sh.dim = a->head_dim;
     sh.buckets = a->bias ? a->buckets : 0; sh.far = a->max_distance; sh.caches = a->k_lengths != nullptr;
+    sh.narrow = a->dtype != TBE_IO_F32;
     return sh;
 }
 // the kernels' view of a matrix; false: not as it has to be

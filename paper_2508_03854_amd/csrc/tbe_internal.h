@@ -171,6 +171,7 @@ struct AttnShape {
     int64_t q_rows, k_rows;
     int N, H, kv, dim, buckets, far;   // buckets 0: no bias
     bool caches;                       // k_lengths is given
+    bool narrow;                       // elements of 16 bits
 };
 struct AttnPlan {
     int D;        // elements of a row as the kernels have it
