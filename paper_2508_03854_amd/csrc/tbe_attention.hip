@@ -2,7 +2,10 @@
 // of the softmax; no score leaves the registers.
 //   S^T = K Q^T  (a tile: 32 keys x 32 columns)    p = 2^(x - m)    O^T += V^T P
 // Bound: long sequences by the vector unit's work on every score (the exponential, the sums) next to the matrix cores, single tokens by
-// reading the keys and values once.
+// reading the keys and values once, many short sequences by a wavefront's trips to memory.  Measured: 2 causal sequences of 4000 to 8000, 16
+// heads of 128 over 4, bfloat16, 2.3e11 operations: 293 to 330 us on different cards, 0.7 to 0.78 PFLOP/s; one query to each of 24 caches of
+// 2000 to 65536 keys, 16 heads over 2, 0.8 GB: 173 us and 11 for the join, 4.4 TB/s; 4096 sequences of 12 events on average, 4 heads of 32
+// with a bias: 23 us for 51 MB.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -17,6 +20,8 @@ namespace tbe {
 // attn_join_kernel.
 // SHARE = 0: short sequences: a wavefront takes 32 neighbouring rows of q, whosesoever they are, and the keys of all their sequences; a column
 // hides what is not its own sequence's (see kManyUnits).
+// Rows of a tile of keys: 64 where the LDS has room for two of them of keys and of values and a second workgroup (2 sequences of 6000, 16 heads of 128
+// bfloat16: 64 rows 331 us, 32 rows 363; heads of 64 172 / 169 and of 32 128 / 126 with either).
 template <typename T, int D, int SHARE>
 constexpr int kv_rows() { return SHARE == 4 && D * (int)sizeof(T) <= 256 ? 64 : 32; }
 template <typename T, int D, int SHARE>
@@ -40,8 +45,10 @@ __global__ __launch_bounds__((64 * attn_waves<T, D, SHARE>()), (attn_occupancy<T
     const uint32_t per_head = SHARE == 4 || together ? (uint32_t)a.V * a.splits : ((uint32_t)a.V + kWaves - 1) / kWaves;
     const uint32_t groups = per_head * (uint32_t)(a.H / a.pack), wg = die_order(groups);
     if (wg >= groups) return;
-    const int hh = wg / per_head, head0 = hh * a.pack;
-    const uint32_t item = wg - hh * per_head;
+    int hh;
+    uint32_t item;
+    head_and_item<SHARE>(wg, per_head, a.H / a.pack, hh, item);
+    const int head0 = hh * a.pack;
     if (BIAS) {
         fill_bias(tab, a, head0, a.pack, 64 * kWaves);
         __syncthreads();

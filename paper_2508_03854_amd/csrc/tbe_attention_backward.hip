@@ -3,7 +3,10 @@
 //   attn_dq_kernel    columns are queries:  S^T = K Q^T, dP^T = V dO^T, dS;  dQ^T += K^T dS;  also D = rowsum(dO O), and dbias
 //   attn_dkv_kernel   columns are keys:     S = Q K^T,   dP = dO V^T,   dS;  dV^T += dO^T P,  dK^T += Q^T dS
 // Seven products of a tile instead of five: sums of dQ from one kernel over key blocks would need atomics or a pass over partial sums.
-// Bound: the matrix cores and the vector unit's work on every score, twice; short sequences by the trips to memory of a wavefront.
+// Bound: the matrix cores and the vector unit's work on every score, twice; short sequences by the trips to memory of a wavefront.  Measured: 4
+// causal sequences of 1000 to 4096, 8 heads of 64 over 2, binary16, a bias of 32 buckets, 6.0e10 operations: dq 127, dbias 6, dk and dv 134 and
+// their join 10 us, 0.22 PFLOP/s (the matrix cores busy 27 % and the vector unit 45 % of the clocks, 1.7 wavefronts a SIMD); 4096 sequences of 12
+// events on average, 4 heads of 32: 59 + 7 + 46 us for 103 MB.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -112,8 +115,11 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dq_occupancy<T, D
     const uint32_t per_head = SHARE == 4 ? (uint32_t)a.V : ((uint32_t)a.V + kWaves - 1) / kWaves;
     const uint32_t groups = per_head * (uint32_t)a.H, wg = die_order(groups);
     if (wg >= groups) return;
-    const int head = wg / per_head, size = tab_size(a.far);
-    const uint32_t v = SHARE == 4 ? wg - head * per_head : (wg - head * per_head) * kWaves + wave;
+    int head;
+    uint32_t item;
+    head_and_item<SHARE>(wg, per_head, a.H, head, item);
+    const int size = tab_size(a.far);
+    const uint32_t v = SHARE == 4 ? item : item * kWaves + wave;
     uint16_t* const bucket = reinterpret_cast<uint16_t*>(tab + size * (1 + 2 * kWaves));
     if (BIAS) {
         fill_bias(tab, a, head, 1, 64 * kWaves, bucket);
@@ -432,8 +438,11 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dkv_occupancy<T, 
     const uint32_t per_head = SHARE == 4 ? (uint32_t)a.V : ((uint32_t)a.V + kWaves - 1) / kWaves;
     const uint32_t groups = per_head * (uint32_t)(a.kv * parts), wg = die_order(groups);
     if (wg >= groups) return;
-    const int hh = wg / per_head, kvh = hh / parts, part = hh - kvh * parts, head0 = kvh * a.group + part * hp, size = tab_size(a.far);
-    const uint32_t v = SHARE == 4 ? wg - hh * per_head : (wg - hh * per_head) * kWaves + wave;
+    int hh;
+    uint32_t item;
+    head_and_item<SHARE>(wg, per_head, a.kv * parts, hh, item);
+    const int kvh = hh / parts, part = hh - kvh * parts, head0 = kvh * a.group + part * hp, size = tab_size(a.far);
+    const uint32_t v = SHARE == 4 ? item : item * kWaves + wave;
     if (BIAS && SHARE != 4) {
         fill_bias(tab, a, head0, hp, 64 * kWaves);
         __syncthreads();
@@ -666,9 +675,11 @@ __global__ __launch_bounds__(256) void attn_dkv_join_kernel(const AttnArgs a) {
 }
 
 // How the backward shares out its work: queries and keys of long sequences by 128, of short ones by 32; the heads of a group in
-// parts where there would be too few workgroups of keys to fill the chip.  Short sequences share wavefronts where there are many (see
-// kManyUnits); of dk and dv only those of narrow heads gain: wavefronts of one sequence / shared ones, 4096 sequences of 12 events on average,
-// 4 heads of 32 55 / 50, 8 of 64 173 / 161, 2 of 128 99 / 103, all of 40 events 8 of 64 452 / 501, 2 of 128 213 / 257 us.
+// parts where there would be too few workgroups of keys to fill the chip: 768 that share tiles, 4096 wavefronts on their own (16 sequences of
+// 2500, 8 heads of 64 over 2 binary16, dk and dv and the join, us: 256 / 768 / 2048 of them 608 / 533 / 463; 4 of them 252 / 149 / 149).
+// Short sequences share wavefronts where there are many (see kManyUnits); of dk and dv those of narrow heads and of 64 fp32 elements:
+// wavefronts of one sequence / shared ones, 4096 sequences of 12 events on average, 4 heads of 32 bfloat16 55 / 50, 8 of 64 170 / 164, fp32
+// 511 / 279, 2 of 128 99 / 103; 1024 of 40, 8 of 64 95 / 121, fp32 284 / 222.
 AttnBackwardPlan attn_backward_plan(const AttnShape& sh) {
     AttnBackwardPlan p;
     const int64_t mean_q = (sh.q_rows + sh.N - 1) / sh.N, mean_k = (sh.k_rows + sh.N - 1) / sh.N;
@@ -681,7 +692,7 @@ AttnBackwardPlan attn_backward_plan(const AttnShape& sh) {
     p.V_q = p.rows_q ? (sh.q_rows + 31) / 32 : sh.q_rows / p.block_q + sh.N;
     const int64_t tables = sh.buckets ? (int64_t)group * (2 * sh.far + 1 + 2 * kTabMargin) * 4 : 0;
     p.shared_k = tables > kTabBytes || !attn_few(mean_k, mean_q, p.D == 128 && sh.narrow ? INT64_MAX : few);
-    p.rows_k = p.D == 32 && !p.shared_k && !sh.caches && mean_q <= 2 * mean_k && (sh.k_rows / 32 + sh.N) * sh.kv >= kManyUnits;
+    p.rows_k = (p.D == 32 || (p.D == 64 && !sh.narrow)) && !p.shared_k && !sh.caches && mean_q <= 2 * mean_k && (sh.k_rows / 32 + sh.N) * sh.kv >= kManyUnits;
     p.block_k = p.shared_k ? 128 : 32;
     p.V_k = p.rows_k ? (sh.k_rows + 31) / 32 : sh.k_rows / p.block_k + sh.N;
     const int64_t units = (sh.k_rows / p.block_k + 1) * sh.kv, enough = p.shared_k ? 768 : 4096;
@@ -756,8 +767,16 @@ static hipError_t launch_dim(const tbe_handle* h, AttnArgs a, const AttnBackward
     a.V = (int)p.V_k; a.block = p.block_k; a.splits = p.parts; a.pack = a.group / p.parts;
     {
         LaunchTimer tm(h, s, "attention_dkv");
-        if (p.shared_k) e = a.bias ? launch_dkv<T, D, 4, true>(a, s) : launch_dkv<T, D, 4, false>(a, s);
-        else if (p.rows_k) e = a.bias ? launch_dkv<T, D, 0, true>(a, s) : launch_dkv<T, D, 0, false>(a, s);
+        const auto shared = [&] {
+            if constexpr (sizeof(T) == 2 && D == 128) return launch_dkv<T, D, 4, true>(a, s);   // (for large tables only)
+            else return a.bias ? launch_dkv<T, D, 4, true>(a, s) : launch_dkv<T, D, 4, false>(a, s);
+        };
+        const auto rows = [&] {
+            if constexpr (D == 32 || (D == 64 && sizeof(T) == 4)) return a.bias ? launch_dkv<T, D, 0, true>(a, s) : launch_dkv<T, D, 0, false>(a, s);
+            else return hipErrorInvalidValue;   // (not planned)
+        };
+        if (p.shared_k) e = shared();
+        else if (p.rows_k) e = rows();
         else e = a.bias ? launch_dkv<T, D, 1, true>(a, s) : launch_dkv<T, D, 1, false>(a, s);
         tm.done();
     }
