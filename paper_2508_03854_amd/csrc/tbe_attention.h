@@ -211,6 +211,13 @@ __device__ __forceinline__ float halves_max(const float x) {
     return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
+// Wide rows: beyond this, one fp32 number for lse (here as an exponent of 2) has too few bits left for the logarithm of the sum, which moves all
+// probabilities of the row by up to 2^-23 |lse|: 8e-6 of themselves in fp32, 6e-5 in types that are rounded to 2^-9 or 2^-12.
+template <typename T>
+__device__ __forceinline__ bool wide_row(const float lse2) {
+    return fabsf(lse2) > (sizeof(T) == 4 ? 64.f : 512.f) && lse2 < __builtin_inff();
+}
+
 // A matrix [rows][heads][dim]: bytes from row to row and from head to head.
 struct RowsView {
     const char* p;
@@ -221,7 +228,9 @@ struct RowsView {
 struct AttnArgs {
     RowsView q, k, v, o, dout, dq, dk, dv;
     float* lse;               // [H][q_rows]
-    float *delta, *lse2;      // [H][q_rows] of the backward: row sums of P dP; lse as an exponent of 2, +infinity for rows that saw nothing
+    // [H][q_rows] of the backward: row sums of P dP; a row's probabilities are weight 2^(x - lse2), where lse2 is +infinity for rows that saw
+    // nothing and weight 1 for all but wide rows
+    float *delta, *lse2, *weight;
     IdxView q_off, k_off, k_len;   // k_len.p may be null
     int N, H, kv, group, dim, causal;
     int64_t q_rows, k_rows;

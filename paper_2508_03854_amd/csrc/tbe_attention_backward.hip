@@ -110,6 +110,7 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dq_occupancy<T, D
     constexpr int kTile = BK * D * (int)sizeof(T), kLds = SHARE == 4 ? kTile : kWaves * kTile, kSharers = SHARE == 4 ? 4 : 1;
     constexpr bool kRows = SHARE == 0;
     __shared__ __align__(16) char keys0[kLds], keys1[kLds], values0[kLds], values1[kLds];
+    __shared__ int votes[kWaves];
     extern __shared__ float tab[];   // the bias by distance, sums by distance - two arrays of that size for each wavefront -, the buckets
     const int wave = uniform(threadIdx.x >> 6), lane = lane_id(), col = lane & 31, half = lane >> 5;
     const uint32_t per_head = SHARE == 4 ? (uint32_t)a.V : ((uint32_t)a.V + kWaves - 1) / kWaves;
@@ -195,6 +196,18 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dq_occupancy<T, D
     constexpr int kFew = 4;
     float delta = 0.f, dsum;
     bool one, sums_only;   // all keys in one tile of 32; a first run over the keys for D alone
+    // Wide rows find their maximum and the sum below it again, in a run over the keys of its own: lse becomes the maximum, weight one over the sum.
+    const bool wide = wide_row<T>(lse);
+    bool any_wide = __any(wide);
+    if (SHARE == 4) {   // (who shares tiles runs together)
+        if (lane == 0) votes[wave] = any_wide;
+        __syncthreads();
+        any_wide = false;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) any_wide |= votes[w] != 0;
+        any_wide = uniform(any_wide);
+    }
+    float weight = 1.f;
     const int kvh = head / a.group;
     const char* const kb = a.k.at(q.k0, kvh);
     const char* const vb = a.v.at(q.k0, kvh);
@@ -213,6 +226,28 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dq_occupancy<T, D
         beyond = tab[kTabMargin];
         ahead = a.causal ? 0.f : tab[2 * a.far + kTabMargin];
     }
+    // the exponents of a tile's probabilities: its products, scaled, with their bias, less `by`
+    auto exponents = [&](f32x16_t& x, const int j0, const float by) __attribute__((always_inline)) {
+        const bool all_beyond = first - (j0 + 31) >= a.far, all_ahead = wave_last - j0 <= -a.far;
+        if (!BIAS) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) x[r] = fmaf(x[r], a.scale2, -by);
+        } else if (all_beyond || all_ahead) {
+            const float flat = all_beyond ? beyond : ahead;
+            // (scores beside a wide row's are rounded with their bias, as in the forward and in other tiles, and not with its difference to lse)
+            const float b = any_wide ? flat : flat - by;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) x[r] = fmaf(x[r], a.scale2, b);
+            if (any_wide) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) x[r] -= by;
+            }
+        } else {
+            const float* const from = tab + (j0 + 4 * half - pos + a.far + kTabMargin);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) x[r] = fmaf(x[r], a.scale2, from[8 * (r / 4) + r % 4]) - by;
+        }
+    };
     bool clean = false, poisoned = false;   // see below
     auto step = [&](const int t, const char* const kt_, const char* const vt_, char* const kn, char* const vn) __attribute__((always_inline)) {
         loads_done();
@@ -236,19 +271,9 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dq_occupancy<T, D
             reads_ahead<2 * kC, 1, Mma<T>::kMfmas, 4>();
             settle<T>();
             const bool all_beyond = first - (j0 + 31) >= a.far, all_ahead = wave_last - j0 <= -a.far;
-            const int at = j0 + 4 * half - pos + a.far + kTabMargin;   // of this lane's first key among the distances
-            if (!BIAS) {
+            exponents(x, j0, lse);
 #pragma unroll
-                for (int r = 0; r < 16; ++r) x[r] = __builtin_amdgcn_exp2f(fmaf(x[r], a.scale2, -lse));
-            } else if (all_beyond || all_ahead) {
-                const float b = (all_beyond ? beyond : ahead) - lse;
-#pragma unroll
-                for (int r = 0; r < 16; ++r) x[r] = __builtin_amdgcn_exp2f(fmaf(x[r], a.scale2, b));
-            } else {
-                const float* const from = tab + at;
-#pragma unroll
-                for (int r = 0; r < 16; ++r) x[r] = __builtin_amdgcn_exp2f(fmaf(x[r], a.scale2, from[8 * (r / 4) + r % 4]) - lse);
-            }
+            for (int r = 0; r < 16; ++r) x[r] = __builtin_amdgcn_exp2f(x[r]);
             if constexpr (kRows) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
@@ -258,6 +283,10 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dq_occupancy<T, D
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
                     if (j0 + 8 * (r / 4) + 4 * half + r % 4 >= end) x[r] = g[r] = 0.f;
+            }
+            if (any_wide) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) x[r] *= weight;
             }
             if (sums_only || one) {
                 float sum = 0.f;
@@ -316,6 +345,50 @@ again:
             tiles = jbase < last ? (last - jbase + BK - 1) / BK : 0;
         } else {
             todo = 0;
+        }
+        if (any_wide) {
+            float top = -__builtin_inff(), sum = 0.f;
+            const bool here = wide && (!kRows || lo < end);
+            const int from = kRows ? lo : 0, to = kRows ? end : (a.causal && pos + 1 < q.nk ? pos + 1 : q.nk);
+#pragma unroll 1
+            for (int t = 0; t < tiles; ++t) {
+                if (SHARE == 4) __syncthreads();
+                Tile<T, D>::template fetch<BK, kSharers>(keys0 + own, kb, a.k.row, jbase + t * BK, q.nk, a.dim, fw);
+                loads_done();
+                if (SHARE == 4) __syncthreads();
+#pragma unroll 1
+                for (int k = 0; k < kT; ++k) {
+                    const int j0 = jbase + t * BK + 32 * k;
+                    f32x16_t x = f32x16_t{};
+#pragma unroll
+                    for (int c = 0; c < kC; ++c) x = Mma<T>::mma(Tile<T, D>::along(keys0 + own, 32 * k + col, c, half), fq[c], x);
+                    settle<T>();
+                    exponents(x, j0, 0.f);
+                    float most = top;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const int j = j0 + 8 * (r / 4) + 4 * half + r % 4;
+                        if (j < from || j >= to) x[r] = -__builtin_inff();
+                        most = fmaxf(most, x[r]);
+                    }
+                    most = halves_max(most);
+                    const float at = most == -__builtin_inff() ? 0.f : most;
+                    sum *= __builtin_amdgcn_exp2f(top - at);
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) sum += __builtin_amdgcn_exp2f(x[r] - at);
+                    top = most;
+                }
+            }
+            if (SHARE == 4) __syncthreads();
+            sum = pair_sum<32>(sum);
+            if (here && sum != 0.f) {
+                lse = top;
+                weight = 1.f / sum;
+                if (!wide_row<T>(lse)) {   // (attn_dkv_kernel goes by lse)
+                    lse += __builtin_amdgcn_logf(sum);
+                    weight = 1.f;
+                }
+            }
         }
         one = kT == 1 && tiles == 1;
         sums_only = tiles <= kFew && !one;
@@ -377,6 +450,7 @@ again:
     if (is && half == 0) {   // for attn_dkv_kernel
         a.delta[(int64_t)head * a.q_rows + row] = delta;
         a.lse2[(int64_t)head * a.q_rows + row] = lse;
+        a.weight[(int64_t)head * a.q_rows + row] = weight;
     }
     if (is) store_column<T, D>(const_cast<char*>(a.dq.at(row, head)), dq, a.scale, half, a.dim);
     if (!BIAS) return;
@@ -564,6 +638,16 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dkv_occupancy<T, 
                     g_[r] = x[r] * (g_[r] - d[e]);
                 }
             }
+            if (__any(wide_row<T>(st_[own_stats + 32 * k + col]))) {
+                const float* const weights = a.weight + (int64_t)(head0 + g) * a.q_rows + q.q0;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int i = i0 + 8 * (r / 4) + 4 * half + r % 4;
+                    const float by = i < q.nq ? weights[i] : 1.f;
+                    x[r] *= by;
+                    g_[r] *= by;
+                }
+            }
             if constexpr (kRows) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
@@ -702,7 +786,7 @@ AttnBackwardPlan attn_backward_plan(const AttnShape& sh) {
         while (group % next != 0) ++next;
         p.parts = next;
     }
-    p.delta = 2 * (((size_t)sh.H * (size_t)sh.q_rows * 4 + 255) & ~(size_t)255);   // with lse, as an exponent of 2
+    p.delta = 3 * (((size_t)sh.H * (size_t)sh.q_rows * 4 + 255) & ~(size_t)255);   // with lse2 and weight
     p.part_bias = sh.buckets ? ((size_t)sh.H * (size_t)p.V_q * (size_t)sh.buckets * 4 + 255) & ~(size_t)255 : 0;
     p.part_kv = p.parts > 1 ? 2 * (size_t)p.parts * (size_t)sh.k_rows * (size_t)sh.kv * (size_t)p.D * 4 : 0;
     p.grid_ok = (int64_t)sh.H * p.V_q < ((int64_t)1 << 31) - 64 && (int64_t)sh.kv * p.parts * p.V_k < ((int64_t)1 << 31) - 64;
@@ -795,7 +879,8 @@ static hipError_t launch_type(const tbe_handle* h, const AttnArgs& a, const Attn
 hipError_t launch_attention_backward(const tbe_handle* h, AttnArgs a, const AttnBackwardPlan& p, int io, void* dbias, void* workspace, hipStream_t s) {
     char* const ws = static_cast<char*>(workspace);
     a.delta = reinterpret_cast<float*>(ws);
-    a.lse2 = reinterpret_cast<float*>(ws + p.delta / 2);
+    a.lse2 = reinterpret_cast<float*>(ws + p.delta / 3);
+    a.weight = reinterpret_cast<float*>(ws + p.delta / 3 * 2);
     a.part_bias = reinterpret_cast<float*>(ws + p.delta);
     a.part_o = reinterpret_cast<float*>(ws + p.delta + p.part_bias);
     return io == 0 ? launch_type<float>(h, a, p, dbias, s) : (io == 1 ? launch_type<__half>(h, a, p, dbias, s) : launch_type<bf16_t>(h, a, p, dbias, s));
