@@ -48,6 +48,23 @@ inline bool attn_few(const int64_t mean, const int64_t other, const int64_t most
 // Sixteen zero bytes: what stands behind a sequence's end, or behind a row's, is read from here.
 static __device__ const uint4 attn_zeros = {0u, 0u, 0u, 0u};
 
+// A load of what is there, or of zeros, without a branch.  Where registers are short, the compiler was seen to place copies of registers that live on
+// at the head of the block behind such a branch, before the lanes that were off come back (ROCm 7.2): these lanes lost the values,
+// and a gradient of the bias came out wrong now and then.  So nothing that the tiles' loops are reached through, or that runs within them, lets
+// lanes go different ways.
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ uint4 load_or_zeros(const bool there, const void* from) {
+    const auto a = (const __attribute__((address_space(1))) u32x4_t*)from;
+    const auto z = (const __attribute__((address_space(1))) u32x4_t*)&attn_zeros;
+    const u32x4_t v = *(there ? a : z);
+    return make_uint4(v.x, v.y, v.z, v.w);
+}
+__device__ __forceinline__ float load_or_zero(const bool there, const float* from) {
+    const auto a = (const __attribute__((address_space(1))) float*)from;
+    const auto z = (const __attribute__((address_space(1))) float*)&attn_zeros;
+    return *(there ? a : z);
+}
+
 template <typename T>
 struct Mma {   // 16-bit types: fragments of 8 elements a lane, 16 of the summed axis at a time
     static constexpr int kE = 8, kK = 16, kDown = 2, kMfmas = 1;   // kDown: LDS reads of a fragment down the rows; kMfmas: of its product

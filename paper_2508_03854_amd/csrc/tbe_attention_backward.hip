@@ -36,8 +36,7 @@ __device__ __forceinline__ void column_row(uint4 (&f)[D / Mma<T>::kK], const cha
 #pragma unroll
     for (int c = 0; c < D / kK; ++c) {
         const int e = kK * c + kE * half;
-        f[c] = make_uint4(0u, 0u, 0u, 0u);
-        if (is && e < dim) f[c] = *reinterpret_cast<const uint4*>(row + e * sizeof(T));
+        f[c] = load_or_zeros(is && e < dim, row + e * sizeof(T));
     }
 }
 template <typename T, int N>
@@ -187,8 +186,9 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dq_occupancy<T, D
     column_row<T, D>(fq, a.q.at(row, head), is, half, a.dim);
     column_row<T, D>(fy, a.dout.at(row, head), is, half, a.dim);
     if (a.negative) flip_signs<T, kC>(fq);
-    float lse = is ? a.lse[(int64_t)head * a.q_rows + row] : __builtin_inff();   // (columns without a query: probabilities 0)
-    lse = lse == -__builtin_inff() ? __builtin_inff() : lse * kLog2e;   // (a row that saw nothing: all its probabilities 2^-inf)
+    float lse = load_or_zero(is, a.lse + (int64_t)head * a.q_rows + row);
+    // (columns without a query, rows that saw nothing: all their probabilities are 2^-inf)
+    lse = !is || lse == -__builtin_inff() ? __builtin_inff() : lse * kLog2e;
 
     // D of a row from its few keys' P and dP, or else from the forward's result.  That was rounded, which against the sum over few keys is
     // as much as the rounding of dS and of the gradient: 4096 bfloat16 sequences of 12 events on average have dq 1.6 times as far from
@@ -381,14 +381,9 @@ again:
             }
             if (SHARE == 4) __syncthreads();
             sum = pair_sum<32>(sum);
-            if (here && sum != 0.f) {
-                lse = top;
-                weight = 1.f / sum;
-                if (!wide_row<T>(lse)) {   // (attn_dkv_kernel goes by lse)
-                    lse += __builtin_amdgcn_logf(sum);
-                    weight = 1.f;
-                }
-            }
+            const bool found = here && sum != 0.f, apart = wide_row<T>(top);   // (attn_dkv_kernel goes by lse)
+            lse = !found ? lse : (apart ? top : top + __builtin_amdgcn_logf(sum));
+            weight = found && apart ? 1.f / sum : weight;
         }
         one = kT == 1 && tiles == 1;
         sums_only = tiles <= kFew && !one;
@@ -643,7 +638,7 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dkv_occupancy<T, 
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const int i = i0 + 8 * (r / 4) + 4 * half + r % 4;
-                    const float by = i < q.nq ? weights[i] : 1.f;
+                    const float by = weights[i < q.nq ? i : q.nq - 1];   // (behind the last query all is 0)
                     x[r] *= by;
                     g_[r] *= by;
                 }
