@@ -18,6 +18,11 @@ typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
 
+// x, as a value that the compiler does not know: what is computed from it is computed again, not kept in registers through the loops in between
+__device__ __forceinline__ int anew(int x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
 // a value that all lanes hold, as a scalar
 __device__ __forceinline__ int uniform(const int x) { return __builtin_amdgcn_readfirstlane(x); }
 
@@ -48,23 +53,6 @@ inline bool attn_few(const int64_t mean, const int64_t other, const int64_t most
 // Sixteen zero bytes: what stands behind a sequence's end, or behind a row's, is read from here.
 static __device__ const uint4 attn_zeros = {0u, 0u, 0u, 0u};
 
-// A load of what is there, or of zeros, without a branch.  Where registers are short, the compiler was seen to place copies of registers that live on
-// at the head of the block behind such a branch, before the lanes that were off come back (ROCm 7.2): these lanes lost the values,
-// and a gradient of the bias came out wrong now and then.  So nothing that the tiles' loops are reached through, or that runs within them, lets
-// lanes go different ways.
-typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
-__device__ __forceinline__ uint4 load_or_zeros(const bool there, const void* from) {
-    const auto a = (const __attribute__((address_space(1))) u32x4_t*)from;
-    const auto z = (const __attribute__((address_space(1))) u32x4_t*)&attn_zeros;
-    const u32x4_t v = *(there ? a : z);
-    return make_uint4(v.x, v.y, v.z, v.w);
-}
-__device__ __forceinline__ float load_or_zero(const bool there, const float* from) {
-    const auto a = (const __attribute__((address_space(1))) float*)from;
-    const auto z = (const __attribute__((address_space(1))) float*)&attn_zeros;
-    return *(there ? a : z);
-}
-
 template <typename T>
 struct Mma {   // 16-bit types: fragments of 8 elements a lane, 16 of the summed axis at a time
     static constexpr int kE = 8, kK = 16, kDown = 2, kMfmas = 1;   // kDown: LDS reads of a fragment down the rows; kMfmas: of its product
@@ -94,6 +82,48 @@ struct Mma<float> {   // four products of two of the summed axis each
         return make_uint4(__float_as_uint(s[4 * m]), __float_as_uint(s[4 * m + 1]), __float_as_uint(s[4 * m + 2]), __float_as_uint(s[4 * m + 3]));
     }
 };
+
+// whether an element of a result is not finite
+template <int N>
+__device__ __forceinline__ bool not_finite(const f32x16_t (&o)[N]) {
+    float test = 0.f;   // stays 0, or becomes NaN
+#pragma unroll
+    for (int d = 0; d < N; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) test = fmaf(o[d][r], 0.f, test);
+    return test != 0.f;
+}
+
+// The fragments of one column's row of D elements, dim of them there; `is` false: zeros (the row is one that can be read all the same).
+// Without a branch between the lanes: where registers are short, the compiler was seen to place copies of registers that live on at the head of the
+// block behind such a branch, before the lanes that were off come back (ROCm 7.2).  These lanes lost the values, and a gradient of the bias came
+// out wrong now and then.  So nothing that the tiles' loops are reached through, or that runs within them, lets lanes go different ways.
+template <typename T, int D>
+__device__ __forceinline__ void column_row(uint4 (&f)[D / Mma<T>::kK], const char* row, const bool is, const int half, const int dim) {
+    constexpr int kE = Mma<T>::kE, kK = Mma<T>::kK;
+    if (dim == D) {
+#pragma unroll
+        for (int c = 0; c < D / kK; ++c) f[c] = *reinterpret_cast<const uint4*>(row + (kK * c + kE * half) * sizeof(T));
+    } else {
+#pragma unroll
+        for (int c = 0; c < D / kK; ++c) {
+            const int e = kK * c + kE * half;
+            f[c] = *reinterpret_cast<const uint4*>(row + (e < dim ? e : 0) * sizeof(T));
+        }
+    }
+#pragma unroll
+    for (int c = 0; c < D / kK; ++c) {
+        const bool there = is && kK * c + kE * half < dim;
+        f[c] = make_uint4(there ? f[c].x : 0u, there ? f[c].y : 0u, there ? f[c].z : 0u, there ? f[c].w : 0u);
+    }
+}
+// the sign of the scale
+template <typename T, int N>
+__device__ __forceinline__ void flip_signs(uint4 (&f)[N]) {
+    constexpr uint32_t sign = sizeof(T) == 2 ? 0x80008000u : 0x80000000u;
+#pragma unroll
+    for (int c = 0; c < N; ++c) f[c] = make_uint4(f[c].x ^ sign, f[c].y ^ sign, f[c].z ^ sign, f[c].w ^ sign);
+}
 
 // every lane's BYTES bytes to LDS, one lane's behind the other's
 template <int BYTES>
@@ -140,6 +170,7 @@ __device__ __forceinline__ void reads_ahead() {
 template <typename T, int D>
 struct Tile {
     static constexpr int kChunks = D * (int)sizeof(T) / 16;   // of a row: 4 to 32
+    static constexpr uint32_t kLower = sizeof(T) == 4 ? 0x7F800000u : (__is_same(T, bf16_t) ? 0x7F80u : 0x7C00u);   // an exponent of all ones
     static __device__ __forceinline__ int swizzle(const int r) {
         return kChunks == 4 ? (r >> 2) & 3 : (kChunks == 8 ? ((r >> 1) & 1) << 2 | ((r >> 2) & 3) : (r & 3) << 2 | ((r >> 2) & 3));
     }
@@ -148,8 +179,8 @@ struct Tile {
         return *reinterpret_cast<const uint4*>(lds + (r * kChunks + ((2 * c + half) ^ swizzle(r))) * 16);
     }
     // fragment m down the rows first + ..., column 32 t + l % 32: the rows that registers of fragment m stand for
-    static __device__ __forceinline__ uint4 down(const char* lds, const int first, const int m, const int t) {
-        const int l = lane_id(), half = l >> 5;
+    static __device__ __forceinline__ uint4 down(const char* lds, const int first, const int m, const int t, const int l = lane_id()) {
+        const int half = l >> 5;
         if constexpr (sizeof(T) == 2) {
             // sixteen lanes read four rows of sixteen columns, and get a column of four rows each
             typedef __attribute__((address_space(3))) s16x4_t* lds_ptr;
@@ -192,23 +223,83 @@ struct Tile {
         for (int i = 32; i; i >>= 1) rows |= __shfl_xor(rows, i);
         return rows;
     }
+    // What a column does not see has the factor 0, but 0 times an element that is not finite is not 0.  Where a product's results are not finite
+    // though not all is seen, it is taken once more, of fragments without such elements (cleaned), and the elements themselves are multiplied
+    // one by one for those columns that see them (add_not_finite): the other columns' results are, bit by bit, as if these were not there.
+    static __device__ __forceinline__ uint4 cleaned(const uint4 v) {
+        uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            w[i] = (w[i] & kLower) == kLower ? w[i] & (sizeof(T) == 4 ? 0u : 0xFFFF0000u) : w[i];
+            w[i] = sizeof(T) == 2 && (w[i] >> 16 & kLower) == kLower ? w[i] & 0xFFFFu : w[i];
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    // the rows first .. first + 31 with an element that is not finite, a bit each
+    static __device__ __forceinline__ uint32_t not_finite(const char* lds, const int first, const int l) {
+        uint32_t rows = 0;
+#pragma unroll 1
+        for (int i = 0; i < 32 * kChunks; i += 64) {
+            const int n = i + l;
+            const uint4 v = *reinterpret_cast<const uint4*>(lds + (first * kChunks + n) * 16), c = cleaned(v);
+            rows |= (v.x ^ c.x) | (v.y ^ c.y) | (v.z ^ c.z) | (v.w ^ c.w) ? 1u << (n / kChunks) : 0u;
+        }
+#pragma unroll
+        for (int i = 32; i; i >>= 1) rows |= __shfl_xor(rows, i);
+        return (uint32_t)uniform((int)rows);
+    }
+    // o += x times the elements that are not finite of rows first .. first + 31, for the columns that see them: column l % 32 the rows first + lo ..
+    // first + end - 1
+    static __device__ __forceinline__ void add_not_finite(f32x16_t (&o)[D / 32], const char* lds, const int first, const f32x16_t& x, const int lo, const int end, const int l) {
+        const int col = l & 31, half = l >> 5;
+#pragma unroll 1
+        for (uint32_t rows = not_finite(lds, first, l); rows; rows &= rows - 1) {
+            const int j = __ffs(rows) - 1, r = first + j;
+            float by = 0.f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) by = 4 * (j >> 3) + (j & 3) == i ? x[i] : by;
+            by = __shfl(by, col + 8 * (j & 4));
+            const bool sees = j >= lo && j < end;
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    const char* const p = lds + r * kChunks * 16;
+                    float e[4];
+                    if constexpr (sizeof(T) == 4) {
+                        const float4 v = *reinterpret_cast<const float4*>(p + ((8 * d + 2 * i + half) ^ swizzle(r)) * 16);
+                        e[0] = v.x; e[1] = v.y; e[2] = v.z; e[3] = v.w;
+                    } else {
+                        const uint2 v = *reinterpret_cast<const uint2*>(p + ((4 * d + i) ^ swizzle(r)) * 16 + 8 * half);
+                        float both[8];
+                        Frag<T>::unpack(make_uint4(v.x, v.y, 0u, 0u), both);
+                        e[0] = both[0]; e[1] = both[1]; e[2] = both[2]; e[3] = both[3];
+                    }
+#pragma unroll
+                    for (int n = 0; n < 4; ++n)
+                        o[d][4 * i + n] = fmaf(by, sees && !(fabsf(e[n]) < __builtin_inff()) ? e[n] : 0.f, o[d][4 * i + n]);
+                }
+        }
+    }
     // ROWS rows from row j0 of a sequence on, of which there are `rows`, by WAVES wavefronts (this one is number w); complete after
     // loads_done().  `stride`: bytes from row to row
     template <int ROWS, int WAVES>
-    static __device__ __forceinline__ void fetch(char* lds, const char* base, const int64_t stride, const int j0, const int rows, const int dim, const int w) {
+    static __device__ __forceinline__ void fetch(char* lds, const char* base, const int64_t stride, const int j0, const int rows, const int dim, const int w,
+                                                 const int l = lane_id()) {
         constexpr int kLoads = ROWS * kChunks / 64 / WAVES;
         static_assert(kLoads * 64 * WAVES == ROWS * kChunks, "whole loads");
         const char* const from = base + (int64_t)j0 * stride;
         if (j0 + ROWS <= rows && dim == D) {   // (offsets that stay the same from tile to tile)
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
-                const int n = (w * kLoads + i) * 64 + lane_id(), r = n / kChunks, c = (n % kChunks) ^ swizzle(r);
+                const int n = (w * kLoads + i) * 64 + l, r = n / kChunks, c = (n % kChunks) ^ swizzle(r);
                 load_lds<16>(from + (uint32_t)(r * (uint32_t)stride + c * 16), lds + (w * kLoads + i) * 1024);
             }
         } else {
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
-                const int n = (w * kLoads + i) * 64 + lane_id(), r = n / kChunks, c = (n % kChunks) ^ swizzle(r);
+                const int n = (w * kLoads + i) * 64 + l, r = n / kChunks, c = (n % kChunks) ^ swizzle(r);
                 const bool there = j0 + r < rows && c * 16 < dim * (int)sizeof(T);
                 load_lds<16>(there ? from + (uint32_t)(r * (uint32_t)stride + c * 16) : reinterpret_cast<const char*>(&attn_zeros), lds + (w * kLoads + i) * 1024);
             }

@@ -39,6 +39,7 @@ __global__ __launch_bounds__((64 * attn_waves<T, D, SHARE>()), (attn_occupancy<T
     // two buffers each, as arrays of their own: loads into one of them are seen not to concern what is read from another
     constexpr int kLds = SHARE == 4 ? kTile : kWaves * kTile;
     __shared__ __align__(16) char keys0[kLds], keys1[kLds], values0[kLds], values1[kLds];
+    __shared__ int votes[kWaves];
     extern __shared__ float tab[];
     const int wave = uniform(threadIdx.x >> 6), lane = lane_id(), col = lane & 31, half = lane >> 5;
     const bool together = SHARE == 1 && a.together;
@@ -106,19 +107,8 @@ __global__ __launch_bounds__((64 * attn_waves<T, D, SHARE>()), (attn_occupancy<T
     }
 
     uint4 fq[kC];
-    {
-        const char* const row = a.q.at(q.q0 + (is ? i : 0), head);
-#pragma unroll
-        for (int c = 0; c < kC; ++c) {
-            const int e = kK * c + kE * half;
-            fq[c] = make_uint4(0u, 0u, 0u, 0u);
-            if (is && e < a.dim) fq[c] = *reinterpret_cast<const uint4*>(row + e * sizeof(T));
-            if (a.negative) {   // the sign of the scale
-                constexpr uint32_t sign = sizeof(T) == 2 ? 0x80008000u : 0x80000000u;
-                fq[c] = make_uint4(fq[c].x ^ sign, fq[c].y ^ sign, fq[c].z ^ sign, fq[c].w ^ sign);
-            }
-        }
-    }
+    column_row<T, D>(fq, a.q.at(q.q0 + (is ? i : 0), head), is, half, a.dim);
+    if (a.negative) flip_signs<T, kC>(fq);
     // ... or a part of them
     int t0 = 0, t1, jbase = 0, lo = 0, end = 0;
     {
@@ -133,9 +123,9 @@ __global__ __launch_bounds__((64 * attn_waves<T, D, SHARE>()), (attn_occupancy<T
     const char* const kb = a.k.at(q.k0, kvh);
     const char* const vb = a.v.at(q.k0, kvh);
     const int own = SHARE == 4 ? 0 : wave * kTile, fw = SHARE == 4 ? wave : 0;
-    auto fetch = [&](const int t, char* const kt, char* const vt) __attribute__((always_inline)) {
-        Tile<T, D>::template fetch<BK, kSharers>(kt + own, kb, a.k.row, jbase + t * BK, q.nk, a.dim, fw);
-        Tile<T, D>::template fetch<BK, kSharers>(vt + own, vb, a.v.row, jbase + t * BK, q.nk, a.dim, fw);
+    auto fetch = [&](const int t, char* const kt, char* const vt, const int l) __attribute__((always_inline)) {
+        Tile<T, D>::template fetch<BK, kSharers>(kt + own, kb, a.k.row, jbase + t * BK, q.nk, a.dim, fw, l);
+        Tile<T, D>::template fetch<BK, kSharers>(vt + own, vb, a.v.row, jbase + t * BK, q.nk, a.dim, fw, l);
     };
 
     f32x16_t o[kD];
@@ -149,26 +139,53 @@ __global__ __launch_bounds__((64 * attn_waves<T, D, SHARE>()), (attn_occupancy<T
         ahead = a.causal ? 0.f : ht[2 * a.far + kTabMargin];
     }
 
-    bool clean = false, poisoned = false;   // SHARE = 0, see below
-    bool met = false;      // a tile some of whose keys are hidden from some columns
-    uint64_t before = 0;   // lanes whose results were not finite before the first of them
-    auto not_finite = [&]() __attribute__((always_inline)) {
-        float test = 0.f;
+    // 32 keys from key j on: scores with their bias (as exponents of 2; without a bias they are scaled later), hidden ones at -infinity
+    auto biased = [&](f32x16_t& x, const int j) __attribute__((always_inline)) {
+        if (first - (j + 31) >= a.far || wave_last - j <= -a.far) {
+            const float b = first - (j + 31) >= a.far ? beyond : ahead;
 #pragma unroll
-        for (int d = 0; d < kD; ++d)
+            for (int r = 0; r < 16; ++r) x[r] = fmaf(x[r], a.scale2, b);
+        } else {
+            const float* const from = ht + (j + 4 * half - pos + a.far + kTabMargin);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) test = fmaf(o[d][r], 0.f, test);   // 0, or NaN
-        return test != 0.f;
+            for (int r = 0; r < 16; ++r) x[r] = fmaf(x[r], a.scale2, from[8 * (r / 4) + r % 4]);
+        }
     };
+    auto hidden = [&](f32x16_t& x, const int j) __attribute__((always_inline)) {
+        if constexpr (kRows) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if ((uint32_t)(j + 8 * (r / 4) + 4 * half + r % 4 - lo) >= (uint32_t)(end - lo)) x[r] = -__builtin_inff();
+        } else {
+            const int upto = a.causal && pos + 1 < q.nk ? pos + 1 : q.nk;   // the keys that this column sees end here
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (j + 8 * (r / 4) + 4 * half + r % 4 >= upto) x[r] = -__builtin_inff();
+        }
+    };
+    // A maximum that grows by less than 2^8 is left as it is: the probabilities stay below 2^8, and what they are divided by in the end is
+    // added up from them.
+    auto raise = [&](const float top) __attribute__((always_inline)) {
+        if (__any(top > m + 8.f)) {
+            const float grown = fmaxf(m, top);
+            const float shrink = grown == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(m - grown);
+            m = grown;
+            sum *= shrink;
+#pragma unroll
+            for (int d = 0; d < kD; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[d][r] *= shrink;
+        }
+    };
+    auto hides = [&](const int j0) { return kRows || j0 + BK > q.nk || (a.causal && j0 + BK - 1 > first); };
     auto step = [&](const int t, const char* const kt_, const char* const vt_, char* const kn, char* const vn) __attribute__((always_inline)) {
         loads_done();
         if (SHARE == 4) __syncthreads();
-        if (t + 1 < t1) fetch(t + 1, kn, vn);
+        if (t + 1 < t1) fetch(t + 1, kn, vn, lane);
         const int j0 = jbase + t * BK;
         const char* const kt = kt_ + own;
         const char* const vt = vt_ + own;
         if (SHARE == 4 && ((a.causal && j0 > wave_last) || iw >= q.nq)) return;
-        if (kRows && clean) poisoned |= meets(Tile<T, D>::clean(const_cast<char*>(vt)), j0, lo, end);
         f32x16_t x[kT];
 #pragma unroll
         for (int k = 0; k < kT; ++k) {
@@ -180,33 +197,11 @@ __global__ __launch_bounds__((64 * attn_waves<T, D, SHARE>()), (attn_occupancy<T
         settle<T>();
         if (BIAS) {
 #pragma unroll
-            for (int k = 0; k < kT; ++k) {
-                const int j = j0 + 32 * k;
-                if (first - (j + 31) >= a.far || wave_last - j <= -a.far) {
-                    const float b = first - (j + 31) >= a.far ? beyond : ahead;
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) x[k][r] = fmaf(x[k][r], a.scale2, b);
-                } else {
-                    const float* const from = ht + (j + 4 * half - pos + a.far + kTabMargin);
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) x[k][r] = fmaf(x[k][r], a.scale2, from[8 * (r / 4) + r % 4]);
-                }
-            }
+            for (int k = 0; k < kT; ++k) biased(x[k], j0 + 32 * k);
         }
-        const bool masked = kRows || j0 + BK > q.nk || (a.causal && j0 + BK - 1 > first);
-        if constexpr (kRows) {
+        if (hides(j0)) {
 #pragma unroll
-            for (int k = 0; k < kT; ++k)
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if ((uint32_t)(j0 + 32 * k + 8 * (r / 4) + 4 * half + r % 4 - lo) >= (uint32_t)(end - lo)) x[k][r] = -__builtin_inff();
-        } else if (masked) {
-            const int end = a.causal && pos + 1 < q.nk ? pos + 1 : q.nk;   // the keys that this column sees end here
-#pragma unroll
-            for (int k = 0; k < kT; ++k)
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (j0 + 32 * k + 8 * (r / 4) + 4 * half + r % 4 >= end) x[k][r] = -__builtin_inff();
+            for (int k = 0; k < kT; ++k) hidden(x[k], j0 + 32 * k);
         }
         float top = x[0][0];
 #pragma unroll
@@ -215,18 +210,7 @@ __global__ __launch_bounds__((64 * attn_waves<T, D, SHARE>()), (attn_occupancy<T
             for (int r = 0; r < 16; ++r) top = fmaxf(top, x[k][r]);
         top = halves_max(top);
         if (!BIAS) top *= a.scale2;
-        // A maximum that grows by less than 2^8 is left as it is: the probabilities stay below 2^8, and what they are divided by
-        // in the end is added up from them.
-        if (__any(top > m + 8.f || (m == -__builtin_inff() && top != m))) {
-            const float grown = fmaxf(m, top);
-            const float shrink = grown == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(m - grown);
-            m = grown;
-            sum *= shrink;
-#pragma unroll
-            for (int d = 0; d < kD; ++d)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) o[d][r] *= shrink;
-        }
+        raise(top);
         const float at = m == -__builtin_inff() ? 0.f : m;   // (nothing seen so far: every probability is 2^-inf = 0)
 #pragma unroll
         for (int k = 0; k < kT; ++k)
@@ -240,10 +224,6 @@ __global__ __launch_bounds__((64 * attn_waves<T, D, SHARE>()), (attn_occupancy<T
         for (int k = 0; k < kT; ++k)
 #pragma unroll
             for (int c = 0; c < kM; ++c) p[k][c] = Mma<T>::pack(x[k], c);
-        if (!kRows && masked && !met) {
-            met = true;
-            before = __ballot(not_finite());
-        }
 #pragma unroll
         for (int k = 0; k < kT; ++k)
 #pragma unroll
@@ -253,103 +233,108 @@ __global__ __launch_bounds__((64 * attn_waves<T, D, SHARE>()), (attn_occupancy<T
         reads_ahead<kT * kM * kD, Mma<T>::kDown, Mma<T>::kMfmas, 4>();
         settle<T>();
     };
-again:
-    uint64_t todo = kRows ? __ballot(is) : 1;
-    while (todo) {
-        if constexpr (kRows) {
-            // Columns whose places lie as their rows do go together: all of them where queries and keys are the same rows.
-            const int shift = uniform(bcast_lane(own_pos - col, __ffsll((unsigned long long)todo) - 1));
-            const bool mine = is && own_pos - col == shift;
-            todo &= ~__ballot(mine);
-            first = shift;
-            pos = first + col;
-            wave_last = first + 31;
-            lo = mine ? own_lo : 0;
-            end = mine ? own_end : 0;
-            jbase = wave_min_i32(lo < end ? lo : 0x7FFFFFFF);
-            const int last = wave_max_i32(lo < end ? end : 0);
-            t1 = jbase < last ? (last - jbase + BK - 1) / BK : 0;
-        } else {
-            todo = 0;
+    // The same with care for values that are not finite: their elements are multiplied one by one, for the columns that see them (see
+    // Tile::cleaned).  Every number is the step's own, bit by bit; 32 keys and one tile at a time, since registers are short.
+    auto careful_step = [&](const int t) __attribute__((always_inline)) {
+        if (SHARE == 4) __syncthreads();
+        const int l = anew(lane), c32 = l & 31, h = l >> 5;
+        fetch(t, keys0, values0, l);
+        loads_done();
+        if (SHARE == 4) __syncthreads();
+        const int j0 = jbase + t * BK;
+        if (SHARE == 4 && ((a.causal && j0 > wave_last) || iw >= q.nq)) return;
+        f32x16_t x;
+        auto scores = [&](const int k) __attribute__((always_inline)) {
+            x = f32x16_t{};
+#pragma unroll
+            for (int c = 0; c < kC; ++c) x = Mma<T>::mma(Tile<T, D>::along(keys0 + own, 32 * k + c32, c, h), fq[c], x);
+            reads_ahead<kC, 1, Mma<T>::kMfmas, 2>();
+            settle<T>();
+            if (BIAS) biased(x, j0 + 32 * k);
+            if (hides(j0)) hidden(x, j0 + 32 * k);
+        };
+        float top = -__builtin_inff();
+#pragma unroll 1
+        for (int k = 0; k < kT; ++k) {
+            scores(k);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) top = fmaxf(top, x[r]);
         }
-        if (t0 < t1) fetch(t0, keys0, values0);
+        top = halves_max(top);
+        if (!BIAS) top *= a.scale2;
+        raise(top);
+        const float at = m == -__builtin_inff() ? 0.f : m;
+#pragma unroll 1
+        for (int k = 0; k < kT; ++k) {
+            const int j = j0 + 32 * k;
+            scores(k);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                x[r] = __builtin_amdgcn_exp2f(BIAS ? x[r] - at : fmaf(x[r], a.scale2, -at));
+                sum += x[r];
+            }
+            Tile<T, D>::add_not_finite(o, values0 + own, 32 * k, x, (kRows ? lo : 0) - j, (kRows ? end : (a.causal && pos + 1 < q.nk ? pos + 1 : q.nk)) - j, l);
+#pragma unroll
+            for (int c = 0; c < kM; ++c) {
+                const uint4 p = Mma<T>::pack(x, c);
+#pragma unroll
+                for (int d = 0; d < kD; ++d) {
+                    o[d] = Mma<T>::mma(Tile<T, D>::cleaned(Tile<T, D>::down(values0 + own, 32 * k, c, d, l)), p, o[d]);
+                    __builtin_amdgcn_sched_barrier(0);   // (few registers rather than many loads under way)
+                }
+            }
+            settle<T>();
+        }
+    };
+    // SHARE = 0: columns whose places lie as their rows do go together: all of them where queries and keys are the same rows.
+    auto take_some = [&](uint64_t& todo) __attribute__((always_inline)) {
+        const int shift = uniform(bcast_lane(own_pos - col, __ffsll((unsigned long long)todo) - 1));
+        const bool mine = is && own_pos - col == shift;
+        todo &= ~__ballot(mine);
+        first = shift;
+        pos = first + col;
+        wave_last = first + 31;
+        lo = mine ? own_lo : 0;
+        end = mine ? own_end : 0;
+        jbase = wave_min_i32(lo < end ? lo : 0x7FFFFFFF);
+        const int last = wave_max_i32(lo < end ? end : 0);
+        t1 = jbase < last ? (last - jbase + BK - 1) / BK : 0;
+    };
+    for (uint64_t todo = kRows ? __ballot(is) : 1; todo;) {
+        if constexpr (kRows) take_some(todo);
+        else todo = 0;
+        if (t0 < t1) fetch(t0, keys0, values0, lane);
         for (int t = t0; t < t1; t += 2) {
             step(t, keys0, values0, keys1, values1);
             if (t + 1 < t1) step(t + 1, keys1, values1, keys0, values0);
         }
     }
-    // The probability of a hidden key is 0, but 0 times a value that is not finite is not.  Columns whose results stopped being finite in a
-    // tile with hidden keys are computed once more, key by key, without these.  With SHARE = 0, where they may be another sequence's, all
-    // is first done again on tiles in which such values are 0, which is right, bit by bit, for the columns that see none of them.
-    if (kRows && !clean && __any(not_finite())) {
+    // The probability of a hidden key is 0, but 0 times a value that is not finite is not: where some keys are hidden and a result is not finite, all is
+    // done once more (see Tile::cleaned).  Who shares tiles runs together.
+    if (kRows || a.causal) {
+        bool once_more = __any(is && not_finite(o));
+        if (SHARE == 4) {
+            if (lane == 0) votes[wave] = once_more;
+            __syncthreads();
 #pragma unroll
-        for (int d = 0; d < kD; ++d) o[d] = f32x16_t{};
-        m = -__builtin_inff();
-        sum = 0.f;
-        clean = true;
-        goto again;
-    }
-    if (!kRows) judge(a, looks, v, peek);
-    sum = pair_sum<32>(sum);
-    if (kRows ? clean : met) {
-        uint64_t bad = kRows ? __ballot(poisoned) : __ballot(not_finite()) & ~before;
-        bad |= bad >> 32 | bad << 32;
-        if (bad) {
-            int from = t0 * BK, last = t1 * BK < jend ? t1 * BK : jend;
-            if constexpr (kRows) {
-                from = wave_min_i32(own_lo < own_end ? own_lo : 0x7FFFFFFF);
-                last = wave_max_i32(own_lo < own_end ? own_end : 0);
-            } else {
-                own_end = a.causal && pos + 1 < last ? pos + 1 : last;
-                own_pos = pos;
-            }
-            float sm, ss;
+            for (int w = 0; w < kWaves; ++w) once_more |= votes[w] != 0;
+            once_more = uniform(once_more);
+        }
+        if (once_more) {
 #pragma unroll
-            for (int d = 0; d < kD; ++d) {   // (32 elements of the result at a time: it is registers that are short)
-                f32x16_t so = f32x16_t{};
-                sm = -__builtin_inff();
-                ss = 0.f;
+            for (int d = 0; d < kD; ++d) o[d] = f32x16_t{};
+            m = -__builtin_inff();
+            sum = 0.f;
+            for (uint64_t todo = kRows ? __ballot(is) : 1; todo;) {
+                if constexpr (kRows) take_some(todo);
+                else todo = 0;
 #pragma unroll 1
-                for (int j = from; j < last; ++j) {
-                    const T* const kr = reinterpret_cast<const T*>(kb + j * a.k.row);
-                    float x = 0.f;
-#pragma unroll
-                    for (int c = 0; c < kC; ++c) {
-                        const int e = kK * c + kE * half;
-                        if (e < a.dim) {
-                            float qe[kE], ke[kE];
-                            Frag<T>::unpack(fq[c], qe);
-                            Frag<T>::unpack(*reinterpret_cast<const uint4*>(kr + e), ke);
-#pragma unroll
-                            for (int n = 0; n < kE; ++n) x = fmaf(qe[n], ke[n], x);
-                        }
-                    }
-                    x = pair_sum<32>(x) * a.scale2;
-                    if (BIAS) {
-                        const int apart = own_pos - j;
-                        x += ht[a.far + kTabMargin - (apart > a.far ? a.far : (apart < -a.far ? -a.far : apart))];
-                    }
-                    if (j < own_lo || j >= own_end || (x == -__builtin_inff() && sm == x)) continue;
-                    const float grown = fmaxf(sm, x), shrink = __builtin_amdgcn_exp2f(sm - grown);
-                    float p = __builtin_amdgcn_exp2f(x - grown);
-                    sm = grown;
-                    ss = fmaf(ss, shrink, p);
-                    p = elem_float(elem_round<T>(p));
-                    const T* const vr = reinterpret_cast<const T*>(vb + j * a.v.row);
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int e = 32 * d + 8 * (r / 4) + 4 * half + r % 4;
-                        so[r] = fmaf(so[r], shrink, e < a.dim ? p * elem_float(vr[e]) : 0.f);
-                    }
-                }
-                if (bad >> lane & 1) o[d] = so;
-            }
-            if (bad >> lane & 1) {
-                m = sm;
-                sum = ss;
+                for (int t = t0; t < t1; ++t) careful_step(t);
             }
         }
     }
+    if (!kRows) judge(a, looks, v, peek);
+    sum = pair_sum<32>(sum);
     if (SHARE == 1 && together) {
         // The parts' results meet where the tiles were, as fp32 rows of D elements, sixteen bytes of a row at place c ^ column: a column's
         // lanes do not all fall on the same banks.

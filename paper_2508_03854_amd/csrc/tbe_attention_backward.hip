@@ -29,22 +29,6 @@ constexpr int dq_occupancy() { return sizeof(T) == 2 && (D <= 64 || SHARE == 4) 
 template <typename T, int D>
 constexpr int dkv_occupancy() { return sizeof(T) == 2 && D <= 64 ? 2 : 1; }
 
-// The fragments of one column's row of D elements, dim of them there; nothing: zeros
-template <typename T, int D>
-__device__ __forceinline__ void column_row(uint4 (&f)[D / Mma<T>::kK], const char* row, const bool is, const int half, const int dim) {
-    constexpr int kE = Mma<T>::kE, kK = Mma<T>::kK;
-#pragma unroll
-    for (int c = 0; c < D / kK; ++c) {
-        const int e = kK * c + kE * half;
-        f[c] = load_or_zeros(is && e < dim, row + e * sizeof(T));
-    }
-}
-template <typename T, int N>
-__device__ __forceinline__ void flip_signs(uint4 (&f)[N]) {
-    constexpr uint32_t sign = sizeof(T) == 2 ? 0x80008000u : 0x80000000u;
-#pragma unroll
-    for (int c = 0; c < N; ++c) f[c] = make_uint4(f[c].x ^ sign, f[c].y ^ sign, f[c].z ^ sign, f[c].w ^ sign);
-}
 // a column's share of a transposed result, times `by`, to its row
 template <typename T, int D>
 __device__ __forceinline__ void store_column(char* row, const f32x16_t (&o)[D / 32], const float by, const int half, const int dim) {
@@ -186,7 +170,7 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dq_occupancy<T, D
     column_row<T, D>(fq, a.q.at(row, head), is, half, a.dim);
     column_row<T, D>(fy, a.dout.at(row, head), is, half, a.dim);
     if (a.negative) flip_signs<T, kC>(fq);
-    float lse = load_or_zero(is, a.lse + (int64_t)head * a.q_rows + row);
+    float lse = a.lse[(int64_t)head * a.q_rows + row];
     // (columns without a query, rows that saw nothing: all their probabilities are 2^-inf)
     lse = !is || lse == -__builtin_inff() ? __builtin_inff() : lse * kLog2e;
 
