@@ -199,30 +199,6 @@ struct Tile {
             return make_uint4(w[0], w[1], w[2], w[3]);
         }
     }
-    // what is not finite in the tile's first 32 rows becomes 0; the rows that had such, a bit each
-    static __device__ __forceinline__ uint32_t clean(char* lds) {
-        constexpr uint32_t lower = sizeof(T) == 4 ? 0x7F800000u : (__is_same(T, bf16_t) ? 0x7F80u : 0x7C00u);
-        uint32_t rows = 0;
-#pragma unroll 1
-        for (int n = lane_id(); n < 32 * kChunks; n += 64) {
-            uint4* const p = reinterpret_cast<uint4*>(lds + n * 16);
-            const uint4 v = *p;
-            uint32_t w[4] = {v.x, v.y, v.z, v.w};
-            bool bad = false;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if ((w[i] & lower) == lower) { w[i] &= sizeof(T) == 4 ? 0u : 0xFFFF0000u; bad = true; }
-                if (sizeof(T) == 2 && (w[i] >> 16 & lower) == lower) { w[i] &= 0xFFFFu; bad = true; }
-            }
-            if (bad) {
-                *p = make_uint4(w[0], w[1], w[2], w[3]);
-                rows |= 1u << (n / kChunks);
-            }
-        }
-#pragma unroll
-        for (int i = 32; i; i >>= 1) rows |= __shfl_xor(rows, i);
-        return rows;
-    }
     // What a column does not see has the factor 0, but 0 times an element that is not finite is not 0.  Where a product's results are not finite
     // though not all is seen, it is taken once more, of fragments without such elements (cleaned), and the elements themselves are multiplied
     // one by one for those columns that see them (add_not_finite): the other columns' results are, bit by bit, as if these were not there.
@@ -445,11 +421,6 @@ __device__ __forceinline__ LaneSequence lane_numbers(const AttnArgs& a, const in
 // All sequences looked over by `units` wavefronts, 64 at a time.
 __device__ __forceinline__ void judge_all(const AttnArgs& a, const uint32_t unit, const uint32_t units) {
     for (int64_t s = (int64_t)unit * 64 + lane_id(); s < a.N; s += (int64_t)units * 64) (void)lane_numbers(a, (int)s);
-}
-// whether any of the 32 rows from j0 on that `rows` names lies in [lo, end)
-__device__ __forceinline__ bool meets(const uint32_t rows, const int j0, const int lo, const int end) {
-    const int from = lo - j0 < 0 ? 0 : lo - j0, to = end - j0 > 32 ? 32 : end - j0;
-    return from < to && (rows >> from & (to - from >= 32 ? 0xFFFFFFFFu : (1u << (to - from)) - 1u)) != 0;
 }
 __device__ __forceinline__ int wave_min_i32(const int x) { return -wave_max_i32(-x); }
 

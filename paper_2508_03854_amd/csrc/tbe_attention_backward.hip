@@ -27,7 +27,7 @@ constexpr int bwd_waves() { return SHARE == 4 ? 4 : (D * (int)sizeof(T) <= 128 ?
 template <typename T, int D, int SHARE>   // wavefronts of a SIMD that the registers are to leave room for
 constexpr int dq_occupancy() { return sizeof(T) == 2 && (D <= 64 || SHARE == 4) ? 2 : 1; }
 template <typename T, int D>
-constexpr int dkv_occupancy() { return sizeof(T) == 2 && D <= 64 ? 2 : 1; }
+constexpr int dkv_occupancy() { return sizeof(T) == 2 ? (D == 32 ? 3 : (D == 64 ? 2 : 1)) : 1; }
 
 // a column's share of a transposed result, times `by`, to its row
 template <typename T, int D>
@@ -196,9 +196,9 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dq_occupancy<T, D
     const char* const kb = a.k.at(q.k0, kvh);
     const char* const vb = a.v.at(q.k0, kvh);
     const int own = SHARE == 4 ? 0 : wave * kTile, fw = SHARE == 4 ? wave : 0;
-    auto fetch = [&](const int t, char* const kt, char* const vt) __attribute__((always_inline)) {
-        Tile<T, D>::template fetch<BK, kSharers>(kt + own, kb, a.k.row, jbase + t * BK, q.nk, a.dim, fw);
-        Tile<T, D>::template fetch<BK, kSharers>(vt + own, vb, a.v.row, jbase + t * BK, q.nk, a.dim, fw);
+    auto fetch = [&](const int t, char* const kt, char* const vt, const int l) __attribute__((always_inline)) {
+        Tile<T, D>::template fetch<BK, kSharers>(kt + own, kb, a.k.row, jbase + t * BK, q.nk, a.dim, fw, l);
+        Tile<T, D>::template fetch<BK, kSharers>(vt + own, vb, a.v.row, jbase + t * BK, q.nk, a.dim, fw, l);
     };
     f32x16_t dq[kD];
 #pragma unroll
@@ -232,17 +232,25 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dq_occupancy<T, D
             for (int r = 0; r < 16; ++r) x[r] = fmaf(x[r], a.scale2, from[8 * (r / 4) + r % 4]) - by;
         }
     };
-    bool clean = false, poisoned = false;   // see below
+    // what is hidden of 32 keys from j0 on becomes 0
+    auto hide = [&](f32x16_t& x, f32x16_t& g, const int j0) __attribute__((always_inline)) {
+        if constexpr (kRows) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if ((uint32_t)(j0 + 8 * (r / 4) + 4 * half + r % 4 - lo) >= (uint32_t)(end - lo)) x[r] = g[r] = 0.f;
+        } else if (j0 + 32 > q.nk || (a.causal && j0 + 31 > first)) {
+            const int end = a.causal && pos + 1 < q.nk ? pos + 1 : q.nk;
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (j0 + 8 * (r / 4) + 4 * half + r % 4 >= end) x[r] = g[r] = 0.f;
+        }
+    };
     auto step = [&](const int t, const char* const kt_, const char* const vt_, char* const kn, char* const vn) __attribute__((always_inline)) {
         loads_done();
         if (SHARE == 4) __syncthreads();
-        if (t + 1 < tiles) fetch(t + 1, kn, vn);
+        if (t + 1 < tiles) fetch(t + 1, kn, vn, lane);
         const char* const kt = kt_ + own;
         const char* const vt = vt_ + own;
-        if (kRows && clean) {
-            const uint32_t rows = Tile<T, D>::clean(const_cast<char*>(kt)) | Tile<T, D>::clean(const_cast<char*>(vt));
-            poisoned |= meets(rows, jbase + t * BK, lo, end);
-        }
 #pragma unroll
         for (int k = 0; k < kT; ++k) {
             const int j0 = jbase + t * BK + 32 * k;
@@ -258,16 +266,7 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dq_occupancy<T, D
             exponents(x, j0, lse);
 #pragma unroll
             for (int r = 0; r < 16; ++r) x[r] = __builtin_amdgcn_exp2f(x[r]);
-            if constexpr (kRows) {
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if ((uint32_t)(j0 + 8 * (r / 4) + 4 * half + r % 4 - lo) >= (uint32_t)(end - lo)) x[r] = g[r] = 0.f;
-            } else if (j0 + 32 > q.nk || (a.causal && j0 + 31 > first)) {
-                const int end = a.causal && pos + 1 < q.nk ? pos + 1 : q.nk;
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (j0 + 8 * (r / 4) + 4 * half + r % 4 >= end) x[r] = g[r] = 0.f;
-            }
+            hide(x, g, j0);
             if (any_wide) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) x[r] *= weight;
@@ -283,7 +282,7 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dq_occupancy<T, D
             }
 #pragma unroll
             for (int r = 0; r < 16; ++r) g[r] = x[r] * (g[r] - delta);
-            if (BIAS && !(kRows && clean)) {
+            if (BIAS) {
                 if (all_beyond || all_ahead) {
                     float sum = 0.f;
 #pragma unroll
@@ -310,34 +309,68 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dq_occupancy<T, D
             settle<T>();
         }
     };
-    // SHARE = 0: what is hidden has dS = 0, but 0 times a key that is not finite is not 0.  Where a result is not finite, all is done once
-    // more on tiles in which such elements are 0, and columns of whose own keys some are not finite become NaN.
-again:
-    uint64_t todo = kRows ? __ballot(is) : 1;
-    while (todo) {
-        if constexpr (kRows) {   // columns whose places lie as their rows do go together
-            const int shift = uniform(bcast_lane(own_pos - col, __ffsll((unsigned long long)todo) - 1));
-            const bool mine = is && own_pos - col == shift;
-            todo &= ~__ballot(mine);
-            first = shift;
-            pos = first + col;
-            wave_last = first + 31;
-            lo = mine ? own_lo : 0;
-            end = mine ? own_end : 0;
-            jbase = wave_min_i32(lo < end ? lo : 0x7FFFFFFF);
-            const int last = wave_max_i32(lo < end ? end : 0);
-            tiles = jbase < last ? (last - jbase + BK - 1) / BK : 0;
-        } else {
-            todo = 0;
+    // What is hidden has dS = 0, but 0 times a key that is not finite is not 0.  The step once more for such keys: their elements are multiplied one
+    // by one, for the columns that see them (see Tile::cleaned); dS is the step's own, bit by bit, and its sums have been taken.
+    auto careful_step = [&](const int t) __attribute__((always_inline)) {
+        const int l = anew(lane), c32 = l & 31, h = l >> 5;
+        fetch(t, keys0, values0, l);
+        loads_done();
+#pragma unroll 1
+        for (int k = 0; k < kT; ++k) {
+            const int j0 = jbase + t * BK + 32 * k;
+            f32x16_t x = f32x16_t{}, g = f32x16_t{};
+#pragma unroll
+            for (int c = 0; c < kC; ++c) x = Mma<T>::mma(Tile<T, D>::along(keys0 + own, 32 * k + c32, c, h), fq[c], x);
+#pragma unroll
+            for (int c = 0; c < kC; ++c) g = Mma<T>::mma(Tile<T, D>::along(values0 + own, 32 * k + c32, c, h), fy[c], g);
+            reads_ahead<2 * kC, 1, Mma<T>::kMfmas, 2>();
+            settle<T>();
+            exponents(x, j0, lse);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) x[r] = __builtin_amdgcn_exp2f(x[r]) * weight;
+            hide(x, g, j0);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) g[r] = x[r] * (g[r] - delta);
+            const int upto = kRows ? end : (a.causal && pos + 1 < q.nk ? pos + 1 : q.nk);
+            Tile<T, D>::add_not_finite(dq, keys0 + own, 32 * k, g, (kRows ? lo : 0) - j0, upto - j0, l);
+#pragma unroll
+            for (int c = 0; c < kM; ++c) {
+                const uint4 p = Mma<T>::pack(g, c);
+#pragma unroll
+                for (int d = 0; d < kD; ++d) {
+                    dq[d] = Mma<T>::mma(Tile<T, D>::cleaned(Tile<T, D>::down(keys0 + own, 32 * k, c, d, l)), p, dq[d]);
+                    __builtin_amdgcn_sched_barrier(0);   // (few registers rather than many loads under way)
+                }
+            }
+            settle<T>();
         }
+    };
+    // SHARE = 0: columns whose places lie as their rows do go together
+    auto take_some = [&](uint64_t& todo) __attribute__((always_inline)) {
+        const int shift = uniform(bcast_lane(own_pos - col, __ffsll((unsigned long long)todo) - 1));
+        const bool mine = is && own_pos - col == shift;
+        todo &= ~__ballot(mine);
+        first = shift;
+        pos = first + col;
+        wave_last = first + 31;
+        lo = mine ? own_lo : 0;
+        end = mine ? own_end : 0;
+        jbase = wave_min_i32(lo < end ? lo : 0x7FFFFFFF);
+        const int last = wave_max_i32(lo < end ? end : 0);
+        tiles = jbase < last ? (last - jbase + BK - 1) / BK : 0;
+    };
+    for (uint64_t todo = kRows ? __ballot(is) : 1; todo;) {
+        if constexpr (kRows) take_some(todo);
+        else todo = 0;
         if (any_wide) {
             float top = -__builtin_inff(), sum = 0.f;
             const bool here = wide && (!kRows || lo < end);
             const int from = kRows ? lo : 0, to = kRows ? end : (a.causal && pos + 1 < q.nk ? pos + 1 : q.nk);
+            const int l = anew(lane), c32 = l & 31, h = l >> 5;
 #pragma unroll 1
             for (int t = 0; t < tiles; ++t) {
                 if (SHARE == 4) __syncthreads();
-                Tile<T, D>::template fetch<BK, kSharers>(keys0 + own, kb, a.k.row, jbase + t * BK, q.nk, a.dim, fw);
+                Tile<T, D>::template fetch<BK, kSharers>(keys0 + own, kb, a.k.row, jbase + t * BK, q.nk, a.dim, fw, l);
                 loads_done();
                 if (SHARE == 4) __syncthreads();
 #pragma unroll 1
@@ -345,7 +378,7 @@ again:
                     const int j0 = jbase + t * BK + 32 * k;
                     f32x16_t x = f32x16_t{};
 #pragma unroll
-                    for (int c = 0; c < kC; ++c) x = Mma<T>::mma(Tile<T, D>::along(keys0 + own, 32 * k + col, c, half), fq[c], x);
+                    for (int c = 0; c < kC; ++c) x = Mma<T>::mma(Tile<T, D>::along(keys0 + own, 32 * k + c32, c, h), fq[c], x);
                     settle<T>();
                     exponents(x, j0, 0.f);
                     float most = top;
@@ -388,7 +421,7 @@ again:
             delta = !kRows || lo < end ? d : delta;
         }
         for (;;) {
-            if (tiles > 0) fetch(0, keys0, values0);
+            if (tiles > 0) fetch(0, keys0, values0, lane);
             for (int t = 0; t < tiles; t += 2) {
                 step(t, keys0, values0, keys1, values1);
                 if (t + 1 < tiles) step(t + 1, keys1, values1, keys0, values0);
@@ -407,24 +440,15 @@ again:
         }
     }
     if (!kRows) judge(a, looks, v, peek);
-    if (kRows && !clean) {
-        float test = 0.f;
+    // With SHARE = 0, where the hidden keys may be another sequence's, all is done once more where a result is not finite.
+    if (kRows && __any(is && not_finite(dq))) {
 #pragma unroll
-        for (int d = 0; d < kD; ++d)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) test = fmaf(dq[d][r], 0.f, test);
-        if (__any(test != 0.f)) {
-#pragma unroll
-            for (int d = 0; d < kD; ++d) dq[d] = f32x16_t{};
-            clean = true;
-            goto again;
+        for (int d = 0; d < kD; ++d) dq[d] = f32x16_t{};
+        for (uint64_t todo = __ballot(is); todo;) {
+            take_some(todo);
+#pragma unroll 1
+            for (int t = 0; t < tiles; ++t) careful_step(t);
         }
-    }
-    if (kRows && poisoned) {
-#pragma unroll
-        for (int d = 0; d < kD; ++d)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) dq[d][r] = __builtin_nanf("");
     }
     if (is && half == 0) {   // for attn_dkv_kernel
         a.delta[(int64_t)head * a.q_rows + row] = delta;
@@ -547,13 +571,13 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dkv_occupancy<T, 
     if (a.negative) flip_signs<T, kC>(fk);
 
     const int own = SHARE == 4 ? 0 : wave * kTile, own_stats = SHARE == 4 ? 0 : wave * 128, fw = SHARE == 4 ? wave : 0;
-    auto fetch = [&](const int g, const int t, char* const qt, char* const yt, float* const st) __attribute__((always_inline)) {
+    auto fetch = [&](const int g, const int t, char* const qt, char* const yt, float* const st, const int l_) __attribute__((always_inline)) {
         const int head = head0 + g;
-        Tile<T, D>::template fetch<BQ, kSharers>(qt + own, a.q.at(q.q0, head), a.q.row, ibase + t * BQ, q.nq, a.dim, fw);
-        Tile<T, D>::template fetch<BQ, kSharers>(yt + own, a.dout.at(q.q0, head), a.dout.row, ibase + t * BQ, q.nq, a.dim, fw);
+        Tile<T, D>::template fetch<BQ, kSharers>(qt + own, a.q.at(q.q0, head), a.q.row, ibase + t * BQ, q.nq, a.dim, fw, l_);
+        Tile<T, D>::template fetch<BQ, kSharers>(yt + own, a.dout.at(q.q0, head), a.dout.row, ibase + t * BQ, q.nq, a.dim, fw, l_);
         if (SHARE != 4 || wave < 2) {
-            const int i = ibase + t * BQ + lane;
-            const bool there = lane < BQ && i < q.nq;
+            const int i = ibase + t * BQ + l_;
+            const bool there = l_ < BQ && i < q.nq;
             const int64_t at = (int64_t)head * a.q_rows + q.q0 + i;
             const float* const l = there ? a.lse2 + at : &attn_inf;
             const float* const d = there ? a.delta + at : reinterpret_cast<const float*>(&attn_zeros);
@@ -566,7 +590,48 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dkv_occupancy<T, 
     f32x16_t dk[kD], dv[kD];
 #pragma unroll
     for (int d = 0; d < kD; ++d) dk[d] = dv[d] = f32x16_t{};
-    bool clean = false, poisoned = false;   // as in attn_dq_kernel
+    // P and dS of 32 rows of q from row i0 on, of head g: from their products; st: lse and delta of these rows
+    auto probabilities = [&](f32x16_t& x, f32x16_t& g_, const int g, const int i0, const float* const st, const int col, const int half) __attribute__((always_inline)) {
+        const float* const ht = SHARE == 4 ? tab : tab + g * size;
+        const int first = lead + i0;   // the first query's place
+        const float* const lse = st + 4 * half;
+        const bool all_beyond = first - (jw + 31) >= a.far, all_ahead = first + 31 - jw <= -a.far;
+        float flat = 0.f;
+        if (BIAS && (all_beyond || all_ahead)) flat = all_beyond ? ht[kTabMargin] : (a.causal ? 0.f : ht[2 * a.far + kTabMargin]);
+        const bool by_distance = BIAS && !all_beyond && !all_ahead;
+        const float* const from = by_distance ? ht + (j - first - 4 * half + a.far + kTabMargin) - 27 : nullptr;
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+            const float4 l4 = *reinterpret_cast<const float4*>(lse + 8 * n), d4 = *reinterpret_cast<const float4*>(lse + 64 + 8 * n);
+            const float l[4] = {l4.x, l4.y, l4.z, l4.w}, d[4] = {d4.x, d4.y, d4.z, d4.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int r = 4 * n + e;
+                if (!BIAS) x[r] = __builtin_amdgcn_exp2f(fmaf(x[r], a.scale2, -l[e]));
+                else x[r] = __builtin_amdgcn_exp2f(fmaf(x[r], a.scale2, by_distance ? from[27 - 8 * n - e] : flat) - l[e]);
+                g_[r] = x[r] * (g_[r] - d[e]);
+            }
+        }
+        if (__any(wide_row<T>(st[col]))) {
+            const float* const weights = a.weight + (int64_t)(head0 + g) * a.q_rows + q.q0;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int i = i0 + 8 * (r / 4) + 4 * half + r % 4;
+                const float by = weights[i < q.nq ? i : q.nq - 1];   // (behind the last query all is 0)
+                x[r] *= by;
+                g_[r] *= by;
+            }
+        }
+        if constexpr (kRows) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if ((uint32_t)(i0 + 8 * (r / 4) + 4 * half + r % 4 - lo) >= (uint32_t)(end - lo)) x[r] = g_[r] = 0.f;
+        } else if (a.causal && first < jw + 31) {   // hidden: queries before the key's place
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (first + 8 * (r / 4) + 4 * half + r % 4 < j) x[r] = g_[r] = 0.f;
+        }
+    };
     // the step after (g, t) is (g, t + 1) or the next head's first
     auto step = [&](const int g, const int t, const bool more, const char* const qt_, const char* const yt_, const float* const st_, char* const qn,
                     char* const yn, float* const sn) __attribute__((always_inline)) {
@@ -574,7 +639,7 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dkv_occupancy<T, 
         if (SHARE == 4) __syncthreads();
         if (more) {
             const bool next = t + 1 == t0 + tiles;
-            fetch(next ? g + 1 : g, next ? t0 : t + 1, qn, yn, sn);
+            fetch(next ? g + 1 : g, next ? t0 : t + 1, qn, yn, sn, lane);
         }
         if (BIAS && SHARE == 4 && t == t0) {
             fill_bias(tab, a, head0 + g, 1, 64 * kWaves);
@@ -582,11 +647,6 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dkv_occupancy<T, 
         }
         const char* const qt = qt_ + own;
         const char* const yt = yt_ + own;
-        const float* const ht = SHARE == 4 ? tab : tab + g * size;
-        if (kRows && clean) {
-            const uint32_t rows = Tile<T, D>::clean(const_cast<char*>(qt)) | Tile<T, D>::clean(const_cast<char*>(yt));
-            poisoned |= meets(rows, ibase + t * BQ, lo, end);
-        }
 #pragma unroll
         for (int k = 0; k < kT; ++k) {
             const int i0 = ibase + t * BQ + 32 * k, first = lead + i0;   // the first query and its place
@@ -599,43 +659,7 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dkv_occupancy<T, 
             for (int c = 0; c < kC; ++c) g_ = Mma<T>::mma(Tile<T, D>::along(yt, 32 * k + col, c, half), fv[c], g_);
             reads_ahead<2 * kC, 1, Mma<T>::kMfmas, 4>();
             settle<T>();
-            const float* const lse = st_ + own_stats + 32 * k + 4 * half;
-            const bool all_beyond = first - (jw + 31) >= a.far, all_ahead = first + 31 - jw <= -a.far;
-            float flat = 0.f;
-            if (BIAS && (all_beyond || all_ahead)) flat = all_beyond ? ht[kTabMargin] : (a.causal ? 0.f : ht[2 * a.far + kTabMargin]);
-            const bool by_distance = BIAS && !all_beyond && !all_ahead;
-            const float* const from = by_distance ? ht + (j - first - 4 * half + a.far + kTabMargin) - 27 : nullptr;
-#pragma unroll
-            for (int n = 0; n < 4; ++n) {
-                const float4 l4 = *reinterpret_cast<const float4*>(lse + 8 * n), d4 = *reinterpret_cast<const float4*>(lse + 64 + 8 * n);
-                const float l[4] = {l4.x, l4.y, l4.z, l4.w}, d[4] = {d4.x, d4.y, d4.z, d4.w};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int r = 4 * n + e;
-                    if (!BIAS) x[r] = __builtin_amdgcn_exp2f(fmaf(x[r], a.scale2, -l[e]));
-                    else x[r] = __builtin_amdgcn_exp2f(fmaf(x[r], a.scale2, by_distance ? from[27 - 8 * n - e] : flat) - l[e]);
-                    g_[r] = x[r] * (g_[r] - d[e]);
-                }
-            }
-            if (__any(wide_row<T>(st_[own_stats + 32 * k + col]))) {
-                const float* const weights = a.weight + (int64_t)(head0 + g) * a.q_rows + q.q0;
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int i = i0 + 8 * (r / 4) + 4 * half + r % 4;
-                    const float by = weights[i < q.nq ? i : q.nq - 1];   // (behind the last query all is 0)
-                    x[r] *= by;
-                    g_[r] *= by;
-                }
-            }
-            if constexpr (kRows) {
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if ((uint32_t)(i0 + 8 * (r / 4) + 4 * half + r % 4 - lo) >= (uint32_t)(end - lo)) x[r] = g_[r] = 0.f;
-            } else if (a.causal && first < jw + 31) {   // hidden: queries before the key's place
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (first + 8 * (r / 4) + 4 * half + r % 4 < j) x[r] = g_[r] = 0.f;
-            }
+            probabilities(x, g_, g, i0, st_ + own_stats + 32 * k, col, half);
 #pragma unroll
             for (int c = 0; c < kM; ++c) {
                 const uint4 p = Mma<T>::pack(x, c), ds = Mma<T>::pack(g_, c);
@@ -649,23 +673,54 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dkv_occupancy<T, 
             settle<T>();
         }
     };
-again:
-    uint64_t todo = kRows ? __ballot(is) : 1;
-    while (todo) {
-        if constexpr (kRows) {   // keys whose queries' places lie alike go together
-            lead = uniform(bcast_lane(own_lead, __ffsll((unsigned long long)todo) - 1)) - (int)q.k0;
-            const bool mine = is && own_lead - (int)q.k0 == lead;
-            todo &= ~__ballot(mine);
-            lo = mine ? own_lo : 0;
-            end = mine ? own_end : 0;
-            ibase = wave_min_i32(lo < end ? lo : 0x7FFFFFFF);
-            const int last = wave_max_i32(lo < end ? end : 0);
-            tiles = ibase < last ? (last - ibase + BQ - 1) / BQ : 0;
-        } else {
-            todo = 0;
+    // The step once more where elements of q or dout are not finite, as in attn_dq_kernel.
+    auto careful_step = [&](const int g, const int t) __attribute__((always_inline)) {
+        const int l = anew(lane), c32 = l & 31, h = l >> 5;
+        fetch(g, t, rows0, grads0, stats0, l);
+        loads_done();
+#pragma unroll 1
+        for (int k = 0; k < kT; ++k) {
+            const int i0 = ibase + t * BQ + 32 * k, first = lead + i0;
+            f32x16_t x = f32x16_t{}, g_ = f32x16_t{};
+#pragma unroll
+            for (int c = 0; c < kC; ++c) x = Mma<T>::mma(Tile<T, D>::along(rows0 + own, 32 * k + c32, c, h), fk[c], x);
+#pragma unroll
+            for (int c = 0; c < kC; ++c) g_ = Mma<T>::mma(Tile<T, D>::along(grads0 + own, 32 * k + c32, c, h), fv[c], g_);
+            reads_ahead<2 * kC, 1, Mma<T>::kMfmas, 2>();
+            settle<T>();
+            probabilities(x, g_, g, i0, stats0 + own_stats + 32 * k, c32, h);
+            const int from = kRows ? lo - i0 : (a.causal ? j - first : 0), to = kRows ? end - i0 : 32;
+            Tile<T, D>::add_not_finite(dv, grads0 + own, 32 * k, x, from, to, l);
+            Tile<T, D>::add_not_finite(dk, rows0 + own, 32 * k, g_, from, to, l);
+#pragma unroll
+            for (int c = 0; c < kM; ++c) {
+                const uint4 p = Mma<T>::pack(x, c), ds = Mma<T>::pack(g_, c);
+#pragma unroll
+                for (int d = 0; d < kD; ++d) {
+                    dv[d] = Mma<T>::mma(Tile<T, D>::cleaned(Tile<T, D>::down(grads0 + own, 32 * k, c, d, l)), p, dv[d]);
+                    dk[d] = Mma<T>::mma(Tile<T, D>::cleaned(Tile<T, D>::down(rows0 + own, 32 * k, c, d, l)), ds, dk[d]);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            settle<T>();
         }
+    };
+    // SHARE = 0: keys whose queries' places lie alike go together
+    auto take_some = [&](uint64_t& todo) __attribute__((always_inline)) {
+        lead = uniform(bcast_lane(own_lead, __ffsll((unsigned long long)todo) - 1)) - (int)q.k0;
+        const bool mine = is && own_lead - (int)q.k0 == lead;
+        todo &= ~__ballot(mine);
+        lo = mine ? own_lo : 0;
+        end = mine ? own_end : 0;
+        ibase = wave_min_i32(lo < end ? lo : 0x7FFFFFFF);
+        const int last = wave_max_i32(lo < end ? end : 0);
+        tiles = ibase < last ? (last - ibase + BQ - 1) / BQ : 0;
+    };
+    for (uint64_t todo = kRows ? __ballot(is) : 1; todo;) {
+        if constexpr (kRows) take_some(todo);
+        else todo = 0;
         const int steps = tiles * hp;
-        if (steps > 0) fetch(0, t0, rows0, grads0, stats0);
+        if (steps > 0) fetch(0, t0, rows0, grads0, stats0, lane);
         int g = 0, t = t0;
         for (int n = 0; n < steps; n += 2) {
             step(g, t, n + 1 < steps, rows0, grads0, stats0, rows1, grads1, stats1);
@@ -675,24 +730,16 @@ again:
             if (++t == t0 + tiles) { t = t0; ++g; }
         }
     }
-    if (kRows && !clean) {
-        float test = 0.f;
+    if (kRows && __any(is && (not_finite(dk) || not_finite(dv)))) {   // as in attn_dq_kernel
 #pragma unroll
-        for (int d = 0; d < kD; ++d)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) test = fmaf(dk[d][r], 0.f, fmaf(dv[d][r], 0.f, test));
-        if (__any(test != 0.f)) {   // as in attn_dq_kernel
-#pragma unroll
-            for (int d = 0; d < kD; ++d) dk[d] = dv[d] = f32x16_t{};
-            clean = true;
-            goto again;
+        for (int d = 0; d < kD; ++d) dk[d] = dv[d] = f32x16_t{};
+        for (uint64_t todo = __ballot(is); todo;) {
+            take_some(todo);
+#pragma unroll 1
+            for (int g = 0; g < hp; ++g)
+#pragma unroll 1
+                for (int t = t0; t < t0 + tiles; ++t) careful_step(g, t);
         }
-    }
-    if (kRows && poisoned) {
-#pragma unroll
-        for (int d = 0; d < kD; ++d)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) dk[d][r] = dv[d][r] = __builtin_nanf("");
     }
     if (!writes) return;
     const float by = is ? 1.f : 0.f;   // (a cache's room: zeros)

@@ -1,11 +1,13 @@
-"""Attention beside values that are not finite: by the definition, over the pairs that see each other alone, some elements of the
-sequence's results are not finite, and the kernels' are so exactly there; all others are, bit by bit, what they are without these values."""
+"""Gradients of attention beside values that are not finite: by the definition, over the pairs that see each other alone, some elements of the
+sequence's results are not finite, and the kernels' are so exactly there; all others are, bit by bit, what they are without these values
+(those of its own sequence too, unless the value takes a key out of a softmax)."""
 import math
 
 import pytest
 import torch
 
 from test_gpu_attention import TYPES, problem, run
+from test_gpu_attention_backward import NAMES, back, upstream
 
 pytestmark = pytest.mark.gpu
 INF, NAN = math.inf, math.nan
@@ -17,6 +19,75 @@ def tbe():
         pytest.skip("no GPU")
     from paper_2508_03854_amd import TBE
     return TBE([16], [8])
+
+
+def over_seen(x, y, seen):
+    """sum_j x[i, j] y[j, :] over the pairs that are seen: what is not seen is left out, whatever it is."""
+    return torch.where(seen[..., None], x[..., None] * y, torch.zeros((), dtype=y.dtype, device=y.device)).sum(1)
+
+
+def definition(p, dout, s):
+    """Of sequence s: where its results are finite."""
+    q0, c, n, m = sum(p["nq"][:s]), p["k0"][s], p["nq"][s], p["nk"][s]
+    q, k, v, f64 = p["q"], p["k"], p["v"], torch.float64
+    H, K, D = q.shape[1], k.shape[1], q.shape[2]
+    r = {"dq": torch.zeros(n, H, D, dtype=f64, device=q.device), "dk": torch.zeros(m, K, D, dtype=f64, device=q.device),
+         "dv": torch.zeros(m, K, D, dtype=f64, device=q.device)}
+    if p["bias"] is not None:
+        r["dbias"] = torch.zeros(p["bias"].shape, dtype=f64, device=q.device)
+    d = torch.arange(m - n, m, device=q.device)[:, None] - torch.arange(m, device=q.device)
+    seen = d >= 0 if p["causal"] else torch.ones_like(d, dtype=torch.bool)
+    for h in range(H):
+        kh = h // (H // K)
+        Q, dy, Kk, V = q[q0:q0 + n, h].to(f64), dout[q0:q0 + n, h].to(f64), k[c:c + m, kh].to(f64), v[c:c + m, kh].to(f64)
+        x = (Q[:, None] * Kk).sum(2) * D ** -0.5
+        if p["bias"] is not None:
+            far = p["bucket_map"].numel() // 2
+            at = p["bucket_map"].long()[d.clamp(-far, far) + far]
+            x = x + p["bias"][h].to(f64)[at]
+        x = torch.where(seen, x, torch.full((), -INF, dtype=f64, device=q.device))
+        P = torch.softmax(x, 1)
+        P = torch.where(seen.any(1)[:, None], P, torch.zeros_like(P))
+        dP = torch.where(seen, (dy[:, None] * V).sum(2), torch.zeros_like(x))
+        dS = P * (dP - (P * dP).sum(1, keepdim=True))
+        r["dq"][:, h] = over_seen(dS, Kk, seen)
+        r["dk"][:, kh] += over_seen(dS.t(), Q, seen.t())
+        r["dv"][:, kh] += over_seen(P.t(), dy, seen.t())
+        if p["bias"] is not None:
+            r["dbias"][h].index_add_(0, at[seen], dS[seen])
+    return {n: torch.isfinite(t) for n, t in r.items()}
+
+
+def agree(tbe, p, s, row, what, head=1, col=3):
+    """Every operand in turn has an element of sequence s that is not finite."""
+    H, K = p["q"].shape[1], p["k"].shape[1]
+    dout, q0, k0 = upstream(p), sum(p["nq"][:s]), p["k0"][s]
+    fwd = run(tbe, p)
+    clean = back(tbe, p, dout, fwd)
+    for name, x, at, value in (("v", p["v"], k0, INF), ("v", p["v"], k0, NAN), ("k", p["k"], k0, NAN), ("k", p["k"], k0, INF), ("k", p["k"], k0, -INF),
+                               ("q", p["q"], q0, NAN), ("dout", dout, q0, INF), ("dout", dout, q0, NAN)):
+        h = head if x.shape[1] == H else head // (H // K)
+        keep = x[at + row, h, col].clone()
+        x[at + row, h, col] = value
+        got = back(tbe, p, dout, run(tbe, p))
+        finite = definition(p, dout, s)
+        x[at + row, h, col] = keep
+        for n, a, b in zip(NAMES, got, clean):
+            if a is None:
+                continue
+            expect = torch.ones_like(a, dtype=torch.bool)
+            if n == "dbias":
+                expect = finite[n]
+            else:
+                lo = q0 if n == "dq" else k0
+                expect[lo:lo + finite[n].shape[0]] = finite[n]
+            said = f"{what}: {n} with {name} {value}"
+            assert torch.equal(torch.isfinite(a), expect), f"{said}: {int((torch.isfinite(a) != expect).sum())} of {a.numel()}, {int((torch.isfinite(a) & ~expect).sum())} of these finite"
+            if name == "k" and abs(value) == INF and n != "dbias":
+                # a score of -infinity takes the key out of a row's softmax: the row's other probabilities are not what they were
+                expect[lo:lo + finite[n].shape[0]] = False
+            if n != "dbias":
+                assert torch.equal(a[expect], b[expect]), f"{said}: {int((a[expect] != b[expect]).sum())} others changed"
 
 
 @pytest.mark.parametrize("io", ["f32", "f16", "bf16"])
@@ -38,3 +109,14 @@ def test_values_that_are_hidden_beside_such_that_are_seen(tbe, io, n, H, K):
                 expect[q0 + later:q0 + n[s], :H // K, 1] = False
                 assert torch.equal(torch.isfinite(got[0]), expect), (D, far, s, int((torch.isfinite(got[0]) != expect).sum()))
                 assert torch.equal(got[0][expect], clean[0][expect]) and torch.equal(got[1], clean[1]), (D, far, s)
+
+
+@pytest.mark.parametrize("io", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("causal", [True, False])
+def test_sequences_that_share_wavefronts(tbe, io, causal):
+    n = [7, 9, 20, 5, 70, 3] * 75
+    for D in (32, 64) if io == "f32" else (32,):
+        for buckets in (0, 4):
+            p = problem(n, n, 8, 8, D, TYPES[io], buckets=buckets, far=6, causal=causal)
+            agree(tbe, p, 67, 4, f"{D} {buckets}", 3)       # a sequence of 9 between one of 7 and one of 20
+            agree(tbe, p, 70, 40, f"{D} {buckets} 70", 3)   # one of 70
