@@ -62,9 +62,18 @@ struct Mma {   // 16-bit types: fragments of 8 elements a lane, 16 of the summed
         else
             return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
     }
-    // registers 8 m .. 8 m + 7 of a tile as an operand; each is rounded once
-    static __device__ __forceinline__ uint4 pack(const f32x16_t& s, const int m) {
+    // registers 8 m .. 8 m + 7 of a tile as an operand; each is rounded once.  (As numbers of fp32: where a product is next rounded to binary16, the
+    // compiler does both at once in one copy of a loop and not in another, and the two would differ.)
+    static __device__ __forceinline__ uint4 pack(f32x16_t s, const int m) {
         const T* const t = nullptr;
+        if constexpr (__is_same(T, __half)) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                float x = s[8 * m + i];
+                asm("" : "+v"(x));
+                s[8 * m + i] = x;
+            }
+        }
         return make_uint4(pack2(t, s[8 * m], s[8 * m + 1]), pack2(t, s[8 * m + 2], s[8 * m + 3]), pack2(t, s[8 * m + 4], s[8 * m + 5]),
                           pack2(t, s[8 * m + 6], s[8 * m + 7]));
     }
@@ -125,6 +134,18 @@ __device__ __forceinline__ void flip_signs(uint4 (&f)[N]) {
     for (int c = 0; c < N; ++c) f[c] = make_uint4(f[c].x ^ sign, f[c].y ^ sign, f[c].z ^ sign, f[c].w ^ sign);
 }
 
+// whether a lane of those that share tiles says so: of the workgroup's four wavefronts (SHARE = 4, all of them here; votes: LDS that is used for
+// nothing else), or of this one
+template <int SHARE>
+__device__ __forceinline__ bool any_sharer(const bool here, int* votes, const int wave) {
+    bool any = __any(here);
+    if constexpr (SHARE == 4) {
+        if (lane_id() == 0) votes[wave] = any;
+        __syncthreads();
+        any = uniform(votes[0] | votes[1] | votes[2] | votes[3]) != 0;
+    }
+    return any;
+}
 // every lane's BYTES bytes to LDS, one lane's behind the other's
 template <int BYTES>
 __device__ __forceinline__ void load_lds(const void* from, void* to) {

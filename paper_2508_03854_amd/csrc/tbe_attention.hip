@@ -311,26 +311,16 @@ __global__ __launch_bounds__((64 * attn_waves<T, D, SHARE>()), (attn_occupancy<T
     }
     // The probability of a hidden key is 0, but 0 times a value that is not finite is not: where some keys are hidden and a result is not finite, all is
     // done once more (see Tile::cleaned).  Who shares tiles runs together.
-    if (kRows || a.causal) {
-        bool once_more = __any(is && not_finite(o));
-        if (SHARE == 4) {
-            if (lane == 0) votes[wave] = once_more;
-            __syncthreads();
+    if ((kRows || a.causal) && any_sharer<SHARE>(is && not_finite(o), votes, wave)) {
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) once_more |= votes[w] != 0;
-            once_more = uniform(once_more);
-        }
-        if (once_more) {
-#pragma unroll
-            for (int d = 0; d < kD; ++d) o[d] = f32x16_t{};
-            m = -__builtin_inff();
-            sum = 0.f;
-            for (uint64_t todo = kRows ? __ballot(is) : 1; todo;) {
-                if constexpr (kRows) take_some(todo);
-                else todo = 0;
+        for (int d = 0; d < kD; ++d) o[d] = f32x16_t{};
+        m = -__builtin_inff();
+        sum = 0.f;
+        for (uint64_t todo = kRows ? __ballot(is) : 1; todo;) {
+            if constexpr (kRows) take_some(todo);
+            else todo = 0;
 #pragma unroll 1
-                for (int t = t0; t < t1; ++t) careful_step(t);
-            }
+            for (int t = t0; t < t1; ++t) careful_step(t);
         }
     }
     if (!kRows) judge(a, looks, v, peek);

@@ -93,7 +93,7 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dq_occupancy<T, D
     constexpr int kTile = BK * D * (int)sizeof(T), kLds = SHARE == 4 ? kTile : kWaves * kTile, kSharers = SHARE == 4 ? 4 : 1;
     constexpr bool kRows = SHARE == 0;
     __shared__ __align__(16) char keys0[kLds], keys1[kLds], values0[kLds], values1[kLds];
-    __shared__ int votes[kWaves];
+    __shared__ int votes[2 * kWaves];
     extern __shared__ float tab[];   // the bias by distance, sums by distance - two arrays of that size for each wavefront -, the buckets
     const int wave = uniform(threadIdx.x >> 6), lane = lane_id(), col = lane & 31, half = lane >> 5;
     const uint32_t per_head = SHARE == 4 ? (uint32_t)a.V : ((uint32_t)a.V + kWaves - 1) / kWaves;
@@ -182,15 +182,7 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dq_occupancy<T, D
     bool one, sums_only;   // all keys in one tile of 32; a first run over the keys for D alone
     // Wide rows find their maximum and the sum below it again, in a run over the keys of its own: lse becomes the maximum, weight one over the sum.
     const bool wide = wide_row<T>(lse);
-    bool any_wide = __any(wide);
-    if (SHARE == 4) {   // (who shares tiles runs together)
-        if (lane == 0) votes[wave] = any_wide;
-        __syncthreads();
-        any_wide = false;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) any_wide |= votes[w] != 0;
-        any_wide = uniform(any_wide);
-    }
+    const bool any_wide = any_sharer<SHARE>(wide, votes, wave);
     float weight = 1.f;
     const int kvh = head / a.group;
     const char* const kb = a.k.at(q.k0, kvh);
@@ -313,11 +305,14 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dq_occupancy<T, D
     // by one, for the columns that see them (see Tile::cleaned); dS is the step's own, bit by bit, and its sums have been taken.
     auto careful_step = [&](const int t) __attribute__((always_inline)) {
         const int l = anew(lane), c32 = l & 31, h = l >> 5;
+        if (SHARE == 4) __syncthreads();
         fetch(t, keys0, values0, l);
         loads_done();
+        if (SHARE == 4) __syncthreads();
 #pragma unroll 1
         for (int k = 0; k < kT; ++k) {
             const int j0 = jbase + t * BK + 32 * k;
+            if (!kRows && (j0 >= q.nk || (a.causal && j0 > wave_last) || iw >= q.nq)) return;
             f32x16_t x = f32x16_t{}, g = f32x16_t{};
 #pragma unroll
             for (int c = 0; c < kC; ++c) x = Mma<T>::mma(Tile<T, D>::along(keys0 + own, 32 * k + c32, c, h), fq[c], x);
@@ -440,12 +435,12 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dq_occupancy<T, D
         }
     }
     if (!kRows) judge(a, looks, v, peek);
-    // With SHARE = 0, where the hidden keys may be another sequence's, all is done once more where a result is not finite.
-    if (kRows && __any(is && not_finite(dq))) {
+    if ((kRows || a.causal) && any_sharer<SHARE>(is && not_finite(dq), votes + kWaves, wave)) {   // (some keys are hidden)
 #pragma unroll
         for (int d = 0; d < kD; ++d) dq[d] = f32x16_t{};
-        for (uint64_t todo = __ballot(is); todo;) {
-            take_some(todo);
+        for (uint64_t todo = kRows ? __ballot(is) : 1; todo;) {
+            if constexpr (kRows) take_some(todo);
+            else todo = 0;
 #pragma unroll 1
             for (int t = 0; t < tiles; ++t) careful_step(t);
         }
@@ -509,6 +504,7 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dkv_occupancy<T, 
     constexpr bool kRows = SHARE == 0;
     __shared__ __align__(16) char rows0[kLds], rows1[kLds], grads0[kLds], grads1[kLds];
     __shared__ __align__(16) float stats0[kSets * 128], stats1[kSets * 128];   // lse and delta of 64 rows
+    __shared__ int votes[kWaves];
     extern __shared__ float tab[];
     const int wave = uniform(threadIdx.x >> 6), lane = lane_id(), col = lane & 31, half = lane >> 5;
     const int parts = a.splits, hp = a.pack;
@@ -590,8 +586,8 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dkv_occupancy<T, 
     f32x16_t dk[kD], dv[kD];
 #pragma unroll
     for (int d = 0; d < kD; ++d) dk[d] = dv[d] = f32x16_t{};
-    // P and dS of 32 rows of q from row i0 on, of head g: from their products; st: lse and delta of these rows
-    auto probabilities = [&](f32x16_t& x, f32x16_t& g_, const int g, const int i0, const float* const st, const int col, const int half) __attribute__((always_inline)) {
+    // P and dS of 32 rows of q from row i0 on, of head g: from their products; st: lse and delta of these rows; wide: some are
+    auto probabilities = [&](f32x16_t& x, f32x16_t& g_, const int g, const int i0, const float* const st, const bool wide, const int half) __attribute__((always_inline)) {
         const float* const ht = SHARE == 4 ? tab : tab + g * size;
         const int first = lead + i0;   // the first query's place
         const float* const lse = st + 4 * half;
@@ -612,7 +608,7 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dkv_occupancy<T, 
                 g_[r] = x[r] * (g_[r] - d[e]);
             }
         }
-        if (__any(wide_row<T>(st[col]))) {
+        if (wide) {
             const float* const weights = a.weight + (int64_t)(head0 + g) * a.q_rows + q.q0;
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
@@ -647,6 +643,7 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dkv_occupancy<T, 
         }
         const char* const qt = qt_ + own;
         const char* const yt = yt_ + own;
+        const bool wide = __any(wide_row<T>(st_[own_stats + lane % BQ]));
 #pragma unroll
         for (int k = 0; k < kT; ++k) {
             const int i0 = ibase + t * BQ + 32 * k, first = lead + i0;   // the first query and its place
@@ -659,7 +656,7 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dkv_occupancy<T, 
             for (int c = 0; c < kC; ++c) g_ = Mma<T>::mma(Tile<T, D>::along(yt, 32 * k + col, c, half), fv[c], g_);
             reads_ahead<2 * kC, 1, Mma<T>::kMfmas, 4>();
             settle<T>();
-            probabilities(x, g_, g, i0, st_ + own_stats + 32 * k, col, half);
+            probabilities(x, g_, g, i0, st_ + own_stats + 32 * k, wide, half);
 #pragma unroll
             for (int c = 0; c < kM; ++c) {
                 const uint4 p = Mma<T>::pack(x, c), ds = Mma<T>::pack(g_, c);
@@ -676,11 +673,17 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dkv_occupancy<T, 
     // The step once more where elements of q or dout are not finite, as in attn_dq_kernel.
     auto careful_step = [&](const int g, const int t) __attribute__((always_inline)) {
         const int l = anew(lane), c32 = l & 31, h = l >> 5;
+        if (SHARE == 4) __syncthreads();
         fetch(g, t, rows0, grads0, stats0, l);
+        if (BIAS && SHARE == 4 && t == t0) fill_bias(tab, a, head0 + g, 1, 64 * kWaves);
         loads_done();
+        if (SHARE == 4) __syncthreads();
+        const bool wide = __any(wide_row<T>(stats0[own_stats + l % BQ]));
 #pragma unroll 1
         for (int k = 0; k < kT; ++k) {
             const int i0 = ibase + t * BQ + 32 * k, first = lead + i0;
+            if (!kRows && (i0 >= q.nq || jw >= q.nk)) return;
+            if (!kRows && a.causal && first + 31 < jw) continue;
             f32x16_t x = f32x16_t{}, g_ = f32x16_t{};
 #pragma unroll
             for (int c = 0; c < kC; ++c) x = Mma<T>::mma(Tile<T, D>::along(rows0 + own, 32 * k + c32, c, h), fk[c], x);
@@ -688,7 +691,7 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dkv_occupancy<T, 
             for (int c = 0; c < kC; ++c) g_ = Mma<T>::mma(Tile<T, D>::along(grads0 + own, 32 * k + c32, c, h), fv[c], g_);
             reads_ahead<2 * kC, 1, Mma<T>::kMfmas, 2>();
             settle<T>();
-            probabilities(x, g_, g, i0, stats0 + own_stats + 32 * k, c32, h);
+            probabilities(x, g_, g, i0, stats0 + own_stats + 32 * k, wide, h);
             const int from = kRows ? lo - i0 : (a.causal ? j - first : 0), to = kRows ? end - i0 : 32;
             Tile<T, D>::add_not_finite(dv, grads0 + own, 32 * k, x, from, to, l);
             Tile<T, D>::add_not_finite(dk, rows0 + own, 32 * k, g_, from, to, l);
@@ -730,11 +733,12 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dkv_occupancy<T, 
             if (++t == t0 + tiles) { t = t0; ++g; }
         }
     }
-    if (kRows && __any(is && (not_finite(dk) || not_finite(dv)))) {   // as in attn_dq_kernel
+    if ((kRows || a.causal) && any_sharer<SHARE>(is && (not_finite(dk) || not_finite(dv)), votes, wave)) {   // as in attn_dq_kernel
 #pragma unroll
         for (int d = 0; d < kD; ++d) dk[d] = dv[d] = f32x16_t{};
-        for (uint64_t todo = __ballot(is); todo;) {
-            take_some(todo);
+        for (uint64_t todo = kRows ? __ballot(is) : 1; todo;) {
+            if constexpr (kRows) take_some(todo);
+            else todo = 0;
 #pragma unroll 1
             for (int g = 0; g < hp; ++g)
 #pragma unroll 1

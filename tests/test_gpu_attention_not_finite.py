@@ -120,3 +120,25 @@ def test_sequences_that_share_wavefronts(tbe, io, causal):
             p = problem(n, n, 8, 8, D, TYPES[io], buckets=buckets, far=6, causal=causal)
             agree(tbe, p, 67, 4, f"{D} {buckets}", 3)       # a sequence of 9 between one of 7 and one of 20
             agree(tbe, p, 70, 40, f"{D} {buckets} 70", 3)   # one of 70
+
+
+@pytest.mark.parametrize("io", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("D", [32, 64, 128])
+def test_own_wavefronts_and_shared_tiles(tbe, io, D):
+    """Sequences on their own wavefronts, and on tiles that a workgroup shares; D = 128 has the latter in both kernels of the backward only beside
+    tables of many distances.  Heads of a group one after the other, other numbers of keys than of queries."""
+    for n, H, K, s, row in (([40, 100, 33], 2, 1, 1, 60), ([20, 9, 31, 70], 4, 2, 2, 4), ([500, 130, 330], 2, 1, 0, 301), ([700, 450], 2, 2, 1, 77)):
+        for causal, buckets, far in ((True, 0, 0), (True, 8, 20), (True, 8, 1024), (False, 8, 20)):
+            agree(tbe, problem(n, n, H, K, D, TYPES[io], buckets=buckets, far=far, causal=causal), s, row, f"{n} {causal} {buckets} {far}")
+    for nq, nk, s, row in (([33, 20], [150, 60], 0, 25), ([200, 300], [260, 310], 1, 199), ([70, 150], [30, 100], 1, 66)):
+        agree(tbe, problem(nq, nk, 2, 1, D, TYPES[io], buckets=8, far=20), s, row, f"{nq} {nk}")
+
+
+def test_sequences_that_share_wavefronts_in_one_kernel(tbe):
+    """Heads whose queries share wavefronts and whose keys do not."""
+    n = [7, 9, 20, 5, 70, 3] * 75
+    for io, D in (("f32", 128), ("f16", 64), ("bf16", 64), ("bf16", 128)):
+        for causal, buckets in ((True, 0), (True, 4), (False, 4)):
+            p = problem(n, n, 8, 8, D, TYPES[io], buckets=buckets, far=6, causal=causal)
+            agree(tbe, p, 67, 4, f"{io} {D} {buckets}", 3)
+            agree(tbe, p, 70, 40, f"{io} {D} {buckets} 70", 3)
