@@ -180,9 +180,9 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dq_occupancy<T, D
     constexpr int kFew = 4;
     float delta = 0.f, dsum;
     bool one, sums_only;   // all keys in one tile of 32; a first run over the keys for D alone
-    // Wide rows find their maximum and the sum below it again, in a run over the keys of its own: lse becomes the maximum, weight one over the sum.
-    const bool wide = wide_row<T>(lse);
-    const bool any_wide = any_sharer<SHARE>(wide, votes, wave);
+    // Where a row is wide, the unit's rows find their maxima and the sums below them again, in a run over the keys of its own: lse becomes the
+    // maximum, weight one over the sum.
+    const bool any_wide = any_sharer<SHARE>(wide_row<T>(lse), votes, wave);
     float weight = 1.f;
     const int kvh = head / a.group;
     const char* const kb = a.k.at(q.k0, kvh);
@@ -202,39 +202,23 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dq_occupancy<T, D
         beyond = tab[kTabMargin];
         ahead = a.causal ? 0.f : tab[2 * a.far + kTabMargin];
     }
-    // the exponents of a tile's probabilities: its products, scaled, with their bias, less `by`
-    auto exponents = [&](f32x16_t& x, const int j0, const float by) __attribute__((always_inline)) {
+    // dbias: what 32 keys from j0 on add to the sums by distance
+    auto count = [&](const f32x16_t& g, const int j0, const int col, const int half) __attribute__((always_inline)) {
         const bool all_beyond = first - (j0 + 31) >= a.far, all_ahead = wave_last - j0 <= -a.far;
-        if (!BIAS) {
+        if (all_beyond || all_ahead) {
+            float sum = 0.f;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) x[r] = fmaf(x[r], a.scale2, -by);
-        } else if (all_beyond || all_ahead) {
-            const float flat = all_beyond ? beyond : ahead;
-            // (scores beside a wide row's are rounded with their bias, as in the forward and in other tiles, and not with its difference to lse)
-            const float b = any_wide ? flat : flat - by;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) x[r] = fmaf(x[r], a.scale2, b);
-            if (any_wide) {
-#pragma unroll
-                for (int r = 0; r < 16; ++r) x[r] -= by;
-            }
+            for (int r = 0; r < 16; ++r) sum += g[r];
+            if (all_beyond) sum_beyond += sum;
+            else sum_ahead += sum;
         } else {
-            const float* const from = tab + (j0 + 4 * half - pos + a.far + kTabMargin);
-#pragma unroll
-            for (int r = 0; r < 16; ++r) x[r] = fmaf(x[r], a.scale2, from[8 * (r / 4) + r % 4]) - by;
-        }
-    };
-    // what is hidden of 32 keys from j0 on becomes 0
-    auto hide = [&](f32x16_t& x, f32x16_t& g, const int j0) __attribute__((always_inline)) {
-        if constexpr (kRows) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-                if ((uint32_t)(j0 + 8 * (r / 4) + 4 * half + r % 4 - lo) >= (uint32_t)(end - lo)) x[r] = g[r] = 0.f;
-        } else if (j0 + 32 > q.nk || (a.causal && j0 + 31 > first)) {
-            const int end = a.causal && pos + 1 < q.nk ? pos + 1 : q.nk;
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-                if (j0 + 8 * (r / 4) + 4 * half + r % 4 >= end) x[r] = g[r] = 0.f;
+            // What a tile has of one distance lies on a diagonal; see diagonal_sums.  A distance of a half's array is met by two
+            // neighbouring tiles and stored once, with the second.
+            const float2 now = diagonal_sums(g);
+            float* const to = sums + half * size + j0 - first + a.far + kTabMargin + 4 * half - col;
+            *to = now.x + carry + (kRows ? *to : 0.f);   // (other columns' places may have met these distances before)
+            carry = now.y;
+            carry_at = j0 + 32;
         }
     };
     auto step = [&](const int t, const char* const kt_, const char* const vt_, char* const kn, char* const vn) __attribute__((always_inline)) {
@@ -255,13 +239,28 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dq_occupancy<T, D
             reads_ahead<2 * kC, 1, Mma<T>::kMfmas, 4>();
             settle<T>();
             const bool all_beyond = first - (j0 + 31) >= a.far, all_ahead = wave_last - j0 <= -a.far;
-            exponents(x, j0, lse);
+            const int at = j0 + 4 * half - pos + a.far + kTabMargin;   // of this lane's first key among the distances
+            if (!BIAS) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r) x[r] = __builtin_amdgcn_exp2f(x[r]);
-            hide(x, g, j0);
-            if (any_wide) {
+                for (int r = 0; r < 16; ++r) x[r] = __builtin_amdgcn_exp2f(fmaf(x[r], a.scale2, -lse));
+            } else if (all_beyond || all_ahead) {
+                const float b = (all_beyond ? beyond : ahead) - lse;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) x[r] *= weight;
+                for (int r = 0; r < 16; ++r) x[r] = __builtin_amdgcn_exp2f(fmaf(x[r], a.scale2, b));
+            } else {
+                const float* const from = tab + at;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) x[r] = __builtin_amdgcn_exp2f(fmaf(x[r], a.scale2, from[8 * (r / 4) + r % 4]) - lse);
+            }
+            if constexpr (kRows) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if ((uint32_t)(j0 + 8 * (r / 4) + 4 * half + r % 4 - lo) >= (uint32_t)(end - lo)) x[r] = g[r] = 0.f;
+            } else if (j0 + 32 > q.nk || (a.causal && j0 + 31 > first)) {
+                const int end = a.causal && pos + 1 < q.nk ? pos + 1 : q.nk;
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (j0 + 8 * (r / 4) + 4 * half + r % 4 >= end) x[r] = g[r] = 0.f;
             }
             if (sums_only || one) {
                 float sum = 0.f;
@@ -274,23 +273,7 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dq_occupancy<T, D
             }
 #pragma unroll
             for (int r = 0; r < 16; ++r) g[r] = x[r] * (g[r] - delta);
-            if (BIAS) {
-                if (all_beyond || all_ahead) {
-                    float sum = 0.f;
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) sum += g[r];
-                    if (all_beyond) sum_beyond += sum;
-                    else sum_ahead += sum;
-                } else {
-                    // What a tile has of one distance lies on a diagonal; see diagonal_sums.  A distance of a half's array is met by two
-                    // neighbouring tiles and stored once, with the second.
-                    const float2 now = diagonal_sums(g);
-                    float* const to = sums + half * size + j0 - first + a.far + kTabMargin + 4 * half - col;
-                    *to = now.x + carry + (kRows ? *to : 0.f);   // (other columns' places may have met these distances before)
-                    carry = now.y;
-                    carry_at = j0 + 32;
-                }
-            }
+            if (BIAS) count(g, j0, col, half);
 #pragma unroll
             for (int c = 0; c < kM; ++c) {
                 const uint4 p = Mma<T>::pack(g, c);
@@ -301,10 +284,8 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dq_occupancy<T, D
             settle<T>();
         }
     };
-    // What is hidden has dS = 0, but 0 times a key that is not finite is not 0.  The step once more for such keys: their elements are multiplied one
-    // by one, for the columns that see them (see Tile::cleaned); dS is the step's own, bit by bit, and its sums have been taken.
-    auto careful_step = [&](const int t) __attribute__((always_inline)) {
-        const int l = anew(lane), c32 = l & 31, h = l >> 5;
+    // The rare ways, one tile at a time.  Their addresses and places are computed anew, so that they take no registers in the loop above.
+    auto alone = [&](const int t, const int l, const auto run) __attribute__((always_inline)) {   // `run` on 32 rows of tile t after the others
         if (SHARE == 4) __syncthreads();
         fetch(t, keys0, values0, l);
         loads_done();
@@ -313,6 +294,74 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dq_occupancy<T, D
         for (int k = 0; k < kT; ++k) {
             const int j0 = jbase + t * BK + 32 * k;
             if (!kRows && (j0 >= q.nk || (a.causal && j0 > wave_last) || iw >= q.nq)) return;
+            run(k, j0);
+        }
+    };
+    // the exponents of 32 keys' probabilities: their products, scaled, with their bias, less `by`
+    auto exponents = [&](f32x16_t& x, const int j0, const float by, const int place, const int half) __attribute__((always_inline)) {
+        const bool all_beyond = first - (j0 + 31) >= a.far, all_ahead = wave_last - j0 <= -a.far;
+        if (!BIAS) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) x[r] = fmaf(x[r], a.scale2, -by);
+        } else if (all_beyond || all_ahead) {
+            const float flat = all_beyond ? beyond : ahead;
+            // (a wide row's scores are rounded with their bias, as in the forward and in other tiles, and not with its difference to lse)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) x[r] = any_wide ? fmaf(x[r], a.scale2, flat) - by : fmaf(x[r], a.scale2, flat - by);
+        } else {
+            const float* const from = tab + (j0 + 4 * half - place + a.far + kTabMargin);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) x[r] = fmaf(x[r], a.scale2, from[8 * (r / 4) + r % 4]) - by;
+        }
+    };
+    auto find_statistics = [&]() __attribute__((always_inline)) {
+        const int l = anew(lane), c32 = l & 31, h = l >> 5, place = anew(pos);
+        const int from = kRows ? lo : 0, to = kRows ? end : (a.causal && place + 1 < q.nk ? place + 1 : q.nk);
+        float top = -__builtin_inff(), sum = 0.f, d = 0.f;
+#pragma unroll 1
+        for (int t = 0; t < tiles; ++t)
+            alone(t, l, [&](const int k, const int j0) __attribute__((always_inline)) {
+                f32x16_t x = f32x16_t{}, g = f32x16_t{};
+#pragma unroll
+                for (int c = 0; c < kC; ++c) x = Mma<T>::mma(Tile<T, D>::along(keys0 + own, 32 * k + c32, c, h), fq[c], x);
+#pragma unroll
+                for (int c = 0; c < kC; ++c) g = Mma<T>::mma(Tile<T, D>::along(values0 + own, 32 * k + c32, c, h), fy[c], g);
+                settle<T>();
+                exponents(x, j0, 0.f, place, h);
+                float most = top;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int j = j0 + 8 * (r / 4) + 4 * h + r % 4;
+                    const bool sees = j >= from && j < to;
+                    x[r] = sees ? x[r] : -__builtin_inff();
+                    g[r] = sees ? g[r] : 0.f;
+                    most = fmaxf(most, x[r]);
+                }
+                most = halves_max(most);
+                const float at = most == -__builtin_inff() ? 0.f : most, shrink = __builtin_amdgcn_exp2f(top - at);
+                sum *= shrink;
+                d *= shrink;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const float p = __builtin_amdgcn_exp2f(x[r] - at);
+                    sum += p;
+                    d = fmaf(p, g[r], d);
+                }
+                top = most;
+            });
+        sum = pair_sum<32>(sum);
+        d = pair_sum<32>(d);
+        const bool found = sum != 0.f, apart = wide_row<T>(top);   // (attn_dkv_kernel goes by lse)
+        lse = !found ? lse : (apart ? top : top + __builtin_amdgcn_logf(sum));
+        weight = found && apart ? 1.f / sum : weight;
+        delta = found ? d / sum : delta;
+    };
+    // The step's dS, bit by bit.  What is hidden has dS = 0, but 0 times a key that is not finite is not 0: its elements are multiplied one by one, for
+    // the columns that see them (see Tile::cleaned).
+    auto careful_step = [&](const int t, const bool counts) __attribute__((always_inline)) {
+        const int l = anew(lane), c32 = l & 31, h = l >> 5, place = anew(pos);
+        const int from = kRows ? lo : 0, to = kRows ? end : (a.causal && place + 1 < q.nk ? place + 1 : q.nk);
+        alone(t, l, [&](const int k, const int j0) __attribute__((always_inline)) {
             f32x16_t x = f32x16_t{}, g = f32x16_t{};
 #pragma unroll
             for (int c = 0; c < kC; ++c) x = Mma<T>::mma(Tile<T, D>::along(keys0 + own, 32 * k + c32, c, h), fq[c], x);
@@ -320,14 +369,14 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dq_occupancy<T, D
             for (int c = 0; c < kC; ++c) g = Mma<T>::mma(Tile<T, D>::along(values0 + own, 32 * k + c32, c, h), fy[c], g);
             reads_ahead<2 * kC, 1, Mma<T>::kMfmas, 2>();
             settle<T>();
-            exponents(x, j0, lse);
+            exponents(x, j0, lse, place, h);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) x[r] = __builtin_amdgcn_exp2f(x[r]) * weight;
-            hide(x, g, j0);
-#pragma unroll
-            for (int r = 0; r < 16; ++r) g[r] = x[r] * (g[r] - delta);
-            const int upto = kRows ? end : (a.causal && pos + 1 < q.nk ? pos + 1 : q.nk);
-            Tile<T, D>::add_not_finite(dq, keys0 + own, 32 * k, g, (kRows ? lo : 0) - j0, upto - j0, l);
+            for (int r = 0; r < 16; ++r) {
+                const int j = j0 + 8 * (r / 4) + 4 * h + r % 4;
+                g[r] = j >= from && j < to ? __builtin_amdgcn_exp2f(x[r]) * weight * (g[r] - delta) : 0.f;
+            }
+            if (BIAS && counts) count(g, j0, c32, h);
+            Tile<T, D>::add_not_finite(dq, keys0 + own, 32 * k, g, from - j0, to - j0, l);
 #pragma unroll
             for (int c = 0; c < kM; ++c) {
                 const uint4 p = Mma<T>::pack(g, c);
@@ -338,7 +387,7 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dq_occupancy<T, D
                 }
             }
             settle<T>();
-        }
+        });
     };
     // SHARE = 0: columns whose places lie as their rows do go together
     auto take_some = [&](uint64_t& todo) __attribute__((always_inline)) {
@@ -354,49 +403,18 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dq_occupancy<T, D
         const int last = wave_max_i32(lo < end ? end : 0);
         tiles = jbase < last ? (last - jbase + BK - 1) / BK : 0;
     };
-    for (uint64_t todo = kRows ? __ballot(is) : 1; todo;) {
+    // the last tile's share of dbias
+    auto count_rest = [&]() __attribute__((always_inline)) {
+        if (BIAS && carry_at >= 0) {
+            float* const to = sums + half * size + carry_at - first + a.far + kTabMargin + 4 * half - col;
+            *to = carry + (kRows ? *to : 0.f);
+            carry = 0.f;
+            carry_at = -1;
+        }
+    };
+    for (uint64_t todo = any_wide ? 0 : (kRows ? __ballot(is) : 1); todo;) {
         if constexpr (kRows) take_some(todo);
         else todo = 0;
-        if (any_wide) {
-            float top = -__builtin_inff(), sum = 0.f;
-            const bool here = wide && (!kRows || lo < end);
-            const int from = kRows ? lo : 0, to = kRows ? end : (a.causal && pos + 1 < q.nk ? pos + 1 : q.nk);
-            const int l = anew(lane), c32 = l & 31, h = l >> 5;
-#pragma unroll 1
-            for (int t = 0; t < tiles; ++t) {
-                if (SHARE == 4) __syncthreads();
-                Tile<T, D>::template fetch<BK, kSharers>(keys0 + own, kb, a.k.row, jbase + t * BK, q.nk, a.dim, fw, l);
-                loads_done();
-                if (SHARE == 4) __syncthreads();
-#pragma unroll 1
-                for (int k = 0; k < kT; ++k) {
-                    const int j0 = jbase + t * BK + 32 * k;
-                    f32x16_t x = f32x16_t{};
-#pragma unroll
-                    for (int c = 0; c < kC; ++c) x = Mma<T>::mma(Tile<T, D>::along(keys0 + own, 32 * k + c32, c, h), fq[c], x);
-                    settle<T>();
-                    exponents(x, j0, 0.f);
-                    float most = top;
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int j = j0 + 8 * (r / 4) + 4 * half + r % 4;
-                        if (j < from || j >= to) x[r] = -__builtin_inff();
-                        most = fmaxf(most, x[r]);
-                    }
-                    most = halves_max(most);
-                    const float at = most == -__builtin_inff() ? 0.f : most;
-                    sum *= __builtin_amdgcn_exp2f(top - at);
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) sum += __builtin_amdgcn_exp2f(x[r] - at);
-                    top = most;
-                }
-            }
-            if (SHARE == 4) __syncthreads();
-            sum = pair_sum<32>(sum);
-            const bool found = here && sum != 0.f, apart = wide_row<T>(top);   // (attn_dkv_kernel goes by lse)
-            lse = !found ? lse : (apart ? top : top + __builtin_amdgcn_logf(sum));
-            weight = found && apart ? 1.f / sum : weight;
-        }
         one = kT == 1 && tiles == 1;
         sums_only = tiles <= kFew && !one;
         dsum = 0.f;
@@ -427,22 +445,21 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dq_occupancy<T, D
             delta = !kRows || lo < end ? d : delta;
             if (SHARE == 4) __syncthreads();   // (the first tile's place may still be read)
         }
-        if (BIAS && carry_at >= 0) {
-            float* const to = sums + half * size + carry_at - first + a.far + kTabMargin + 4 * half - col;
-            *to = carry + (kRows ? *to : 0.f);
-            carry = 0.f;
-            carry_at = -1;
-        }
+        count_rest();
     }
     if (!kRows) judge(a, looks, v, peek);
-    if ((kRows || a.causal) && any_sharer<SHARE>(is && not_finite(dq), votes + kWaves, wave)) {   // (some keys are hidden)
+    bool carefully = any_wide;
+    if ((kRows || a.causal) && !any_wide) carefully = any_sharer<SHARE>(is && not_finite(dq), votes + kWaves, wave);   // (where some keys are hidden)
+    if (carefully) {
 #pragma unroll
         for (int d = 0; d < kD; ++d) dq[d] = f32x16_t{};
         for (uint64_t todo = kRows ? __ballot(is) : 1; todo;) {
             if constexpr (kRows) take_some(todo);
             else todo = 0;
+            if (any_wide) find_statistics();
 #pragma unroll 1
-            for (int t = 0; t < tiles; ++t) careful_step(t);
+            for (int t = 0; t < tiles; ++t) careful_step(t, any_wide);   // (dbias has been counted otherwise)
+            count_rest();
         }
     }
     if (is && half == 0) {   // for attn_dkv_kernel
@@ -586,48 +603,7 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dkv_occupancy<T, 
     f32x16_t dk[kD], dv[kD];
 #pragma unroll
     for (int d = 0; d < kD; ++d) dk[d] = dv[d] = f32x16_t{};
-    // P and dS of 32 rows of q from row i0 on, of head g: from their products; st: lse and delta of these rows; wide: some are
-    auto probabilities = [&](f32x16_t& x, f32x16_t& g_, const int g, const int i0, const float* const st, const bool wide, const int half) __attribute__((always_inline)) {
-        const float* const ht = SHARE == 4 ? tab : tab + g * size;
-        const int first = lead + i0;   // the first query's place
-        const float* const lse = st + 4 * half;
-        const bool all_beyond = first - (jw + 31) >= a.far, all_ahead = first + 31 - jw <= -a.far;
-        float flat = 0.f;
-        if (BIAS && (all_beyond || all_ahead)) flat = all_beyond ? ht[kTabMargin] : (a.causal ? 0.f : ht[2 * a.far + kTabMargin]);
-        const bool by_distance = BIAS && !all_beyond && !all_ahead;
-        const float* const from = by_distance ? ht + (j - first - 4 * half + a.far + kTabMargin) - 27 : nullptr;
-#pragma unroll
-        for (int n = 0; n < 4; ++n) {
-            const float4 l4 = *reinterpret_cast<const float4*>(lse + 8 * n), d4 = *reinterpret_cast<const float4*>(lse + 64 + 8 * n);
-            const float l[4] = {l4.x, l4.y, l4.z, l4.w}, d[4] = {d4.x, d4.y, d4.z, d4.w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int r = 4 * n + e;
-                if (!BIAS) x[r] = __builtin_amdgcn_exp2f(fmaf(x[r], a.scale2, -l[e]));
-                else x[r] = __builtin_amdgcn_exp2f(fmaf(x[r], a.scale2, by_distance ? from[27 - 8 * n - e] : flat) - l[e]);
-                g_[r] = x[r] * (g_[r] - d[e]);
-            }
-        }
-        if (wide) {
-            const float* const weights = a.weight + (int64_t)(head0 + g) * a.q_rows + q.q0;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int i = i0 + 8 * (r / 4) + 4 * half + r % 4;
-                const float by = weights[i < q.nq ? i : q.nq - 1];   // (behind the last query all is 0)
-                x[r] *= by;
-                g_[r] *= by;
-            }
-        }
-        if constexpr (kRows) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-                if ((uint32_t)(i0 + 8 * (r / 4) + 4 * half + r % 4 - lo) >= (uint32_t)(end - lo)) x[r] = g_[r] = 0.f;
-        } else if (a.causal && first < jw + 31) {   // hidden: queries before the key's place
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-                if (first + 8 * (r / 4) + 4 * half + r % 4 < j) x[r] = g_[r] = 0.f;
-        }
-    };
+    bool met_wide = false;   // (wide rows' probabilities have weights: see below)
     // the step after (g, t) is (g, t + 1) or the next head's first
     auto step = [&](const int g, const int t, const bool more, const char* const qt_, const char* const yt_, const float* const st_, char* const qn,
                     char* const yn, float* const sn) __attribute__((always_inline)) {
@@ -643,7 +619,8 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dkv_occupancy<T, 
         }
         const char* const qt = qt_ + own;
         const char* const yt = yt_ + own;
-        const bool wide = __any(wide_row<T>(st_[own_stats + lane % BQ]));
+        const float* const ht = SHARE == 4 ? tab : tab + g * size;
+        met_wide |= wide_row<T>(st_[own_stats + lane % BQ]);
 #pragma unroll
         for (int k = 0; k < kT; ++k) {
             const int i0 = ibase + t * BQ + 32 * k, first = lead + i0;   // the first query and its place
@@ -656,7 +633,38 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dkv_occupancy<T, 
             for (int c = 0; c < kC; ++c) g_ = Mma<T>::mma(Tile<T, D>::along(yt, 32 * k + col, c, half), fv[c], g_);
             reads_ahead<2 * kC, 1, Mma<T>::kMfmas, 4>();
             settle<T>();
-            probabilities(x, g_, g, i0, st_ + own_stats + 32 * k, wide, half);
+            const float* const lse = st_ + own_stats + 32 * k + 4 * half;
+            const bool all_beyond = first - (jw + 31) >= a.far, all_ahead = first + 31 - jw <= -a.far;
+            if (BIAS && (all_beyond || all_ahead)) {
+                const float flat = all_beyond ? ht[kTabMargin] : (a.causal ? 0.f : ht[2 * a.far + kTabMargin]);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) x[r] = fmaf(x[r], a.scale2, flat);
+            } else if (BIAS) {
+                const float* const from = ht + (j - first - 4 * half + a.far + kTabMargin) - 27;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) x[r] = fmaf(x[r], a.scale2, from[27 - 8 * (r / 4) - r % 4]);
+            }
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+                const float4 l4 = *reinterpret_cast<const float4*>(lse + 8 * n), d4 = *reinterpret_cast<const float4*>(lse + 64 + 8 * n);
+                const float l[4] = {l4.x, l4.y, l4.z, l4.w}, d[4] = {d4.x, d4.y, d4.z, d4.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int r = 4 * n + e;
+                    if (!BIAS) x[r] = __builtin_amdgcn_exp2f(fmaf(x[r], a.scale2, -l[e]));
+                    else x[r] = __builtin_amdgcn_exp2f(x[r] - l[e]);
+                    g_[r] = x[r] * (g_[r] - d[e]);
+                }
+            }
+            if constexpr (kRows) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if ((uint32_t)(i0 + 8 * (r / 4) + 4 * half + r % 4 - lo) >= (uint32_t)(end - lo)) x[r] = g_[r] = 0.f;
+            } else if (a.causal && first < jw + 31) {   // hidden: queries before the key's place
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (first + 8 * (r / 4) + 4 * half + r % 4 < j) x[r] = g_[r] = 0.f;
+            }
 #pragma unroll
             for (int c = 0; c < kM; ++c) {
                 const uint4 p = Mma<T>::pack(x, c), ds = Mma<T>::pack(g_, c);
@@ -670,15 +678,19 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dkv_occupancy<T, 
             settle<T>();
         }
     };
-    // The step once more where elements of q or dout are not finite, as in attn_dq_kernel.
+    // The step with weights, and with care for elements of q and dout that are not finite, as in attn_dq_kernel; otherwise the same bit by bit.
     auto careful_step = [&](const int g, const int t) __attribute__((always_inline)) {
-        const int l = anew(lane), c32 = l & 31, h = l >> 5;
+        const int l = anew(lane), c32 = l & 31, h = l >> 5, place = anew(j);
         if (SHARE == 4) __syncthreads();
         fetch(g, t, rows0, grads0, stats0, l);
+        if (SHARE != 4 || wave == 0) {   // the rows' weights
+            const int i = ibase + t * BQ + l;
+            const float* const w = a.weight + (int64_t)(head0 + g) * a.q_rows + q.q0 + i;
+            load_lds<4>(l < BQ && i < q.nq ? w : reinterpret_cast<const float*>(&attn_zeros), stats1 + own_stats);
+        }
         if (BIAS && SHARE == 4 && t == t0) fill_bias(tab, a, head0 + g, 1, 64 * kWaves);
         loads_done();
         if (SHARE == 4) __syncthreads();
-        const bool wide = __any(wide_row<T>(stats0[own_stats + l % BQ]));
 #pragma unroll 1
         for (int k = 0; k < kT; ++k) {
             const int i0 = ibase + t * BQ + 32 * k, first = lead + i0;
@@ -691,8 +703,27 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dkv_occupancy<T, 
             for (int c = 0; c < kC; ++c) g_ = Mma<T>::mma(Tile<T, D>::along(grads0 + own, 32 * k + c32, c, h), fv[c], g_);
             reads_ahead<2 * kC, 1, Mma<T>::kMfmas, 2>();
             settle<T>();
-            probabilities(x, g_, g, i0, stats0 + own_stats + 32 * k, wide, h);
-            const int from = kRows ? lo - i0 : (a.causal ? j - first : 0), to = kRows ? end - i0 : 32;
+            const float* const lse = stats0 + own_stats + 32 * k + 4 * h;
+            const float* const ht = SHARE == 4 ? tab : tab + g * size;
+            const float* const weights = stats1 + own_stats + 32 * k + 4 * h;
+            const bool all_beyond = first - (jw + 31) >= a.far, all_ahead = first + 31 - jw <= -a.far;
+            float flat = 0.f;
+            if (BIAS && (all_beyond || all_ahead)) flat = all_beyond ? ht[kTabMargin] : (a.causal ? 0.f : ht[2 * a.far + kTabMargin]);
+            const bool by_distance = BIAS && !all_beyond && !all_ahead;
+            const float* const near = by_distance ? ht + (place - first - 4 * h + a.far + kTabMargin) - 27 : nullptr;
+            const int from = kRows ? lo - i0 : (a.causal ? place - first : 0), to = kRows ? end - i0 : 32;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int e = 8 * (r / 4) + r % 4, i = 4 * h + e;
+                if (!BIAS) x[r] = fmaf(x[r], a.scale2, -lse[e]);
+                else x[r] = fmaf(x[r], a.scale2, by_distance ? near[27 - e] : flat) - lse[e];
+                x[r] = __builtin_amdgcn_exp2f(x[r]);
+                g_[r] = x[r] * (g_[r] - lse[64 + e]);
+                const bool sees = i >= from && i < to;
+                x[r] = sees ? x[r] * weights[e] : 0.f;
+                g_[r] = sees ? g_[r] * weights[e] : 0.f;
+                if (r % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // (few registers rather than many loads under way)
+            }
             Tile<T, D>::add_not_finite(dv, grads0 + own, 32 * k, x, from, to, l);
             Tile<T, D>::add_not_finite(dk, rows0 + own, 32 * k, g_, from, to, l);
 #pragma unroll
@@ -733,7 +764,7 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dkv_occupancy<T, 
             if (++t == t0 + tiles) { t = t0; ++g; }
         }
     }
-    if ((kRows || a.causal) && any_sharer<SHARE>(is && (not_finite(dk) || not_finite(dv)), votes, wave)) {   // as in attn_dq_kernel
+    if (any_sharer<SHARE>(met_wide || ((kRows || a.causal) && is && (not_finite(dk) || not_finite(dv))), votes, wave)) {
 #pragma unroll
         for (int d = 0; d < kD; ++d) dk[d] = dv[d] = f32x16_t{};
         for (uint64_t todo = kRows ? __ballot(is) : 1; todo;) {
