@@ -480,9 +480,16 @@ __device__ __forceinline__ void fill_bias(float* tab, const AttnArgs& a, const i
 
 // Workgroups are dealt to the 8 dies one by one; each die takes a run of neighbours, so that those that read the same keys share its
 // level-2 cache: 2 sequences of 6000, 16 heads of 128 over 4 bfloat16, forward in the order of the grid 342 us, in this one 297; 48 sequences with
-// 61 queries each, 8 heads of 64, 79 / 65; 4 of 2500, 8 heads of 64 over 2, dq 164 / 132, dk and dv 154 / 140.  The grid has 8 * ceil(n / 8)
-// workgroups.
-__device__ __forceinline__ uint32_t die_order(const uint32_t n) { return (blockIdx.x & 7u) * ((n + 7u) / 8u) + (blockIdx.x >> 3); }
+// 61 queries each, 8 heads of 64, 79 / 65; 4 of 2500, 8 heads of 64 over 2, dq 164 / 132, dk and dv 154 / 140.  n or more: nothing to do.
+__device__ __forceinline__ uint32_t die_order(const uint32_t n) {
+    const uint32_t wg = blockIdx.y * gridDim.x + blockIdx.x, run = (n + 7u) / 8u;
+    return (wg >> 3) < run ? (wg & 7u) * run + (wg >> 3) : n;
+}
+// The grid for it: a side of a grid has fewer than 2^32 lanes, which 2^20 sequences of a few events with 64 heads exceed.
+inline dim3 die_grid(const uint64_t n) {
+    const uint64_t all = (n + 7) / 8 * 8, side = (uint64_t)1 << 22;
+    return all <= side ? dim3((unsigned)all) : dim3((unsigned)side, (unsigned)((all + side - 1) / side));
+}
 // A workgroup's head (or heads) and which of the head's items it has: one head after the other, which keeps the keys of few heads in the cache; short
 // sequences (SHARE = 0), whose wavefronts wait for memory first of all, one item after the other, so that heads that lie in the same cache
 // lines are read together: 4096 sequences of 12 events on average, 4 heads of 32 bfloat16, head after head / item after item, us: forward 30.5 /

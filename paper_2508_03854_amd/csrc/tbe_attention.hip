@@ -504,7 +504,7 @@ static hipError_t launch_one(const AttnArgs& a, hipStream_t s) {
     const size_t table = BIAS ? (size_t)a.pack * (2 * a.far + 1 + 2 * kTabMargin) * 4 : 0;
     const uint64_t per_head = SHARE == 4 || a.together ? (uint64_t)a.V * a.splits : ((uint64_t)a.V + kWaves - 1) / kWaves;
     const uint64_t groups = per_head * (uint64_t)(a.H / a.pack);
-    attn_kernel<T, D, SHARE, BIAS><<<(unsigned)((groups + 7) / 8 * 8), 64 * kWaves, table, s>>>(a);
+    attn_kernel<T, D, SHARE, BIAS><<<die_grid(groups), 64 * kWaves, table, s>>>(a);
     return hipGetLastError();
 }
 template <typename T, int D>

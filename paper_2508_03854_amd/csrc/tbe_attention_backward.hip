@@ -877,7 +877,7 @@ static hipError_t launch_dq(const AttnArgs& a, hipStream_t s) {
     const uint64_t per_head = SHARE == 4 ? (uint64_t)a.V : ((uint64_t)a.V + kWaves - 1) / kWaves;
     const hipError_t e = room_for(reinterpret_cast<const void*>(attn_dq_kernel<T, D, SHARE, BIAS>), table);
     if (e != hipSuccess) return e;
-    attn_dq_kernel<T, D, SHARE, BIAS><<<(unsigned)((per_head * a.H + 7) / 8 * 8), 64 * kWaves, table, s>>>(a);
+    attn_dq_kernel<T, D, SHARE, BIAS><<<die_grid(per_head * a.H), 64 * kWaves, table, s>>>(a);
     return hipGetLastError();
 }
 template <typename T, int D, int SHARE, bool BIAS>
@@ -885,7 +885,7 @@ static hipError_t launch_dkv(const AttnArgs& a, hipStream_t s) {
     constexpr int kWaves = bwd_waves<T, D, SHARE>();
     const size_t table = BIAS ? (size_t)(SHARE == 4 ? 1 : a.pack) * (2 * a.far + 1 + 2 * kTabMargin) * 4 : 0;
     const uint64_t per_head = SHARE == 4 ? (uint64_t)a.V : ((uint64_t)a.V + kWaves - 1) / kWaves;
-    attn_dkv_kernel<T, D, SHARE, BIAS><<<(unsigned)((per_head * a.kv * a.splits + 7) / 8 * 8), 64 * kWaves, table, s>>>(a);
+    attn_dkv_kernel<T, D, SHARE, BIAS><<<die_grid(per_head * a.kv * a.splits), 64 * kWaves, table, s>>>(a);
     return hipGetLastError();
 }
 template <typename T, int D>
