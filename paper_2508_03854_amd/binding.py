@@ -1,6 +1,7 @@
 """Thin ctypes binding of libtbe355.so: same names as the C ABI, argument marshalling only.
 
-torch is used for device memory and streams.  There is no fallback: if the HIP library is missing or a
+torch is used for device memory and streams: with stream=, results that are not given are allocated on that stream, and whoever uses them
+on another one waits for it, as for any work there.  There is no fallback: if the HIP library is missing or a
 call fails, an exception is raised."""
 from __future__ import annotations
 
@@ -226,6 +227,14 @@ def _stream_ptr(stream: Optional[torch.cuda.Stream]) -> int:
     return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
+def _empty(shape, dtype: torch.dtype, device, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
+    """A result's tensor, allocated on the stream that writes it: its memory may still be in use by earlier work there, and by that alone."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 class TBE:
     """One table set (tbe_handle).  Methods mirror the C entry points one to one."""
 
@@ -272,7 +281,7 @@ class TBE:
                 out: Optional[torch.Tensor] = None, D_offsets: Optional[torch.Tensor] = None,
                 stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
         if out is None:
-            out = torch.empty(B, self.sum_D, dtype=torch.float32, device=tables.device)
+            out = _empty((B, self.sum_D), torch.float32, tables.device, stream)
         if tables.numel() != self.total_elems or out.shape != (B, self.sum_D):
             raise ValueError("tables / out shape does not match the handle")
         if offsets.numel() != self.T * B + 1:
@@ -292,7 +301,7 @@ class TBE:
                    D_offsets: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
         """int64 or int32 indices/offsets (both the same); float32, float16 or bfloat16 out."""
         if out is None:
-            out = torch.empty(B, self.sum_D, dtype=out_dtype, device=tables.device)
+            out = _empty((B, self.sum_D), out_dtype, tables.device, stream)
         if out.dtype not in _IO:
             raise TypeError(f"out must be float32, float16 or bfloat16, got {out.dtype}")
         if tables.numel() != self.total_elems or out.shape != (B, self.sum_D):
@@ -502,11 +511,11 @@ class TBE:
         params = weight if weight is not None else bias
         if weight is not None and bias is not None and weight.dtype != bias.dtype:
             raise TypeError(f"weight and bias must be of one type, got {weight.dtype} / {bias.dtype}")
-        out = torch.empty(rows, cols, dtype=x.dtype, device=x.device) if out is None else out
+        out = _empty((rows, cols), x.dtype, x.device, stream) if out is None else out
         if stats and mean is None:
-            mean = torch.empty(rows, dtype=torch.float32, device=x.device)
+            mean = _empty(rows, torch.float32, x.device, stream)
         if stats and rstd is None:
-            rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
+            rstd = _empty(rows, torch.float32, x.device, stream)
         st = self._lib.tbe_layer_norm(self._h, _rows_ptr(x, None, "x"), x.stride(0), _IO[x.dtype], rows, cols,
                                       _param_ptr(weight, cols, None, "weight"), _param_ptr(bias, cols, None, "bias"),
                                       IO_F32 if params is None else _IO[params.dtype], float(eps), _rows_ptr(out, x, "out"), out.stride(0),
@@ -539,11 +548,11 @@ class TBE:
         pt = given[0] if given else (param_dtype or torch.float32)
         if pt not in _IO or any(t != pt for t in given) or (param_dtype or pt) != pt:
             raise TypeError(f"weight and its gradients must be of one type, got {given}")
-        grad_x = torch.empty(rows, cols, dtype=x.dtype, device=x.device) if grad_x is None else grad_x
+        grad_x = _empty((rows, cols), x.dtype, x.device, stream) if grad_x is None else grad_x
         if params and grad_weight is None:
-            grad_weight = torch.empty(cols, dtype=pt, device=x.device)
+            grad_weight = _empty(cols, pt, x.device, stream)
         if params and grad_bias is None:
-            grad_bias = torch.empty(cols, dtype=pt, device=x.device)
+            grad_bias = _empty(cols, pt, x.device, stream)
         st = self._lib.tbe_layer_norm_backward(
             self._h, _rows_ptr(grad_out, x, "grad_out"), grad_out.stride(0), _rows_ptr(x, None, "x"), x.stride(0), _IO[x.dtype], rows, cols,
             _param_ptr(weight, cols, None, "weight"), _IO[pt], _param_ptr(mean, rows, torch.float32, "mean"),
@@ -612,9 +621,9 @@ class TBE:
         unless given; bias: [heads, buckets], bucket_map: int32 [2 * max_distance + 1].  Returns (out, lse), lse float32
         [heads, q_rows]; stats=False: no lse unless it is given."""
         a = self._attention_args(q, k, v, q_offsets, k_offsets, k_lengths, causal, scale, bias, bucket_map)
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
+        out = _empty(q.shape, q.dtype, q.device, stream) if out is None else out
         if stats and lse is None:
-            lse = torch.empty(q.shape[1], q.shape[0], dtype=torch.float32, device=q.device)
+            lse = _empty((q.shape[1], q.shape[0]), torch.float32, q.device, stream)
         st = self._lib.tbe_attention(self._h, a, _heads(out, q, "out"),
                                      _param_ptr(lse, q.shape[0] * q.shape[1], torch.float32, "lse"),
                                      _dev_ptr(workspace, torch.uint8, "workspace"), 0 if workspace is None else int(workspace.numel()),
@@ -633,13 +642,13 @@ class TBE:
                            ) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor, Optional[torch.Tensor]]:
         """Arguments as of attention(), its out and lse, and the upstream gradient.  Returns (grad_q, grad_k, grad_v, grad_bias)."""
         a = self._attention_args(q, k, v, q_offsets, k_offsets, k_lengths, causal, scale, bias, bucket_map)
-        grad_q = torch.empty(q.shape, dtype=q.dtype, device=q.device) if grad_q is None else grad_q
-        grad_k = torch.empty(k.shape, dtype=q.dtype, device=q.device) if grad_k is None else grad_k
-        grad_v = torch.empty(v.shape, dtype=q.dtype, device=q.device) if grad_v is None else grad_v
+        grad_q = _empty(q.shape, q.dtype, q.device, stream) if grad_q is None else grad_q
+        grad_k = _empty(k.shape, q.dtype, q.device, stream) if grad_k is None else grad_k
+        grad_v = _empty(v.shape, q.dtype, q.device, stream) if grad_v is None else grad_v
         if bias is None and grad_bias is not None:
             raise ValueError("grad_bias without bias")
         if bias is not None and grad_bias is None:
-            grad_bias = torch.empty_like(bias)
+            grad_bias = _empty(bias.shape, bias.dtype, bias.device, stream)
         st = self._lib.tbe_attention_backward(
             self._h, a, _heads(out, q, "out"), _param_ptr(lse, q.shape[0] * q.shape[1], torch.float32, "lse"),
             _heads(grad_out, q, "grad_out"), _heads(grad_q, q, "grad_q"), _heads(grad_k, k, "grad_k"), _heads(grad_v, v, "grad_v"),
