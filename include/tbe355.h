@@ -324,7 +324,7 @@ tbe_status tbe_layer_norm_backward(const tbe_handle* h, const void* dy, int64_t 
  * Rows of dk and dv that no query saw, or that are a cache's room, become zero.
  *   q, k, v, out and gradients   DEVICE, [rows][heads or kv_heads][head_dim] of dtype: consecutive rows row_stride, consecutive heads
  *             head_stride elements apart, so that they may be column blocks of one matrix.  16-byte aligned, strides multiples of 16
- *             bytes, 0 <= row_stride < 2^22 (a result's at least head_dim); head_dim <= 128, a multiple of 8 (4 for TBE_IO_F32).  Results
+ *             bytes, 0 <= row_stride < 2^22 (a result's strides at least head_dim); head_dim <= 128, a multiple of 8 (4 for TBE_IO_F32).  Results
  *             share no byte with each other or with what is read
  *   q_offsets, k_offsets   DEVICE, sequences + 1 of index_dtype, ascending from 0 to q_rows resp. k_rows;  k_lengths  DEVICE,
  *             `sequences` of the same type, or NULL.  A sequence whose numbers do not fit, and with

@@ -84,12 +84,12 @@ static AttnShape attention_shape(const tbe_attention_args* a) {
     return sh;
 }
 // the kernels' view of a matrix; false: not as it has to be
-static bool rows_view(const tbe_rows& m, const int64_t rows, const tbe_attention_args* a, const bool result, RowsView& v) {
+static bool rows_view(const tbe_rows& m, const int64_t rows, const int32_t heads, const tbe_attention_args* a, const bool result, RowsView& v) {
     const int64_t e = (int64_t)io_size(a->dtype);
     if (!m.data && rows > 0) return false;
     if (!multiple_of(m.data, 16) || m.row_stride < 0 || m.row_stride >= 1 << 22 || m.row_stride * e % 16 != 0) return false;
     if (m.head_stride < 0 || m.head_stride >= (int64_t)1 << 40 || m.head_stride * e % 16 != 0) return false;
-    if (result && rows > 1 && m.row_stride < a->head_dim) return false;
+    if (result && ((rows > 1 && m.row_stride < a->head_dim) || (rows > 0 && heads > 1 && m.head_stride < a->head_dim))) return false;   // (two writers of one element)
     v.p = static_cast<const char*>(m.data); v.row = m.row_stride * e; v.head = m.head_stride * e;
     return true;
 }
@@ -103,7 +103,8 @@ static tbe_status attention_args(const tbe_handle* h, const tbe_attention_args* 
     if (!a->q_offsets || !a->k_offsets || !multiple_of(a->q_offsets, ia) || !multiple_of(a->k_offsets, ia) || !multiple_of(a->k_lengths, ia)) return TBE_EINVAL;
     if (!isfinite(a->scale)) return TBE_EINVAL;
     k = AttnArgs{};
-    if (!rows_view(a->q, a->q_rows, a, false, k.q) || !rows_view(a->k, a->k_rows, a, false, k.k) || !rows_view(a->v, a->k_rows, a, false, k.v)) return TBE_EINVAL;
+    if (!rows_view(a->q, a->q_rows, a->heads, a, false, k.q) || !rows_view(a->k, a->k_rows, a->kv_heads, a, false, k.k) ||
+        !rows_view(a->v, a->k_rows, a->kv_heads, a, false, k.v)) return TBE_EINVAL;
     const int is32 = a->index_dtype == TBE_I32;
     k.q_off = IdxView{a->q_offsets, is32}; k.k_off = IdxView{a->k_offsets, is32}; k.k_len = IdxView{a->k_lengths, is32};
     k.N = a->sequences; k.H = a->heads; k.kv = a->kv_heads; k.group = a->heads / a->kv_heads; k.dim = a->head_dim; k.causal = a->causal != 0;
@@ -135,7 +136,7 @@ tbe_status tbe_attention(const tbe_handle* h, const tbe_attention_args* args, tb
     AttnArgs k;
     const tbe_status st = attention_args(h, args, k);
     if (st != TBE_OK) return st;
-    if (!rows_view(out, args->q_rows, args, true, k.o) || !multiple_of(lse, 4)) return TBE_EINVAL;
+    if (!rows_view(out, args->q_rows, args->heads, args, true, k.o) || !multiple_of(lse, 4)) return TBE_EINVAL;
     k.lse = lse;
     const AttnShape sh = attention_shape(args);
     const AttnPlan p = attn_plan(sh);
@@ -155,8 +156,9 @@ tbe_status tbe_attention_backward(const tbe_handle* h, const tbe_attention_args*
     AttnArgs k;
     const tbe_status st = attention_args(h, args, k);
     if (st != TBE_OK) return st;
-    if (!rows_view(out, args->q_rows, args, false, k.o) || !rows_view(dout, args->q_rows, args, false, k.dout)) return TBE_EINVAL;
-    if (!rows_view(dq, args->q_rows, args, true, k.dq) || !rows_view(dk, args->k_rows, args, true, k.dk) || !rows_view(dv, args->k_rows, args, true, k.dv)) return TBE_EINVAL;
+    if (!rows_view(out, args->q_rows, args->heads, args, false, k.o) || !rows_view(dout, args->q_rows, args->heads, args, false, k.dout)) return TBE_EINVAL;
+    if (!rows_view(dq, args->q_rows, args->heads, args, true, k.dq) || !rows_view(dk, args->k_rows, args->kv_heads, args, true, k.dk) ||
+        !rows_view(dv, args->k_rows, args->kv_heads, args, true, k.dv)) return TBE_EINVAL;
     if ((!lse && args->q_rows > 0) || !multiple_of(lse, 4)) return TBE_EINVAL;
     if (dbias && (!args->bias || !multiple_of(dbias, io_size(args->bias_dtype)))) return TBE_EINVAL;
     k.lse = const_cast<float*>(lse);
