@@ -142,3 +142,14 @@ def test_sequences_that_share_wavefronts_in_one_kernel(tbe):
             p = problem(n, n, 8, 8, D, TYPES[io], buckets=buckets, far=6, causal=causal)
             agree(tbe, p, 67, 4, f"{io} {D} {buckets}", 3)
             agree(tbe, p, 70, 40, f"{io} {D} {buckets} 70", 3)
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+def test_beside_scores_at_a_low_value(tbe, io):
+    """Rows that find their maxima and sums again meet values that are not finite on the way."""
+    for n, H, K, s, row, head in (([40, 100, 33], 2, 1, 1, 60, 1), ([500, 130, 330], 2, 1, 0, 301, 1), ([7, 9, 20, 5, 70, 3] * 75, 8, 8, 67, 4, 3)):
+        for causal in (True, False):
+            p = problem(n, n, H, K, 32, TYPES[io], buckets=4, far=10, causal=causal)
+            p["q"] *= 2.0 ** -24
+            p["bias"][:] = -1e9
+            agree(tbe, p, s, row, f"{n[:3]} {causal}", head)
