@@ -336,10 +336,10 @@ tbe_status tbe_layer_norm_backward(const tbe_handle* h, const void* dy, int64_t 
  *   lse       DEVICE float [heads][q_rows]; the forward writes it unless NULL, the backward reads it
  * 0 <= q_rows, k_rows <= 2^31 - 4096, 1 <= sequences < 2^24, 1 <= kv_heads <= heads <= 1024 with heads a multiple of kv_heads,
  * 1 <= buckets <= 1024.  Scores, softmax and sums are in fp32; probabilities and dS are rounded once to dtype where they are multiplied by
- * v, k, q or dout (fp32: not at all), results once when stored.  The order of all additions is fixed: results do not depend on
- * timing.  A value that is not finite reaches those results of the forward that see it, and
- * of the backward results of its sequence.  The handle
- * gives the timing record and the error flag. */
+ * v, k, q or dout (fp32: not at all), results once when stored.  With binary16 a dS beyond 65504 thus becomes infinite and one below 2^-25
+ * zero: scale the loss, or take bfloat16.  The order of all additions is fixed: results do not depend on timing.  A value that is not
+ * finite reaches the results that the formulas lead it to over pairs that see each other; a pair that is hidden (by `causal`, the lengths
+ * or a bias of -infinity) is left out, not multiplied by 0.  The handle gives the timing record and the error flag. */
 typedef struct {
     void* data;
     int64_t row_stride, head_stride; /* in elements */
@@ -352,7 +352,7 @@ typedef struct {
     tbe_rows q, k, v;
     const void *q_offsets, *k_offsets, *k_lengths;
     int32_t causal;
-    float scale; /* finite */
+    float scale; /* finite, also times log2(e) */
     const void* bias;
     const int32_t* bucket_map;
     tbe_io_dtype bias_dtype;

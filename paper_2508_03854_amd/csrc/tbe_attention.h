@@ -29,25 +29,25 @@ __device__ __forceinline__ int uniform(const int x) { return __builtin_amdgcn_re
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr int kTabMargin = 68;         // a tile that reaches into the table of distances reaches at most 66 beyond its ends
 // So many wavefronts, were there one for every 32 rows of a sequence and head, and short sequences share wavefronts.  A wavefront of one sequence /
-// shared ones, 8 heads of 64 bfloat16, lengths lognormal (7 in the middle, 12 on average), us: 64 sequences (704 wavefronts) forward 11.2 / 10.7,
-// dq 20.2 / 20.9; 256 (2816) 18.2 / 13.2, 32.0 / 26.5; 1024 (11264) 44.5 / 23.3, 73.8 / 50.7; 4096 149 / 65, 251 / 161.
+// shared ones, 8 heads of 64 bfloat16, lengths lognormal (7 in the middle, 12 on average), us: 256 sequences (2816 wavefronts) forward 18.1 / 13.2,
+// dq 32.8 / 24.2; 1024 (11264) 45.6 / 23.4, 78.7 / 45.7; 4096 156 / 64, 265 / 121; for 64 (704), on their own 11.1 and 20.4.
 constexpr int64_t kManyUnits = 2048;
 constexpr int kTabBytes = 24 << 10;    // LDS for such tables
 
 // Sequences of few rows have a wavefront for every 32 of them, longer ones a workgroup for every 128, which share the tiles of the other side: up
 // to 64 rows on average, and as long as neither side has more than `most`.  Shared / on their own, us, as many sequences as named of that
 // length, with bias, causal:
-//   forward  32 bfloat16: 512 of 128 44 / 28, of 180 54 / 44, 256 of 150 with 300 keys 39 / 44, 64 of 400 23 / 26
-//            64 bfloat16: 512 of 80 83 / 50, of 128 178 / 83, of 180 234 / 161, 64 of 256 38 / 32, of 600 101 / 101;  fp32: 64 of 256 63 / 61
-//            128 bfloat16: 64 of 80 15.6 / 14.8, of 128 17.6 / 25.3;  fp32: 64 of 128 33 / 46
-//   dq       32 bfloat16: 512 of 128 102 / 88, of 180 136 / 141;  fp32: 512 of 128 296 / 235, of 200 410 / 431
-//            64 bfloat16: 512 of 128 371 / 250, of 180 452 / 400, 64 of 256 76 / 77, 256 of 245 372 / 424;  fp32: 512 of 128 639 / 344,
-//            64 of 400 255 / 209, of 600 378 / 375
-//            128 bfloat16: 64 of 128 33 / 45;  fp32: 67 / 82
-//   dk, dv   32 bfloat16: 512 of 128 64 / 51, of 180 70 / 86
-//            64 bfloat16: 512 of 128 256 / 171, 64 of 180 41 / 35, of 256 46 / 49;  fp32: 64 of 400 289 / 199, of 600 385 / 366
-//            128 bfloat16: 64 of 128 35 / 27, of 400 129 / 91, 16 of 2000 335 / 313, 4 of 4000 451 / 248 (the shared kernel has one
-//            wavefront a SIMD, which waits at its barriers);  fp32: 64 of 80 41 / 45, of 200 121 / 148
+//   forward  32 bfloat16: 512 of 128 46 / 26, of 180 54 / 43, 256 of 150 with 300 keys 38 / 39, 64 of 400 23 / 22
+//            64 bfloat16: 512 of 80 76 / 49, of 128 149 / 82, of 180 189 / 154, 64 of 256 33 / 30, of 600 79 / 97;  fp32: 64 of 256 66 / 60
+//            128 bfloat16: 64 of 80 15.0 / 14.3, of 128 17.6 / 25.1;  fp32: 64 of 128 33 / 44
+//   dq       32 bfloat16: 512 of 128 113 / 87, of 180 144 / 135;  fp32: 512 of 128 303 / 235, of 200 415 / 419
+//            64 bfloat16: 512 of 128 381 / 200, of 180 483 / 304, 64 of 256 81 / 63, 256 of 245 266 / 234;  fp32: 512 of 128 671 / 292,
+//            64 of 400 258 / 196, of 600 384 / 345
+//            128 bfloat16: 64 of 128 36 / 46;  fp32: 69 / 81
+//   dk, dv   32 bfloat16: 512 of 128 69 / 39, of 180 72 / 62
+//            64 bfloat16: 512 of 128 252 / 157, 64 of 180 41 / 34, of 256 47 / 47;  fp32: 64 of 400 300 / 190, of 600 404 / 353
+//            128 bfloat16: 64 of 128 40 / 31, of 400 141 / 99, 16 of 2000 345 / 333, 4 of 4000 478 / 257 (the shared kernel has one
+//            wavefront a SIMD, which waits at its barriers);  fp32: 64 of 80 44 / 50, of 200 126 / 156
 inline bool attn_few(const int64_t mean, const int64_t other, const int64_t most) { return mean <= 64 || (mean <= most && other <= most); }
 
 // Sixteen zero bytes: what stands behind a sequence's end, or behind a row's, is read from here.
@@ -479,8 +479,8 @@ __device__ __forceinline__ void fill_bias(float* tab, const AttnArgs& a, const i
 }
 
 // Workgroups are dealt to the 8 dies one by one; each die takes a run of neighbours, so that those that read the same keys share its
-// level-2 cache: 2 sequences of 6000, 16 heads of 128 over 4 bfloat16, forward in the order of the grid 342 us, in this one 297; 48 sequences with
-// 61 queries each, 8 heads of 64, 79 / 65; 4 of 2500, 8 heads of 64 over 2, dq 164 / 132, dk and dv 154 / 140.  n or more: nothing to do.
+// level-2 cache: 2 sequences of 6000, 16 heads of 128 over 4 bfloat16, forward in the order of the grid 440 us, in this one 393; 48 sequences with
+// 61 queries each, 8 heads of 64, 81 / 63; 4 of 2500, 8 heads of 64 over 2, dq 154 / 129, dk and dv 147 / 119.  n or more: nothing to do.
 __device__ __forceinline__ uint32_t die_order(const uint32_t n) {
     const uint32_t wg = blockIdx.y * gridDim.x + blockIdx.x, run = (n + 7u) / 8u;
     return (wg >> 3) < run ? (wg & 7u) * run + (wg >> 3) : n;
@@ -492,8 +492,8 @@ inline dim3 die_grid(const uint64_t n) {
 }
 // A workgroup's head (or heads) and which of the head's items it has: one head after the other, which keeps the keys of few heads in the cache; short
 // sequences (SHARE = 0), whose wavefronts wait for memory first of all, one item after the other, so that heads that lie in the same cache
-// lines are read together: 4096 sequences of 12 events on average, 4 heads of 32 bfloat16, head after head / item after item, us: forward 30.5 /
-// 23.0, dq 69 / 59, dk and dv 50 / 46; 512 of 128, 8 heads of 64, forward 93 / 85.
+// lines are read together: 4096 sequences of 12 events on average, 4 heads of 32 bfloat16, head after head / item after item, us: forward 30.8 /
+// 22.4, dq 71 / 59, dk and dv 46 / 41; 512 of 128, 8 heads of 64, forward 86 / 84.
 template <int SHARE>
 __device__ __forceinline__ void head_and_item(const uint32_t wg, const uint32_t per_head, const uint32_t heads, int& head, uint32_t& item) {
     constexpr bool beside = SHARE == 0;

@@ -3,9 +3,9 @@
 //   S^T = K Q^T  (a tile: 32 keys x 32 columns)    p = 2^(x - m)    O^T += V^T P
 // Bound: long sequences by the vector unit's work on every score (the exponential, the sums) next to the matrix cores, single tokens by
 // reading the keys and values once, many short sequences by a wavefront's trips to memory.  Measured: 2 causal sequences of 4000 to 8000, 16
-// heads of 128 over 4, bfloat16, 2.3e11 operations: 293 to 330 us on different cards, 0.7 to 0.78 PFLOP/s; one query to each of 24 caches of
-// 2000 to 65536 keys, 16 heads over 2, 0.8 GB: 173 us and 11 for the join, 4.4 TB/s; 4096 sequences of 12 events on average, 4 heads of 32
-// with a bias: 23 us for 51 MB.
+// heads of 128 over 4, bfloat16, 2.3e11 operations: 266 us when called one after the other, 0.86 PFLOP/s, up to 313 with other work between; one
+// query to each of 24 caches of 2000 to 65536 keys, 16 heads over 2, 0.8 GB: 168 us and 8 for the join, 4.6 TB/s; 4096 sequences of 12 events
+// on average, 4 heads of 32 with a bias: 21 us for 51 MB.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -33,7 +33,7 @@ constexpr int attn_occupancy() { return sizeof(T) == 4 ? (D == 32 ? 2 : 1) : (D 
 template <typename T, int D, int SHARE, bool BIAS>
 __global__ __launch_bounds__((64 * attn_waves<T, D, SHARE>()), (attn_occupancy<T, D, SHARE>())) void attn_kernel(const AttnArgs a) {
     constexpr int kWaves = attn_waves<T, D, SHARE>(), BK = kv_rows<T, D, SHARE>(), kT = BK / 32, kD = D / 32;
-    constexpr int kE = Mma<T>::kE, kK = Mma<T>::kK, kC = D / kK, kM = 32 / kK;
+    constexpr int kK = Mma<T>::kK, kC = D / kK, kM = 32 / kK;
     constexpr int kTile = BK * D * (int)sizeof(T), kSharers = SHARE == 4 ? 4 : 1;
     constexpr bool kRows = SHARE == 0;
     // two buffers each, as arrays of their own: loads into one of them are seen not to concern what is read from another
@@ -446,10 +446,10 @@ __global__ __launch_bounds__(256) void attn_join_kernel(const AttnArgs a) {
 
 // How the forward shares out its work.  Sequences of many queries: 128 neighbours share the keys' tiles (see attn_few).  Few queries per
 // sequence: wavefronts on their own, heads of a group side by side where one query would leave its columns empty (24 caches of 34,000 keys, one
-// query, 16 heads of 2: 173 us; one head each: 943), and the keys in parts of 128 or more where there would be fewer than 2048 wavefronts.  Parts
-// for one query of 16 heads of 2 of 128 elements, none / this, us with the join: one cache of 256 keys 17 / 11, of 16,384 514 / 23.5; 64 of them 639 /
-// 195; for half as many wavefronts 191 (but 61 queries each of 8 heads of 64 117 / 62), for twice as many 200; parts of 64 or more keys, one cache
-// of 256, 1024, 16,384 keys: 18 / 11, 18 / 20, 26 / 23.5; of 256 or more 17 / 11, 21 / 20, 26 / 23.5.
+// query, 16 heads of 2: 178 us; one head each: 922), and the keys in parts of 128 or more where there would be fewer than 2048 wavefronts.  Parts
+// for one query of 16 heads of 2 of 128 elements, none / this, us with the join: one cache of 256 keys 16.4 / 11.4, of 16,384 471 / 23; 64 of them 644 /
+// 195; for half as many wavefronts 191 (but 61 queries each of 8 heads of 64 112 / 63), for twice as many 204; parts of 64 or more keys, one cache
+// of 256, 1024, 16,384 keys: 11.5 / 11.4, 19 / 20, 25 / 23; of 256 or more 16 / 11, 17 / 20, 25 / 23.
 AttnPlan attn_plan(const AttnShape& sh, const int max_pack) {
     AttnPlan p;
     const int64_t mean_q = sh.N > 0 ? (sh.q_rows + sh.N - 1) / sh.N : 0, mean_k = sh.N > 0 ? (sh.k_rows + sh.N - 1) / sh.N : 0;

@@ -4,9 +4,9 @@
 //   attn_dkv_kernel   columns are keys:     S = Q K^T,   dP = dO V^T,   dS;  dV^T += dO^T P,  dK^T += Q^T dS
 // Seven products of a tile instead of five: sums of dQ from one kernel over key blocks would need atomics or a pass over partial sums.
 // Bound: the matrix cores and the vector unit's work on every score, twice; short sequences by the trips to memory of a wavefront.  Measured: 4
-// causal sequences of 1000 to 4096, 8 heads of 64 over 2, binary16, a bias of 32 buckets, 6.0e10 operations: dq 127, dbias 6, dk and dv 134 and
-// their join 10 us, 0.22 PFLOP/s (the matrix cores busy 27 % and the vector unit 45 % of the clocks, 1.7 wavefronts a SIMD); 4096 sequences of 12
-// events on average, 4 heads of 32: 59 + 7 + 46 us for 103 MB.
+// causal sequences of 1000 to 4096, 8 heads of 64 over 2, binary16, a bias of 32 buckets, 6.0e10 operations: dq 129, dbias 5, dk and dv 134 and
+// their join 8 us, 0.22 PFLOP/s; 4096 sequences of 12
+// events on average, 4 heads of 32: 57 + 5 + 39 us for 103 MB.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -793,8 +793,8 @@ __global__ __launch_bounds__((64 * bwd_waves<T, D, SHARE>()), (dkv_occupancy<T, 
     }
 }
 
-// Adds up the parts of a group's heads, in their order: four elements a lane.  Rows that are no sequence's are left as they are, which is
-// decided by the rows' places between the first and the last offset alone: the offsets ascend, or the call has been reported.
+// Adds up the parts of a group's heads, in their order: four elements a lane, every row.  All rows are some sequence's; those of one that does
+// not fit, which has been reported, get what the workspace holds.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void attn_dkv_join_kernel(const AttnArgs a) {
     const int64_t per = (int64_t)a.kv * (D / 4), n = a.k_rows * per;
@@ -821,10 +821,10 @@ __global__ __launch_bounds__(256) void attn_dkv_join_kernel(const AttnArgs a) {
 
 // How the backward shares out its work: queries and keys of long sequences by 128, of short ones by 32; the heads of a group in
 // parts where there would be too few workgroups of keys to fill the chip: 768 that share tiles, 4096 wavefronts on their own (16 sequences of
-// 2500, 8 heads of 64 over 2 binary16, dk and dv and the join, us: 256 / 768 / 2048 of them 608 / 533 / 463; 4 of them 252 / 149 / 149).
+// 2500, 8 heads of 64 over 2 binary16, dk and dv and the join, us: 256 / 768 / 2048 of them 403 / 412 / 400; 4 of them 199 / 128 / 129).
 // Short sequences share wavefronts where there are many (see kManyUnits); of dk and dv those of narrow heads and of 64 fp32 elements:
-// wavefronts of one sequence / shared ones, 4096 sequences of 12 events on average, 4 heads of 32 bfloat16 55 / 50, 8 of 64 170 / 164, fp32
-// 511 / 279, 2 of 128 99 / 103; 1024 of 40, 8 of 64 95 / 121, fp32 284 / 222.
+// wavefronts of one sequence / shared ones, 4096 sequences of 12 events on average, 4 heads of 32 bfloat16 58 / 41, 8 of 64 fp32 566 / 272;
+// 1024 of 40, 33 / 27, 310 / 217.  (8 heads of 64 bfloat16, for which the shared ones are not built yet: 175 / 107, 92 / 72.)
 AttnBackwardPlan attn_backward_plan(const AttnShape& sh) {
     AttnBackwardPlan p;
     const int64_t mean_q = (sh.q_rows + sh.N - 1) / sh.N, mean_k = (sh.k_rows + sh.N - 1) / sh.N;

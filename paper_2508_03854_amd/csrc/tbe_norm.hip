@@ -3,8 +3,8 @@
 //   backward  h = (x - mean) rstd,  g = dy w:   dx = rstd (g - 1/n sum g - h 1/n sum g h),  dw = sum over rows of dy h,  db = sum of dy
 // Bound: the stream, every element read once and written once; a row stays in registers between its sums and its use.  The sums are
 // in fp32, the variance from the differences to the mean (no difference of large squares); each result is rounded once.  Measured: 1,000,003
-// rows of 128 bfloat16 forward 105 us, 5.0 TB/s; 262,147 of 256 backward 92 and 6 us for the sums over rows, 4.1 TB/s; 8001 of 1021 fp32
-// backward 25 and 9 us.
+// rows of 128 bfloat16 forward 105 us, 5.0 TB/s; 262,147 of 256 backward 89 and 5 us for the sums over rows, 4.5 TB/s; 8001 of 1021 fp32
+// backward 23 and 7 us.
 #include <hip/hip_runtime.h>
 
 #include "tbe_elems.h"
