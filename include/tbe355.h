@@ -369,6 +369,59 @@ tbe_status tbe_attention_backward(const tbe_handle* h, const tbe_attention_args*
                                   tbe_rows dq, tbe_rows dk, tbe_rows dv, void* dbias, void* workspace, size_t workspace_bytes,
                                   void* hip_stream);
 
+/* Heads of queries and keys normed and rotated by their rows' positions, before attention (what gives attention its distances where it has no bias
+ * by distance; the paper leaves it open).  For every row and head of q, and of k, with n = head_dim:
+ *   z_e = x_e w_e / sqrt(1/n sum_i x_i^2 + eps) with `norm`, otherwise z = x;
+ *   y = z, but for the first rotary_dim elements, which are turned in pairs (a, b) = (j, j + rotary_dim / 2), or (2 j, 2 j + 1) with `interleaved`,
+ *   j < rotary_dim / 2, by t_j = positions[row] * frequencies[j] radians:
+ *   y_a = amplitude (z_a cos t_j - z_b sin t_j),  y_b = amplitude (z_b cos t_j + z_a sin t_j).
+ * Gradients: dz is dy turned back (by -t_j, times amplitude); dx = dz without `norm`, otherwise with r = 1 / sqrt(1/n sum x^2 + eps), h = x r,
+ * u = dz w:  dx_e = r (u_e - h_e 1/n sum_i u_i h_i),  dw_e = sum over the rows and heads of dz_e h_e (of q for q's weight, of k for k's).
+ *   q, k, results and gradients   DEVICE, [rows][q_heads or k_heads][head_dim] of dtype: consecutive rows row_stride, consecutive heads head_stride
+ *             elements apart (0 <= strides < 2^40), at any address that is a multiple of the element's size.  A result may be the matrix it is made from, with
+ *             equal strides; otherwise results share no byte with each other or with what is read, and neither do their rows and heads
+ *   positions   DEVICE, [rows] of index_dtype, any numbers
+ *   frequencies DEVICE, [rotary_dim / 2], radians a position, in 64 bits: angles of far positions keep their fraction.  tbe_rotary_frequencies
+ *             makes the customary ones.  May be NULL where rotary_dim is 0 (norm alone)
+ *   q_weight, k_weight   DEVICE, [head_dim] of weight_dtype, or NULL: 1 (without `norm`: not read)
+ * 0 <= rows < 2^31, 0 <= q_heads, k_heads <= 1024 and not both 0 (that matrix is then not read or written), 1 <= head_dim <= 256, rotary_dim even,
+ * 0 <= rotary_dim <= head_dim; eps finite and >= 0, amplitude finite.  Arithmetic is in fp32, angles in 64 bits; each result is rounded once; the
+ * order of all additions is fixed.  Squares beyond fp32's range make a head's norm infinite, and the head 0.  The handle gives the timing record. */
+typedef struct {
+    int32_t q_heads, k_heads, head_dim, rotary_dim;
+    int64_t rows;
+    tbe_io_dtype dtype;
+    tbe_index_dtype index_dtype;
+    const void* positions;
+    const double* frequencies;
+    int32_t interleaved;
+    float amplitude;
+    int32_t norm;
+    float eps;
+    const void *q_weight, *k_weight;
+    tbe_io_dtype weight_dtype;
+} tbe_rotation_args;
+tbe_status tbe_rotate_heads(const tbe_handle* h, const tbe_rotation_args* args, tbe_rows q, tbe_rows k, tbe_rows q_out, tbe_rows k_out,
+                            void* hip_stream);
+/* Workspace for calls with these sizes (no pointer is read).  Only weights' gradients need one. */
+tbe_status tbe_rotate_workspace_bytes(const tbe_handle* h, const tbe_rotation_args* args, size_t* bytes);
+/* q and k, the forward's, are read with `norm` only.  dq_weight, dk_weight: of weight_dtype, each may be NULL; both without `norm`. */
+tbe_status tbe_rotate_heads_backward(const tbe_handle* h, const tbe_rotation_args* args, tbe_rows dq_out, tbe_rows dk_out, tbe_rows q,
+                                     tbe_rows k, tbe_rows dq, tbe_rows dk, void* dq_weight, void* dk_weight, void* workspace,
+                                     size_t workspace_bytes, void* hip_stream);
+
+/* The customary frequencies, f_j = base^(-2 j / rotary_dim), and three ways to make them serve contexts `factor` times as long:
+ *   TBE_ROTARY_LINEAR  f_j / factor (positions are pressed together);
+ *   TBE_ROTARY_BASE    base grows by factor^(rotary_dim / (rotary_dim - 2)): the slowest pair turns `factor` times more slowly, the fastest as before
+ *                      (rotary_dim >= 4);
+ *   TBE_ROTARY_TURNS   by how often a pair turns in the `context` positions it was made for, n_j = context f_j / 2 pi: f_j / factor up to low_turns, f_j from
+ *                      high_turns on, a line in n_j between them.  (Goes with an amplitude of 0.1 log(factor) + 1.)
+ * frequencies: HOST, [rotary_dim / 2].  rotary_dim even, 2 .. 256; base > 1, factor >= 1, context > 0, 0 <= low_turns < high_turns, all finite; those that
+ * a way does not use are not looked at. */
+typedef enum { TBE_ROTARY_PLAIN = 0, TBE_ROTARY_LINEAR = 1, TBE_ROTARY_BASE = 2, TBE_ROTARY_TURNS = 3 } tbe_rotary_scaling;
+tbe_status tbe_rotary_frequencies(int32_t rotary_dim, double base, tbe_rotary_scaling scaling, double factor, double context, double low_turns,
+                                  double high_turns, double* frequencies);
+
 const char* tbe_status_string(tbe_status s);
 
 /* "tbe355 gfx950 <digest>": the digest names the sources and build settings this library was compiled from (twelve

@@ -21,6 +21,7 @@ F32, F16 = 0, 1
 SUM, MEAN = 0, 1
 I64, I32 = 0, 1                       # tbe_index_dtype
 IO_F32, IO_F16, IO_BF16 = 0, 1, 2     # tbe_io_dtype
+ROTARY_SCALING = {"plain": 0, "linear": 1, "base": 2, "turns": 3}   # tbe_rotary_scaling
 FWD_WAVEFRONT_PER_BAG, FWD_LANE_GROUPS, FWD_HOT_ROWS, FWD_LONG_BAGS = 1, 2, 4, 8   # TBE_FWD_*
 TUNABLES = {"hot_rows_min_workgroups": 0}   # tbe_tunable
 TUNE_AUTO = -(1 << 63)                 # TBE_TUNE_AUTO
@@ -33,7 +34,8 @@ EXPORTS = ["tbe_create", "tbe_destroy", "tbe_workspace_bytes", "tbe_forward", "t
            "tbe_backward_apply_rowwise_adagrad", "tbe_backward_apply_sgd", "tbe_backward_sgd", "tbe_replica_mean", "tbe_lookup_seq",
            "tbe_backward_seq_rowwise_adagrad", "tbe_debug_sorted", "tbe_debug_hot_rows", "tbe_debug_forward_kernels", "tbe_poll_index_error", "tbe_set_tunable", "tbe_timing_enable",
            "tbe_timing_count", "tbe_timing_read", "tbe_calibration_copy", "tbe_calibration_gather", "tbe_status_string", "tbe_build_info",
-           "tbe_layer_norm", "tbe_layer_norm_workspace_bytes", "tbe_layer_norm_backward", "tbe_attention_workspace_bytes", "tbe_attention", "tbe_attention_backward"]
+           "tbe_layer_norm", "tbe_layer_norm_workspace_bytes", "tbe_layer_norm_backward", "tbe_attention_workspace_bytes", "tbe_attention", "tbe_attention_backward",
+           "tbe_rotate_heads", "tbe_rotate_workspace_bytes", "tbe_rotate_heads_backward", "tbe_rotary_frequencies"]
 
 
 class TbeError(RuntimeError):
@@ -56,8 +58,17 @@ class AttentionArgs(ctypes.Structure):
                 ("bucket_map", ctypes.c_void_p), ("bias_dtype", ctypes.c_int), ("buckets", ctypes.c_int32), ("max_distance", ctypes.c_int32)]
 
 
+class RotationArgs(ctypes.Structure):
+    """tbe_rotation_args"""
+    _fields_ = [("q_heads", ctypes.c_int32), ("k_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("rotary_dim", ctypes.c_int32),
+                ("rows", ctypes.c_int64), ("dtype", ctypes.c_int), ("index_dtype", ctypes.c_int), ("positions", ctypes.c_void_p),
+                ("frequencies", ctypes.c_void_p), ("interleaved", ctypes.c_int32), ("amplitude", ctypes.c_float), ("norm", ctypes.c_int32),
+                ("eps", ctypes.c_float), ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("weight_dtype", ctypes.c_int)]
+
+
 # The same fields packed in one go: filling the structure field by field takes 6 us of a call that is otherwise over in ten.
 _PACK_ATTENTION = struct.Struct("@4i2q2i" + "Pqq" * 3 + "3Pif2P3i4x").pack
+_PACK_ROTATION = struct.Struct("@4iq2i2Pifif2Pi4x").pack
 
 _lib = None
 
@@ -146,6 +157,15 @@ def load_library():
     L.tbe_attention.argtypes = [vp, vp, Rows, vp, vp, ctypes.c_size_t, vp]
     L.tbe_attention_backward.restype = ctypes.c_int
     L.tbe_attention_backward.argtypes = [vp, vp, Rows, vp, Rows, Rows, Rows, Rows, vp, vp, ctypes.c_size_t, vp]
+    L.tbe_rotate_heads.restype = ctypes.c_int
+    L.tbe_rotate_heads.argtypes = [vp, vp, Rows, Rows, Rows, Rows, vp]
+    L.tbe_rotate_workspace_bytes.restype = ctypes.c_int
+    L.tbe_rotate_workspace_bytes.argtypes = [vp, vp, ctypes.POINTER(ctypes.c_size_t)]
+    L.tbe_rotate_heads_backward.restype = ctypes.c_int
+    L.tbe_rotate_heads_backward.argtypes = [vp, vp, Rows, Rows, Rows, Rows, Rows, Rows, vp, vp, vp, ctypes.c_size_t, vp]
+    f64 = ctypes.c_double
+    L.tbe_rotary_frequencies.restype = ctypes.c_int
+    L.tbe_rotary_frequencies.argtypes = [i32, f64, ctypes.c_int, f64, f64, f64, f64, vp]
     L.tbe_build_info.restype = ctypes.c_char_p
     L.tbe_build_info.argtypes = []
     L.tbe_status_string.restype = ctypes.c_char_p
@@ -233,6 +253,15 @@ def _empty(shape, dtype: torch.dtype, device, stream: Optional[torch.cuda.Stream
         return torch.empty(shape, dtype=dtype, device=device)
     with torch.cuda.stream(stream):
         return torch.empty(shape, dtype=dtype, device=device)
+
+
+def rotary_frequencies(rotary_dim: int, base: float = 10000.0, scaling: str = "plain", factor: float = 1.0, context: float = 0.0,
+                       low_turns: float = 1.0, high_turns: float = 32.0, device="cuda") -> torch.Tensor:
+    """tbe_rotary_frequencies: float64 [rotary_dim / 2] on `device`; scaling: "plain", "linear", "base" or "turns"."""
+    f = torch.empty(max(0, int(rotary_dim)) // 2, dtype=torch.float64)
+    _check(load_library().tbe_rotary_frequencies(int(rotary_dim), float(base), ROTARY_SCALING[scaling], float(factor), float(context),
+                                                 float(low_turns), float(high_turns), f.data_ptr()), "tbe_rotary_frequencies")
+    return f.to(device)
 
 
 class TBE:
@@ -656,6 +685,112 @@ class TBE:
             _dev_ptr(workspace, torch.uint8, "workspace"), 0 if workspace is None else int(workspace.numel()), _stream_ptr(stream))
         _check(st, "tbe_attention_backward")
         return grad_q, grad_k, grad_v, grad_bias
+
+    # ---- tbe_rotate_heads
+    def _rotation_args(self, q, k, like, positions, frequencies, interleaved, amplitude, norm, eps, q_weight, k_weight, weight_dtype) -> bytes:
+        """tbe_rotation_args; q and k (or their gradients) of like's type"""
+        rows, dim = like.shape[0], like.shape[2]
+        if q is not None and k is not None and (k.dim() != 3 or k.dtype != q.dtype or k.shape[0] != rows or k.shape[2] != dim):
+            raise ValueError("q and k must agree in type, rows and head_dim")
+        if positions.dtype not in _IDX:
+            raise TypeError(f"positions must be int64 or int32, got {positions.dtype}")
+        if positions.numel() != rows:
+            raise ValueError(f"positions must have {rows} entries, got {positions.numel()}")
+        turned = 0 if frequencies is None else 2 * frequencies.numel()
+        if not norm and (q_weight is not None or k_weight is not None):
+            raise ValueError("weights without norm")
+        if q_weight is not None and k_weight is not None and q_weight.dtype != k_weight.dtype:
+            raise TypeError(f"q_weight and k_weight must be of one type, got {q_weight.dtype} / {k_weight.dtype}")
+        return _PACK_ROTATION(0 if q is None else q.shape[1], 0 if k is None else k.shape[1], dim, turned, rows, _IO[like.dtype], _IDX[positions.dtype],
+                              _dev_ptr(positions, positions.dtype, "positions"), _dev_ptr(frequencies, torch.float64, "frequencies") or 0,
+                              bool(interleaved), float(amplitude), bool(norm), float(eps), _param_ptr(q_weight, dim, None, "q_weight") or 0,
+                              _param_ptr(k_weight, dim, None, "k_weight") or 0, _IO[weight_dtype])
+
+    @staticmethod
+    def _heads_or_none(t: Optional[torch.Tensor], like: Optional[torch.Tensor], what: str) -> Rows:
+        return Rows() if t is None else _heads(t, like, what)
+
+    def rotate_heads(self, q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions: torch.Tensor, frequencies: Optional[torch.Tensor], *,
+                     interleaved: bool = False, amplitude: float = 1.0, norm: bool = False, eps: float = 1e-6,
+                     q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                     k_out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None
+                     ) -> Tuple[Optional[torch.Tensor], Optional[torch.Tensor]]:
+        """q: [rows, q_heads, head_dim], k: [rows, k_heads, head_dim] (float32, float16 or bfloat16; last axis contiguous, column blocks of one
+        matrix are fine; one of them may be None); positions: [rows], int64 or int32; frequencies: float64 [rotary_dim / 2] (see
+        rotary_frequencies), None: no rotation; weights: [head_dim].  Returns (q_out, k_out); they may be q and k."""
+        like = q if q is not None else k
+        if like is None or like.dim() != 3:
+            raise ValueError("q and k must have three axes: rows, heads, head_dim; one of them may be None")
+        qp, kp = self._heads_or_none(q, None, "q"), self._heads_or_none(k, None, "k")
+        weight = q_weight if q_weight is not None else k_weight
+        a = self._rotation_args(q, k, like, positions, frequencies, interleaved, amplitude, norm, eps, q_weight, k_weight,
+                                torch.float32 if weight is None else weight.dtype)
+        if q is not None and q_out is None:
+            q_out = _empty(q.shape, q.dtype, q.device, stream)
+        if k is not None and k_out is None:
+            k_out = _empty(k.shape, k.dtype, k.device, stream)
+        if (q is None and q_out is not None) or (k is None and k_out is not None):
+            raise ValueError("q_out without q, or k_out without k")
+        st = self._lib.tbe_rotate_heads(self._h, a, qp, kp, self._heads_or_none(q_out, q, "q_out"), self._heads_or_none(k_out, k, "k_out"),
+                                        _stream_ptr(stream))
+        _check(st, "tbe_rotate_heads")
+        return q_out, k_out
+
+    # ---- tbe_rotate_workspace_bytes
+    def rotate_workspace_bytes(self, rows: int, q_heads: int, k_heads: int, head_dim: int) -> int:
+        """For rotate_heads_backward with norm, of any element type."""
+        a = RotationArgs(q_heads=int(q_heads), k_heads=int(k_heads), head_dim=int(head_dim), rows=int(rows))
+        n = ctypes.c_size_t()
+        _check(self._lib.tbe_rotate_workspace_bytes(self._h, ctypes.addressof(a), ctypes.byref(n)), "tbe_rotate_workspace_bytes")
+        return int(n.value)
+
+    def alloc_rotate_workspace(self, rows: int, q_heads: int, k_heads: int, head_dim: int, device="cuda") -> torch.Tensor:
+        return torch.empty(self.rotate_workspace_bytes(rows, q_heads, k_heads, head_dim), dtype=torch.uint8, device=device)
+
+    # ---- tbe_rotate_heads_backward
+    def rotate_heads_backward(self, grad_q_out: Optional[torch.Tensor], grad_k_out: Optional[torch.Tensor], positions: torch.Tensor,
+                              frequencies: Optional[torch.Tensor], workspace: Optional[torch.Tensor] = None, *, q: Optional[torch.Tensor] = None,
+                              k: Optional[torch.Tensor] = None, interleaved: bool = False, amplitude: float = 1.0, norm: bool = False,
+                              eps: float = 1e-6, q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None,
+                              grad_q: Optional[torch.Tensor] = None, grad_k: Optional[torch.Tensor] = None,
+                              grad_q_weight: Optional[torch.Tensor] = None, grad_k_weight: Optional[torch.Tensor] = None, params: bool = True,
+                              param_dtype: Optional[torch.dtype] = None, stream: Optional[torch.cuda.Stream] = None
+                              ) -> Tuple[Optional[torch.Tensor], Optional[torch.Tensor], Optional[torch.Tensor], Optional[torch.Tensor]]:
+        """From the upstream gradients, and with norm the q and k that rotate_heads was given.  Returns (grad_q, grad_k, grad_q_weight, grad_k_weight);
+        the last two, of the weights' type (param_dtype, or float32, where there is no weight), are made with norm, unless params=False leaves out
+        those that are not given."""
+        like = grad_q_out if grad_q_out is not None else grad_k_out
+        if like is None or like.dim() != 3:
+            raise ValueError("grad_q_out and grad_k_out must have three axes: rows, heads, head_dim; one of them may be None")
+        dim = like.shape[2]
+        given = [t.dtype for t in (q_weight, k_weight, grad_q_weight, grad_k_weight) if t is not None]
+        pt = given[0] if given else (param_dtype or torch.float32)
+        if pt not in _IO or any(t != pt for t in given) or (param_dtype or pt) != pt:
+            raise TypeError(f"weights and their gradients must be of one type, got {given}")
+        dqo, dko = self._heads_or_none(grad_q_out, None, "grad_q_out"), self._heads_or_none(grad_k_out, None, "grad_k_out")
+        a = self._rotation_args(grad_q_out, grad_k_out, like, positions, frequencies, interleaved, amplitude, norm, eps, q_weight, k_weight, pt)
+        for up, x, g, gw, name in ((grad_q_out, q, grad_q, grad_q_weight, "q"), (grad_k_out, k, grad_k, grad_k_weight, "k")):
+            if up is None and any(t is not None for t in (x, g, gw)):
+                raise ValueError(f"{name} or its gradients without grad_{name}_out")
+            if norm and up is not None and x is None:
+                raise ValueError(f"{name} is needed with norm")
+            if not norm and gw is not None:
+                raise ValueError("weights' gradients without norm")
+        if grad_q_out is not None and grad_q is None:
+            grad_q = _empty(grad_q_out.shape, like.dtype, like.device, stream)
+        if grad_k_out is not None and grad_k is None:
+            grad_k = _empty(grad_k_out.shape, like.dtype, like.device, stream)
+        if norm and params and grad_q_weight is None and grad_q_out is not None:
+            grad_q_weight = _empty(dim, pt, like.device, stream)
+        if norm and params and grad_k_weight is None and grad_k_out is not None:
+            grad_k_weight = _empty(dim, pt, like.device, stream)
+        st = self._lib.tbe_rotate_heads_backward(
+            self._h, a, dqo, dko, self._heads_or_none(q if norm else None, grad_q_out, "q"), self._heads_or_none(k if norm else None, grad_k_out, "k"),
+            self._heads_or_none(grad_q, grad_q_out, "grad_q"), self._heads_or_none(grad_k, grad_k_out, "grad_k"),
+            _param_ptr(grad_q_weight, dim, pt, "grad_q_weight"), _param_ptr(grad_k_weight, dim, pt, "grad_k_weight"),
+            _dev_ptr(workspace, torch.uint8, "workspace"), 0 if workspace is None else int(workspace.numel()), _stream_ptr(stream))
+        _check(st, "tbe_rotate_heads_backward")
+        return grad_q, grad_k, grad_q_weight, grad_k_weight
 
     # ---- tbe_debug_sorted
     def debug_sorted(self, workspace: torch.Tensor, B: int, nnz: int) -> Dict[str, torch.Tensor]:

@@ -172,4 +172,119 @@ tbe_status tbe_attention_backward(const tbe_handle* h, const tbe_attention_args*
     return done(launch_attention_backward(h, k, p, (int)args->dtype, dbias, workspace, static_cast<hipStream_t>(hip_stream)));
 }
 
+static tbe_status check_rotation(const tbe_handle* h, const tbe_rotation_args* a) {
+    if (!h || !a) return TBE_EINVAL;
+    if (!io_known(a->dtype) || (a->index_dtype != TBE_I64 && a->index_dtype != TBE_I32)) return TBE_EDTYPE;
+    if (a->rows < 0 || a->rows >= (int64_t)1 << 31 || a->q_heads < 0 || a->q_heads > 1024 || a->k_heads < 0 || a->k_heads > 1024) return TBE_ESHAPE;
+    if (a->q_heads + a->k_heads == 0 || a->head_dim < 1 || a->head_dim > kRotateMaxDim) return TBE_ESHAPE;
+    return a->rotary_dim < 0 || a->rotary_dim > a->head_dim || a->rotary_dim % 2 != 0 ? TBE_ESHAPE : TBE_OK;
+}
+// a matrix of heads at any element's address
+static bool loose_rows_ok(const tbe_rows& m, const tbe_rotation_args* a, const int32_t heads) {
+    if (heads == 0 || a->rows == 0) return true;
+    const auto stride_ok = [](const int64_t s) { return s >= 0 && s < (int64_t)1 << 40; };
+    return m.data && multiple_of(m.data, io_size(a->dtype)) && stride_ok(m.row_stride) && stride_ok(m.head_stride);
+}
+// ... that is written: no element twice, and as its source where it is that
+static bool loose_result_ok(const tbe_rows& m, const tbe_rotation_args* a, const int32_t heads) {
+    if (!loose_rows_ok(m, a, heads)) return false;
+    return heads == 0 || ((a->rows <= 1 || m.row_stride >= a->head_dim) && (heads <= 1 || m.head_stride >= a->head_dim));
+}
+static bool apart_or_same(const tbe_rows& from, const tbe_rows& to, const tbe_rotation_args* a, const int32_t heads) {
+    if (from.data != to.data || heads == 0) return true;
+    return (a->rows <= 1 || from.row_stride == to.row_stride) && (heads == 1 || from.head_stride == to.head_stride);
+}
+static tbe_status rotation_call(const tbe_handle* h, const tbe_rotation_args* a, RotateCall& r) {
+    const tbe_status st = check_rotation(h, a);
+    if (st != TBE_OK) return st;
+    if (a->norm && (a->q_weight || a->k_weight) && !io_known(a->weight_dtype)) return TBE_EDTYPE;
+    const size_t w = a->norm && io_known(a->weight_dtype) ? io_size(a->weight_dtype) : 1;
+    if (a->norm && (!multiple_of(a->q_weight, w) || !multiple_of(a->k_weight, w))) return TBE_EINVAL;
+    if ((!a->positions && a->rows > 0) || !multiple_of(a->positions, a->index_dtype == TBE_I32 ? 4 : 8)) return TBE_EINVAL;
+    if ((!a->frequencies && a->rotary_dim > 0) || !multiple_of(a->frequencies, 8)) return TBE_EINVAL;
+    if (!isfinite(a->amplitude) || (a->norm && (!isfinite(a->eps) || a->eps < 0.f))) return TBE_EINVAL;
+    r = RotateCall{};
+    r.positions = a->positions; r.positions32 = a->index_dtype == TBE_I32;
+    r.frequencies = a->frequencies;
+    r.rows = a->rows; r.dim = a->head_dim; r.turned = a->rotary_dim;
+    r.io = (int)a->dtype; r.param_io = (int)a->weight_dtype;
+    r.pairs = a->interleaved != 0; r.norm = a->norm != 0;
+    r.eps = a->eps; r.amplitude = a->amplitude;
+    r.part[0].heads = a->q_heads; r.part[1].heads = a->k_heads;
+    if (r.norm) {
+        r.part[0].weight = a->q_weight; r.part[1].weight = a->k_weight;
+    }
+    return TBE_OK;
+}
+
+tbe_status tbe_rotate_heads(const tbe_handle* h, const tbe_rotation_args* args, tbe_rows q, tbe_rows k, tbe_rows q_out, tbe_rows k_out,
+                            void* hip_stream) {
+    RotateCall r;
+    const tbe_status st = rotation_call(h, args, r);
+    if (st != TBE_OK) return st;
+    if (!loose_rows_ok(q, args, args->q_heads) || !loose_rows_ok(k, args, args->k_heads)) return TBE_EINVAL;
+    if (!loose_result_ok(q_out, args, args->q_heads) || !loose_result_ok(k_out, args, args->k_heads)) return TBE_EINVAL;
+    if (!apart_or_same(q, q_out, args, args->q_heads) || !apart_or_same(k, k_out, args, args->k_heads)) return TBE_EINVAL;
+    if (args->rows == 0) return TBE_OK;
+    r.part[0].x = q; r.part[0].y = q_out;
+    r.part[1].x = k; r.part[1].y = k_out;
+    return done(launch_rotate(h, r, false, static_cast<hipStream_t>(hip_stream)));
+}
+
+tbe_status tbe_rotate_workspace_bytes(const tbe_handle* h, const tbe_rotation_args* args, size_t* bytes) {
+    if (!bytes) return TBE_EINVAL;
+    const tbe_status st = check_rotation(h, args);
+    if (st == TBE_OK) *bytes = rotate_workspace(args->head_dim);
+    return st;
+}
+
+tbe_status tbe_rotate_heads_backward(const tbe_handle* h, const tbe_rotation_args* args, tbe_rows dq_out, tbe_rows dk_out, tbe_rows q,
+                                     tbe_rows k, tbe_rows dq, tbe_rows dk, void* dq_weight, void* dk_weight, void* workspace,
+                                     size_t workspace_bytes, void* hip_stream) {
+    RotateCall r;
+    const tbe_status st = rotation_call(h, args, r);
+    if (st != TBE_OK) return st;
+    const int32_t nq = args->q_heads, nk = args->k_heads;
+    if (!loose_rows_ok(dq_out, args, nq) || !loose_rows_ok(dk_out, args, nk) || !loose_result_ok(dq, args, nq) || !loose_result_ok(dk, args, nk)) return TBE_EINVAL;
+    if (!apart_or_same(dq_out, dq, args, nq) || !apart_or_same(dk_out, dk, args, nk)) return TBE_EINVAL;
+    if (r.norm) {
+        if (!loose_rows_ok(q, args, nq) || !loose_rows_ok(k, args, nk) || !apart_or_same(q, dq, args, nq) || !apart_or_same(k, dk, args, nk)) return TBE_EINVAL;
+    } else if (dq_weight || dk_weight) {
+        return TBE_EINVAL;
+    }
+    if (dq_weight || dk_weight) {
+        if (!io_known(args->weight_dtype)) return TBE_EDTYPE;
+        const size_t w = io_size(args->weight_dtype);
+        if (!multiple_of(dq_weight, w) || !multiple_of(dk_weight, w) || !workspace || !multiple_of(workspace, 256)) return TBE_EINVAL;
+        if (workspace_bytes < rotate_workspace(args->head_dim)) return TBE_EWORKSPACE;
+    } else if (args->rows == 0) {
+        return TBE_OK;
+    }
+    r.part[0].dy = dq_out; r.part[0].x = q; r.part[0].y = dq; r.part[0].dw = dq_weight;
+    r.part[1].dy = dk_out; r.part[1].x = k; r.part[1].y = dk; r.part[1].dw = dk_weight;
+    r.workspace = workspace;
+    return done(launch_rotate(h, r, true, static_cast<hipStream_t>(hip_stream)));
+}
+
+tbe_status tbe_rotary_frequencies(int32_t rotary_dim, double base, tbe_rotary_scaling scaling, double factor, double context, double low_turns,
+                                  double high_turns, double* frequencies) {
+    if (rotary_dim < 2 || rotary_dim > kRotateMaxDim || rotary_dim % 2 != 0 || (scaling == TBE_ROTARY_BASE && rotary_dim < 4)) return TBE_ESHAPE;
+    if (scaling < TBE_ROTARY_PLAIN || scaling > TBE_ROTARY_TURNS) return TBE_EDTYPE;
+    if (!frequencies || !isfinite(base) || !(base > 1.0)) return TBE_EINVAL;
+    if (scaling != TBE_ROTARY_PLAIN && !(isfinite(factor) && factor >= 1.0)) return TBE_EINVAL;
+    if (scaling == TBE_ROTARY_TURNS && !(isfinite(context) && context > 0.0 && low_turns >= 0.0 && low_turns < high_turns && isfinite(high_turns))) return TBE_EINVAL;
+    if (scaling == TBE_ROTARY_BASE) base *= pow(factor, (double)rotary_dim / (rotary_dim - 2));
+    if (!isfinite(base)) return TBE_EINVAL;
+    for (int j = 0; j < rotary_dim / 2; ++j) {
+        double f = pow(base, -2.0 * j / rotary_dim);
+        if (scaling == TBE_ROTARY_LINEAR) f /= factor;
+        if (scaling == TBE_ROTARY_TURNS) {
+            const double at = (context * f / 6.283185307179586477 - low_turns) / (high_turns - low_turns), kept = at < 0.0 ? 0.0 : (at > 1.0 ? 1.0 : at);
+            f = kept * f + (1.0 - kept) * f / factor;
+        }
+        frequencies[j] = f;
+    }
+    return TBE_OK;
+}
+
 }  // extern "C"

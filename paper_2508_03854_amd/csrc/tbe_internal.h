@@ -165,6 +165,27 @@ hipError_t launch_layer_norm_backward(const tbe_handle* h, const void* dy, int64
                                       int64_t rows, int n, const void* weight, int param_io, const float* mean, const float* rstd,
                                       void* dx, int64_t dx_stride, void* dw, void* db, void* workspace, hipStream_t s);
 
+// heads normed and rotated by position (tbe_rotate.hip)
+constexpr int kRotateMaxDim = 256;
+struct RotateMatrix {
+    tbe_rows x, dy, y;   // forward: x to y; backward: dy (and x) to y
+    const void* weight;
+    void* dw;
+    int heads;
+};
+struct RotateCall {
+    RotateMatrix part[2];   // q, k
+    const void* positions;
+    const double* frequencies;
+    int64_t rows;
+    int dim, turned, io, param_io, positions32;
+    bool pairs, norm;
+    float eps, amplitude;
+    void* workspace;
+};
+size_t rotate_workspace(int dim);
+hipError_t launch_rotate(const tbe_handle* h, const RotateCall& r, bool back, hipStream_t s);
+
 // attention over packed sequences (tbe_attention.hip, tbe_attention_backward.hip)
 constexpr int kAttnMaxDim = 128, kAttnMaxFar = 1024;
 struct AttnShape {

@@ -1,0 +1,345 @@
+// Heads of queries and keys, normed and rotated by their rows' positions, and the gradients.
+//   forward   z = x w / sqrt(1/n sum x^2 + eps)  (or z = x);   y = z with every pair (z_a, z_b) of the first `turned` elements turned:
+//             y_a = A (z_a cos t - z_b sin t),  y_b = A (z_b cos t + z_a sin t),  t = position * frequency of the pair
+//   backward  g: dy turned back (by -t, times A);  dx = g, or with r = 1 / sqrt(1/n sum x^2 + eps), h = x r, u = g w:
+//             dx = r (u - h 1/n sum u h),  dw = sum over rows and heads of g h
+// Bound: the stream, every element read once and written once.  A head's elements stay in registers between its sum and its turn; a pair lies
+// in one lane, in either layout, so that nothing but the sum crosses lanes.  The turns are counted in 64 bits and reduced to an eighth of a turn
+// before they become fp32; a lane finds sine and cosine of its pairs once for all heads of a row that it meets.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "tbe_elems.h"
+#include "tbe_internal.h"
+
+namespace tbe {
+
+// Cosine and sine of a number of turns.  What is left after whole and quarter turns are taken off, at most an eighth of a turn, is rounded to
+// fp32 once (2^-25 of its value); the series end where the next term is below 2^-28 (sine) and 2^-32 (cosine).
+__device__ __forceinline__ float2 cos_sin(double turns) {
+    turns -= __builtin_rint(turns);
+    const float quarters = rintf(4.f * (float)turns);
+    const float t = (float)(fma(-0.25, (double)quarters, turns) * 6.283185307179586477);
+    const float q = t * t;
+    float s = fmaf(q, 1.f / 362880.f, -1.f / 5040.f);
+    s = fmaf(q, s, 1.f / 120.f);
+    s = fmaf(q, s, -1.f / 6.f);
+    s = fmaf(q * t, s, t);
+    float c = fmaf(q, -1.f / 3628800.f, 1.f / 40320.f);
+    c = fmaf(q, c, -1.f / 720.f);
+    c = fmaf(q, c, 1.f / 24.f);
+    c = fmaf(q, c, -0.5f);
+    c = fmaf(q, c, 1.f);
+    const int k = (int)quarters;
+    const float a = k & 1 ? s : c, b = k & 1 ? c : s;
+    return make_float2(k & 2 ? (k & 1 ? a : -a) : (k & 1 ? -a : a), k & 2 ? -b : b);
+}
+
+// The n elements at p, as fp32; those behind them are 0 and are not read.
+template <typename T>
+__device__ __forceinline__ void load_some(const T* p, const int n, float (&x)[Frag<T>::kN]) {
+    constexpr int kN = Frag<T>::kN;
+    if (n == kN) {
+        Frag<T>::unpack(Frag<T>::load(p), x);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kN; ++i) x[i] = i < n ? elem_float(p[i]) : 0.f;
+    }
+}
+template <typename T>
+__device__ __forceinline__ void store_some(T* p, const int n, const float (&x)[Frag<T>::kN]) {
+    constexpr int kN = Frag<T>::kN;
+    if (n == kN) {
+        Frag<T>::store(p, x);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kN; ++i)
+            if (i < n) p[i] = elem_round<T>(x[i]);
+    }
+}
+
+__device__ __forceinline__ void turn(const bool turned, const float c, const float s, float& x, float& y) {
+    const float a = x, b = y;
+    x = turned ? a * c - b * s : a;
+    y = turned ? b * c + a * s : b;
+}
+
+// q or k.  Wavefronts take units: `per` rows, of each `beside` heads beside each other, `turns` times; `pieces` units cover all heads of the rows.
+struct TurnPart {
+    const void *x, *dy, *weight;
+    void* y;
+    int64_t x_row, x_head, dy_row, dy_head, y_row, y_head;   // elements
+    float* partial;   // [blocks][dim], or null
+    uint32_t units, blocks;
+    int heads, lg_beside, turns, pieces;
+};
+struct TurnArgs {
+    TurnPart part[2];
+    IdxView positions;
+    const double* frequencies;
+    int64_t rows;
+    int dim, half, lanes_log2, param_io;   // half: pairs
+    float eps, amplitude;
+};
+
+constexpr int kTurnThreads = 256;
+
+template <typename T, bool BACK, bool NORM, bool PAIRS>
+__global__ __launch_bounds__(kTurnThreads) void rotate_kernel(const TurnArgs a) {
+    constexpr int kN = Frag<T>::kN;
+    __shared__ float join[4][256];
+    const bool second = blockIdx.x >= a.part[0].blocks;
+    const TurnPart& p = a.part[second];
+    const uint32_t block = second ? blockIdx.x - a.part[0].blocks : blockIdx.x;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = lane_id(), lg = a.lanes_log2, l = lane & ((1 << lg) - 1), group = lane >> lg;
+    const int lg_per = 6 - lg - p.lg_beside;
+    // This lane's elements of a head: two runs of up to kN.  Pairs (j, j + half): the runs lie `half` apart, behind them the elements that are not
+    // turned; pairs (2 j, 2 j + 1): the runs follow each other.
+    int ea, eb, na, nb, first;   // first: number of the first pair
+    if (PAIRS) {
+        ea = 2 * kN * l;
+        eb = ea + kN;
+        first = ea / 2;
+        na = a.dim - ea;
+        nb = a.dim - eb;
+    } else {
+        const int turning = (a.half + kN - 1) / kN;
+        first = l * kN;
+        ea = l < turning ? first : 2 * a.half + 2 * kN * (l - turning);
+        eb = l < turning ? a.half + first : ea + kN;
+        na = l < turning ? a.half - first : a.dim - ea;
+        nb = l < turning ? na : a.dim - eb;
+        if (l >= turning) first = a.half;   // (no pair)
+    }
+    na = na < 0 ? 0 : (na < kN ? na : kN);
+    nb = nb < 0 ? 0 : (nb < kN ? nb : kN);
+    double f[kN];
+    float wa[kN], wb[kN], dwa[kN], dwb[kN];
+#pragma unroll
+    for (int j = 0; j < kN; ++j) {
+        f[j] = first + j < a.half ? a.frequencies[first + j] * 0.15915494309189533577 : 0.0;   // turns a position
+        wa[j] = NORM && p.weight && j < na ? param_load(p.weight, a.param_io, ea + j) : 1.f;
+        wb[j] = NORM && p.weight && j < nb ? param_load(p.weight, a.param_io, eb + j) : 1.f;
+        dwa[j] = dwb[j] = 0.f;
+    }
+    const float inv = 1.f / (float)a.dim;
+    for (uint32_t u = block * 4 + wave; u < p.units; u += p.blocks * 4) {
+        const uint32_t step = u / (uint32_t)p.pieces;
+        const int piece = (int)(u - step * (uint32_t)p.pieces);
+        const int64_t row = ((int64_t)step << lg_per) + (group >> p.lg_beside);
+        const bool is = row < a.rows;
+        const int64_t at = is ? row : 0;
+        const double position = (double)a.positions[at];
+        float c[kN], s[kN];
+#pragma unroll
+        for (int j = 0; j < kN; ++j) {
+            const float2 cs = cos_sin(position * f[j]);
+            c[j] = cs.x * a.amplitude;
+            s[j] = BACK ? -cs.y * a.amplitude : cs.y * a.amplitude;
+        }
+        // (all lanes of a wavefront stay in the loop together: the sums across lanes need them)
+        for (int k = 0; k < p.turns; ++k) {
+            const int head = (((piece * p.turns + k) << p.lg_beside)) + (group & ((1 << p.lg_beside) - 1));
+            const bool here = is && head < p.heads;
+            const int h0 = here ? head : 0, n0 = here ? na : 0, n1 = here ? nb : 0;
+            const T* const from = static_cast<const T*>(BACK ? p.dy : p.x) + (BACK ? at * p.dy_row + h0 * p.dy_head : at * p.x_row + h0 * p.x_head);
+            float ua[kN], ub[kN], xa[kN], xb[kN];
+            load_some<T>(from + ea, n0, ua);
+            load_some<T>(from + eb, n1, ub);
+            if constexpr (BACK && NORM) {
+                const T* const in = static_cast<const T*>(p.x) + at * p.x_row + h0 * p.x_head;
+                load_some<T>(in + ea, n0, xa);
+                load_some<T>(in + eb, n1, xb);
+            }
+            if constexpr (!BACK && NORM) {
+                float q = 0.f;
+#pragma unroll
+                for (int j = 0; j < kN; ++j) q = fmaf(ua[j], ua[j], q);
+#pragma unroll
+                for (int j = 0; j < kN; ++j) q = fmaf(ub[j], ub[j], q);
+                const float r = 1.f / sqrtf(group_sum(q, 1 << lg) * inv + a.eps);
+#pragma unroll
+                for (int j = 0; j < kN; ++j) {
+                    ua[j] = ua[j] * r * wa[j];
+                    ub[j] = ub[j] * r * wb[j];
+                }
+            }
+            // (elements that are not turned are left as they are: 0 times a neighbour that is not finite is not 0)
+            if constexpr (PAIRS) {
+#pragma unroll
+                for (int j = 0; j < kN; j += 2) {
+                    turn(first + j / 2 < a.half, c[j / 2], s[j / 2], ua[j], ua[j + 1]);
+                    turn(first + (kN + j) / 2 < a.half, c[(kN + j) / 2], s[(kN + j) / 2], ub[j], ub[j + 1]);
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < kN; ++j) turn(first < a.half, c[j], s[j], ua[j], ub[j]);
+            }
+            if constexpr (BACK && NORM) {
+                float q = 0.f, m = 0.f;
+#pragma unroll
+                for (int j = 0; j < kN; ++j) {
+                    q = fmaf(xa[j], xa[j], q);
+                    m = fmaf(ua[j] * wa[j], xa[j], m);
+                }
+#pragma unroll
+                for (int j = 0; j < kN; ++j) {
+                    q = fmaf(xb[j], xb[j], q);
+                    m = fmaf(ub[j] * wb[j], xb[j], m);
+                }
+                float r = 1.f / sqrtf(group_sum(q, 1 << lg) * inv + a.eps);
+                r = here ? r : 0.f;
+                m = group_sum(m, 1 << lg) * inv * r;   // the mean of u h
+#pragma unroll
+                for (int j = 0; j < kN; ++j) {
+                    const float ha = xa[j] * r, hb = xb[j] * r;
+                    dwa[j] = fmaf(ua[j], ha, dwa[j]);
+                    dwb[j] = fmaf(ub[j], hb, dwb[j]);
+                    ua[j] = r * (ua[j] * wa[j] - ha * m);
+                    ub[j] = r * (ub[j] * wb[j] - hb * m);
+                }
+            }
+            T* const to = static_cast<T*>(p.y) + at * p.y_row + h0 * p.y_head;
+            store_some<T>(to + ea, n0, ua);
+            store_some<T>(to + eb, n1, ub);
+        }
+    }
+    if constexpr (BACK && NORM) {
+        if (!p.partial) return;
+        // the groups of a wavefront, then the wavefronts, in a fixed order
+        for (int w = 1 << lg; w < 64; w <<= 1)
+#pragma unroll
+            for (int j = 0; j < kN; ++j) {
+                dwa[j] += __shfl_xor(dwa[j], w);
+                dwb[j] += __shfl_xor(dwb[j], w);
+            }
+        if (group == 0) {
+#pragma unroll
+            for (int j = 0; j < kN; ++j) {
+                if (j < na) join[wave][ea + j] = dwa[j];
+                if (j < nb) join[wave][eb + j] = dwb[j];
+            }
+        }
+        __syncthreads();
+        for (int e = threadIdx.x; e < a.dim; e += kTurnThreads)
+            p.partial[(int64_t)block * a.dim + e] = (join[0][e] + join[1][e]) + (join[2][e] + join[3][e]);
+    }
+}
+
+// The weights' gradients from the workgroups' sums: 8 columns a workgroup, 32 slices of the workgroups beside each other; q's columns, then k's.
+__global__ __launch_bounds__(256) void rotate_params_kernel(const float* __restrict__ partial, const int blocks_q, const int blocks_k, const int n, void* dq,
+                                                            void* dk, const int io) {
+    __shared__ float part[32][9];
+    const int c = threadIdx.x % 8, k = threadIdx.x / 8, e = blockIdx.x * 8 + c;
+    const bool second = e >= n;
+    const float* const from = partial + (second ? (int64_t)blocks_q * n + (e - n) : e);
+    part[k][c] = e < 2 * n ? strided_sum(from, n, k, second ? blocks_k : blocks_q, 32) : 0.f;
+    __syncthreads();
+    if (k == 0 && e < 2 * n) {
+        float t = 0.f;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) t += part[i][c];
+        void* const to = second ? dk : dq;
+        if (to) param_store(to, io, second ? e - n : e, t);
+    }
+}
+
+static int log2_up(const int64_t x) {
+    int n = 0;
+    while (((int64_t)1 << n) < x) ++n;
+    return n;
+}
+// lanes of a head (log2), at most 64
+static int turn_lanes_log2(const int dim, const int half, const bool pairs, const int kN) {
+    const int lanes = pairs ? (dim + 2 * kN - 1) / (2 * kN) : (half + kN - 1) / kN + (dim - 2 * half + 2 * kN - 1) / (2 * kN);
+    return log2_up(lanes);
+}
+// How the heads of q or k are shared among wavefronts: as many beside each other as there are and a wavefront has room for, the others one
+// after the other with the same sines and cosines, unless there would be few wavefronts then.
+static void turn_units(TurnPart& p, const int64_t rows, const int heads, const int lg) {
+    p.heads = heads;
+    p.units = 0;
+    p.pieces = p.turns = 1;
+    p.lg_beside = 0;
+    if (heads == 0) return;
+    p.lg_beside = std::min(6 - lg, log2_up(heads));
+    const int lg_per = 6 - lg - p.lg_beside;
+    const int64_t steps = (rows + ((int64_t)1 << lg_per) - 1) >> lg_per, all = (heads + (1 << p.lg_beside) - 1) >> p.lg_beside;
+    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(all, 8192 / std::max<int64_t>(1, steps)));
+    p.turns = (int)((all + want - 1) / want);
+    p.pieces = (int)((all + p.turns - 1) / p.turns);
+    p.units = (uint32_t)(steps * p.pieces);
+}
+// Workgroups of q and of k: at most `most` in all, in proportion to their heads, so that they end together.
+static void turn_blocks(TurnPart& q, TurnPart& k, const int64_t most) {
+    const int64_t heads = q.heads + k.heads;
+    const auto some = [&](const TurnPart& p) {
+        return p.units == 0 ? 0u : (uint32_t)std::min<int64_t>(((int64_t)p.units + 3) / 4, std::max<int64_t>(1, most * p.heads / heads));
+    };
+    q.blocks = some(q);
+    k.blocks = some(k);
+}
+constexpr int64_t kTurnBlocksForward = 2048, kTurnBlocksBackward = 1024;
+
+size_t rotate_workspace(const int dim) {   // (of any element type and layout)
+    return (((size_t)kTurnBlocksBackward + 2) * (size_t)dim * sizeof(float) + 255) & ~(size_t)255;
+}
+
+template <typename T, bool BACK, bool NORM>
+static void launch_layout(const TurnArgs& a, const bool pairs, const unsigned blocks, hipStream_t s) {
+    if (pairs) rotate_kernel<T, BACK, NORM, true><<<blocks, kTurnThreads, 0, s>>>(a);
+    else rotate_kernel<T, BACK, NORM, false><<<blocks, kTurnThreads, 0, s>>>(a);
+}
+template <typename T, bool BACK>
+static void launch_norm(const TurnArgs& a, const bool norm, const bool pairs, const unsigned blocks, hipStream_t s) {
+    if (norm) launch_layout<T, BACK, true>(a, pairs, blocks, s);
+    else launch_layout<T, BACK, false>(a, pairs, blocks, s);
+}
+template <typename T>
+static void launch_turn(const TurnArgs& a, const bool back, const bool norm, const bool pairs, const unsigned blocks, hipStream_t s) {
+    if (back) launch_norm<T, true>(a, norm, pairs, blocks, s);
+    else launch_norm<T, false>(a, norm, pairs, blocks, s);
+}
+
+hipError_t launch_rotate(const tbe_handle* h, const RotateCall& r, const bool back, hipStream_t s) {
+    TurnArgs a{};
+    a.positions = IdxView{r.positions, r.positions32};
+    a.frequencies = r.frequencies;
+    a.rows = r.rows; a.dim = r.dim; a.half = r.turned / 2; a.param_io = r.param_io;
+    a.eps = r.eps; a.amplitude = r.amplitude;
+    a.lanes_log2 = turn_lanes_log2(r.dim, a.half, r.pairs, r.io == 0 ? 4 : 8);
+    for (int i = 0; i < 2; ++i) {
+        const RotateMatrix& m = r.part[i];
+        TurnPart& p = a.part[i];
+        p.x = m.x.data; p.x_row = m.x.row_stride; p.x_head = m.x.head_stride;
+        p.dy = m.dy.data; p.dy_row = m.dy.row_stride; p.dy_head = m.dy.head_stride;
+        p.y = m.y.data; p.y_row = m.y.row_stride; p.y_head = m.y.head_stride;
+        p.weight = m.weight;
+        turn_units(p, r.rows, m.heads, a.lanes_log2);
+    }
+    turn_blocks(a.part[0], a.part[1], back ? kTurnBlocksBackward : kTurnBlocksForward);
+    const bool weights = back && r.norm && (r.part[0].dw || r.part[1].dw);
+    if (weights) {
+        a.part[0].partial = static_cast<float*>(r.workspace);
+        a.part[1].partial = a.part[0].partial + (size_t)a.part[0].blocks * r.dim;
+    }
+    const unsigned blocks = a.part[0].blocks + a.part[1].blocks;
+    if (blocks > 0) {
+        LaunchTimer tm(h, s, back ? "rotate_backward" : "rotate");
+        if (r.io == 0) launch_turn<float>(a, back, r.norm, r.pairs, blocks, s);
+        else if (r.io == 1) launch_turn<__half>(a, back, r.norm, r.pairs, blocks, s);
+        else launch_turn<bf16_t>(a, back, r.norm, r.pairs, blocks, s);
+        tm.done();
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    if (!weights) return hipSuccess;
+    LaunchTimer tp(h, s, "rotate_params");
+    rotate_params_kernel<<<(2 * r.dim + 7) / 8, 256, 0, s>>>(a.part[0].partial, (int)a.part[0].blocks, (int)a.part[1].blocks, r.dim, r.part[0].dw, r.part[1].dw,
+                                                             r.param_io);
+    tp.done();
+    return hipGetLastError();
+}
+
+}  // namespace tbe
