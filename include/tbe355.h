@@ -422,6 +422,44 @@ typedef enum { TBE_ROTARY_PLAIN = 0, TBE_ROTARY_LINEAR = 1, TBE_ROTARY_BASE = 2,
 tbe_status tbe_rotary_frequencies(int32_t rotary_dim, double base, tbe_rotary_scaling scaling, double factor, double context, double low_turns,
                                   double high_turns, double* frequencies);
 
+/* Caches of keys and values with one byte an element, a code, and a scale for every row and head: a value is code * scale.
+ *   TBE_CODE_E4M3  codes are 8-bit floating point numbers of 4 exponent and 3 fraction bits (no infinity, 0x7F and 0xFF are not numbers, +-448 the
+ *                  largest).  tbe_cache_write takes as scale the least power of two with which a head's largest magnitude is at most 448 (at least
+ *                  2^-126; 1 for zeros), and rounds x / scale to the nearest code, ties to even
+ *   TBE_CODE_I8    codes are whole numbers -127 .. 127.  The scale is the largest magnitude / 127 rounded to fp32 (at least 2^-126; 1 for zeros), the
+ *                  code the whole number nearest to x / scale, ties to even
+ * A head with an element that is not finite gets codes 0 and the scale NaN: all of it reads as NaN.
+ *   k, v      DEVICE, codes [rows][heads][head_dim]: consecutive rows row_stride, consecutive heads head_stride bytes apart, 16-byte aligned, strides
+ *             multiples of 16, row_stride < 2^22, both at least head_dim (they are written); head_dim a multiple of 16, at most 128
+ *   k_scales, v_scales  DEVICE float [heads][rows] */
+typedef enum { TBE_CODE_E4M3 = 0, TBE_CODE_I8 = 1 } tbe_code;
+typedef struct {
+    int64_t rows;              /* 0 .. 2^31 - 4096 */
+    int32_t heads, head_dim;   /* 1 <= heads <= 1024 */
+    tbe_code code;
+    tbe_rows k, v;             /* strides in bytes */
+    float *k_scales, *v_scales;
+} tbe_cache;
+/* Row r of k and v, [rows][heads][head_dim] of dtype at any address that is a multiple of the element's size, goes to the cache's row slots[r]; rows with a slot
+ * below 0 go nowhere.  All other rows of the cache keep their bytes.  A slot at or beyond the cache's rows is left out and reported by
+ * tbe_poll_index_error.  Slots from 0 on differ from each other: what the row of one that is named twice then holds is not specified.
+ *   slots     DEVICE, `rows` of index_dtype;  0 <= rows < 2^31 */
+tbe_status tbe_cache_write(const tbe_handle* h, const tbe_cache* cache, tbe_rows k, tbe_rows v, tbe_io_dtype dtype, const void* slots,
+                           tbe_index_dtype index_dtype, int64_t rows, void* hip_stream);
+/* The reverse: row r of k and v becomes the values of the cache's row slots[r] (the product in fp32, rounded to dtype); zeros where the slot is below 0,
+ * or beyond the cache's rows, which is reported likewise.  Slots may repeat. */
+tbe_status tbe_cache_read(const tbe_handle* h, const tbe_cache* cache, const void* slots, tbe_index_dtype index_dtype, int64_t rows, tbe_rows k,
+                          tbe_rows v, tbe_io_dtype dtype, void* hip_stream);
+
+/* Attention over such a cache: tbe_attention with k = the codes of cache->k times their scales, v likewise, none of which is written out.  args as there, but
+ * its k and v are not looked at; kv_heads, head_dim and k_rows are the cache's heads, head_dim and rows (TBE_ESHAPE), so head_dim is a multiple of 16.  dtype
+ * is that of q and out.  Products are exact in q and the codes and added in fp32, scales are multiplied in fp32; a probability times its value's scale is
+ * rounded to bfloat16 where dtype is TBE_IO_BF16, to 16 bits or more for TBE_IO_F16, not at all for TBE_IO_F32; results once when stored.  What is hidden is
+ * left out, scales and codes that are not numbers among it; a scale that is infinite may make NaN of what sees it. */
+tbe_status tbe_cache_attention_workspace_bytes(const tbe_handle* h, const tbe_attention_args* args, size_t* bytes);
+tbe_status tbe_cache_attention(const tbe_handle* h, const tbe_attention_args* args, const tbe_cache* cache, tbe_rows out, float* lse, void* workspace,
+                               size_t workspace_bytes, void* hip_stream);
+
 const char* tbe_status_string(tbe_status s);
 
 /* "tbe355 gfx950 <digest>": the digest names the sources and build settings this library was compiled from (twelve

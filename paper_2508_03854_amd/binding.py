@@ -21,6 +21,8 @@ F32, F16 = 0, 1
 SUM, MEAN = 0, 1
 I64, I32 = 0, 1                       # tbe_index_dtype
 IO_F32, IO_F16, IO_BF16 = 0, 1, 2     # tbe_io_dtype
+CODE_E4M3, CODE_I8 = 0, 1             # tbe_code
+_CODE = {torch.float8_e4m3fn: CODE_E4M3, torch.int8: CODE_I8}
 ROTARY_SCALING = {"plain": 0, "linear": 1, "base": 2, "turns": 3}   # tbe_rotary_scaling
 FWD_WAVEFRONT_PER_BAG, FWD_LANE_GROUPS, FWD_HOT_ROWS, FWD_LONG_BAGS = 1, 2, 4, 8   # TBE_FWD_*
 TUNABLES = {"hot_rows_min_workgroups": 0}   # tbe_tunable
@@ -35,7 +37,8 @@ EXPORTS = ["tbe_create", "tbe_destroy", "tbe_workspace_bytes", "tbe_forward", "t
            "tbe_backward_seq_rowwise_adagrad", "tbe_debug_sorted", "tbe_debug_hot_rows", "tbe_debug_forward_kernels", "tbe_poll_index_error", "tbe_set_tunable", "tbe_timing_enable",
            "tbe_timing_count", "tbe_timing_read", "tbe_calibration_copy", "tbe_calibration_gather", "tbe_status_string", "tbe_build_info",
            "tbe_layer_norm", "tbe_layer_norm_workspace_bytes", "tbe_layer_norm_backward", "tbe_attention_workspace_bytes", "tbe_attention", "tbe_attention_backward",
-           "tbe_rotate_heads", "tbe_rotate_workspace_bytes", "tbe_rotate_heads_backward", "tbe_rotary_frequencies"]
+           "tbe_rotate_heads", "tbe_rotate_workspace_bytes", "tbe_rotate_heads_backward", "tbe_rotary_frequencies",
+           "tbe_cache_write", "tbe_cache_read", "tbe_cache_attention_workspace_bytes", "tbe_cache_attention"]
 
 
 class TbeError(RuntimeError):
@@ -66,8 +69,15 @@ class RotationArgs(ctypes.Structure):
                 ("eps", ctypes.c_float), ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("weight_dtype", ctypes.c_int)]
 
 
+class CacheArgs(ctypes.Structure):
+    """tbe_cache"""
+    _fields_ = [("rows", ctypes.c_int64), ("heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("code", ctypes.c_int), ("k", Rows), ("v", Rows),
+                ("k_scales", ctypes.c_void_p), ("v_scales", ctypes.c_void_p)]
+
+
 # The same fields packed in one go: filling the structure field by field takes 6 us of a call that is otherwise over in ten.
 _PACK_ATTENTION = struct.Struct("@4i2q2i" + "Pqq" * 3 + "3Pif2P3i4x").pack
+_PACK_CACHE = struct.Struct("@q3i4xPqqPqq2P").pack
 _PACK_ROTATION = struct.Struct("@4iq2i2Pifif2Pi4x").pack
 
 _lib = None
@@ -166,6 +176,14 @@ def load_library():
     f64 = ctypes.c_double
     L.tbe_rotary_frequencies.restype = ctypes.c_int
     L.tbe_rotary_frequencies.argtypes = [i32, f64, ctypes.c_int, f64, f64, f64, f64, vp]
+    L.tbe_cache_write.restype = ctypes.c_int
+    L.tbe_cache_write.argtypes = [vp, vp, Rows, Rows, ctypes.c_int, vp, ctypes.c_int, i64, vp]
+    L.tbe_cache_read.restype = ctypes.c_int
+    L.tbe_cache_read.argtypes = [vp, vp, vp, ctypes.c_int, i64, Rows, Rows, ctypes.c_int, vp]
+    L.tbe_cache_attention_workspace_bytes.restype = ctypes.c_int
+    L.tbe_cache_attention_workspace_bytes.argtypes = [vp, vp, ctypes.POINTER(ctypes.c_size_t)]
+    L.tbe_cache_attention.restype = ctypes.c_int
+    L.tbe_cache_attention.argtypes = [vp, vp, vp, Rows, vp, vp, ctypes.c_size_t, vp]
     L.tbe_build_info.restype = ctypes.c_char_p
     L.tbe_build_info.argtypes = []
     L.tbe_status_string.restype = ctypes.c_char_p
@@ -262,6 +280,33 @@ def rotary_frequencies(rotary_dim: int, base: float = 10000.0, scaling: str = "p
     _check(load_library().tbe_rotary_frequencies(int(rotary_dim), float(base), ROTARY_SCALING[scaling], float(factor), float(context),
                                                  float(low_turns), float(high_turns), f.data_ptr()), "tbe_rotary_frequencies")
     return f.to(device)
+
+
+class Cache:
+    """tbe_cache: keys and values as one byte an element, k and v [rows, heads, head_dim] float8_e4m3fn or int8 (last axis contiguous), and scales,
+    k_scales and v_scales float32 [heads, rows]; a value is code * scale.  TBE.alloc_cache makes an empty one."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scales: torch.Tensor, v_scales: torch.Tensor):
+        if k.dim() != 3 or v.shape != k.shape:
+            raise ValueError("k and v must have three axes: rows, heads, head_dim, and one shape")
+        if k.dtype not in _CODE or v.dtype != k.dtype:
+            raise TypeError(f"k and v must both be float8_e4m3fn or both int8, got {k.dtype} / {v.dtype}")
+        if not (k.is_cuda and v.is_cuda):
+            raise ValueError("k and v must be device tensors")
+        if any(t.stride(2) != 1 and t.shape[2] > 1 and t.numel() for t in (k, v)):
+            raise ValueError("the last axis of k and v must be contiguous")
+        for t, what in ((k_scales, "k_scales"), (v_scales, "v_scales")):
+            _dev_ptr(t, torch.float32, what)
+            if t.shape != (k.shape[1], k.shape[0]):
+                raise ValueError(f"{what} must be [heads, rows], got {tuple(t.shape)}")
+        self.k, self.v, self.k_scales, self.v_scales = k, v, k_scales, v_scales
+
+    def _args(self) -> bytes:
+        k, v = self.k, self.v
+        rows, heads, dim = k.shape
+        ks, vs = k.stride(), v.stride()
+        return _PACK_CACHE(rows, heads, dim, _CODE[k.dtype], k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1], self.k_scales.data_ptr(),
+                           self.v_scales.data_ptr())
 
 
 class TBE:
@@ -614,11 +659,17 @@ class TBE:
             raise ValueError("q, k and v must have three axes: rows, heads, head_dim")
         if q.dtype not in _IO:
             raise TypeError(f"q must be float32, float16 or bfloat16, got {q.dtype}")
-        q_rows, heads, dim = q.shape
-        k_rows, kv_heads, k_dim = k.shape
         dtype = q.dtype
-        if k.dtype != dtype or v.dtype != dtype or v.shape != k.shape or k_dim != dim:
+        if k.dtype != dtype or v.dtype != dtype or v.shape != k.shape or k.shape[2] != q.shape[2]:
             raise ValueError("q, k and v must agree in type and head_dim, k and v in shape")
+        kp, vp = _rows_ptr(k, None, "k"), _rows_ptr(v, None, "v")
+        ks, vs = k.stride(), v.stride()
+        return self._pack_attention(q, k.shape, (kp, ks[0], ks[1], vp, vs[0], vs[1]), q_offsets, k_offsets, k_lengths, causal, scale, bias, bucket_map)
+
+    def _pack_attention(self, q, k_shape, kv, q_offsets, k_offsets, k_lengths, causal, scale, bias, bucket_map) -> bytes:
+        """... from the matrices of k and v as they stand in it"""
+        q_rows, heads, dim = q.shape
+        k_rows, kv_heads, _ = k_shape
         n = q_offsets.numel() - 1
         if k_offsets.numel() != n + 1 or (k_lengths is not None and k_lengths.numel() != n):
             raise ValueError("q_offsets and k_offsets must have one entry more than k_lengths")
@@ -632,10 +683,9 @@ class TBE:
                 raise ValueError("bias must be [heads, buckets] and bucket_map [2 * max_distance + 1]")
             table, map_ = _param_ptr(bias, bias.numel(), None, "bias"), _dev_ptr(bucket_map, torch.int32, "bucket_map")
             bias_io, buckets, far = _IO[bias.dtype], bias.shape[1], bucket_map.numel() // 2
-        qp, kp, vp = _rows_ptr(q, None, "q"), _rows_ptr(k, None, "k"), _rows_ptr(v, None, "v")
-        qs, ks, vs = q.stride(), k.stride(), v.stride()
-        return _PACK_ATTENTION(n, heads, kv_heads, dim, q_rows, k_rows, _IO[dtype], _index_dtype(q_offsets, k_offsets), qp, qs[0], qs[1], kp, ks[0],
-                               ks[1], vp, vs[0], vs[1], _dev_ptr(q_offsets, it, "q_offsets"), _dev_ptr(k_offsets, it, "k_offsets"),
+        qp, qs = _rows_ptr(q, None, "q"), q.stride()
+        return _PACK_ATTENTION(n, heads, kv_heads, dim, q_rows, k_rows, _IO[q.dtype], _index_dtype(q_offsets, k_offsets), qp, qs[0], qs[1], *kv,
+                               _dev_ptr(q_offsets, it, "q_offsets"), _dev_ptr(k_offsets, it, "k_offsets"),
                                _dev_ptr(k_lengths, it, "k_lengths") or 0, bool(causal), dim ** -0.5 if scale is None else float(scale), table, map_,
                                bias_io, buckets, far)
 
@@ -791,6 +841,85 @@ class TBE:
             _dev_ptr(workspace, torch.uint8, "workspace"), 0 if workspace is None else int(workspace.numel()), _stream_ptr(stream))
         _check(st, "tbe_rotate_heads_backward")
         return grad_q, grad_k, grad_q_weight, grad_k_weight
+
+    # ---- tbe_cache_write
+    def alloc_cache(self, rows: int, heads: int, head_dim: int, code: torch.dtype = torch.float8_e4m3fn, device="cuda") -> Cache:
+        """A cache of zeros; code: torch.float8_e4m3fn or torch.int8."""
+        if code not in _CODE:
+            raise TypeError(f"code must be float8_e4m3fn or int8, got {code}")
+        k, v = (torch.zeros(rows, heads, head_dim, dtype=torch.uint8, device=device).view(code) for _ in range(2))
+        return Cache(k, v, torch.ones(heads, rows, device=device), torch.ones(heads, rows, device=device))
+
+    @staticmethod
+    def _cache_rows(cache: Cache, slots: torch.Tensor) -> int:
+        if slots.dtype not in _IDX:
+            raise TypeError(f"slots must be int64 or int32, got {slots.dtype}")
+        return slots.numel()
+
+    def cache_write(self, cache: Cache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, *,
+                    stream: Optional[torch.cuda.Stream] = None) -> None:
+        """Row r of k and v ([rows, heads, head_dim], float32, float16 or bfloat16; column blocks of one matrix are fine) goes to the cache's row
+        slots[r] (int64 or int32; below 0: nowhere)."""
+        rows = self._cache_rows(cache, slots)
+        if k.dim() != 3 or k.shape != (rows, *cache.k.shape[1:]):
+            raise ValueError(f"k must be {(rows, *cache.k.shape[1:])}, got {tuple(k.shape)}")
+        st = self._lib.tbe_cache_write(self._h, cache._args(), _heads(k, None, "k"), _heads(v, k, "v"), _IO[k.dtype],
+                                       _dev_ptr(slots, slots.dtype, "slots"), _IDX[slots.dtype], rows, _stream_ptr(stream))
+        _check(st, "tbe_cache_write")
+
+    # ---- tbe_cache_read
+    def cache_read(self, cache: Cache, slots: torch.Tensor, *, dtype: torch.dtype = torch.float32, k_out: Optional[torch.Tensor] = None,
+                   v_out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+        """The values of the cache's rows `slots` (zeros where one is below 0), [rows, heads, head_dim] of dtype, or into k_out and v_out."""
+        rows = self._cache_rows(cache, slots)
+        shape = (rows, *cache.k.shape[1:])
+        given = k_out if k_out is not None else v_out
+        dtype = dtype if given is None else given.dtype
+        k_out = _empty(shape, dtype, cache.k.device, stream) if k_out is None else k_out
+        v_out = _empty(shape, dtype, cache.k.device, stream) if v_out is None else v_out
+        if k_out.shape != shape:
+            raise ValueError(f"k_out must be {shape}, got {tuple(k_out.shape)}")
+        st = self._lib.tbe_cache_read(self._h, cache._args(), _dev_ptr(slots, slots.dtype, "slots"), _IDX[slots.dtype], rows,
+                                      _heads(k_out, None, "k_out"), _heads(v_out, k_out, "v_out"), _IO[k_out.dtype], _stream_ptr(stream))
+        _check(st, "tbe_cache_read")
+        return k_out, v_out
+
+    # ---- tbe_cache_attention_workspace_bytes
+    def cache_attention_workspace_bytes(self, sequences: int, q_rows: int, k_rows: int, heads: int, kv_heads: int, head_dim: int, *, buckets: int = 0) -> int:
+        """For calls of these sizes, with a bias of `buckets` buckets (0: without), of any element type."""
+        a = AttentionArgs(sequences=int(sequences), heads=int(heads), kv_heads=int(kv_heads), head_dim=int(head_dim), q_rows=int(q_rows),
+                          k_rows=int(k_rows), dtype=IO_BF16, buckets=int(buckets))
+        n = ctypes.c_size_t()
+        _check(self._lib.tbe_cache_attention_workspace_bytes(self._h, ctypes.addressof(a), ctypes.byref(n)), "tbe_cache_attention_workspace_bytes")
+        return int(n.value)
+
+    def alloc_cache_attention_workspace(self, sequences: int, q_rows: int, k_rows: int, heads: int, kv_heads: int, head_dim: int, *, buckets: int = 0,
+                                        device="cuda") -> torch.Tensor:
+        return torch.empty(self.cache_attention_workspace_bytes(sequences, q_rows, k_rows, heads, kv_heads, head_dim, buckets=buckets), dtype=torch.uint8,
+                           device=device)
+
+    # ---- tbe_cache_attention
+    def cache_attention(self, q: torch.Tensor, cache: Cache, q_offsets: torch.Tensor, k_offsets: torch.Tensor, workspace: Optional[torch.Tensor], *,
+                        causal: bool = True, scale: Optional[float] = None, k_lengths: Optional[torch.Tensor] = None,
+                        bias: Optional[torch.Tensor] = None, bucket_map: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                        lse: Optional[torch.Tensor] = None, stats: bool = True, stream: Optional[torch.cuda.Stream] = None
+                        ) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+        """attention() with the cache's values as k and v; k_offsets are places in the cache.  Returns (out, lse)."""
+        if q.dim() != 3 or q.dtype not in _IO:
+            raise ValueError(f"q must be float32, float16 or bfloat16 and have three axes: rows, heads, head_dim; got {q.dtype} {tuple(q.shape)}")
+        shape = cache.k.shape
+        if shape[2] != q.shape[2]:
+            raise ValueError(f"q and the cache must agree in head_dim, got {q.shape[2]} / {shape[2]}")
+        a = self._pack_attention(q, shape, (0, 0, 0, 0, 0, 0), q_offsets, k_offsets, k_lengths, causal, scale, bias, bucket_map)
+        out = _empty(q.shape, q.dtype, q.device, stream) if out is None else out
+        if stats and lse is None:
+            lse = _empty((q.shape[1], q.shape[0]), torch.float32, q.device, stream)
+        st = self._lib.tbe_cache_attention(self._h, a, cache._args(), _heads(out, q, "out"),
+                                           _param_ptr(lse, q.shape[0] * q.shape[1], torch.float32, "lse"),
+                                           _dev_ptr(workspace, torch.uint8, "workspace"), 0 if workspace is None else int(workspace.numel()),
+                                           _stream_ptr(stream))
+        _check(st, "tbe_cache_attention")
+        return out, lse
 
     # ---- tbe_debug_sorted
     def debug_sorted(self, workspace: torch.Tensor, B: int, nnz: int) -> Dict[str, torch.Tensor]:

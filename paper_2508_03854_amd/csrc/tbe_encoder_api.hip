@@ -2,6 +2,7 @@
 #include <math.h>
 
 #include "tbe_attention.h"
+#include "tbe_cache.h"
 
 using namespace tbe;
 
@@ -93,7 +94,7 @@ static bool rows_view(const tbe_rows& m, const int64_t rows, const int32_t heads
     v.p = static_cast<const char*>(m.data); v.row = m.row_stride * e; v.head = m.head_stride * e;
     return true;
 }
-static tbe_status attention_args(const tbe_handle* h, const tbe_attention_args* a, AttnArgs& k) {
+static tbe_status attention_args(const tbe_handle* h, const tbe_attention_args* a, AttnArgs& k, const bool keys = true) {
     const tbe_status st = check_attention_sizes(h, a);
     if (st != TBE_OK) return st;
     if (a->bias && !io_known(a->bias_dtype)) return TBE_EDTYPE;
@@ -103,8 +104,8 @@ static tbe_status attention_args(const tbe_handle* h, const tbe_attention_args* 
     if (!a->q_offsets || !a->k_offsets || !multiple_of(a->q_offsets, ia) || !multiple_of(a->k_offsets, ia) || !multiple_of(a->k_lengths, ia)) return TBE_EINVAL;
     if (!isfinite(a->scale)) return TBE_EINVAL;
     k = AttnArgs{};
-    if (!rows_view(a->q, a->q_rows, a->heads, a, false, k.q) || !rows_view(a->k, a->k_rows, a->kv_heads, a, false, k.k) ||
-        !rows_view(a->v, a->k_rows, a->kv_heads, a, false, k.v)) return TBE_EINVAL;
+    if (!rows_view(a->q, a->q_rows, a->heads, a, false, k.q)) return TBE_EINVAL;
+    if (keys && (!rows_view(a->k, a->k_rows, a->kv_heads, a, false, k.k) || !rows_view(a->v, a->k_rows, a->kv_heads, a, false, k.v))) return TBE_EINVAL;
     const int is32 = a->index_dtype == TBE_I32;
     k.q_off = IdxView{a->q_offsets, is32}; k.k_off = IdxView{a->k_offsets, is32}; k.k_len = IdxView{a->k_lengths, is32};
     k.N = a->sequences; k.H = a->heads; k.kv = a->kv_heads; k.group = a->heads / a->kv_heads; k.dim = a->head_dim; k.causal = a->causal != 0;
@@ -285,6 +286,84 @@ tbe_status tbe_rotary_frequencies(int32_t rotary_dim, double base, tbe_rotary_sc
         frequencies[j] = f;
     }
     return TBE_OK;
+}
+
+static bool code_rows(const tbe_rows& m, float* scales, const tbe_cache* c, CodeRows& v) {
+    if (c->rows > 0 && (!m.data || !scales)) return false;
+    if (!multiple_of(m.data, 16) || !multiple_of(scales, 4)) return false;
+    if (m.row_stride < 0 || m.row_stride >= 1 << 22 || m.row_stride % 16 != 0 || m.head_stride < 0 || m.head_stride >= (int64_t)1 << 40 || m.head_stride % 16 != 0) return false;
+    if ((c->rows > 1 && m.row_stride < c->head_dim) || (c->heads > 1 && m.head_stride < c->head_dim)) return false;
+    v.codes.p = static_cast<const char*>(m.data); v.codes.row = m.row_stride; v.codes.head = m.head_stride;
+    v.scales = scales;
+    return true;
+}
+static tbe_status check_cache(const tbe_handle* h, const tbe_cache* c, CodeRows (&v)[2]) {
+    if (!h || !c) return TBE_EINVAL;
+    if (c->code != TBE_CODE_E4M3 && c->code != TBE_CODE_I8) return TBE_EDTYPE;
+    if (c->rows < 0 || c->rows > ((int64_t)1 << 31) - 4096 || c->heads < 1 || c->heads > 1024) return TBE_ESHAPE;
+    if (c->head_dim < 16 || c->head_dim > kAttnMaxDim || c->head_dim % 16 != 0) return TBE_ESHAPE;
+    return code_rows(c->k, c->k_scales, c, v[0]) && code_rows(c->v, c->v_scales, c, v[1]) ? TBE_OK : TBE_EINVAL;
+}
+static tbe_status cache_copy(const tbe_handle* h, const tbe_cache* cache, const tbe_rows& k, const tbe_rows& v, const tbe_io_dtype dtype, const void* slots,
+                             const tbe_index_dtype index_dtype, const int64_t rows, const bool write, void* hip_stream) {
+    CacheCopyCall c{};
+    const tbe_status st = check_cache(h, cache, c.cache);
+    if (st != TBE_OK) return st;
+    if (!io_known(dtype) || (index_dtype != TBE_I64 && index_dtype != TBE_I32)) return TBE_EDTYPE;
+    if (rows < 0 || rows >= (int64_t)1 << 31) return TBE_ESHAPE;
+    tbe_rotation_args as{};   // (the same kind of matrix)
+    as.dtype = dtype; as.rows = rows; as.head_dim = cache->head_dim;
+    if (write ? !loose_rows_ok(k, &as, cache->heads) || !loose_rows_ok(v, &as, cache->heads)
+              : !loose_result_ok(k, &as, cache->heads) || !loose_result_ok(v, &as, cache->heads)) return TBE_EINVAL;
+    if ((!slots && rows > 0) || !multiple_of(slots, index_dtype == TBE_I32 ? 4 : 8)) return TBE_EINVAL;
+    if (rows == 0) return TBE_OK;
+    c.rows_of[0] = k; c.rows_of[1] = v;
+    c.slots = slots; c.slots32 = index_dtype == TBE_I32;
+    c.rows = rows; c.cache_rows = cache->rows; c.heads = cache->heads; c.dim = cache->head_dim; c.io = (int)dtype; c.i8 = cache->code == TBE_CODE_I8;
+    return done(launch_cache_copy(h, c, write, static_cast<hipStream_t>(hip_stream)));
+}
+
+tbe_status tbe_cache_write(const tbe_handle* h, const tbe_cache* cache, tbe_rows k, tbe_rows v, tbe_io_dtype dtype, const void* slots,
+                           tbe_index_dtype index_dtype, int64_t rows, void* hip_stream) {
+    return cache_copy(h, cache, k, v, dtype, slots, index_dtype, rows, true, hip_stream);
+}
+tbe_status tbe_cache_read(const tbe_handle* h, const tbe_cache* cache, const void* slots, tbe_index_dtype index_dtype, int64_t rows, tbe_rows k,
+                          tbe_rows v, tbe_io_dtype dtype, void* hip_stream) {
+    return cache_copy(h, cache, k, v, dtype, slots, index_dtype, rows, false, hip_stream);
+}
+
+tbe_status tbe_cache_attention_workspace_bytes(const tbe_handle* h, const tbe_attention_args* args, size_t* bytes) {
+    if (!bytes) return TBE_EINVAL;
+    const tbe_status st = check_attention_sizes(h, args);
+    if (st != TBE_OK) return st;
+    if (args->head_dim % 16 != 0) return TBE_ESHAPE;
+    AttnShape sh = attention_shape(args);
+    sh.buckets = args->buckets;
+    *bytes = cache_attn_workspace(sh);
+    return TBE_OK;
+}
+
+tbe_status tbe_cache_attention(const tbe_handle* h, const tbe_attention_args* args, const tbe_cache* cache, tbe_rows out, float* lse, void* workspace,
+                               size_t workspace_bytes, void* hip_stream) {
+    CodeRows rows[2];
+    tbe_status st = check_cache(h, cache, rows);
+    if (st != TBE_OK) return st;
+    AttnArgs k;
+    st = attention_args(h, args, k, false);
+    if (st != TBE_OK) return st;
+    if (args->kv_heads != cache->heads || args->head_dim != cache->head_dim || args->k_rows != cache->rows) return TBE_ESHAPE;
+    if (!rows_view(out, args->q_rows, args->heads, args, true, k.o) || !multiple_of(lse, 4)) return TBE_EINVAL;
+    k.lse = lse;
+    const AttnShape sh = attention_shape(args);
+    const CacheAttnPlan p = cache_attn_plan(sh);
+    const size_t need = p.part_ml + p.part_o;
+    if (need > 0) {
+        if (!workspace || !multiple_of(workspace, 256)) return TBE_EINVAL;
+        if (workspace_bytes < need) return TBE_EWORKSPACE;
+    }
+    if (!cache_attn_grid_ok(sh, p)) return TBE_ESHAPE;
+    if (args->q_rows == 0) return TBE_OK;
+    return done(launch_cache_attention(h, k, rows, cache->code == TBE_CODE_I8, p, (int)args->dtype, workspace, static_cast<hipStream_t>(hip_stream)));
 }
 
 }  // extern "C"
