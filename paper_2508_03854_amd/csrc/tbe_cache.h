@@ -37,10 +37,10 @@ hipError_t launch_cache_copy(const tbe_handle* h, const CacheCopyCall& c, bool w
 
 // attention over such a cache (tbe_cache_attention.hip)
 struct CacheAttnPlan {
-    int D, pack, block, cut_log2, qblocks;   // D: elements of a row as the kernels have it; the others: see CacheAttnArgs
+    int D, pack, block, ranges, qblocks;   // D: elements of a row as the kernels have it; the others: see CacheAttnArgs
     bool own;
     int64_t V;
-    size_t part_ml, part_o;   // bytes
+    size_t spans, part_ml, part_o;   // bytes
 };
 // max_pack: heads side by side at most
 CacheAttnPlan cache_attn_plan(const AttnShape& sh, int max_pack = 32);

@@ -72,6 +72,13 @@ __device__ __forceinline__ uint4 codes_bf16(const uint32_t lo, const uint32_t hi
     }
 }
 
+// Waits until at most N of this wavefront's loads are under way (vmcnt N, the other counters as they are; see loads_done).
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+    __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | (N >> 4) << 14);
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // How many bfloat16 parts a factor of the type of q has: its significant bits, eight at a time.
 template <typename T>
 constexpr int parts() { return sizeof(T) == 4 ? 3 : (__is_same(T, bf16_t) ? 1 : 2); }
@@ -100,59 +107,83 @@ __device__ __forceinline__ void cut(float (&x)[8], uint4 (&to)[P]) {
 
 struct CacheAttnArgs : AttnArgs {
     const float *ks, *vs;   // [kv][k_rows]
-    // Parts of the keys: a sequence's rows in the cache are cut every 2^cut_log2 of them; part v of the cache belongs to sequence s if s owns it as it
-    // would own a unit of queries (see find_sequence).  qblocks: units of queries of one sequence that are handed out with each part.
-    int cut_log2, qblocks;
+    // Keys in strides of kCacheWaves tiles, all sequences' one after the other (a sequence without keys has one too), are shared out in `ranges` runs as
+    // long as each other, over the ends of sequences.  qblocks: units of queries of one sequence that go with each run.
+    int ranges, qblocks;
     int own;                // a wavefront has a unit of queries and all its keys instead
+    int2* spans;            // [N]: the first and the last run of a sequence's keys, the same where there is nothing to join
 };
 
-// The sequence of part v.  All lanes of a wavefront together, 64 offsets at a time.
-__device__ __forceinline__ int find_part(const IdxView off, const int N, const uint32_t v, const int cut_log2) {
-    int lo = 0, hi = N;
-    while (hi - lo > 1) {
-        const int step = (hi - lo + 63) / 64, s = lo + lane_id() * step;
-        const uint64_t m = __ballot(s < hi && (off[s] >> cut_log2) + s <= (int64_t)v);
-        const int k = m ? 63 - __builtin_clzll(m) : 0;
-        lo += k * step;
-        hi = hi < lo + step ? hi : lo + step;
-    }
-    return uniform(lo);
-}
-
-// What a part of the keys has to do.
-struct PartWork {
-    int block, step, blocks;   // units of queries: the first, how far to the next, the end
-    int lo, hi, parts;         // keys; into how many parts the keys of a query are cut
-};
-__device__ __forceinline__ int part_count(const CacheAttnArgs& a, const int keys) {
-    const int n = (int)(((int64_t)keys + ((int64_t)1 << a.cut_log2) - 1) >> a.cut_log2);
-    return n < 1 ? 1 : n;
-}
-// Part n of a sequence, unit qb of those that go with it; false: nothing.  Sequences with more units of queries than go with a part are not cut: their
-// parts take units in turn, with all the keys.
-__device__ __forceinline__ bool part_work(const CacheAttnArgs& a, const Sequence& q, const int n, const int qb, PartWork& w) {
-    w.blocks = (int)(((int64_t)q.nq + a.block - 1) / a.block);
-    w.parts = part_count(a, q.nk);
-    if (n >= w.parts) return false;
-    if (w.blocks > a.qblocks) {
-        w.block = n * a.qblocks + qb;
-        w.step = w.parts * a.qblocks;
-        w.lo = 0;
-        w.hi = q.nk;
-        w.parts = 1;
-    } else {
-        w.block = qb;
-        w.step = w.blocks > 0 ? w.blocks : 1;
-        w.lo = (int)((int64_t)n << a.cut_log2);
-        w.hi = w.parts == 1 ? q.nk : (int)(((int64_t)n + 1) << a.cut_log2 < q.nk ? ((int64_t)n + 1) << a.cut_log2 : q.nk);
-    }
-    return w.block < w.blocks;
-}
-
-constexpr int kCacheWaves = 4;
+constexpr int kCacheWaves = 4, kCacheThreads = 64 * kCacheWaves;
 template <int D>
 constexpr int cache_tile_rows() { return D == 128 ? 32 : 64; }
+constexpr int stride_log2(const int D) { return D == 128 ? 7 : 8; }   // (of keys)
 
+// Run r of `ranges` over all `strides` begins here; the run that a stride belongs to.
+__device__ __forceinline__ int64_t range_begin(const int64_t strides, const int ranges, const int r) { return strides * r / ranges; }
+__device__ __forceinline__ int range_of(const int64_t strides, const int ranges, const int64_t at) { return (int)(((at + 1) * ranges - 1) / strides); }
+
+// Where run r begins: the sequence, its first stride's number, and how many strides there are.  All of the workgroup together; every
+// sequence is judged on the way.  An ill-formed sequence counts as one without keys.
+struct RangeStart {
+    int64_t strides, begin;   // of all; before the sequence
+    int s;
+};
+__device__ __forceinline__ int64_t sequence_strides(const AttnArgs& a, const int s, const int log2) {
+    const LaneSequence n = lane_numbers(a, s);
+    const int64_t room = n.k1 - n.k0, keys = a.k_len.p ? a.k_len[s] : room;
+    if (n.fits && (keys < 0 || keys > room)) *a.err = 1;
+    const bool good = n.fits && keys > 0 && keys <= room;
+    return good ? (keys + ((int64_t)1 << log2) - 1) >> log2 : 1;
+}
+__device__ __forceinline__ RangeStart range_start(const CacheAttnArgs& a, const int r, const int log2) {
+    __shared__ int64_t waves[kCacheWaves];
+    __shared__ int64_t found_begin;
+    __shared__ int found;
+    const int each = (a.N + kCacheThreads - 1) / kCacheThreads, lane = lane_id(), wave = threadIdx.x >> 6;
+    const int s0 = (int)threadIdx.x * each, s1 = s0 + each < a.N ? s0 + each : a.N;
+    int64_t mine = 0;
+    for (int s = s0; s < s1; ++s) mine += sequence_strides(a, s, log2);
+    int64_t upto = mine;   // ... and of all threads before
+#pragma unroll
+    for (int k = 1; k < 64; k <<= 1) {
+        const int64_t x = __shfl_up(upto, k);
+        if (lane >= k) upto += x;
+    }
+    if (lane == 63) waves[wave] = upto;
+    __syncthreads();
+    RangeStart out;
+    out.strides = 0;
+#pragma unroll
+    for (int k = 0; k < kCacheWaves; ++k) {
+        if (k < wave) upto += waves[k];
+        out.strides += waves[k];
+    }
+    const int64_t at = range_begin(out.strides, a.ranges, r);
+    int64_t begin = upto - mine;
+    if (at >= begin && at < upto) {
+        int s = s0;
+        for (; s + 1 < s1; ++s) {
+            const int64_t n = sequence_strides(a, s, log2);
+            if (at < begin + n) break;
+            begin += n;
+        }
+        found = s;
+        found_begin = begin;
+    }
+    __syncthreads();
+    out.s = uniform(found);
+    out.begin = lane_i64(found_begin, 0);
+    out.strides = lane_i64(out.strides, 0);
+    return out;
+}
+
+// What a workgroup does with the part of a sequence's keys that lies in its run.
+struct PartWork {
+    int block, step, blocks;   // units of queries: the first, how far to the next, the end
+    int lo, hi;                // keys
+    int cell;                  // 0, 1: where the results go to be joined; -1: these are all keys
+};
 template <typename T, int D, bool I8, bool BIAS>
 __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attn_kernel(const CacheAttnArgs a) {
     constexpr int kWaves = kCacheWaves, BK = cache_tile_rows<D>(), kT = BK / 32, kD = D / 32, kC = D / 16, kP = parts<T>();
@@ -161,56 +192,88 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attn_kernel(const C
     typedef CodeTile<D> Codes;
     // two buffers each, as arrays of their own: loads into one of them are seen not to concern what is read from another
     __shared__ __align__(16) char keys0[kWaves * kTile], keys1[kWaves * kTile], values0[kWaves * kTile], values1[kWaves * kTile];
-    __shared__ __align__(16) float scales0[kWaves * 2 * BK], scales1[kWaves * 2 * BK];   // keys' and values' of each wavefront's tile
+    __shared__ __align__(16) float key_scales0[kWaves * 64], key_scales1[kWaves * 64], value_scales0[kWaves * 64], value_scales1[kWaves * 64];
     __shared__ float2 stats[kWaves * 32];
     extern __shared__ float tab[];
     static_assert(kWaves * kTile >= 32 * D * 4, "a wavefront's results find room in one of the arrays");
-    const int wave = uniform(threadIdx.x >> 6), lane = lane_id(), col = lane & 31, half = lane >> 5;
-    const int packs = a.H / a.pack;
+    const int wave = uniform(threadIdx.x >> 6), packs = a.H / a.pack;
 
-    // the heads; the part of the keys and the unit of queries that go with it, or this wavefront's unit of queries
-    int hh, qb = 0;
-    uint32_t v;
+    // the heads; the run of keys and the unit of queries that goes with it, or this wavefront's unit of queries
+    int hh, qb = 0, r = 0;
+    uint32_t v = 0;
     if (a.own) {
         const uint32_t groups = ((uint32_t)a.V + kWaves - 1) / kWaves * (uint32_t)packs, wg = die_order(groups);
         if (wg >= groups) return;
         hh = uniform((int)(wg % (uint32_t)packs));
         v = uniform((int)(wg / (uint32_t)packs * kWaves + wave));
     } else {
-        // Parts are dealt to the 8 dies one by one, and each die has all heads and units of queries of its parts, which read the same lines.
-        const uint32_t wg = blockIdx.y * gridDim.x + blockIdx.x, each = (uint32_t)packs * a.qblocks, n = wg >> 3, turn = n / each, rest = n - turn * each;
-        v = uniform((int)(turn * 8 + (wg & 7u)));
+        // Runs are dealt to the 8 dies one by one, and each die has all heads and units of queries of its runs, which read the same lines.
+        const uint32_t wg = blockIdx.y * gridDim.x + blockIdx.x, each = (uint32_t)packs * a.qblocks, dies = a.ranges >= 8 ? 8 : 1;
+        const uint32_t n = wg / dies, turn = n / each, rest = n - turn * each;
+        r = uniform((int)(turn * dies + wg % dies));
         hh = uniform((int)(rest % (uint32_t)packs));
         qb = uniform((int)(rest / (uint32_t)packs));
-        if (v >= (uint32_t)a.V) return;
+        if (r >= a.ranges) return;
     }
     const int head0 = hh * a.pack;
     if (BIAS) {
-        fill_bias(tab, a, head0, a.pack, 64 * kWaves);
+        fill_bias(tab, a, head0, a.pack, kCacheThreads);
         __syncthreads();
     }
-    if (v >= (uint32_t)a.V) return;
-    const bool looks = hh == 0 && qb == 0 && (a.own || wave == 0) && v < (uint32_t)a.N;
-    const int64_t peek = looks ? sequence_numbers(a, v) : 0;
+    constexpr int kLog = stride_log2(D);
+    static_assert(1 << kLog == kWaves * BK, "a stride is a tile for each wavefront");
+    const bool looks = a.own && hh == 0 && v < (uint32_t)a.N;
+    int64_t peek = 0, at = 0, end = 1, begin = 0, strides = 0;   // own: one turn of the loop below
+    int s = 0;
+    if (a.own) {
+        if (v >= (uint32_t)a.V) return;
+        peek = looks ? sequence_numbers(a, v) : 0;
+        s = find_sequence(a.q_off, a.N, v, a.block);
+    } else {
+        const RangeStart start = range_start(a, r, kLog);
+        s = start.s;
+        begin = start.begin;
+        strides = start.strides;
+        at = range_begin(strides, a.ranges, r);
+        end = range_begin(strides, a.ranges, r + 1);
+    }
+    for (; at < end; ++s) {
     Sequence q;
     PartWork w;
-    int part = 0;
+    const bool fits = take_sequence(a, s, sequence_numbers(a, s), q);
     if (a.own) {
-        const int s = find_sequence(a.q_off, a.N, v, a.block);
-        const bool fits = take_sequence(a, s, sequence_numbers(a, s), q);
         const uint32_t start = (uint32_t)q.q0 / a.block + s, blocks = ((uint32_t)q.nq + a.block - 1) / a.block;
         if (!fits || v < start || v - start >= blocks) return judge(a, looks, v, peek);
         w.block = uniform((int)(v - start));
         w.blocks = w.block + 1;
-        w.step = w.parts = 1;
+        w.step = 1;
         w.lo = 0;
         w.hi = q.nk;
+        w.cell = -1;
+        at = end;
     } else {
-        const int s = find_part(a.k_off, a.N, v, a.cut_log2);
-        const bool fits = take_sequence(a, s, sequence_numbers(a, s), q);
-        const int64_t n = (int64_t)v - (s + (q.k0 >> a.cut_log2));
-        part = uniform((int)n);
-        if (!fits || n < 0 || n > q.nk || !part_work(a, q, part, qb, w)) return judge(a, looks, v, peek);
+        const int64_t n = fits && q.nk > 0 ? ((int64_t)q.nk + kWaves * BK - 1) >> kLog : 1;
+        const int64_t a0 = at - begin, a1 = end - begin < n ? end - begin : n;   // strides of this sequence
+        w.blocks = (int)(((int64_t)q.nq + a.block - 1) / a.block);
+        w.block = qb;
+        w.step = a.qblocks;
+        w.lo = (int)(a0 << kLog);
+        w.hi = a1 < n ? (int)(a1 << kLog) : q.nk;
+        w.cell = a0 > 0 ? 0 : (a1 < n ? 1 : -1);
+        if (w.blocks > a.qblocks) {
+            // More units of queries than go with a run: units in turn, with all the keys.  Turn m belongs to the run with stride m n / turns.
+            const int64_t turns = (w.blocks + a.qblocks - 1) / a.qblocks, m0 = (a0 * turns + n - 1) / n, m1 = (a1 * turns + n - 1) / n;
+            w.block = (int)m0 * a.qblocks + qb;
+            w.blocks = w.blocks < (int)m1 * a.qblocks ? w.blocks : (int)m1 * a.qblocks;
+            w.lo = 0;
+            w.hi = q.nk;
+            w.cell = -1;
+        }
+        if (a0 == 0 && hh == 0 && qb == 0 && threadIdx.x == 0)
+            a.spans[s] = w.cell < 0 ? make_int2(0, 0) : make_int2(r, range_of(strides, a.ranges, begin + n - 1));
+        begin += n;
+        at = begin;
+        if (!fits) continue;
     }
 
     const int kvh = head0 / a.group;
@@ -218,17 +281,18 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attn_kernel(const C
     const char* const vb = a.v.at(q.k0, kvh);
     const float* const ks = a.ks + (int64_t)kvh * a.k_rows + q.k0;
     const float* const vs = a.vs + (int64_t)kvh * a.k_rows + q.k0;
-    const int own = wave * kTile, own_scales = wave * 2 * BK, ci = col / a.pack, cg = col - ci * a.pack, head = head0 + cg;
+    const int own = wave * kTile, own_scales = wave * 64;
     const int t_step = a.own ? 1 : kWaves;
-    float beyond = 0.f, ahead = 0.f;
-    const float* const ht = tab + cg * tab_size(a.far);
-    if (BIAS) {
-        beyond = ht[kTabMargin];
-        ahead = a.causal ? 0.f : ht[2 * a.far + kTabMargin];
-    }
-
     for (int block = w.block; block < w.blocks; block += w.step) {
+        const int lane = anew(lane_id()), col = lane & 31, half = lane >> 5;
+        const int ci = col / a.pack, cg = col - ci * a.pack, head = head0 + cg;
         const int iw = block * a.block, i = iw + ci;
+        float beyond = 0.f, ahead = 0.f;
+        const float* const ht = tab + cg * tab_size(a.far);
+        if (BIAS) {
+            beyond = ht[kTabMargin];
+            ahead = a.causal ? 0.f : ht[2 * a.far + kTabMargin];
+        }
         const bool is = ci < a.qpt && i < q.nq;
         const int first = q.nk - q.nq + iw, pos = first + ci, wave_last = first + a.qpt - 1;   // places among the keys
         int jend = w.hi;   // keys of this unit: all that its last query sees
@@ -280,23 +344,18 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attn_kernel(const C
             m = -__builtin_inff();
             sum = 0.f;
         };
-        auto fetch = [&](const int t, char* const kt, char* const vt, float* const st) __attribute__((always_inline)) {
-            const int j0 = w.lo + t * BK;
-            Codes::template fetch<BK>(kt + own, kb, a.k.row, j0, q.nk, a.dim, lane);
-            Codes::template fetch<BK>(vt + own, vb, a.v.row, j0, q.nk, a.dim, lane);
-#pragma unroll
-            for (int n = 0; n < 2 * BK / 64; ++n) {
-                const int at = 64 * n + lane, j = j0 + (at & (BK - 1));
-                const float* const src = (at < BK ? ks : vs) + j;
-                load_lds<4>(j < q.nk ? reinterpret_cast<const char*>(src) : reinterpret_cast<const char*>(&attn_zeros), st + own_scales + 64 * n);
-            }
+        auto fetch = [&](const int t, char* const to, float* const st, const char* const from, const int64_t stride, const float* const scales, const int l) __attribute__((always_inline)) {
+            const int j0 = w.lo + t * BK, j = j0 + (l & (BK - 1));
+            Codes::template fetch<BK>(to + own, from, stride, j0, q.nk, a.dim, l);
+            load_lds<4>(j < q.nk ? reinterpret_cast<const char*>(scales + j) : reinterpret_cast<const char*>(&attn_zeros), st + own_scales);
         };
-        auto step = [&](const int t, const char* const kt_, const char* const vt_, const float* const st_) __attribute__((always_inline)) {
-            const int j0 = w.lo + t * BK;
+        auto fetch_keys = [&](const int t, char* const to, float* const st, const int l) __attribute__((always_inline)) { fetch(t, to, st, kb, a.k.row, ks, l); };
+        auto fetch_values = [&](const int t, char* const to, float* const st, const int l) __attribute__((always_inline)) { fetch(t, to, st, vb, a.v.row, vs, l); };
+        f32x16_t x[kT];   // a tile's scores
+        auto scores = [&](const int t, const char* const kt_, const float* const st_, const int l) __attribute__((always_inline)) {
+            const int j0 = w.lo + t * BK, col = l & 31, half = l >> 5;
             const char* const kt = kt_ + own;
-            const char* const vt = vt_ + own;
             const float* const st = st_ + own_scales;
-            f32x16_t x[kT];
 #pragma unroll
             for (int k = 0; k < kT; ++k) {
                 x[k] = f32x16_t{};
@@ -313,7 +372,6 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attn_kernel(const C
             }
             settle<bf16_t>();
             const bool hides = j0 + BK > q.nk || (a.causal && j0 + BK - 1 > first);
-            float top = -__builtin_inff();
 #pragma unroll
             for (int k = 0; k < kT; ++k) {
 #pragma unroll
@@ -346,6 +404,12 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attn_kernel(const C
                     for (int r = 0; r < 16; ++r)
                         if (j0 + 32 * k + 8 * (r / 4) + 4 * half + r % 4 >= upto) x[k][r] = -__builtin_inff();
             }
+        };
+        auto apply = [&](const char* const vt_, const float* const st_, const int l) __attribute__((always_inline)) {
+            const int half = l >> 5;
+            const char* const vt = vt_ + own;
+            const float* const st = st_ + own_scales;
+            float top = -__builtin_inff();
 #pragma unroll
             for (int k = 0; k < kT; ++k)
 #pragma unroll
@@ -372,7 +436,7 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attn_kernel(const C
                     float p[8];
 #pragma unroll
                     for (int r = 0; r < 8; r += 4) {
-                        const float4 s4 = *reinterpret_cast<const float4*>(st + BK + 32 * k + 16 * c + 2 * r + 4 * half);
+                        const float4 s4 = *reinterpret_cast<const float4*>(st + 32 * k + 16 * c + 2 * r + 4 * half);
                         const float s[4] = {s4.x, s4.y, s4.z, s4.w};
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
@@ -387,7 +451,7 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attn_kernel(const C
                     cut<kP>(p, f);
 #pragma unroll
                     for (int d = 0; d < kD; ++d) {
-                        const uint2 u = Codes::down(vt, 32 * k, c, d, lane);
+                        const uint2 u = Codes::down(vt, 32 * k, c, d, l);
                         const uint4 g = codes_bf16<I8>(u.x, u.y);
 #pragma unroll
                         for (int p = kP - 1; p >= 0; --p) o[d] = M::mma(g, f[p], o[d]);
@@ -397,8 +461,8 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attn_kernel(const C
         };
         // Codes that are not numbers (e4m3) among the values: a column that does not see their key would get 0 times them from the matrix cores.  They
         // are taken out of the tile, and the columns that see the key get NaN where they stood.
-        auto take_out = [&](const int t) __attribute__((always_inline)) {
-            const int j0 = w.lo + t * BK;
+        auto take_out = [&](const int t, const int l) __attribute__((always_inline)) {
+            const int j0 = w.lo + t * BK, half = l >> 5;
             char* const vt = values0 + own;
             const int upto = a.causal && pos + 1 < q.nk ? pos + 1 : q.nk;
 #pragma unroll 1
@@ -423,7 +487,7 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attn_kernel(const C
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll 1
-            for (int n = lane; n < kTile / 4; n += 64) {
+            for (int n = l; n < kTile / 4; n += 64) {
                 uint32_t u = *reinterpret_cast<const uint32_t*>(vt + 4 * n);
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
@@ -433,26 +497,49 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attn_kernel(const C
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         };
 
-        begin();
-        if (t0 < tiles) fetch(t0, keys0, values0, scales0);
-        for (int t = t0; t < tiles; t += 2 * t_step) {
-            loads_done();
-            if (t + t_step < tiles) fetch(t + t_step, keys1, values1, scales1);
-            step(t, keys0, values0, scales0);
-            if (t + t_step < tiles) {
-                loads_done();
-                if (t + 2 * t_step < tiles) fetch(t + 2 * t_step, keys0, values0, scales0);
-                step(t + t_step, keys1, values1, scales1);
+        // Two tiles of keys and of values are under way or in use; a buffer is filled anew as soon as its tile has been multiplied, so that the loads have
+        // a tile's time and a half.  They end in their order: of those begun after the ones waited for, so many may still run.
+        constexpr int kGroup = BK * D / 1024 + 1;
+        auto one = [&](const int t, char* const kt, float* const kst, char* const vt, float* const vst) __attribute__((always_inline)) {
+            const bool next = t + t_step < tiles, after = t + 2 * t_step < tiles;
+            if (next) wait_loads<3 * kGroup>();
+            else wait_loads<kGroup>();
+            scores(t, kt, kst, lane);
+            if (after) {
+                fetch_keys(t + 2 * t_step, kt, kst, lane);
+                wait_loads<3 * kGroup>();
+            } else if (next) {
+                wait_loads<2 * kGroup>();
+            } else {
+                wait_loads<0>();
             }
+            apply(vt, vst, lane);
+            if (after) fetch_values(t + 2 * t_step, vt, vst, lane);
+        };
+        begin();
+        if (t0 < tiles) {
+            fetch_keys(t0, keys0, key_scales0, lane);
+            fetch_values(t0, values0, value_scales0, lane);
+        }
+        if (t0 + t_step < tiles) {
+            fetch_keys(t0 + t_step, keys1, key_scales1, lane);
+            fetch_values(t0 + t_step, values1, value_scales1, lane);
+        }
+        for (int t = t0; t < tiles; t += 2 * t_step) {
+            one(t, keys0, key_scales0, values0, value_scales0);
+            if (t + t_step < tiles) one(t + t_step, keys1, key_scales1, values1, value_scales1);
         }
         if (!I8 && (a.causal || BIAS) && __any(is && not_finite(o))) {
             begin();
 #pragma unroll 1
             for (int t = t0; t < tiles; t += t_step) {
-                fetch(t, keys0, values0, scales0);
+                const int l = anew(lane);   // (few registers: nothing of this is kept through the loop above)
+                fetch_keys(t, keys0, key_scales0, l);
+                fetch_values(t, values0, value_scales0, l);
                 loads_done();
-                take_out(t);
-                step(t, keys0, values0, scales0);
+                take_out(t, l);
+                scores(t, keys0, key_scales0, l);
+                apply(values0, value_scales0, l);
             }
         }
         sum = pair_sum<32>(sum);
@@ -508,8 +595,8 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attn_kernel(const C
                 x.x = fmaf(y.x, by, x.x); x.y = fmaf(y.y, by, x.y);
                 x.z = fmaf(y.z, by, x.z); x.w = fmaf(y.w, by, x.w);
             }
-            if (w.parts > 1) {
-                const int64_t cell = (((int64_t)v * a.qblocks + qb) * packs + hh) * 32 + c;
+            if (w.cell >= 0) {
+                const int64_t cell = (((int64_t)(2 * r + w.cell) * a.qblocks + qb) * packs + hh) * 32 + c;
                 if (e == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * cell) = make_float2(top, total);
                 *reinterpret_cast<float4*>(a.part_o + cell * D + 4 * e) = x;
                 continue;
@@ -524,10 +611,12 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attn_kernel(const C
         }
         __syncthreads();   // (the next unit's tiles go where these results are)
     }
-    judge(a, looks, v, peek);
+    }
+    if (a.own) judge(a, looks, v, peek);
 }
 
-// Joins the parts of the keys: a workgroup per query and head, its four wavefronts a quarter of the parts each; the order of the additions is fixed.
+// Joins the parts of the keys: a workgroup for four heads of a query, a wavefront for each; where there are many parts, all four for one head after
+// the other, a quarter of the parts each.  The order of the additions is fixed.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void cache_attn_join_kernel(const CacheAttnArgs a) {
     constexpr int kPer = D >= 64 ? D / 64 : 1, kAhead = 8;   // elements a lane; parts under way together
@@ -535,70 +624,81 @@ __global__ __launch_bounds__(256) void cache_attn_join_kernel(const CacheAttnArg
     __shared__ float2 stats[4];
     __shared__ out_t sums[4][64];
     const int lane = lane_id(), wave = uniform(threadIdx.x >> 6), packs = a.H / a.pack;
-    const uint32_t n = blockIdx.y * gridDim.x + blockIdx.x;
-    const int64_t row = n / (uint32_t)a.H;
-    const int head = (int)(n - (uint32_t)row * (uint32_t)a.H);
+    const uint32_t n = blockIdx.y * gridDim.x + blockIdx.x, fours = ((uint32_t)a.H + 3) / 4;
+    const int64_t row = n / fours;
+    const int four = (int)(n - (uint32_t)row * fours) * 4;
     if (row >= a.q_rows) return;
     const int s = find_row(a.q_off, a.N, row);
     Sequence q;
+    const int2 span = a.spans[s];
     if (!take_sequence(a, s, sequence_numbers(a, s), q) || row < q.q0 || row >= q.q0 + q.nq) return;
-    const int i = (int)(row - q.q0), qb = i / a.block, blocks = (int)(((int64_t)q.nq + a.block - 1) / a.block), count = part_count(a, q.nk);
-    if (blocks > a.qblocks || count < 2) return;   // (the result is there already)
-    const int hh = head / a.pack, col = (i - qb * a.block) * a.pack + head - hh * a.pack;
-    const int64_t each = (int64_t)a.qblocks * packs * 32;   // cells of a part
-    const int64_t cell0 = (s + (q.k0 >> a.cut_log2)) * each + ((int64_t)qb * packs + hh) * 32 + col;
-    const float2* const ml = reinterpret_cast<const float2*>(a.part_ml) + cell0;
-    const int quarter = (count + 3) / 4, p0 = wave * quarter, p1 = p0 + quarter < count ? p0 + quarter : count;
-    float m = -__builtin_inff(), sum = 0.f;
-    for (int p = p0 + lane; p < p1; p += 64) m = fmaxf(m, ml[p * each].x);
-#pragma unroll
-    for (int k = 32; k; k >>= 1) m = fmaxf(m, __shfl_xor(m, k));
-    const float at = m == -__builtin_inff() ? 0.f : m;
-    out_t o = {};
+    if (span.x >= span.y) return;   // (the result is there already)
+    const int i = (int)(row - q.q0), qb = i / a.block, count = span.y - span.x + 1;
+    const bool many = count > 16;
+    const int64_t each = (int64_t)a.qblocks * packs * 32;   // cells of half a run's: a run has two, for the sequence that it continues and the one that it begins
     const int e0 = (lane * kPer) & (D - 1);   // (rows of 32 elements: the upper half of the wavefront does the same again)
-    for (int base = p0; base < p1; base += 64) {
-        const bool mine = base + lane < p1;
-        const float2 c = mine ? ml[(base + lane) * each] : make_float2(-__builtin_inff(), 0.f);
-        const float by = mine ? __builtin_amdgcn_exp2f(c.x - at) : 0.f;
-        sum += group_sum(c.y * by, 64);
-        const int end = p1 - base < 64 ? p1 - base : 64;
-        const float* const from = a.part_o + (cell0 + base * each) * D + e0;
-        for (int k = 0; k < end; k += kAhead) {
-            out_t x[kAhead];
+    for (int k = many ? 0 : wave; k < 4; k += many ? 1 : 4) {
+        const int head = four + k;
+        if (head >= a.H) break;
+        const int hh = head / a.pack, col = (i - qb * a.block) * a.pack + head - hh * a.pack;
+        const int64_t cell0 = ((int64_t)qb * packs + hh) * 32 + col;
+        const auto cell_of = [&](const int p) __attribute__((always_inline)) { return cell0 + (2 * (int64_t)(span.x + p) + (p == 0)) * each; };
+        const float2* const ml = reinterpret_cast<const float2*>(a.part_ml);
+        const int share = many ? (count + 3) / 4 : count, p0 = many ? wave * share : 0, p1 = p0 + share < count ? p0 + share : count;
+        float m = -__builtin_inff(), sum = 0.f;
+        for (int p = p0 + lane; p < p1; p += 64) m = fmaxf(m, ml[cell_of(p)].x);
 #pragma unroll
-            for (int j = 0; j < kAhead; ++j) x[j] = *reinterpret_cast<const out_t*>(from + (int64_t)(k + j < end ? k + j : k) * each * D);
+        for (int x = 32; x; x >>= 1) m = fmaxf(m, __shfl_xor(m, x));
+        const float at = m == -__builtin_inff() ? 0.f : m;
+        out_t o = {};
+        for (int base = p0; base < p1; base += 64) {
+            const bool mine = base + lane < p1;
+            const float2 c = mine ? ml[cell_of(base + lane)] : make_float2(-__builtin_inff(), 0.f);
+            const float by = mine ? __builtin_amdgcn_exp2f(c.x - at) : 0.f;
+            sum += group_sum(c.y * by, 64);
+            const int end = p1 - base < 64 ? p1 - base : 64;
+            for (int p = 0; p < end; p += kAhead) {
+                out_t x[kAhead];
 #pragma unroll
-            for (int j = 0; j < kAhead; ++j)
-                if (k + j < end) o += bcast_lane(by, (k + j) & 63) * x[j];
+                for (int j = 0; j < kAhead; ++j) x[j] = *reinterpret_cast<const out_t*>(a.part_o + cell_of(base + (p + j < end ? p + j : p)) * D + e0);
+#pragma unroll
+                for (int j = 0; j < kAhead; ++j)
+                    if (p + j < end) o += bcast_lane(by, (p + j) & 63) * x[j];
+            }
         }
+        if (many) {
+            if (lane == 0) stats[wave] = make_float2(m, sum);
+            sums[wave][lane] = o;
+            __syncthreads();
+            float top = -__builtin_inff();
+#pragma unroll
+            for (int x = 0; x < 4; ++x) top = fmaxf(top, stats[x].x);
+            const float all = top == -__builtin_inff() ? 0.f : top;
+            m = top;
+            sum = 0.f;
+            o = out_t{};
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const float by = __builtin_amdgcn_exp2f(stats[x].x - all);
+                sum = fmaf(stats[x].y, by, sum);
+                o += by * sums[x][lane];
+            }
+            __syncthreads();
+            if (wave != 0) continue;
+        }
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        T* const to = reinterpret_cast<T*>(const_cast<char*>(a.o.at(row, head)));
+#pragma unroll
+        for (int e = 0; e < kPer; ++e)
+            if (e0 + e < a.dim) to[e0 + e] = elem_round<T>((kPer == 1 ? o[0] : o[e]) * inv);
+        if (a.lse && lane == 0) a.lse[(int64_t)head * a.q_rows + row] = sum == 0.f ? -__builtin_inff() : fmaf(m, kLn2, logf(sum));
     }
-    if (lane == 0) stats[wave] = make_float2(m, sum);
-    sums[wave][lane] = o;
-    __syncthreads();
-    if (wave != 0) return;
-    float top = -__builtin_inff(), total = 0.f;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) top = fmaxf(top, stats[k].x);
-    const float all = top == -__builtin_inff() ? 0.f : top;
-    out_t x = {};
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const float by = __builtin_amdgcn_exp2f(stats[k].x - all);
-        total = fmaf(stats[k].y, by, total);
-        x += by * sums[k][lane];
-    }
-    const float inv = total == 0.f ? 0.f : 1.f / total;
-    T* const to = reinterpret_cast<T*>(const_cast<char*>(a.o.at(row, head)));
-#pragma unroll
-    for (int e = 0; e < kPer; ++e)
-        if (e0 + e < a.dim) to[e0 + e] = elem_round<T>((kPer == 1 ? x[0] : x[e]) * inv);
-    if (a.lse && lane == 0) a.lse[(int64_t)head * a.q_rows + row] = total == 0.f ? -__builtin_inff() : fmaf(top, kLn2, logf(total));
 }
 
 // How the work is shared out.  Heads of a group lie side by side in a wavefront's columns where one query would leave them empty.  Short caches, or
-// so many units of queries that the chip is full: a wavefront for each unit.  Otherwise the four wavefronts of a workgroup have the same columns and
-// every fourth tile of a part of the keys, joined in LDS; parts are cut so that there are at least kPartGroups workgroups.
-constexpr int64_t kPartGroups = 2048;
+// so many units of queries that the chip is full: a wavefront for each unit.  Otherwise as many workgroups as the chip holds at once share all
+// keys evenly among them.
+constexpr int64_t kRangeGroups = 512;
 CacheAttnPlan cache_attn_plan(const AttnShape& sh, const int max_pack) {
     CacheAttnPlan p;
     const int64_t mean_q = (sh.q_rows + sh.N - 1) / sh.N, mean_k = (sh.k_rows + sh.N - 1) / sh.N;
@@ -611,28 +711,29 @@ CacheAttnPlan cache_attn_plan(const AttnShape& sh, const int max_pack) {
     p.block = 32 / p.pack;
     const int64_t packs = sh.H / p.pack, units = (sh.q_rows / p.block + sh.N) * packs;
     p.own = mean_k <= 128 || (units >= 4096 && mean_k <= 2048);
-    p.cut_log2 = 32;
-    p.qblocks = 1;
+    p.ranges = p.qblocks = 1;
     p.V = sh.q_rows / p.block + sh.N;
-    p.part_ml = p.part_o = 0;
+    p.spans = p.part_ml = p.part_o = 0;
     if (p.own) return p;
-    // units of queries of a sequence that go with each part: of all sequences that are not much longer than the average
-    p.qblocks = (int)std::max<int64_t>(1, (mean_q + mean_q / 4 + p.block - 1) / p.block);
+    p.qblocks = (int)std::max<int64_t>(1, (mean_q + p.block - 1) / p.block);
     const int64_t each = packs * p.qblocks;
-    p.V = sh.N;
-    for (int c = 31; c >= 8; --c) {
-        if (p.V * each >= kPartGroups) break;
-        p.cut_log2 = c;
-        p.V = (sh.k_rows >> c) + sh.N;
-    }
-    const int64_t cells = p.cut_log2 < 32 ? p.V * each * 32 : 0;
+    p.ranges = (int)std::max<int64_t>(1, kRangeGroups / each);
+    if (p.ranges >= 8) p.ranges &= ~7;
+    // no more than there are strides
+    p.ranges = (int)std::min<int64_t>(p.ranges, (sh.k_rows >> stride_log2(p.D)) + sh.N);
+    p.spans = ((size_t)sh.N * sizeof(int2) + 255) & ~(size_t)255;
+    const int64_t cells = p.ranges > 1 ? 2 * p.ranges * each * 32 : 0;
     p.part_ml = ((size_t)cells * 8 + 255) & ~(size_t)255;
     p.part_o = ((size_t)cells * p.D * 4 + 255) & ~(size_t)255;
     return p;
 }
+static int64_t plan_groups(const AttnShape& sh, const CacheAttnPlan& p) {
+    const int64_t packs = sh.H / p.pack;
+    return p.own ? (p.V + 3) / 4 * packs : (p.ranges >= 8 ? (p.ranges + 7) / 8 * 8 : (int64_t)p.ranges) * packs * p.qblocks;
+}
 bool cache_attn_grid_ok(const AttnShape& sh, const CacheAttnPlan& p) {
-    const int64_t most = ((int64_t)1 << 31) - 64, packs = sh.H / p.pack;
-    return p.own ? (p.V + 3) / 4 * packs < most : (p.V + 7) / 8 * 8 * packs * p.qblocks < most && (p.part_ml == 0 || sh.q_rows * sh.H < most);
+    const int64_t most = ((int64_t)1 << 31) - 64;
+    return plan_groups(sh, p) < most && (p.part_ml == 0 || sh.q_rows * ((sh.H + 3) / 4) < most);
 }
 size_t cache_attn_workspace(const AttnShape& sh) {
     size_t most = 0;
@@ -640,7 +741,7 @@ size_t cache_attn_workspace(const AttnShape& sh) {
         AttnShape any = sh;
         any.far = 0;
         const CacheAttnPlan p = cache_attn_plan(any, pack);
-        most = std::max(most, p.part_ml + p.part_o);
+        most = std::max(most, p.spans + p.part_ml + p.part_o);
     }
     return most;
 }
@@ -662,7 +763,7 @@ static hipError_t launch_dim(const tbe_handle* h, const CacheAttnArgs& a, const 
     const hipError_t e = i8 ? launch_parts<T, D, true>(h, a, groups, s) : launch_parts<T, D, false>(h, a, groups, s);
     if (e != hipSuccess || !join) return e;
     LaunchTimer tm(h, s, "cache_attention_join");
-    cache_attn_join_kernel<T, D><<<die_grid((uint64_t)a.q_rows * (uint64_t)a.H), 256, 0, s>>>(a);
+    cache_attn_join_kernel<T, D><<<die_grid((uint64_t)a.q_rows * (((uint64_t)a.H + 3) / 4)), 256, 0, s>>>(a);
     tm.done();
     return hipGetLastError();
 }
@@ -678,11 +779,13 @@ hipError_t launch_cache_attention(const tbe_handle* h, const AttnArgs& call, con
     a.k = cache[0].codes; a.v = cache[1].codes;
     a.ks = cache[0].scales; a.vs = cache[1].scales;
     a.pack = p.pack; a.qpt = a.block = p.block; a.V = (int)p.V;
-    a.cut_log2 = p.cut_log2; a.qblocks = p.qblocks; a.own = p.own;
-    a.part_ml = static_cast<float*>(workspace);
-    a.part_o = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.part_ml);
-    const uint64_t packs = (uint64_t)(a.H / a.pack);
-    const uint64_t groups = p.own ? ((uint64_t)p.V + 3) / 4 * packs : ((uint64_t)p.V + 7) / 8 * 8 * packs * (uint64_t)p.qblocks;
+    a.ranges = p.ranges; a.qblocks = p.qblocks; a.own = p.own;
+    a.spans = static_cast<int2*>(workspace);
+    a.part_ml = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.spans);
+    a.part_o = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.spans + p.part_ml);
+    AttnShape sh{};
+    sh.H = a.H;
+    const uint64_t groups = (uint64_t)plan_groups(sh, p);
     const bool join = p.part_ml > 0;
     return io == 0 ? launch_type<float>(h, a, p.D, i8, groups, join, s) : (io == 1 ? launch_type<__half>(h, a, p.D, i8, groups, join, s) : launch_type<bf16_t>(h, a, p.D, i8, groups, join, s));
 }

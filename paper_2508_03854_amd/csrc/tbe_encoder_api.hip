@@ -356,7 +356,7 @@ tbe_status tbe_cache_attention(const tbe_handle* h, const tbe_attention_args* ar
     k.lse = lse;
     const AttnShape sh = attention_shape(args);
     const CacheAttnPlan p = cache_attn_plan(sh);
-    const size_t need = p.part_ml + p.part_o;
+    const size_t need = p.spans + p.part_ml + p.part_o;
     if (need > 0) {
         if (!workspace || !multiple_of(workspace, 256)) return TBE_EINVAL;
         if (workspace_bytes < need) return TBE_EWORKSPACE;
