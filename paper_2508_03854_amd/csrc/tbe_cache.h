@@ -38,7 +38,7 @@ hipError_t launch_cache_copy(const tbe_handle* h, const CacheCopyCall& c, bool w
 // attention over such a cache (tbe_cache_attention.hip)
 struct CacheAttnPlan {
     int D, pack, block, ranges, qblocks;   // D: elements of a row as the kernels have it; the others: see CacheAttnArgs
-    bool own;
+    bool own, direct;
     int64_t V;
     size_t spans, part_ml, part_o;   // bytes
 };

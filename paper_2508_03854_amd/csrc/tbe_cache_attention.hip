@@ -8,6 +8,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "tbe_cache.h"
 
@@ -107,29 +108,27 @@ __device__ __forceinline__ void cut(float (&x)[8], uint4 (&to)[P]) {
 
 struct CacheAttnArgs : AttnArgs {
     const float *ks, *vs;   // [kv][k_rows]
-    // Keys in strides of kCacheWaves tiles, all sequences' one after the other (a sequence without keys has one too), are shared out in `ranges` runs as
-    // long as each other, over the ends of sequences.  qblocks: units of queries of one sequence that go with each run.
+    // The tiles of keys of all sequences, one after the other (a sequence without keys has one too), are shared out in `ranges` runs as long as each
+    // other, over the ends of sequences, a run for a wavefront.  qblocks: units of queries of one sequence that go with each run.
     int ranges, qblocks;
-    int own;                // a wavefront has a unit of queries and all its keys instead
+    int own;                // a wavefront has a unit of queries and all its keys instead; 2: all queries of a sequence
     int2* spans;            // [N]: the first and the last run of a sequence's keys, the same where there is nothing to join
 };
 
 constexpr int kCacheWaves = 4, kCacheThreads = 64 * kCacheWaves;
-template <int D>
-constexpr int cache_tile_rows() { return D == 128 ? 32 : 64; }
-constexpr int stride_log2(const int D) { return D == 128 ? 7 : 8; }   // (of keys)
+constexpr int kTileLog2 = 5;   // keys of a tile
 
-// Run r of `ranges` over all `strides` begins here; the run that a stride belongs to.
-__device__ __forceinline__ int64_t range_begin(const int64_t strides, const int ranges, const int r) { return strides * r / ranges; }
-__device__ __forceinline__ int range_of(const int64_t strides, const int ranges, const int64_t at) { return (int)(((at + 1) * ranges - 1) / strides); }
+// Run r of `ranges` over all `tiles` begins here; the run that a tile belongs to.
+__device__ __forceinline__ int64_t range_begin(const int64_t tiles, const int ranges, const int r) { return tiles * r / ranges; }
+__device__ __forceinline__ int range_of(const int64_t tiles, const int ranges, const int64_t at) { return (int)(((at + 1) * ranges - 1) / tiles); }
 
-// Where run r begins: the sequence, its first stride's number, and how many strides there are.  All of the workgroup together; every
-// sequence is judged on the way.  An ill-formed sequence counts as one without keys.
+// Where run r begins: the sequence, the number of its first tile, and how many tiles there are in all.  r: of the workgroup's first wavefront, the
+// others have the next ones.  All of the workgroup together; every sequence is judged on the way.  An ill-formed sequence counts as one without keys.
 struct RangeStart {
-    int64_t strides, begin;   // of all; before the sequence
+    int64_t tiles, begin;
     int s;
 };
-__device__ __forceinline__ int64_t sequence_strides(const AttnArgs& a, const int s, const int log2) {
+__device__ __forceinline__ int64_t sequence_tiles(const AttnArgs& a, const int s, const int log2) {
     const LaneSequence n = lane_numbers(a, s);
     const int64_t room = n.k1 - n.k0, keys = a.k_len.p ? a.k_len[s] : room;
     if (n.fits && (keys < 0 || keys > room)) *a.err = 1;
@@ -137,13 +136,12 @@ __device__ __forceinline__ int64_t sequence_strides(const AttnArgs& a, const int
     return good ? (keys + ((int64_t)1 << log2) - 1) >> log2 : 1;
 }
 __device__ __forceinline__ RangeStart range_start(const CacheAttnArgs& a, const int r, const int log2) {
-    __shared__ int64_t waves[kCacheWaves];
-    __shared__ int64_t found_begin;
-    __shared__ int found;
-    const int each = (a.N + kCacheThreads - 1) / kCacheThreads, lane = lane_id(), wave = threadIdx.x >> 6;
+    __shared__ int64_t waves[kCacheWaves], found_begin[kCacheWaves];
+    __shared__ int found[kCacheWaves];
+    const int each = (a.N + kCacheThreads - 1) / kCacheThreads, lane = lane_id(), wave = uniform(threadIdx.x >> 6);
     const int s0 = (int)threadIdx.x * each, s1 = s0 + each < a.N ? s0 + each : a.N;
     int64_t mine = 0;
-    for (int s = s0; s < s1; ++s) mine += sequence_strides(a, s, log2);
+    for (int s = s0; s < s1; ++s) mine += sequence_tiles(a, s, log2);
     int64_t upto = mine;   // ... and of all threads before
 #pragma unroll
     for (int k = 1; k < 64; k <<= 1) {
@@ -153,49 +151,50 @@ __device__ __forceinline__ RangeStart range_start(const CacheAttnArgs& a, const 
     if (lane == 63) waves[wave] = upto;
     __syncthreads();
     RangeStart out;
-    out.strides = 0;
+    out.tiles = 0;
 #pragma unroll
     for (int k = 0; k < kCacheWaves; ++k) {
         if (k < wave) upto += waves[k];
-        out.strides += waves[k];
+        out.tiles += waves[k];
     }
-    const int64_t at = range_begin(out.strides, a.ranges, r);
-    int64_t begin = upto - mine;
-    if (at >= begin && at < upto) {
-        int s = s0;
-        for (; s + 1 < s1; ++s) {
-            const int64_t n = sequence_strides(a, s, log2);
-            if (at < begin + n) break;
-            begin += n;
+    for (int k = 0; k < kCacheWaves; ++k) {
+        const int64_t at = range_begin(out.tiles, a.ranges, r + k);
+        int64_t begin = upto - mine;
+        if (at >= begin && at < upto) {
+            int s = s0;
+            for (; s + 1 < s1; ++s) {
+                const int64_t n = sequence_tiles(a, s, log2);
+                if (at < begin + n) break;
+                begin += n;
+            }
+            found[k] = s;
+            found_begin[k] = begin;
         }
-        found = s;
-        found_begin = begin;
     }
     __syncthreads();
-    out.s = uniform(found);
-    out.begin = lane_i64(found_begin, 0);
-    out.strides = lane_i64(out.strides, 0);
+    out.s = uniform(found[wave]);
+    out.begin = lane_i64(found_begin[wave], 0);
+    out.tiles = lane_i64(out.tiles, 0);
     return out;
 }
 
-// What a workgroup does with the part of a sequence's keys that lies in its run.
+// What a wavefront does with the part of a sequence's keys that lies in its run.
 struct PartWork {
     int block, step, blocks;   // units of queries: the first, how far to the next, the end
     int lo, hi;                // keys
     int cell;                  // 0, 1: where the results go to be joined; -1: these are all keys
 };
+
 template <typename T, int D, bool I8, bool BIAS>
 __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attn_kernel(const CacheAttnArgs a) {
-    constexpr int kWaves = kCacheWaves, BK = cache_tile_rows<D>(), kT = BK / 32, kD = D / 32, kC = D / 16, kP = parts<T>();
-    constexpr int kTile = BK * D, kRow = D / 4;
+    constexpr int kWaves = kCacheWaves, kLog = kTileLog2, BK = 1 << kLog, kT = BK / 32, kD = D / 32, kC = D / 16, kP = parts<T>();
+    constexpr int kTile = BK * D;
     typedef Mma<bf16_t> M;
     typedef CodeTile<D> Codes;
     // two buffers each, as arrays of their own: loads into one of them are seen not to concern what is read from another
     __shared__ __align__(16) char keys0[kWaves * kTile], keys1[kWaves * kTile], values0[kWaves * kTile], values1[kWaves * kTile];
     __shared__ __align__(16) float key_scales0[kWaves * 64], key_scales1[kWaves * 64], value_scales0[kWaves * 64], value_scales1[kWaves * 64];
-    __shared__ float2 stats[kWaves * 32];
     extern __shared__ float tab[];
-    static_assert(kWaves * kTile >= 32 * D * 4, "a wavefront's results find room in one of the arrays");
     const int wave = uniform(threadIdx.x >> 6), packs = a.H / a.pack;
 
     // the heads; the run of keys and the unit of queries that goes with it, or this wavefront's unit of queries
@@ -207,41 +206,52 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attn_kernel(const C
         hh = uniform((int)(wg % (uint32_t)packs));
         v = uniform((int)(wg / (uint32_t)packs * kWaves + wave));
     } else {
-        // Runs are dealt to the 8 dies one by one, and each die has all heads and units of queries of its runs, which read the same lines.
-        const uint32_t wg = blockIdx.y * gridDim.x + blockIdx.x, each = (uint32_t)packs * a.qblocks, dies = a.ranges >= 8 ? 8 : 1;
+        // Runs are dealt to the 8 dies four by four, and each die has all heads and units of queries of its runs, which read the same lines.
+        const uint32_t wg = blockIdx.y * gridDim.x + blockIdx.x, each = (uint32_t)packs * a.qblocks, dies = a.ranges >= 8 * kWaves ? 8 : 1;
         const uint32_t n = wg / dies, turn = n / each, rest = n - turn * each;
-        r = uniform((int)(turn * dies + wg % dies));
+        r = uniform((int)(turn * dies + wg % dies) * kWaves);
         hh = uniform((int)(rest % (uint32_t)packs));
         qb = uniform((int)(rest / (uint32_t)packs));
         if (r >= a.ranges) return;
     }
     const int head0 = hh * a.pack;
+    const bool looks = a.own && v < (uint32_t)a.N && (hh == 0 || a.own == 2);
+    const int64_t peek = looks ? sequence_numbers(a, v) : 0;
     if (BIAS) {
         fill_bias(tab, a, head0, a.pack, kCacheThreads);
         __syncthreads();
     }
-    constexpr int kLog = stride_log2(D);
-    static_assert(1 << kLog == kWaves * BK, "a stride is a tile for each wavefront");
-    const bool looks = a.own && hh == 0 && v < (uint32_t)a.N;
-    int64_t peek = 0, at = 0, end = 1, begin = 0, strides = 0;   // own: one turn of the loop below
+    int64_t at = 0, end = 1, begin = 0, all = 0;   // own: one turn of the loop below
     int s = 0;
     if (a.own) {
         if (v >= (uint32_t)a.V) return;
-        peek = looks ? sequence_numbers(a, v) : 0;
-        s = find_sequence(a.q_off, a.N, v, a.block);
+        s = a.own == 2 ? (int)v : find_sequence(a.q_off, a.N, v, a.block);
     } else {
         const RangeStart start = range_start(a, r, kLog);
         s = start.s;
         begin = start.begin;
-        strides = start.strides;
-        at = range_begin(strides, a.ranges, r);
-        end = range_begin(strides, a.ranges, r + 1);
+        all = start.tiles;
+        r += wave;
+        if (r >= a.ranges) return;
+        at = range_begin(all, a.ranges, r);
+        end = range_begin(all, a.ranges, r + 1);
     }
+    int64_t numbers = a.own == 2 ? peek : (at < end ? sequence_numbers(a, s) : 0);
     for (; at < end; ++s) {
     Sequence q;
     PartWork w;
-    const bool fits = take_sequence(a, s, sequence_numbers(a, s), q);
-    if (a.own) {
+    const bool fits = take_sequence(a, s, numbers, q);
+    if (!a.own) numbers = s + 1 < a.N ? sequence_numbers(a, s + 1) : 0;   // (under way while this one is worked on)
+    if (a.own == 2) {
+        if (!fits) return;
+        w.block = 0;
+        w.blocks = (int)(((int64_t)q.nq + a.block - 1) / a.block);
+        w.step = 1;
+        w.lo = 0;
+        w.hi = q.nk;
+        w.cell = -1;
+        at = end;
+    } else if (a.own) {
         const uint32_t start = (uint32_t)q.q0 / a.block + s, blocks = ((uint32_t)q.nq + a.block - 1) / a.block;
         if (!fits || v < start || v - start >= blocks) return judge(a, looks, v, peek);
         w.block = uniform((int)(v - start));
@@ -252,8 +262,8 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attn_kernel(const C
         w.cell = -1;
         at = end;
     } else {
-        const int64_t n = fits && q.nk > 0 ? ((int64_t)q.nk + kWaves * BK - 1) >> kLog : 1;
-        const int64_t a0 = at - begin, a1 = end - begin < n ? end - begin : n;   // strides of this sequence
+        const int64_t n = fits && q.nk > 0 ? ((int64_t)q.nk + BK - 1) >> kLog : 1;
+        const int64_t a0 = at - begin, a1 = end - begin < n ? end - begin : n;   // tiles of this sequence
         w.blocks = (int)(((int64_t)q.nq + a.block - 1) / a.block);
         w.block = qb;
         w.step = a.qblocks;
@@ -261,7 +271,7 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attn_kernel(const C
         w.hi = a1 < n ? (int)(a1 << kLog) : q.nk;
         w.cell = a0 > 0 ? 0 : (a1 < n ? 1 : -1);
         if (w.blocks > a.qblocks) {
-            // More units of queries than go with a run: units in turn, with all the keys.  Turn m belongs to the run with stride m n / turns.
+            // More units of queries than go with a run: units in turn, with all the keys.  Turn m belongs to the run with tile m n / turns.
             const int64_t turns = (w.blocks + a.qblocks - 1) / a.qblocks, m0 = (a0 * turns + n - 1) / n, m1 = (a1 * turns + n - 1) / n;
             w.block = (int)m0 * a.qblocks + qb;
             w.blocks = w.blocks < (int)m1 * a.qblocks ? w.blocks : (int)m1 * a.qblocks;
@@ -269,8 +279,8 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attn_kernel(const C
             w.hi = q.nk;
             w.cell = -1;
         }
-        if (a0 == 0 && hh == 0 && qb == 0 && threadIdx.x == 0)
-            a.spans[s] = w.cell < 0 ? make_int2(0, 0) : make_int2(r, range_of(strides, a.ranges, begin + n - 1));
+        if (a0 == 0 && hh == 0 && qb == 0 && lane_id() == 0)
+            a.spans[s] = w.cell < 0 ? make_int2(0, 0) : make_int2(r, range_of(all, a.ranges, begin + n - 1));
         begin += n;
         at = begin;
         if (!fits) continue;
@@ -282,7 +292,6 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attn_kernel(const C
     const float* const ks = a.ks + (int64_t)kvh * a.k_rows + q.k0;
     const float* const vs = a.vs + (int64_t)kvh * a.k_rows + q.k0;
     const int own = wave * kTile, own_scales = wave * 64;
-    const int t_step = a.own ? 1 : kWaves;
     for (int block = w.block; block < w.blocks; block += w.step) {
         const int lane = anew(lane_id()), col = lane & 31, half = lane >> 5;
         const int ci = col / a.pack, cg = col - ci * a.pack, head = head0 + cg;
@@ -300,8 +309,7 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attn_kernel(const C
             const int last = q.nk - q.nq + (iw + a.block < q.nq ? iw + a.block : q.nq);
             jend = jend < last ? jend : last;
         }
-        // this wavefront's tiles: every one, or every fourth
-        const int tiles = jend > w.lo ? (jend - w.lo + BK - 1) / BK : 0, t0 = a.own ? 0 : wave;
+        const int tiles = jend > w.lo ? (jend - w.lo + BK - 1) / BK : 0;
 
         uint4 fq[kC][kP];   // fragment 2 c + s: elements 32 c + 16 half + 8 s + 0 .. 7, the order in which a chunk of codes has them
         {
@@ -404,8 +412,9 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attn_kernel(const C
                     for (int r = 0; r < 16; ++r)
                         if (j0 + 32 * k + 8 * (r / 4) + 4 * half + r % 4 >= upto) x[k][r] = -__builtin_inff();
             }
+            return hides;
         };
-        auto apply = [&](const char* const vt_, const float* const st_, const int l) __attribute__((always_inline)) {
+        auto apply = [&](const char* const vt_, const float* const st_, const bool hides, const int l) __attribute__((always_inline)) {
             const int half = l >> 5;
             const char* const vt = vt_ + own;
             const float* const st = st_ + own_scales;
@@ -429,24 +438,31 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attn_kernel(const C
                     for (int r = 0; r < 16; ++r) o[d][r] *= shrink;
             }
             const float at = m == -__builtin_inff() ? 0.f : m;   // (nothing seen so far: every probability is 2^-inf = 0)
+            // A scale that is not finite must not reach a column that does not see its key.
+            const auto weigh = [&](const auto masked) __attribute__((always_inline)) {
+#pragma unroll
+                for (int k = 0; k < kT; ++k)
+#pragma unroll
+                    for (int r = 0; r < 16; r += 4) {
+                        const float4 s4 = *reinterpret_cast<const float4*>(st + 32 * k + 2 * r + 4 * half);
+                        const float s[4] = {s4.x, s4.y, s4.z, s4.w};
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float y = x[k][r + e], p = __builtin_amdgcn_exp2f(BIAS ? y - at : fmaf(y, a.scale2, -at));
+                            sum += p;
+                            x[k][r + e] = p * (decltype(masked)::value && y == -__builtin_inff() ? 0.f : s[e]);
+                        }
+                    }
+            };
+            if (BIAS || hides) weigh(std::true_type{});
+            else weigh(std::false_type{});
 #pragma unroll
             for (int k = 0; k < kT; ++k)
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
                     float p[8];
 #pragma unroll
-                    for (int r = 0; r < 8; r += 4) {
-                        const float4 s4 = *reinterpret_cast<const float4*>(st + 32 * k + 16 * c + 2 * r + 4 * half);
-                        const float s[4] = {s4.x, s4.y, s4.z, s4.w};
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float y = x[k][8 * c + r + e];
-                            const float at_y = __builtin_amdgcn_exp2f(BIAS ? y - at : fmaf(y, a.scale2, -at));
-                            sum += at_y;
-                            // (a scale that is not finite must not reach a column that does not see its key)
-                            p[r + e] = at_y * (y == -__builtin_inff() ? 0.f : s[e]);
-                        }
-                    }
+                    for (int r = 0; r < 8; ++r) p[r] = x[k][8 * c + r];
                     uint4 f[kP];
                     cut<kP>(p, f);
 #pragma unroll
@@ -454,7 +470,7 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attn_kernel(const C
                         const uint2 u = Codes::down(vt, 32 * k, c, d, l);
                         const uint4 g = codes_bf16<I8>(u.x, u.y);
 #pragma unroll
-                        for (int p = kP - 1; p >= 0; --p) o[d] = M::mma(g, f[p], o[d]);
+                        for (int n = kP - 1; n >= 0; --n) o[d] = M::mma(g, f[n], o[d]);
                     }
                 }
             settle<bf16_t>();
@@ -501,132 +517,93 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attn_kernel(const C
         // a tile's time and a half.  They end in their order: of those begun after the ones waited for, so many may still run.
         constexpr int kGroup = BK * D / 1024 + 1;
         auto one = [&](const int t, char* const kt, float* const kst, char* const vt, float* const vst) __attribute__((always_inline)) {
-            const bool next = t + t_step < tiles, after = t + 2 * t_step < tiles;
+            const bool next = t + 1 < tiles, after = t + 2 < tiles;
             if (next) wait_loads<3 * kGroup>();
             else wait_loads<kGroup>();
-            scores(t, kt, kst, lane);
+            const bool hides = scores(t, kt, kst, lane);
             if (after) {
-                fetch_keys(t + 2 * t_step, kt, kst, lane);
+                fetch_keys(t + 2, kt, kst, lane);
                 wait_loads<3 * kGroup>();
             } else if (next) {
                 wait_loads<2 * kGroup>();
             } else {
                 wait_loads<0>();
             }
-            apply(vt, vst, lane);
-            if (after) fetch_values(t + 2 * t_step, vt, vst, lane);
+            apply(vt, vst, hides, lane);
+            if (after) fetch_values(t + 2, vt, vst, lane);
         };
         begin();
-        if (t0 < tiles) {
-            fetch_keys(t0, keys0, key_scales0, lane);
-            fetch_values(t0, values0, value_scales0, lane);
+        if (tiles > 0) {
+            fetch_keys(0, keys0, key_scales0, lane);
+            fetch_values(0, values0, value_scales0, lane);
         }
-        if (t0 + t_step < tiles) {
-            fetch_keys(t0 + t_step, keys1, key_scales1, lane);
-            fetch_values(t0 + t_step, values1, value_scales1, lane);
+        if (tiles > 1) {
+            fetch_keys(1, keys1, key_scales1, lane);
+            fetch_values(1, values1, value_scales1, lane);
         }
-        for (int t = t0; t < tiles; t += 2 * t_step) {
+        for (int t = 0; t < tiles; t += 2) {
             one(t, keys0, key_scales0, values0, value_scales0);
-            if (t + t_step < tiles) one(t + t_step, keys1, key_scales1, values1, value_scales1);
+            if (t + 1 < tiles) one(t + 1, keys1, key_scales1, values1, value_scales1);
         }
         if (!I8 && (a.causal || BIAS) && __any(is && not_finite(o))) {
             begin();
 #pragma unroll 1
-            for (int t = t0; t < tiles; t += t_step) {
+            for (int t = 0; t < tiles; ++t) {
                 const int l = anew(lane);   // (few registers: nothing of this is kept through the loop above)
                 fetch_keys(t, keys0, key_scales0, l);
                 fetch_values(t, values0, value_scales0, l);
                 loads_done();
                 take_out(t, l);
-                scores(t, keys0, key_scales0, l);
-                apply(values0, value_scales0, l);
+                const bool hides = scores(t, keys0, key_scales0, l);
+                apply(values0, value_scales0, hides, l);
             }
         }
         sum = pair_sum<32>(sum);
 
-        if (a.own) {
-            if (is) {
-                const float inv = sum == 0.f ? 0.f : 1.f / sum;   // (no key seen: zeros)
-                char* const to = const_cast<char*>(a.o.at(q.q0 + i, head));
-#pragma unroll
-                for (int d = 0; d < kD; ++d)
-#pragma unroll
-                    for (int r = 0; r < 16; r += 4) {
-                        const int e = 32 * d + 2 * r + 4 * half;
-                        if (e < a.dim) {
-                            if constexpr (sizeof(T) == 2)
-                                *reinterpret_cast<uint2*>(to + 2 * e) = make_uint2(pack2((const T*)nullptr, o[d][r] * inv, o[d][r + 1] * inv),
-                                                                                   pack2((const T*)nullptr, o[d][r + 2] * inv, o[d][r + 3] * inv));
-                            else *reinterpret_cast<float4*>(to + 4 * e) = make_float4(o[d][r] * inv, o[d][r + 1] * inv, o[d][r + 2] * inv, o[d][r + 3] * inv);
-                        }
-                    }
-                if (a.lse && half == 0) a.lse[(int64_t)head * a.q_rows + q.q0 + i] = sum == 0.f ? -__builtin_inff() : fmaf(m, kLn2, logf(sum));
-            }
-            continue;
-        }
-        // The wavefronts' results meet where the tiles were, as fp32 rows of D elements, sixteen bytes of a row at place c ^ column: a column's
-        // lanes do not all fall on the same banks.
-        auto piece = [&](const int n) __attribute__((always_inline)) { return n == 0 ? keys0 : (n == 1 ? keys1 : (n == 2 ? values0 : values1)); };
-        __syncthreads();
-        {
-            char* const to = piece(wave);
+        if (!is) continue;
+        if (w.cell >= 0) {
+            const int64_t cell = (((int64_t)(2 * r + w.cell) * a.qblocks + qb) * packs + hh) * 32 + col;
+            if (half == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * cell) = make_float2(m, sum);
+            float* const to = a.part_o + cell * D + 4 * half;
 #pragma unroll
             for (int d = 0; d < kD; ++d)
 #pragma unroll
-                for (int r = 0; r < 16; r += 4)
-                    *reinterpret_cast<float4*>(to + (col * kRow + ((8 * d + r / 2 + half) ^ (col % kRow))) * 16) = make_float4(o[d][r], o[d][r + 1], o[d][r + 2], o[d][r + 3]);
-            if (half == 0) stats[wave * 32 + col] = make_float2(m, sum);
+                for (int n = 0; n < 16; n += 4) *reinterpret_cast<float4*>(to + 32 * d + 2 * n) = make_float4(o[d][n], o[d][n + 1], o[d][n + 2], o[d][n + 3]);
+            continue;
         }
-        __syncthreads();
-        for (int n = threadIdx.x; n < 32 * kRow; n += 64 * kWaves) {
-            const int c = n / kRow, e = n % kRow, cc = c / a.pack, ii = iw + cc, hd = head0 + c - cc * a.pack;
-            if (cc >= a.qpt || ii >= q.nq) continue;
-            float top = -__builtin_inff(), total = 0.f;
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;   // (no key seen: zeros)
+        char* const to = const_cast<char*>(a.o.at(q.q0 + i, head));
 #pragma unroll
-            for (int k = 0; k < kWaves; ++k) top = fmaxf(top, stats[k * 32 + c].x);
-            const float at = top == -__builtin_inff() ? 0.f : top;
-            float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int d = 0; d < kD; ++d)
 #pragma unroll
-            for (int k = 0; k < kWaves; ++k) {
-                const float2 ms = stats[k * 32 + c];
-                const float by = __builtin_amdgcn_exp2f(ms.x - at);
-                const float4 y = *reinterpret_cast<const float4*>(piece(k) + (c * kRow + (e ^ (c % kRow))) * 16);
-                total = fmaf(ms.y, by, total);
-                x.x = fmaf(y.x, by, x.x); x.y = fmaf(y.y, by, x.y);
-                x.z = fmaf(y.z, by, x.z); x.w = fmaf(y.w, by, x.w);
+            for (int n = 0; n < 16; n += 4) {
+                const int e = 32 * d + 2 * n + 4 * half;
+                if (e < a.dim) {
+                    if constexpr (sizeof(T) == 2)
+                        *reinterpret_cast<uint2*>(to + 2 * e) = make_uint2(pack2((const T*)nullptr, o[d][n] * inv, o[d][n + 1] * inv),
+                                                                           pack2((const T*)nullptr, o[d][n + 2] * inv, o[d][n + 3] * inv));
+                    else *reinterpret_cast<float4*>(to + 4 * e) = make_float4(o[d][n] * inv, o[d][n + 1] * inv, o[d][n + 2] * inv, o[d][n + 3] * inv);
+                }
             }
-            if (w.cell >= 0) {
-                const int64_t cell = (((int64_t)(2 * r + w.cell) * a.qblocks + qb) * packs + hh) * 32 + c;
-                if (e == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * cell) = make_float2(top, total);
-                *reinterpret_cast<float4*>(a.part_o + cell * D + 4 * e) = x;
-                continue;
-            }
-            const float inv = total == 0.f ? 0.f : 1.f / total;
-            if (4 * e < a.dim) {
-                char* const to = const_cast<char*>(a.o.at(q.q0 + ii, hd)) + 4 * e * sizeof(T);
-                if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(to) = make_uint2(pack2((const T*)nullptr, x.x * inv, x.y * inv), pack2((const T*)nullptr, x.z * inv, x.w * inv));
-                else *reinterpret_cast<float4*>(to) = make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv);
-            }
-            if (a.lse && e == 0) a.lse[(int64_t)hd * a.q_rows + q.q0 + ii] = total == 0.f ? -__builtin_inff() : fmaf(top, kLn2, logf(total));
-        }
-        __syncthreads();   // (the next unit's tiles go where these results are)
+        if (a.lse && half == 0) a.lse[(int64_t)head * a.q_rows + q.q0 + i] = sum == 0.f ? -__builtin_inff() : fmaf(m, kLn2, logf(sum));
     }
     }
-    if (a.own) judge(a, looks, v, peek);
+    if (a.own == 1) judge(a, looks, v, peek);
 }
 
-// Joins the parts of the keys: a workgroup for four heads of a query, a wavefront for each; where there are many parts, all four for one head after
-// the other, a quarter of the parts each.  The order of the additions is fixed.
-template <typename T, int D>
-__global__ __launch_bounds__(256) void cache_attn_join_kernel(const CacheAttnArgs a) {
-    constexpr int kPer = D >= 64 ? D / 64 : 1, kAhead = 8;   // elements a lane; parts under way together
-    typedef float out_t __attribute__((ext_vector_type(kPer)));
+// Joins the parts of the keys: a workgroup for eight heads of a query, a wavefront for two of them, or where there are many parts for one head.  A row
+// of a part is shared by D / 4 lanes, and the lanes' groups take parts in turn, each with its own running maximum: the rows are loaded beside the
+// statistics that weigh them.  The order of the additions is fixed.
+template <typename T, int D, bool many>
+__global__ __launch_bounds__(256, many ? 4 : 8) void cache_attn_join_kernel(const CacheAttnArgs a) {
+    constexpr int kLanes = D / 4, kGroups = 64 / kLanes, kAhead = many ? 8 : 4;   // kAhead: parts of a group under way together
     __shared__ float2 stats[4];
-    __shared__ out_t sums[4][64];
+    __shared__ float4 sums[4][kLanes];
     const int lane = lane_id(), wave = uniform(threadIdx.x >> 6), packs = a.H / a.pack;
-    const uint32_t n = blockIdx.y * gridDim.x + blockIdx.x, fours = ((uint32_t)a.H + 3) / 4;
-    const int64_t row = n / fours;
-    const int four = (int)(n - (uint32_t)row * fours) * 4;
+    const int heads = many ? 1 : 8;
+    const uint32_t n = blockIdx.y * gridDim.x + blockIdx.x, per_row = ((uint32_t)a.H + heads - 1) / heads;
+    const int64_t row = n / per_row;
+    const int head0 = (int)(n - (uint32_t)row * per_row) * heads;
     if (row >= a.q_rows) return;
     const int s = find_row(a.q_off, a.N, row);
     Sequence q;
@@ -634,71 +611,66 @@ __global__ __launch_bounds__(256) void cache_attn_join_kernel(const CacheAttnArg
     if (!take_sequence(a, s, sequence_numbers(a, s), q) || row < q.q0 || row >= q.q0 + q.nq) return;
     if (span.x >= span.y) return;   // (the result is there already)
     const int i = (int)(row - q.q0), qb = i / a.block, count = span.y - span.x + 1;
-    const bool many = count > 16;
     const int64_t each = (int64_t)a.qblocks * packs * 32;   // cells of half a run's: a run has two, for the sequence that it continues and the one that it begins
-    const int e0 = (lane * kPer) & (D - 1);   // (rows of 32 elements: the upper half of the wavefront does the same again)
-    for (int k = many ? 0 : wave; k < 4; k += many ? 1 : 4) {
-        const int head = four + k;
-        if (head >= a.H) break;
+    const int e0 = 4 * (lane % kLanes), group = lane / kLanes + (many ? wave * kGroups : 0), groups = many ? 4 * kGroups : kGroups;
+    for (int head = head0 + (many ? 0 : wave); head < a.H && head < head0 + heads; head += 4) {
         const int hh = head / a.pack, col = (i - qb * a.block) * a.pack + head - hh * a.pack;
         const int64_t cell0 = ((int64_t)qb * packs + hh) * 32 + col;
-        const auto cell_of = [&](const int p) __attribute__((always_inline)) { return cell0 + (2 * (int64_t)(span.x + p) + (p == 0)) * each; };
-        const float2* const ml = reinterpret_cast<const float2*>(a.part_ml);
-        const int share = many ? (count + 3) / 4 : count, p0 = many ? wave * share : 0, p1 = p0 + share < count ? p0 + share : count;
         float m = -__builtin_inff(), sum = 0.f;
-        for (int p = p0 + lane; p < p1; p += 64) m = fmaxf(m, ml[cell_of(p)].x);
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        const auto add = [&](const float2 c, const float4 x) __attribute__((always_inline)) {
+            const float top = fmaxf(m, c.x), at = top == -__builtin_inff() ? 0.f : top;
+            const float old = __builtin_amdgcn_exp2f(m - at), by = __builtin_amdgcn_exp2f(c.x - at);
+            m = top;
+            sum = fmaf(c.y, by, sum * old);
+            o.x = fmaf(x.x, by, o.x * old); o.y = fmaf(x.y, by, o.y * old);
+            o.z = fmaf(x.z, by, o.z * old); o.w = fmaf(x.w, by, o.w * old);
+        };
+        for (int base = group; base < count; base += groups * kAhead) {
+            float2 c[kAhead];
+            float4 x[kAhead];
 #pragma unroll
-        for (int x = 32; x; x >>= 1) m = fmaxf(m, __shfl_xor(m, x));
-        const float at = m == -__builtin_inff() ? 0.f : m;
-        out_t o = {};
-        for (int base = p0; base < p1; base += 64) {
-            const bool mine = base + lane < p1;
-            const float2 c = mine ? ml[cell_of(base + lane)] : make_float2(-__builtin_inff(), 0.f);
-            const float by = mine ? __builtin_amdgcn_exp2f(c.x - at) : 0.f;
-            sum += group_sum(c.y * by, 64);
-            const int end = p1 - base < 64 ? p1 - base : 64;
-            for (int p = 0; p < end; p += kAhead) {
-                out_t x[kAhead];
-#pragma unroll
-                for (int j = 0; j < kAhead; ++j) x[j] = *reinterpret_cast<const out_t*>(a.part_o + cell_of(base + (p + j < end ? p + j : p)) * D + e0);
-#pragma unroll
-                for (int j = 0; j < kAhead; ++j)
-                    if (p + j < end) o += bcast_lane(by, (p + j) & 63) * x[j];
+            for (int j = 0; j < kAhead; ++j) {
+                const int p = base + j * groups < count ? base + j * groups : base;
+                const int64_t cell = cell0 + (2 * (int64_t)(span.x + p) + (p == 0)) * each;
+                c[j] = *reinterpret_cast<const float2*>(a.part_ml + 2 * cell);
+                x[j] = *reinterpret_cast<const float4*>(a.part_o + cell * D + e0);
             }
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j)
+                if (base + j * groups < count) add(c[j], x[j]);
+        }
+#pragma unroll
+        for (int w = kLanes; w < 64; w <<= 1) {
+            const float2 c = make_float2(__shfl_xor(m, w), __shfl_xor(sum, w));
+            const float4 x = make_float4(__shfl_xor(o.x, w), __shfl_xor(o.y, w), __shfl_xor(o.z, w), __shfl_xor(o.w, w));
+            add(c, x);
         }
         if (many) {
             if (lane == 0) stats[wave] = make_float2(m, sum);
-            sums[wave][lane] = o;
+            if (lane < kLanes) sums[wave][lane] = o;
             __syncthreads();
-            float top = -__builtin_inff();
-#pragma unroll
-            for (int x = 0; x < 4; ++x) top = fmaxf(top, stats[x].x);
-            const float all = top == -__builtin_inff() ? 0.f : top;
-            m = top;
+            m = -__builtin_inff();
             sum = 0.f;
-            o = out_t{};
+            o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                const float by = __builtin_amdgcn_exp2f(stats[x].x - all);
-                sum = fmaf(stats[x].y, by, sum);
-                o += by * sums[x][lane];
-            }
-            __syncthreads();
-            if (wave != 0) continue;
+            for (int w = 0; w < 4; ++w) add(stats[w], sums[w][lane % kLanes]);
+            if (wave != 0) return;
         }
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        T* const to = reinterpret_cast<T*>(const_cast<char*>(a.o.at(row, head)));
-#pragma unroll
-        for (int e = 0; e < kPer; ++e)
-            if (e0 + e < a.dim) to[e0 + e] = elem_round<T>((kPer == 1 ? o[0] : o[e]) * inv);
+        if (lane < kLanes && e0 < a.dim) {
+            char* const to = const_cast<char*>(a.o.at(row, head)) + e0 * sizeof(T);
+            if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(to) = make_uint2(pack2((const T*)nullptr, o.x * inv, o.y * inv), pack2((const T*)nullptr, o.z * inv, o.w * inv));
+            else *reinterpret_cast<float4*>(to) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+        }
         if (a.lse && lane == 0) a.lse[(int64_t)head * a.q_rows + row] = sum == 0.f ? -__builtin_inff() : fmaf(m, kLn2, logf(sum));
     }
 }
 
 // How the work is shared out.  Heads of a group lie side by side in a wavefront's columns where one query would leave them empty.  Short caches, or
-// so many units of queries that the chip is full: a wavefront for each unit.  Otherwise as many workgroups as the chip holds at once share all
+// so many units of queries that the chip is full: a wavefront for each unit.  Otherwise as many wavefronts as the chip holds at once share all
 // keys evenly among them.
-constexpr int64_t kRangeGroups = 512;
+constexpr int64_t kRangeGroups = 512, kRangeTiles = 2;
 CacheAttnPlan cache_attn_plan(const AttnShape& sh, const int max_pack) {
     CacheAttnPlan p;
     const int64_t mean_q = (sh.q_rows + sh.N - 1) / sh.N, mean_k = (sh.k_rows + sh.N - 1) / sh.N;
@@ -709,18 +681,19 @@ CacheAttnPlan cache_attn_plan(const AttnShape& sh, const int max_pack) {
     for (int g = 2; g <= group && g <= max_pack; ++g)   // more heads side by side as long as a sequence's queries of all of them fit
         if (group % g == 0 && mean_q * g <= 32 && g * table <= kTabBytes) p.pack = g;
     p.block = 32 / p.pack;
-    const int64_t packs = sh.H / p.pack, units = (sh.q_rows / p.block + sh.N) * packs;
-    p.own = mean_k <= 128 || (units >= 4096 && mean_k <= 2048);
+    const int64_t packs = sh.H / p.pack, units = (sh.q_rows == sh.N ? sh.N : sh.q_rows / p.block + sh.N / 2) * packs;
+    p.direct = sh.q_rows == sh.N;
+    p.own = mean_k <= 320 || (units >= 768 && mean_k <= (p.direct ? 1024 : 512));
     p.ranges = p.qblocks = 1;
-    p.V = sh.q_rows / p.block + sh.N;
+    p.V = p.direct ? sh.N : sh.q_rows / p.block + sh.N;
     p.spans = p.part_ml = p.part_o = 0;
     if (p.own) return p;
     p.qblocks = (int)std::max<int64_t>(1, (mean_q + p.block - 1) / p.block);
     const int64_t each = packs * p.qblocks;
-    p.ranges = (int)std::max<int64_t>(1, kRangeGroups / each);
-    if (p.ranges >= 8) p.ranges &= ~7;
-    // no more than there are strides
-    p.ranges = (int)std::min<int64_t>(p.ranges, (sh.k_rows >> stride_log2(p.D)) + sh.N);
+    p.ranges = (int)std::max<int64_t>(1, kRangeGroups / each) * kCacheWaves;
+    if (p.ranges >= 8 * kCacheWaves) p.ranges &= ~(8 * kCacheWaves - 1);
+    // no shorter than a few tiles
+    p.ranges = (int)std::max<int64_t>(1, std::min<int64_t>(p.ranges, ((sh.k_rows >> kTileLog2) + sh.N) / kRangeTiles));
     p.spans = ((size_t)sh.N * sizeof(int2) + 255) & ~(size_t)255;
     const int64_t cells = p.ranges > 1 ? 2 * p.ranges * each * 32 : 0;
     p.part_ml = ((size_t)cells * 8 + 255) & ~(size_t)255;
@@ -729,11 +702,11 @@ CacheAttnPlan cache_attn_plan(const AttnShape& sh, const int max_pack) {
 }
 static int64_t plan_groups(const AttnShape& sh, const CacheAttnPlan& p) {
     const int64_t packs = sh.H / p.pack;
-    return p.own ? (p.V + 3) / 4 * packs : (p.ranges >= 8 ? (p.ranges + 7) / 8 * 8 : (int64_t)p.ranges) * packs * p.qblocks;
+    return p.own ? (p.V + 3) / 4 * packs : (p.ranges >= 8 * kCacheWaves ? (p.ranges + 8 * kCacheWaves - 1) / (8 * kCacheWaves) * 8 : ((int64_t)p.ranges + kCacheWaves - 1) / kCacheWaves) * packs * p.qblocks;
 }
 bool cache_attn_grid_ok(const AttnShape& sh, const CacheAttnPlan& p) {
     const int64_t most = ((int64_t)1 << 31) - 64;
-    return plan_groups(sh, p) < most && (p.part_ml == 0 || sh.q_rows * ((sh.H + 3) / 4) < most);
+    return plan_groups(sh, p) < most && (p.part_ml == 0 || sh.q_rows * sh.H < most);
 }
 size_t cache_attn_workspace(const AttnShape& sh) {
     size_t most = 0;
@@ -759,16 +732,17 @@ static hipError_t launch_parts(const tbe_handle* h, const CacheAttnArgs& a, cons
     return e;
 }
 template <typename T, int D>
-static hipError_t launch_dim(const tbe_handle* h, const CacheAttnArgs& a, const bool i8, const uint64_t groups, const bool join, hipStream_t s) {
+static hipError_t launch_dim(const tbe_handle* h, const CacheAttnArgs& a, const bool i8, const uint64_t groups, const int join, hipStream_t s) {
     const hipError_t e = i8 ? launch_parts<T, D, true>(h, a, groups, s) : launch_parts<T, D, false>(h, a, groups, s);
     if (e != hipSuccess || !join) return e;
     LaunchTimer tm(h, s, "cache_attention_join");
-    cache_attn_join_kernel<T, D><<<die_grid((uint64_t)a.q_rows * (((uint64_t)a.H + 3) / 4)), 256, 0, s>>>(a);
+    if (join == 2) cache_attn_join_kernel<T, D, true><<<die_grid((uint64_t)a.q_rows * (uint64_t)a.H), 256, 0, s>>>(a);
+    else cache_attn_join_kernel<T, D, false><<<die_grid((uint64_t)a.q_rows * (((uint64_t)a.H + 7) / 8)), 256, 0, s>>>(a);
     tm.done();
     return hipGetLastError();
 }
 template <typename T>
-static hipError_t launch_type(const tbe_handle* h, const CacheAttnArgs& a, const int D, const bool i8, const uint64_t groups, const bool join, hipStream_t s) {
+static hipError_t launch_type(const tbe_handle* h, const CacheAttnArgs& a, const int D, const bool i8, const uint64_t groups, const int join, hipStream_t s) {
     return D == 32 ? launch_dim<T, 32>(h, a, i8, groups, join, s) : (D == 64 ? launch_dim<T, 64>(h, a, i8, groups, join, s) : launch_dim<T, 128>(h, a, i8, groups, join, s));
 }
 
@@ -779,14 +753,14 @@ hipError_t launch_cache_attention(const tbe_handle* h, const AttnArgs& call, con
     a.k = cache[0].codes; a.v = cache[1].codes;
     a.ks = cache[0].scales; a.vs = cache[1].scales;
     a.pack = p.pack; a.qpt = a.block = p.block; a.V = (int)p.V;
-    a.ranges = p.ranges; a.qblocks = p.qblocks; a.own = p.own;
+    a.ranges = p.ranges; a.qblocks = p.qblocks; a.own = p.own ? 1 + p.direct : 0;
     a.spans = static_cast<int2*>(workspace);
     a.part_ml = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.spans);
     a.part_o = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.spans + p.part_ml);
     AttnShape sh{};
     sh.H = a.H;
     const uint64_t groups = (uint64_t)plan_groups(sh, p);
-    const bool join = p.part_ml > 0;
+    const int join = p.part_ml > 0 ? (p.ranges > 16 * (int64_t)a.N ? 2 : 1) : 0;   // 2: many parts
     return io == 0 ? launch_type<float>(h, a, p.D, i8, groups, join, s) : (io == 1 ? launch_type<__half>(h, a, p.D, i8, groups, join, s) : launch_type<bf16_t>(h, a, p.D, i8, groups, join, s));
 }
 
