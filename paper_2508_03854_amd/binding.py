@@ -282,6 +282,13 @@ def rotary_frequencies(rotary_dim: int, base: float = 10000.0, scaling: str = "p
     return f.to(device)
 
 
+def _new_heads(like: torch.Tensor, shape, stream: Optional[torch.cuda.Stream]) -> Tuple[torch.Tensor, Rows]:
+    """A result [rows, heads, head_dim] of like's type, and its rows (without the checks that a given one goes through: they take a quarter of a
+    small call)."""
+    out = like.new_empty(shape) if stream is None else _empty(shape, like.dtype, like.device, stream)
+    return out, Rows(out.data_ptr(), shape[1] * shape[2], shape[2])
+
+
 class Cache:
     """tbe_cache: keys and values as one byte an element, k and v [rows, heads, head_dim] float8_e4m3fn or int8 (last axis contiguous), and scales,
     k_scales and v_scales float32 [heads, rows]; a value is code * scale.  TBE.alloc_cache makes an empty one."""
@@ -775,14 +782,11 @@ class TBE:
         weight = q_weight if q_weight is not None else k_weight
         a = self._rotation_args(q, k, like, positions, frequencies, interleaved, amplitude, norm, eps, q_weight, k_weight,
                                 torch.float32 if weight is None else weight.dtype)
-        if q is not None and q_out is None:
-            q_out = _empty(q.shape, q.dtype, q.device, stream)
-        if k is not None and k_out is None:
-            k_out = _empty(k.shape, k.dtype, k.device, stream)
         if (q is None and q_out is not None) or (k is None and k_out is not None):
             raise ValueError("q_out without q, or k_out without k")
-        st = self._lib.tbe_rotate_heads(self._h, a, qp, kp, self._heads_or_none(q_out, q, "q_out"), self._heads_or_none(k_out, k, "k_out"),
-                                        _stream_ptr(stream))
+        q_out, qo = _new_heads(q, q.shape, stream) if q is not None and q_out is None else (q_out, self._heads_or_none(q_out, q, "q_out"))
+        k_out, ko = _new_heads(k, k.shape, stream) if k is not None and k_out is None else (k_out, self._heads_or_none(k_out, k, "k_out"))
+        st = self._lib.tbe_rotate_heads(self._h, a, qp, kp, qo, ko, _stream_ptr(stream))
         _check(st, "tbe_rotate_heads")
         return q_out, k_out
 
@@ -826,17 +830,21 @@ class TBE:
                 raise ValueError(f"{name} is needed with norm")
             if not norm and gw is not None:
                 raise ValueError("weights' gradients without norm")
-        if grad_q_out is not None and grad_q is None:
-            grad_q = _empty(grad_q_out.shape, like.dtype, like.device, stream)
-        if grad_k_out is not None and grad_k is None:
-            grad_k = _empty(grad_k_out.shape, like.dtype, like.device, stream)
+        if grad_q is None and grad_q_out is not None:
+            grad_q, gq = _new_heads(like, grad_q_out.shape, stream)
+        else:
+            gq = self._heads_or_none(grad_q, grad_q_out, "grad_q")
+        if grad_k is None and grad_k_out is not None:
+            grad_k, gk = _new_heads(like, grad_k_out.shape, stream)
+        else:
+            gk = self._heads_or_none(grad_k, grad_k_out, "grad_k")
         if norm and params and grad_q_weight is None and grad_q_out is not None:
             grad_q_weight = _empty(dim, pt, like.device, stream)
         if norm and params and grad_k_weight is None and grad_k_out is not None:
             grad_k_weight = _empty(dim, pt, like.device, stream)
         st = self._lib.tbe_rotate_heads_backward(
             self._h, a, dqo, dko, self._heads_or_none(q if norm else None, grad_q_out, "q"), self._heads_or_none(k if norm else None, grad_k_out, "k"),
-            self._heads_or_none(grad_q, grad_q_out, "grad_q"), self._heads_or_none(grad_k, grad_k_out, "grad_k"),
+            gq, gk,
             _param_ptr(grad_q_weight, dim, pt, "grad_q_weight"), _param_ptr(grad_k_weight, dim, pt, "grad_k_weight"),
             _dev_ptr(workspace, torch.uint8, "workspace"), 0 if workspace is None else int(workspace.numel()), _stream_ptr(stream))
         _check(st, "tbe_rotate_heads_backward")
@@ -911,10 +919,10 @@ class TBE:
         if shape[2] != q.shape[2]:
             raise ValueError(f"q and the cache must agree in head_dim, got {q.shape[2]} / {shape[2]}")
         a = self._pack_attention(q, shape, (0, 0, 0, 0, 0, 0), q_offsets, k_offsets, k_lengths, causal, scale, bias, bucket_map)
-        out = _empty(q.shape, q.dtype, q.device, stream) if out is None else out
+        out, rows = _new_heads(q, q.shape, stream) if out is None else (out, _heads(out, q, "out"))
         if stats and lse is None:
             lse = _empty((q.shape[1], q.shape[0]), torch.float32, q.device, stream)
-        st = self._lib.tbe_cache_attention(self._h, a, cache._args(), _heads(out, q, "out"),
+        st = self._lib.tbe_cache_attention(self._h, a, cache._args(), rows,
                                            _param_ptr(lse, q.shape[0] * q.shape[1], torch.float32, "lse"),
                                            _dev_ptr(workspace, torch.uint8, "workspace"), 0 if workspace is None else int(workspace.numel()),
                                            _stream_ptr(stream))

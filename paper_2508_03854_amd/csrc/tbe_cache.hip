@@ -163,7 +163,7 @@ __global__ __launch_bounds__(kCacheThreads) void cache_read_kernel(const CacheCo
 
 template <typename T, bool I8>
 static void launch_copy(const CacheCopyArgs& a, const bool write, hipStream_t s) {
-    const dim3 grid(std::min(((a.units + 3) / 4), 4096u), 2);
+    const dim3 grid(std::min((a.units + 3) / 4, 1u << 22), 2);   // (a side of a grid has fewer than 2^32 lanes)
     if (write) cache_write_kernel<T, I8><<<grid, kCacheThreads, 0, s>>>(a);
     else cache_read_kernel<T, I8><<<grid, kCacheThreads, 0, s>>>(a);
 }

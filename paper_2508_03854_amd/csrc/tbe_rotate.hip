@@ -5,7 +5,7 @@
 //             dx = r (u - h 1/n sum u h),  dw = sum over rows and heads of g h
 // Bound: the stream, every element read once and written once.  A head's elements stay in registers between its sum and its turn; a pair lies
 // in one lane, in either layout, so that nothing but the sum crosses lanes.  The turns are counted in 64 bits and reduced to an eighth of a turn
-// before they become fp32; a lane finds sine and cosine of its pairs once for all heads of a row that it meets.
+// before they become fp32; a wavefront finds sine and cosine of its rows' pairs together, once for the heads that it has.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -36,16 +36,19 @@ __device__ __forceinline__ float2 cos_sin(double turns) {
     return make_float2(k & 2 ? (k & 1 ? a : -a) : (k & 1 ? -a : a), k & 2 ? -b : b);
 }
 
-// The n elements at p, as fp32; those behind them are 0 and are not read.
+// The n elements at p as they are; those behind them are 0 and are not read.
 template <typename T>
-__device__ __forceinline__ void load_some(const T* p, const int n, float (&x)[Frag<T>::kN]) {
+__device__ __forceinline__ uint4 load_some(const T* p, const int n) {
     constexpr int kN = Frag<T>::kN;
-    if (n == kN) {
-        Frag<T>::unpack(Frag<T>::load(p), x);
-    } else {
+    if (n == kN) return Frag<T>::load(p);
+    uint32_t w[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
-        for (int i = 0; i < kN; ++i) x[i] = i < n ? elem_float(p[i]) : 0.f;
-    }
+    for (int i = 0; i < kN; ++i)
+        if (i < n) {
+            if constexpr (kN == 4) w[i] = __float_as_uint(p[i]);
+            else w[i / 2] |= (uint32_t)reinterpret_cast<const unsigned short*>(p)[i] << (16 * (i % 2));
+        }
+    return make_uint4(w[0], w[1], w[2], w[3]);
 }
 template <typename T>
 __device__ __forceinline__ void store_some(T* p, const int n, const float (&x)[Frag<T>::kN]) {
@@ -58,11 +61,22 @@ __device__ __forceinline__ void store_some(T* p, const int n, const float (&x)[F
             if (i < n) p[i] = elem_round<T>(x[i]);
     }
 }
+// A run of `from` .. `end` that holds less than kN elements is moved back to kN of them, if there are so many from `lo` on (and, where pairs follow
+// each other, at an even distance): a lane then has some that its neighbour has too, the first `again` of its run.  Both make the same of them; sums
+// leave them out here.
+__device__ __forceinline__ void move_back(int& from, int& n, int& again, const int lo, const int kN, const bool even) {
+    again = 0;
+    if (n > 0 && n < kN && from + n - kN >= lo && !(even && ((kN - n) & 1))) {
+        again = kN - n;
+        from -= again;
+        n = kN;
+    }
+}
 
-__device__ __forceinline__ void turn(const bool turned, const float c, const float s, float& x, float& y) {
+__device__ __forceinline__ void turn(const bool turned, const float2 cs, float& x, float& y) {
     const float a = x, b = y;
-    x = turned ? a * c - b * s : a;
-    y = turned ? b * c + a * s : b;
+    x = turned ? a * cs.x - b * cs.y : a;
+    y = turned ? b * cs.x + a * cs.y : b;
 }
 
 // q or k.  Wavefronts take units: `per` rows, of each `beside` heads beside each other, `turns` times; `pieces` units cover all heads of the rows.
@@ -88,76 +102,116 @@ constexpr int kTurnThreads = 256;
 template <typename T, bool BACK, bool NORM, bool PAIRS>
 __global__ __launch_bounds__(kTurnThreads) void rotate_kernel(const TurnArgs a) {
     constexpr int kN = Frag<T>::kN;
-    __shared__ float join[4][256];
+    __shared__ float2 tables[4][64 * kN + kN];   // cosine and sine of the pairs of a wavefront's rows, times the amplitude
+    __shared__ float join[BACK && NORM ? 4 : 1][256];
     const bool second = blockIdx.x >= a.part[0].blocks;
     const TurnPart& p = a.part[second];
     const uint32_t block = second ? blockIdx.x - a.part[0].blocks : blockIdx.x;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = lane_id(), lg = a.lanes_log2, l = lane & ((1 << lg) - 1), group = lane >> lg;
-    const int lg_per = 6 - lg - p.lg_beside;
+    const int lg_per = 6 - lg - p.lg_beside, beside = 1 << p.lg_beside, mine = group >> p.lg_beside;   // mine: this lane's of the wavefront's rows
     // This lane's elements of a head: two runs of up to kN.  Pairs (j, j + half): the runs lie `half` apart, behind them the elements that are not
     // turned; pairs (2 j, 2 j + 1): the runs follow each other.
-    int ea, eb, na, nb, first;   // first: number of the first pair
+    int ea, eb, na, nb, first, again_a, again_b;   // first: number of the first pair
     if (PAIRS) {
         ea = 2 * kN * l;
         eb = ea + kN;
-        first = ea / 2;
         na = a.dim - ea;
         nb = a.dim - eb;
+        na = na < 0 ? 0 : (na < kN ? na : kN);
+        nb = nb < 0 ? 0 : (nb < kN ? nb : kN);
+        first = ea / 2;   // (of the first run; of the second: below)
+        move_back(ea, na, again_a, 0, kN, true);
+        move_back(eb, nb, again_b, 0, kN, true);
+        first = ea / 2;
     } else {
         const int turning = (a.half + kN - 1) / kN;
-        first = l * kN;
-        ea = l < turning ? first : 2 * a.half + 2 * kN * (l - turning);
-        eb = l < turning ? a.half + first : ea + kN;
-        na = l < turning ? a.half - first : a.dim - ea;
-        nb = l < turning ? na : a.dim - eb;
-        if (l >= turning) first = a.half;   // (no pair)
+        const bool turns = l < turning;
+        ea = turns ? l * kN : 2 * a.half + 2 * kN * (l - turning);
+        na = (turns ? a.half : a.dim) - ea;
+        na = na < 0 ? 0 : (na < kN ? na : kN);
+        eb = ea + kN;
+        nb = a.dim - eb;
+        nb = nb < 0 ? 0 : (nb < kN ? nb : kN);
+        move_back(ea, na, again_a, turns ? 0 : 2 * a.half, kN, false);
+        if (turns) {
+            eb = a.half + ea;
+            nb = na;
+            again_b = again_a;
+        } else {
+            move_back(eb, nb, again_b, 2 * a.half, kN, false);
+        }
+        first = turns ? ea : a.half;   // (no pair)
     }
-    na = na < 0 ? 0 : (na < kN ? na : kN);
-    nb = nb < 0 ? 0 : (nb < kN ? nb : kN);
-    double f[kN];
+    const int first_b = PAIRS ? eb / 2 : first;
     float wa[kN], wb[kN], dwa[kN], dwb[kN];
 #pragma unroll
     for (int j = 0; j < kN; ++j) {
-        f[j] = first + j < a.half ? a.frequencies[first + j] * 0.15915494309189533577 : 0.0;   // turns a position
         wa[j] = NORM && p.weight && j < na ? param_load(p.weight, a.param_io, ea + j) : 1.f;
         wb[j] = NORM && p.weight && j < nb ? param_load(p.weight, a.param_io, eb + j) : 1.f;
         dwa[j] = dwb[j] = 0.f;
     }
     const float inv = 1.f / (float)a.dim;
+    const int pairs = a.half << lg_per;   // of a wavefront's rows
+    float2* const table = tables[wave];
     for (uint32_t u = block * 4 + wave; u < p.units; u += p.blocks * 4) {
         const uint32_t step = u / (uint32_t)p.pieces;
         const int piece = (int)(u - step * (uint32_t)p.pieces);
-        const int64_t row = ((int64_t)step << lg_per) + (group >> p.lg_beside);
+        const int64_t row0 = (int64_t)step << lg_per, row = row0 + mine;
         const bool is = row < a.rows;
         const int64_t at = is ? row : 0;
-        const double position = (double)a.positions[at];
-        float c[kN], s[kN];
-#pragma unroll
-        for (int j = 0; j < kN; ++j) {
-            const float2 cs = cos_sin(position * f[j]);
-            c[j] = cs.x * a.amplitude;
-            s[j] = BACK ? -cs.y * a.amplitude : cs.y * a.amplitude;
-        }
-        // (all lanes of a wavefront stay in the loop together: the sums across lanes need them)
-        for (int k = 0; k < p.turns; ++k) {
-            const int head = (((piece * p.turns + k) << p.lg_beside)) + (group & ((1 << p.lg_beside) - 1));
+        int head = ((piece * p.turns) << p.lg_beside) + (group & (beside - 1));
+        uint4 first_in[NORM && BACK ? 4 : 2];   // the first turn's elements, under way beside the angles
+        const auto load = [&](uint4 (&raw)[NORM && BACK ? 4 : 2]) __attribute__((always_inline)) {
             const bool here = is && head < p.heads;
             const int h0 = here ? head : 0, n0 = here ? na : 0, n1 = here ? nb : 0;
             const T* const from = static_cast<const T*>(BACK ? p.dy : p.x) + (BACK ? at * p.dy_row + h0 * p.dy_head : at * p.x_row + h0 * p.x_head);
-            float ua[kN], ub[kN], xa[kN], xb[kN];
-            load_some<T>(from + ea, n0, ua);
-            load_some<T>(from + eb, n1, ub);
+            raw[0] = load_some<T>(from + ea, n0);
+            raw[1] = load_some<T>(from + eb, n1);
             if constexpr (BACK && NORM) {
                 const T* const in = static_cast<const T*>(p.x) + at * p.x_row + h0 * p.x_head;
-                load_some<T>(in + ea, n0, xa);
-                load_some<T>(in + eb, n1, xb);
+                raw[2] = load_some<T>(in + ea, n0);
+                raw[3] = load_some<T>(in + eb, n1);
+            }
+        };
+        load(first_in);
+        // The rows' pairs shared among the wavefront's lanes: of a row, as many lanes as there are heads beside each other would otherwise do the same.
+        for (int n = lane; n < pairs; n += 64) {
+            const int of = n / a.half, pair = n - of * a.half;
+            const int64_t r = row0 + of < a.rows ? row0 + of : 0;
+            const float2 cs = cos_sin((double)a.positions[r] * (a.frequencies[pair] * 0.15915494309189533577));   // (in turns)
+            table[n] = make_float2(cs.x * a.amplitude, BACK ? -cs.y * a.amplitude : cs.y * a.amplitude);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        float2 cs[kN];   // (PAIRS: kN / 2 of either run)
+#pragma unroll
+        for (int j = 0; j < kN; ++j) {
+            const int pair = PAIRS ? (j < kN / 2 ? first + j : first_b + j - kN / 2) : first + j;
+            cs[j] = table[mine * a.half + (pair < a.half ? pair : 0)];
+        }
+        // (all lanes of a wavefront stay in the loop together: the sums across lanes need them)
+        for (int k = 0; k < p.turns; ++k) {
+            uint4 raw[NORM && BACK ? 4 : 2];
+            if (k > 0) {
+                load(raw);
+            } else {
+#pragma unroll
+                for (int i = 0; i < (NORM && BACK ? 4 : 2); ++i) raw[i] = first_in[i];
+            }
+            const bool here = is && head < p.heads;
+            float ua[kN], ub[kN], xa[kN], xb[kN];
+            Frag<T>::unpack(raw[0], ua);
+            Frag<T>::unpack(raw[1], ub);
+            if constexpr (BACK && NORM) {
+                Frag<T>::unpack(raw[2], xa);
+                Frag<T>::unpack(raw[3], xb);
             }
             if constexpr (!BACK && NORM) {
                 float q = 0.f;
 #pragma unroll
-                for (int j = 0; j < kN; ++j) q = fmaf(ua[j], ua[j], q);
+                for (int j = 0; j < kN; ++j) q = j < again_a ? q : fmaf(ua[j], ua[j], q);
 #pragma unroll
-                for (int j = 0; j < kN; ++j) q = fmaf(ub[j], ub[j], q);
+                for (int j = 0; j < kN; ++j) q = j < again_b ? q : fmaf(ub[j], ub[j], q);
                 const float r = 1.f / sqrtf(group_sum(q, 1 << lg) * inv + a.eps);
 #pragma unroll
                 for (int j = 0; j < kN; ++j) {
@@ -169,24 +223,24 @@ __global__ __launch_bounds__(kTurnThreads) void rotate_kernel(const TurnArgs a) 
             if constexpr (PAIRS) {
 #pragma unroll
                 for (int j = 0; j < kN; j += 2) {
-                    turn(first + j / 2 < a.half, c[j / 2], s[j / 2], ua[j], ua[j + 1]);
-                    turn(first + (kN + j) / 2 < a.half, c[(kN + j) / 2], s[(kN + j) / 2], ub[j], ub[j + 1]);
+                    turn(first + j / 2 < a.half, cs[j / 2], ua[j], ua[j + 1]);
+                    turn(first_b + j / 2 < a.half, cs[(kN + j) / 2], ub[j], ub[j + 1]);
                 }
             } else {
 #pragma unroll
-                for (int j = 0; j < kN; ++j) turn(first < a.half, c[j], s[j], ua[j], ub[j]);
+                for (int j = 0; j < kN; ++j) turn(first < a.half, cs[j], ua[j], ub[j]);
             }
             if constexpr (BACK && NORM) {
                 float q = 0.f, m = 0.f;
 #pragma unroll
                 for (int j = 0; j < kN; ++j) {
-                    q = fmaf(xa[j], xa[j], q);
-                    m = fmaf(ua[j] * wa[j], xa[j], m);
+                    q = j < again_a ? q : fmaf(xa[j], xa[j], q);
+                    m = j < again_a ? m : fmaf(ua[j] * wa[j], xa[j], m);
                 }
 #pragma unroll
                 for (int j = 0; j < kN; ++j) {
-                    q = fmaf(xb[j], xb[j], q);
-                    m = fmaf(ub[j] * wb[j], xb[j], m);
+                    q = j < again_b ? q : fmaf(xb[j], xb[j], q);
+                    m = j < again_b ? m : fmaf(ub[j] * wb[j], xb[j], m);
                 }
                 float r = 1.f / sqrtf(group_sum(q, 1 << lg) * inv + a.eps);
                 r = here ? r : 0.f;
@@ -200,10 +254,12 @@ __global__ __launch_bounds__(kTurnThreads) void rotate_kernel(const TurnArgs a) 
                     ub[j] = r * (ub[j] * wb[j] - hb * m);
                 }
             }
-            T* const to = static_cast<T*>(p.y) + at * p.y_row + h0 * p.y_head;
-            store_some<T>(to + ea, n0, ua);
-            store_some<T>(to + eb, n1, ub);
+            T* const to = static_cast<T*>(p.y) + at * p.y_row + (here ? head : 0) * p.y_head;
+            store_some<T>(to + ea, here ? na : 0, ua);
+            store_some<T>(to + eb, here ? nb : 0, ub);
+            head += beside;
         }
+        __builtin_amdgcn_wave_barrier();   // (the next rows' pairs go where these are)
     }
     if constexpr (BACK && NORM) {
         if (!p.partial) return;
@@ -217,8 +273,8 @@ __global__ __launch_bounds__(kTurnThreads) void rotate_kernel(const TurnArgs a) 
         if (group == 0) {
 #pragma unroll
             for (int j = 0; j < kN; ++j) {
-                if (j < na) join[wave][ea + j] = dwa[j];
-                if (j < nb) join[wave][eb + j] = dwb[j];
+                if (j >= again_a && j < na) join[wave][ea + j] = dwa[j];
+                if (j >= again_b && j < nb) join[wave][eb + j] = dwb[j];
             }
         }
         __syncthreads();
@@ -280,7 +336,7 @@ static void turn_blocks(TurnPart& q, TurnPart& k, const int64_t most) {
     q.blocks = some(q);
     k.blocks = some(k);
 }
-constexpr int64_t kTurnBlocksForward = 2048, kTurnBlocksBackward = 1024;
+constexpr int64_t kTurnBlocksForward = 8192, kTurnBlocksBackward = 3072;
 
 size_t rotate_workspace(const int dim) {   // (of any element type and layout)
     return (((size_t)kTurnBlocksBackward + 2) * (size_t)dim * sizeof(float) + 255) & ~(size_t)255;
