@@ -38,7 +38,7 @@ struct CacheCopyArgs {
     CodeRows cache[2];
     IdxView slots;
     int64_t rows, cache_rows;
-    int heads, dim, lg, lg_beside, turns, pieces;
+    int heads, dim, lanes, beside, per, turns, pieces;   // lanes: of a head, a power of two: its maximum crosses lanes
     uint32_t units;
     int32_t* err;
 };
@@ -49,12 +49,12 @@ struct CopyPlace {
     int head, e;   // first head; first element
 };
 __device__ __forceinline__ CopyPlace copy_place(const CacheCopyArgs& a, const uint32_t u) {
-    const int lane = lane_id(), group = lane >> a.lg;
+    const int lane = lane_id(), group = lane / a.lanes, mine = group / a.beside;
     const uint32_t step = u / (uint32_t)a.pieces, piece = u - step * (uint32_t)a.pieces;
     CopyPlace p;
-    p.row = ((int64_t)step << (6 - a.lg - a.lg_beside)) + (group >> a.lg_beside);
-    p.head = (int)((piece * (uint32_t)a.turns) << a.lg_beside) + (group & ((1 << a.lg_beside) - 1));
-    p.e = 16 * (lane & ((1 << a.lg) - 1));
+    p.row = mine < a.per ? (int64_t)step * a.per + mine : a.rows;
+    p.head = (int)(piece * (uint32_t)(a.turns * a.beside)) + group - mine * a.beside;
+    p.e = 16 * (lane - group * a.lanes);
     p.slot = p.row < a.rows ? a.slots[p.row] : -1;
     if (p.slot >= a.cache_rows) {
         *a.err = 1;
@@ -72,7 +72,7 @@ __global__ __launch_bounds__(kCacheThreads) void cache_write_kernel(const CacheC
     for (uint32_t u = blockIdx.x * 4 + (threadIdx.x >> 6); u < a.units; u += gridDim.x * 4) {
         const CopyPlace p = copy_place(a, u);
         for (int t = 0; t < a.turns; ++t) {
-            const int head = p.head + (t << a.lg_beside);
+            const int head = p.head + t * a.beside;
             const bool is = p.slot >= 0 && head < a.heads, there = is && p.e < a.dim;
             const T* const from = reinterpret_cast<const T*>(a.x[kv] + (is ? p.row * a.row[kv] + head * a.head[kv] : 0)) + (there ? p.e : 0);
             float x[16];
@@ -88,7 +88,7 @@ __global__ __launch_bounds__(kCacheThreads) void cache_write_kernel(const CacheC
                     top = m > top ? m : top;
                 }
             }
-            top = group_max(top, 1 << a.lg);
+            top = group_max(top, a.lanes);
             const bool finite = top < 0x7F800000u;
             float scale = 1.f;
             uint32_t code[4];
@@ -133,7 +133,7 @@ __global__ __launch_bounds__(kCacheThreads) void cache_read_kernel(const CacheCo
         const CopyPlace p = copy_place(a, u);
         if (p.row >= a.rows || p.e >= a.dim) continue;
         for (int t = 0; t < a.turns; ++t) {
-            const int head = p.head + (t << a.lg_beside);
+            const int head = p.head + t * a.beside;
             if (head >= a.heads) continue;
             uint4 c = make_uint4(0u, 0u, 0u, 0u);
             float scale = 0.f;   // (no place: zeros)
@@ -185,17 +185,14 @@ hipError_t launch_cache_copy(const tbe_handle* h, const CacheCopyCall& c, const 
     }
     a.slots = IdxView{c.slots, c.slots32};
     a.rows = c.rows; a.cache_rows = c.cache_rows; a.heads = c.heads; a.dim = c.dim; a.err = h->d_err;
-    // A group of lanes has a row's head; as many heads beside each other as there are and a wavefront has room for, the others one after the other,
-    // unless there would be few wavefronts then.
-    const auto log2_up = [](const int64_t x) {
-        int n = 0;
-        while (((int64_t)1 << n) < x) ++n;
-        return n;
-    };
-    a.lg = log2_up(c.dim / 16);
-    a.lg_beside = std::min(6 - a.lg, log2_up(c.heads));
-    const int lg_per = 6 - a.lg - a.lg_beside;
-    const int64_t steps = (c.rows + ((int64_t)1 << lg_per) - 1) >> lg_per, all = (c.heads + (1 << a.lg_beside) - 1) >> a.lg_beside;
+    // A group of lanes has a row's head; heads that are not beside each other come one after the other, unless there would be few wavefronts then.
+    // (Reading with 6 lanes for 96 elements, more of them busy but a row's heads in several turns, took 151 us where 8 lanes take 136: 120,011 rows of 8.)
+    a.lanes = c.dim / 16;
+    while (a.lanes & (a.lanes - 1)) ++a.lanes;
+    const HeadShare share = share_heads(64 / a.lanes, c.heads);
+    a.beside = share.beside;
+    a.per = share.per;
+    const int64_t steps = (c.rows + a.per - 1) / a.per, all = (c.heads + a.beside - 1) / a.beside;
     const int64_t want = std::max<int64_t>(1, std::min<int64_t>(all, 8192 / std::max<int64_t>(1, steps)));
     a.turns = (int)((all + want - 1) / want);
     a.pieces = (int)((all + a.turns - 1) / a.turns);

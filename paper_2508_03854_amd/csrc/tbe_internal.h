@@ -165,6 +165,25 @@ hipError_t launch_layer_norm_backward(const tbe_handle* h, const void* dy, int64
                                       int64_t rows, int n, const void* weight, int param_io, const float* mean, const float* rstd,
                                       void* dx, int64_t dx_stride, void* dw, void* db, void* workspace, hipStream_t s);
 
+// How a wavefront's groups of lanes, a head of a row for each, take the heads of rows: `beside` heads of `per` rows at a time.  As many heads beside
+// each other as there are, which lie beside each other in memory too, unless with fewer of them a fifth more of the groups are busy.
+struct HeadShare {
+    int beside, per;
+};
+inline HeadShare share_heads(const int groups, const int heads) {
+    HeadShare best{0, 0};
+    double most = 0.0;
+    for (int b = groups < heads ? groups : heads; b >= 1; --b) {
+        const int per = groups / b, turns = (heads + b - 1) / b;
+        const double busy = (double)heads * per / ((double)groups * turns);
+        if (busy > 1.2 * most) {
+            best = HeadShare{b, per};
+            most = busy;
+        }
+    }
+    return best;
+}
+
 // heads normed and rotated by position (tbe_rotate.hip)
 constexpr int kRotateMaxDim = 256;
 struct RotateMatrix {

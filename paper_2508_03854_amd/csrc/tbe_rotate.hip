@@ -86,14 +86,14 @@ struct TurnPart {
     int64_t x_row, x_head, dy_row, dy_head, y_row, y_head;   // elements
     float* partial;   // [blocks][dim], or null
     uint32_t units, blocks;
-    int heads, lg_beside, turns, pieces;
+    int heads, beside, per, turns, pieces;
 };
 struct TurnArgs {
     TurnPart part[2];
     IdxView positions;
     const double* frequencies;
     int64_t rows;
-    int dim, half, lanes_log2, param_io;   // half: pairs
+    int dim, half, lanes, param_io;   // half: pairs; lanes: of a head (with a norm a power of two: their sums cross lanes)
     float eps, amplitude;
 };
 
@@ -107,8 +107,8 @@ __global__ __launch_bounds__(kTurnThreads) void rotate_kernel(const TurnArgs a) 
     const bool second = blockIdx.x >= a.part[0].blocks;
     const TurnPart& p = a.part[second];
     const uint32_t block = second ? blockIdx.x - a.part[0].blocks : blockIdx.x;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = lane_id(), lg = a.lanes_log2, l = lane & ((1 << lg) - 1), group = lane >> lg;
-    const int lg_per = 6 - lg - p.lg_beside, beside = 1 << p.lg_beside, mine = group >> p.lg_beside;   // mine: this lane's of the wavefront's rows
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = lane_id(), lanes = a.lanes, group = lane / lanes, l = lane - group * lanes;
+    const int beside = p.beside, mine = group / beside;   // mine: this lane's of the wavefront's rows (`per` and more: none)
     // This lane's elements of a head: two runs of up to kN.  Pairs (j, j + half): the runs lie `half` apart, behind them the elements that are not
     // turned; pairs (2 j, 2 j + 1): the runs follow each other.
     int ea, eb, na, nb, first, again_a, again_b;   // first: number of the first pair
@@ -151,15 +151,15 @@ __global__ __launch_bounds__(kTurnThreads) void rotate_kernel(const TurnArgs a) 
         dwa[j] = dwb[j] = 0.f;
     }
     const float inv = 1.f / (float)a.dim;
-    const int pairs = a.half << lg_per;   // of a wavefront's rows
+    const int pairs = a.half * p.per;   // of a wavefront's rows
     float2* const table = tables[wave];
     for (uint32_t u = block * 4 + wave; u < p.units; u += p.blocks * 4) {
         const uint32_t step = u / (uint32_t)p.pieces;
         const int piece = (int)(u - step * (uint32_t)p.pieces);
-        const int64_t row0 = (int64_t)step << lg_per, row = row0 + mine;
-        const bool is = row < a.rows;
+        const int64_t row0 = (int64_t)step * p.per, row = row0 + mine;
+        const bool is = mine < p.per && row < a.rows;
         const int64_t at = is ? row : 0;
-        int head = ((piece * p.turns) << p.lg_beside) + (group & (beside - 1));
+        int head = piece * p.turns * beside + group - mine * beside;
         uint4 first_in[NORM && BACK ? 4 : 2];   // the first turn's elements, under way beside the angles
         const auto load = [&](uint4 (&raw)[NORM && BACK ? 4 : 2]) __attribute__((always_inline)) {
             const bool here = is && head < p.heads;
@@ -187,7 +187,7 @@ __global__ __launch_bounds__(kTurnThreads) void rotate_kernel(const TurnArgs a) 
 #pragma unroll
         for (int j = 0; j < kN; ++j) {
             const int pair = PAIRS ? (j < kN / 2 ? first + j : first_b + j - kN / 2) : first + j;
-            cs[j] = table[mine * a.half + (pair < a.half ? pair : 0)];
+            cs[j] = table[is ? mine * a.half + (pair < a.half ? pair : 0) : 0];
         }
         // (all lanes of a wavefront stay in the loop together: the sums across lanes need them)
         for (int k = 0; k < p.turns; ++k) {
@@ -212,7 +212,7 @@ __global__ __launch_bounds__(kTurnThreads) void rotate_kernel(const TurnArgs a) 
                 for (int j = 0; j < kN; ++j) q = j < again_a ? q : fmaf(ua[j], ua[j], q);
 #pragma unroll
                 for (int j = 0; j < kN; ++j) q = j < again_b ? q : fmaf(ub[j], ub[j], q);
-                const float r = 1.f / sqrtf(group_sum(q, 1 << lg) * inv + a.eps);
+                const float r = 1.f / sqrtf(group_sum(q, lanes) * inv + a.eps);
 #pragma unroll
                 for (int j = 0; j < kN; ++j) {
                     ua[j] = ua[j] * r * wa[j];
@@ -242,9 +242,9 @@ __global__ __launch_bounds__(kTurnThreads) void rotate_kernel(const TurnArgs a) 
                     q = j < again_b ? q : fmaf(xb[j], xb[j], q);
                     m = j < again_b ? m : fmaf(ub[j] * wb[j], xb[j], m);
                 }
-                float r = 1.f / sqrtf(group_sum(q, 1 << lg) * inv + a.eps);
+                float r = 1.f / sqrtf(group_sum(q, lanes) * inv + a.eps);
                 r = here ? r : 0.f;
-                m = group_sum(m, 1 << lg) * inv * r;   // the mean of u h
+                m = group_sum(m, lanes) * inv * r;   // the mean of u h
 #pragma unroll
                 for (int j = 0; j < kN; ++j) {
                     const float ha = xa[j] * r, hb = xb[j] * r;
@@ -264,7 +264,7 @@ __global__ __launch_bounds__(kTurnThreads) void rotate_kernel(const TurnArgs a) 
     if constexpr (BACK && NORM) {
         if (!p.partial) return;
         // the groups of a wavefront, then the wavefronts, in a fixed order
-        for (int w = 1 << lg; w < 64; w <<= 1)
+        for (int w = lanes; w < 64; w <<= 1)
 #pragma unroll
             for (int j = 0; j < kN; ++j) {
                 dwa[j] += __shfl_xor(dwa[j], w);
@@ -301,27 +301,23 @@ __global__ __launch_bounds__(256) void rotate_params_kernel(const float* __restr
     }
 }
 
-static int log2_up(const int64_t x) {
-    int n = 0;
-    while (((int64_t)1 << n) < x) ++n;
-    return n;
-}
-// lanes of a head (log2), at most 64
-static int turn_lanes_log2(const int dim, const int half, const bool pairs, const int kN) {
+static int turn_lanes(const int dim, const int half, const bool pairs, const int kN, const bool norm) {
     const int lanes = pairs ? (dim + 2 * kN - 1) / (2 * kN) : (half + kN - 1) / kN + (dim - 2 * half + 2 * kN - 1) / (2 * kN);
-    return log2_up(lanes);
+    int n = 1;
+    while (n < lanes) n <<= 1;
+    return norm ? n : lanes;
 }
-// How the heads of q or k are shared among wavefronts: as many beside each other as there are and a wavefront has room for, the others one
-// after the other with the same sines and cosines, unless there would be few wavefronts then.
-static void turn_units(TurnPart& p, const int64_t rows, const int heads, const int lg) {
+// How the heads of q or k are shared among wavefronts: some beside each other, the others one after the other with the same sines and cosines, unless
+// there would be few wavefronts then.
+static void turn_units(TurnPart& p, const int64_t rows, const int heads, const int lanes) {
     p.heads = heads;
     p.units = 0;
-    p.pieces = p.turns = 1;
-    p.lg_beside = 0;
+    p.pieces = p.turns = p.per = p.beside = 1;
     if (heads == 0) return;
-    p.lg_beside = std::min(6 - lg, log2_up(heads));
-    const int lg_per = 6 - lg - p.lg_beside;
-    const int64_t steps = (rows + ((int64_t)1 << lg_per) - 1) >> lg_per, all = (heads + (1 << p.lg_beside) - 1) >> p.lg_beside;
+    const HeadShare share = share_heads(64 / lanes, heads);
+    p.beside = share.beside;
+    p.per = share.per;
+    const int64_t steps = (rows + p.per - 1) / p.per, all = (heads + p.beside - 1) / p.beside;
     const int64_t want = std::max<int64_t>(1, std::min<int64_t>(all, 8192 / std::max<int64_t>(1, steps)));
     p.turns = (int)((all + want - 1) / want);
     p.pieces = (int)((all + p.turns - 1) / p.turns);
@@ -364,7 +360,7 @@ hipError_t launch_rotate(const tbe_handle* h, const RotateCall& r, const bool ba
     a.frequencies = r.frequencies;
     a.rows = r.rows; a.dim = r.dim; a.half = r.turned / 2; a.param_io = r.param_io;
     a.eps = r.eps; a.amplitude = r.amplitude;
-    a.lanes_log2 = turn_lanes_log2(r.dim, a.half, r.pairs, r.io == 0 ? 4 : 8);
+    a.lanes = turn_lanes(r.dim, a.half, r.pairs, r.io == 0 ? 4 : 8, r.norm);
     for (int i = 0; i < 2; ++i) {
         const RotateMatrix& m = r.part[i];
         TurnPart& p = a.part[i];
@@ -372,7 +368,7 @@ hipError_t launch_rotate(const tbe_handle* h, const RotateCall& r, const bool ba
         p.dy = m.dy.data; p.dy_row = m.dy.row_stride; p.dy_head = m.dy.head_stride;
         p.y = m.y.data; p.y_row = m.y.row_stride; p.y_head = m.y.head_stride;
         p.weight = m.weight;
-        turn_units(p, r.rows, m.heads, a.lanes_log2);
+        turn_units(p, r.rows, m.heads, a.lanes);
     }
     turn_blocks(a.part[0], a.part[1], back ? kTurnBlocksBackward : kTurnBlocksForward);
     const bool weights = back && r.norm && (r.part[0].dw || r.part[1].dw);
