@@ -126,8 +126,9 @@ __device__ __forceinline__ int range_of(const int64_t tiles, const int ranges, c
 // others have the next ones.  All of the workgroup together; every sequence is judged on the way.  An ill-formed sequence counts as one without keys.
 struct RangeStart {
     int64_t tiles, begin;
-    int s;
+    int s, ranges;   // ranges: as many as there are indeed, since caches may be filled to a small part: none without a tile
 };
+constexpr int kRangeTiles = 2;   // a run has so many tiles at least
 __device__ __forceinline__ int64_t sequence_tiles(const AttnArgs& a, const int s, const int log2) {
     const LaneSequence n = lane_numbers(a, s);
     const int64_t room = n.k1 - n.k0, keys = a.k_len.p ? a.k_len[s] : room;
@@ -157,8 +158,10 @@ __device__ __forceinline__ RangeStart range_start(const CacheAttnArgs& a, const 
         if (k < wave) upto += waves[k];
         out.tiles += waves[k];
     }
+    const int64_t most = out.tiles / kRangeTiles;
+    out.ranges = most < 1 ? 1 : (most < a.ranges ? (int)most : a.ranges);
     for (int k = 0; k < kCacheWaves; ++k) {
-        const int64_t at = range_begin(out.tiles, a.ranges, r + k);
+        const int64_t at = range_begin(out.tiles, out.ranges, r + k);
         int64_t begin = upto - mine;
         if (at >= begin && at < upto) {
             int s = s0;
@@ -175,6 +178,7 @@ __device__ __forceinline__ RangeStart range_start(const CacheAttnArgs& a, const 
     out.s = uniform(found[wave]);
     out.begin = lane_i64(found_begin[wave], 0);
     out.tiles = lane_i64(out.tiles, 0);
+    out.ranges = uniform(out.ranges);
     return out;
 }
 
@@ -222,7 +226,7 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attn_kernel(const C
         __syncthreads();
     }
     int64_t at = 0, end = 1, begin = 0, all = 0;   // own: one turn of the loop below
-    int s = 0;
+    int s = 0, ranges = 1;
     if (a.own) {
         if (v >= (uint32_t)a.V) return;
         s = a.own == 2 ? (int)v : find_sequence(a.q_off, a.N, v, a.block);
@@ -231,10 +235,11 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attn_kernel(const C
         s = start.s;
         begin = start.begin;
         all = start.tiles;
+        ranges = start.ranges;
         r += wave;
-        if (r >= a.ranges) return;
-        at = range_begin(all, a.ranges, r);
-        end = range_begin(all, a.ranges, r + 1);
+        if (r >= ranges) return;
+        at = range_begin(all, ranges, r);
+        end = range_begin(all, ranges, r + 1);
     }
     int64_t numbers = a.own == 2 ? peek : (at < end ? sequence_numbers(a, s) : 0);
     for (; at < end; ++s) {
@@ -280,7 +285,7 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attn_kernel(const C
             w.cell = -1;
         }
         if (a0 == 0 && hh == 0 && qb == 0 && lane_id() == 0)
-            a.spans[s] = w.cell < 0 ? make_int2(0, 0) : make_int2(r, range_of(all, a.ranges, begin + n - 1));
+            a.spans[s] = w.cell < 0 ? make_int2(0, 0) : make_int2(r, range_of(all, ranges, begin + n - 1));
         begin += n;
         at = begin;
         if (!fits) continue;
@@ -670,7 +675,7 @@ __global__ __launch_bounds__(256, many ? 4 : 8) void cache_attn_join_kernel(cons
 // How the work is shared out.  Heads of a group lie side by side in a wavefront's columns where one query would leave them empty.  Short caches, or
 // so many units of queries that the chip is full: a wavefront for each unit.  Otherwise as many wavefronts as the chip holds at once share all
 // keys evenly among them.
-constexpr int64_t kRangeGroups = 512, kRangeTiles = 2;
+constexpr int64_t kRangeGroups = 512;
 CacheAttnPlan cache_attn_plan(const AttnShape& sh, const int max_pack) {
     CacheAttnPlan p;
     const int64_t mean_q = (sh.q_rows + sh.N - 1) / sh.N, mean_k = (sh.k_rows + sh.N - 1) / sh.N;

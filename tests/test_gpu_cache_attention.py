@@ -112,6 +112,49 @@ def test_many_sequences(tbe, code):
     compare(tbe, s, nq, nk, "many units")
 
 
+@pytest.mark.parametrize("code", [E4M3, I8])
+def test_caches_that_are_filled_to_a_small_part(tbe, code):
+    """Fewer tiles of keys than there is room for: the keys are shared out by what is there."""
+    for nq, nk, room, H, K, dim in (([1] * 4, [40, 0, 1, 33], [8192] * 4, 8, 2, 128), ([1, 1], [90, 5000], [60_000, 9000], 4, 4, 32), ([40, 3], [64, 70], [6000, 6000], 2, 1, 64),
+                                    ([1], [33], [100_000], 16, 1, 64), ([1] * 3, [0, 0, 0], [4000] * 3, 2, 2, 48)):
+        s = build(tbe, gen(21), nq, nk, room, H, K, dim, torch.bfloat16, code, buckets=0)
+        compare(tbe, s, nq, nk, f"{nk} of {room}")
+
+
+def test_uneven_queries_where_the_average_is_one(tbe):
+    """As many queries as sequences, but not one each: short caches, and long ones."""
+    for nk in ([100, 30, 200, 64, 10], [3000, 300, 900, 2000, 100]):
+        nq = [3, 0, 1, 1, 0]
+        s = build(tbe, gen(22), nq, nk, nk, 4, 2, 64, torch.float16, I8)
+        compare(tbe, s, nq, nk, f"{nq} {nk}")
+    nq, nk = [64] + [0] * 63, [200] + [90] * 63
+    s = build(tbe, gen(23), nq, nk, nk, 4, 2, 64, torch.bfloat16, E4M3)
+    compare(tbe, s, nq, nk, "all of them one's")
+
+
+def test_places_beyond_two_to_the_32nd_byte(tbe):
+    """The last sequence of a cache of 4.5e9 bytes, the first one of which has 2.2e6 keys."""
+    from paper_2508_03854_amd import Cache
+    first, last, H, dim = (1 << 32) // 2048 + 100_000, 300, 16, 128
+    g = gen(24)
+    k, v = (torch.zeros(first + last, H, dim, dtype=I8, device="cuda") for _ in range(2))
+    k[first:] = torch.randint(-127, 128, (last, H, dim), generator=g, device="cuda", dtype=torch.int32).to(I8)
+    v[first:] = torch.randint(-127, 128, (last, H, dim), generator=g, device="cuda", dtype=torch.int32).to(I8)
+    v[first - 1] = 127   # (the first sequence's last key)
+    scales = torch.full((H, first + last), 0.01, device="cuda")
+    cache = Cache(k, v, scales, scales)
+    q = torch.randn(2, H, dim, generator=g, device="cuda").to(torch.bfloat16)
+    qo, ko = torch.tensor([0, 1, 2], device="cuda"), torch.tensor([0, first, first + last], device="cuda")
+    out, lse = tbe.cache_attention(q, cache, qo, ko, tbe.alloc_cache_attention_workspace(2, 2, first + last, H, H, dim))
+    ref = reference(q[1:], k[first:].double() * 0.01, v[first:].double() * 0.01, [1], [last], [0], causal=True, scale=dim ** -0.5)
+    scale32 = float(torch.tensor(0.01)) / 0.01 - 1   # (fp32's 0.01)
+    ref["~out"] += abs(scale32) * (1 + ref["out"].abs()) * 4 + 1e-6
+    ref["~lse"] += abs(scale32) * 4 * ref["lse"].abs() + 1e-6
+    check((out[1:], lse[:, 1:]), ref, ("out", "lse"), "last")
+    assert (lse[:, 0].double() - math.log(first)).abs().max() <= 1e-5   # all scores 0: every key the same
+    assert (out[0].double() * first - 1.27).abs().max() <= 1.27 * 2.0 ** -7
+
+
 def test_long_cache(tbe):
     for code, io, H, K, dim in ((E4M3, torch.bfloat16, 16, 2, 128), (I8, torch.float32, 4, 4, 64), (E4M3, torch.float16, 3, 1, 32)):
         nk = [100_003, 260]
