@@ -42,8 +42,8 @@ struct CacheAttnPlan {
     int64_t V;
     size_t spans, part_ml, part_o;   // bytes
 };
-// max_pack: heads side by side at most
-CacheAttnPlan cache_attn_plan(const AttnShape& sh, int max_pack = 32);
+// light: bfloat16 queries over e4m3; max_pack: heads side by side at most
+CacheAttnPlan cache_attn_plan(const AttnShape& sh, bool light, int max_pack = 32);
 bool cache_attn_grid_ok(const AttnShape& sh, const CacheAttnPlan& p);   // the launches stay below 2^31 workgroups
 size_t cache_attn_workspace(const AttnShape& sh);   // for any max_distance
 hipError_t launch_cache_attention(const tbe_handle* h, const AttnArgs& call, const CodeRows (&cache)[2], bool i8, const CacheAttnPlan& p, int io,

@@ -4,7 +4,10 @@
 // A code has at most eight significant bits, so it is a bfloat16 exactly, and the products run on the matrix cores' bfloat16 form for every type
 // of q: a binary16 or fp32 factor is cut into two or three bfloat16 parts whose products are added (q exactly, probabilities to 2^-16 of
 // themselves or exactly).  bfloat16 probabilities are rounded once.
-// Bound: reading the codes once; 24 caches of long histories are 0.4 GB.
+// Bound: long caches by reading the codes once, a few dozen queries each by the vector unit's work on scores and codes (360 instructions a tile of
+// 64 binary16 elements beside 16 matrix products), short caches by a wavefront's trips to memory.  Measured: one query to each of 24 caches of 2000 to
+// 65536 keys, 16 heads over 2 of 128, bfloat16 over e4m3, 0.41 GB: 90 us and 8 for the join, 4.6 TB/s in the former; 61 queries to each of 48 of 100 to
+// 4000, 8 heads of 64, binary16 over i8: 66 and 15; one to each of 32 of 12 on average, 4 heads of 32 fp32 with a bias: 9.5.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -116,7 +119,7 @@ struct CacheAttnArgs : AttnArgs {
 };
 
 constexpr int kCacheWaves = 4, kCacheThreads = 64 * kCacheWaves;
-constexpr int kTileLog2 = 5;   // keys of a tile
+constexpr int kTileLog2 = 5;   // keys of a tile (heads of 32, 2000 caches of 60 on average: 64 keys 42 us, 32 keys 34; heads of 64: 84 / 82)
 
 // Run r of `ranges` over all `tiles` begins here; the run that a tile belongs to.
 __device__ __forceinline__ int64_t range_begin(const int64_t tiles, const int ranges, const int r) { return tiles * r / ranges; }
@@ -189,8 +192,12 @@ struct PartWork {
     int cell;                  // 0, 1: where the results go to be joined; -1: these are all keys
 };
 
+// Wavefronts of a SIMD that the registers are to leave room for (and the LDS does): heads of 32 2 / 3 / 4, us, 24 caches of 34,000 on average, 16 heads over 2,
+// bfloat16 45 / 43 / 43, fp32 54 / 52 / 54;  of 64 61 / 62 / -, 73 / 81 / - (registers in scratch memory).
+constexpr int cache_occupancy(const int D) { return D == 32 ? 3 : 2; }
+
 template <typename T, int D, bool I8, bool BIAS>
-__global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attn_kernel(const CacheAttnArgs a) {
+__global__ __launch_bounds__(64 * kCacheWaves, cache_occupancy(D)) void cache_attn_kernel(const CacheAttnArgs a) {
     constexpr int kWaves = kCacheWaves, kLog = kTileLog2, BK = 1 << kLog, kT = BK / 32, kD = D / 32, kC = D / 16, kP = parts<T>();
     constexpr int kTile = BK * D;
     typedef Mma<bf16_t> M;
@@ -519,7 +526,8 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attn_kernel(const C
         };
 
         // Two tiles of keys and of values are under way or in use; a buffer is filled anew as soon as its tile has been multiplied, so that the loads have
-        // a tile's time and a half.  They end in their order: of those begun after the ones waited for, so many may still run.
+        // a tile's time and a half (24 caches of long histories: 120 us where the next tile is asked for when this one is there, 93 so; 82 for the loads alone).
+        // They end in their order: of those begun after the ones waited for, so many may still run.
         constexpr int kGroup = BK * D / 1024 + 1;
         auto one = [&](const int t, char* const kt, float* const kst, char* const vt, float* const vst) __attribute__((always_inline)) {
             const bool next = t + 1 < tiles, after = t + 2 < tiles;
@@ -673,10 +681,19 @@ __global__ __launch_bounds__(256, many ? 4 : 8) void cache_attn_join_kernel(cons
 }
 
 // How the work is shared out.  Heads of a group lie side by side in a wavefront's columns where one query would leave them empty.  Short caches, or
-// so many units of queries that the chip is full: a wavefront for each unit.  Otherwise as many wavefronts as the chip holds at once share all
-// keys evenly among them.
-constexpr int64_t kRangeGroups = 512;
-CacheAttnPlan cache_attn_plan(const AttnShape& sh, const int max_pack) {
+// middling ones of enough sequences: a wavefront for each unit of queries, with all its keys.  Otherwise as many wavefronts as the chip holds at once
+// share all keys evenly, whosesoever they are, and what was cut is joined.  On their own / shared evenly, us, one query to each of so many caches
+// of that many keys on average (half to one and a half times as many), 32 heads of 128 over 8, bfloat16 over e4m3:
+//   8 of 128 17 / 22, of 256 24 / 22, of 2048 132 / 28;  32 of 256 25 / 25, of 512 40 / 28;  128 of 256 26 / 35, of 512 43 / 52, of 1024 76 / 82, of 2048 142 /
+//   140;  512 of 128 48 / 70, of 512 131 / 162;  1024 of 256 130 / 177
+// 4 heads of 32: 32 of 512 25 / 23, 256 of 512 27 / 34, of 1024 44 / 42;  61 queries each, 8 heads of 64, binary16 over i8: 8 of 256 23 / 26, 48 of 256 28 / 44, of
+// 1024 74 / 61.
+// Evenly among 512 workgroups, two wavefronts a SIMD (heads of 32: 768); among 256 where the codes' conversions are the cheapest (e4m3 into bfloat16 products of one
+// part), heads have 128 elements and runs are long, since memory then bounds it and fewer streams serve it better: 512 / 256, us, 24 caches of 34,000
+// on average, 16 heads over 2 of 128 bfloat16 101 / 97 (with a bias 122 / 107), 64 of 2250, 32 heads over 8 88 / 81, 128 of 2048 140 / 129;  but over i8 103 / 104,
+// binary16 110 / 110, fp32 136 / 185, heads of 64 61 / 72, 8 of 2048 28 / 33 and 61 queries each to 48 of 2050, 8 heads of 64, 79 / 98.
+constexpr int64_t kRangeGroups = 512, kRangeGroupsLight = 256, kLongRun = 16;   // kLongRun: tiles
+CacheAttnPlan cache_attn_plan(const AttnShape& sh, const bool light, const int max_pack) {
     CacheAttnPlan p;
     const int64_t mean_q = (sh.q_rows + sh.N - 1) / sh.N, mean_k = (sh.k_rows + sh.N - 1) / sh.N;
     p.D = sh.dim <= 32 ? 32 : (sh.dim <= 64 ? 64 : 128);
@@ -695,10 +712,12 @@ CacheAttnPlan cache_attn_plan(const AttnShape& sh, const int max_pack) {
     if (p.own) return p;
     p.qblocks = (int)std::max<int64_t>(1, (mean_q + p.block - 1) / p.block);
     const int64_t each = packs * p.qblocks;
-    p.ranges = (int)std::max<int64_t>(1, kRangeGroups / each) * kCacheWaves;
+    const int64_t tiles = (sh.k_rows >> kTileLog2) + sh.N;
+    const bool few = light && p.D == 128 && p.qblocks == 1 && tiles * each >= kLongRun * kRangeGroups * kCacheWaves;
+    p.ranges = (int)std::max<int64_t>(1, (few ? kRangeGroupsLight : kRangeGroups * cache_occupancy(p.D) / 2) / each) * kCacheWaves;
     if (p.ranges >= 8 * kCacheWaves) p.ranges &= ~(8 * kCacheWaves - 1);
     // no shorter than a few tiles
-    p.ranges = (int)std::max<int64_t>(1, std::min<int64_t>(p.ranges, ((sh.k_rows >> kTileLog2) + sh.N) / kRangeTiles));
+    p.ranges = (int)std::max<int64_t>(1, std::min<int64_t>(p.ranges, tiles / kRangeTiles));
     p.spans = ((size_t)sh.N * sizeof(int2) + 255) & ~(size_t)255;
     const int64_t cells = p.ranges > 1 ? 2 * p.ranges * each * 32 : 0;
     p.part_ml = ((size_t)cells * 8 + 255) & ~(size_t)255;
@@ -718,7 +737,7 @@ size_t cache_attn_workspace(const AttnShape& sh) {
     for (int pack = 1; pack <= 32; ++pack) {   // (how many heads go side by side depends on the bias)
         AttnShape any = sh;
         any.far = 0;
-        const CacheAttnPlan p = cache_attn_plan(any, pack);
+        const CacheAttnPlan p = cache_attn_plan(any, false, pack);
         most = std::max(most, p.spans + p.part_ml + p.part_o);
     }
     return most;
@@ -765,7 +784,8 @@ hipError_t launch_cache_attention(const tbe_handle* h, const AttnArgs& call, con
     AttnShape sh{};
     sh.H = a.H;
     const uint64_t groups = (uint64_t)plan_groups(sh, p);
-    const int join = p.part_ml > 0 ? (p.ranges > 16 * (int64_t)a.N ? 2 : 1) : 0;   // 2: many parts
+    // 2: many parts of each sequence, a workgroup for a head (24 long histories in 43 parts each, 8 heads a workgroup / one: 17 / 8 us)
+    const int join = p.part_ml > 0 ? (p.ranges > 16 * (int64_t)a.N ? 2 : 1) : 0;
     return io == 0 ? launch_type<float>(h, a, p.D, i8, groups, join, s) : (io == 1 ? launch_type<__half>(h, a, p.D, i8, groups, join, s) : launch_type<bf16_t>(h, a, p.D, i8, groups, join, s));
 }
 

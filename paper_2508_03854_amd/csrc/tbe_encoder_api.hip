@@ -355,7 +355,7 @@ tbe_status tbe_cache_attention(const tbe_handle* h, const tbe_attention_args* ar
     if (!rows_view(out, args->q_rows, args->heads, args, true, k.o) || !multiple_of(lse, 4)) return TBE_EINVAL;
     k.lse = lse;
     const AttnShape sh = attention_shape(args);
-    const CacheAttnPlan p = cache_attn_plan(sh);
+    const CacheAttnPlan p = cache_attn_plan(sh, args->dtype == TBE_IO_BF16 && cache->code == TBE_CODE_E4M3);
     const size_t need = p.spans + p.part_ml + p.part_o;
     if (need > 0) {
         if (!workspace || !multiple_of(workspace, 256)) return TBE_EINVAL;

@@ -166,7 +166,9 @@ hipError_t launch_layer_norm_backward(const tbe_handle* h, const void* dy, int64
                                       void* dx, int64_t dx_stride, void* dw, void* db, void* workspace, hipStream_t s);
 
 // How a wavefront's groups of lanes, a head of a row for each, take the heads of rows: `beside` heads of `per` rows at a time.  As many heads beside
-// each other as there are, which lie beside each other in memory too, unless with fewer of them a fifth more of the groups are busy.
+// each other as there are, which lie beside each other in memory too, unless with fewer of them a fifth more of the groups are busy:
+// rotations of 100,000 rows of 12 and 4 heads of 64 bfloat16 (16 groups), 12 beside each other / 4 of 4 rows: 135 / 100 us; of 60,001 rows of 8 and 8 of 80
+// fp32 (6 groups), 6 / 3 of 2 rows: 137 / 140.
 struct HeadShare {
     int beside, per;
 };
