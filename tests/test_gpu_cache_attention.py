@@ -121,6 +121,23 @@ def test_caches_that_are_filled_to_a_small_part(tbe, code):
         compare(tbe, s, nq, nk, f"{nk} of {room}")
 
 
+def test_many_caches_shared_out_evenly(tbe):
+    """More sequences than a workgroup has lanes, in one run or several; some of them empty."""
+    nk = [(37 * i * i + 11 * i) % 900 for i in range(601)]
+    nk[5] = nk[300] = nk[600] = 0
+    for code, io, nq, H, K, dim in ((E4M3, torch.bfloat16, [1] * 601, 1, 1, 128), (I8, torch.float32, [i % 3 for i in range(601)], 2, 2, 32)):
+        s = build(tbe, gen(25), nq, nk, [n + 2 for n in nk], H, K, dim, io, code)
+        compare(tbe, s, nq, nk, "even")
+
+
+def test_largest_tables_of_distances(tbe):
+    for H, K, dim, far in ((4, 1, 128, 1024), (8, 2, 32, 700), (3, 3, 64, 1024), (4, 2, 64, 0)):
+        for nq, nk in (([1, 1, 1], [3000, 900, 40]), ([33, 2], [1500, 2100])):
+            for causal in (True, False):
+                s = build(tbe, gen(26), nq, nk, nk, H, K, dim, torch.bfloat16, E4M3, buckets=20, far=far, causal=causal)
+                compare(tbe, s, nq, nk, f"{H} {dim} {far} {nk}", causal)
+
+
 def test_uneven_queries_where_the_average_is_one(tbe):
     """As many queries as sequences, but not one each: short caches, and long ones."""
     for nk in ([100, 30, 200, 64, 10], [3000, 300, 900, 2000, 100]):
