@@ -454,7 +454,7 @@ tbe_status tbe_cache_read(const tbe_handle* h, const tbe_cache* cache, const voi
 /* Attention over such a cache: tbe_attention with k = the codes of cache->k times their scales, v likewise, none of which is written out.  args as there, but
  * its k and v are not looked at; kv_heads, head_dim and k_rows are the cache's heads, head_dim and rows (TBE_ESHAPE), so head_dim is a multiple of 16.  dtype
  * is that of q and out.  Products are exact in q and the codes and added in fp32, scales are multiplied in fp32; a probability times its value's scale is
- * rounded to bfloat16 where dtype is TBE_IO_BF16, to 16 bits or more for TBE_IO_F16, not at all for TBE_IO_F32; results once when stored.  What is hidden is
+ * rounded to 16 bits, for TBE_IO_F32 not at all; results once when stored.  What is hidden is
  * left out, scales and codes that are not numbers among it; a scale that is infinite may make NaN of what sees it. */
 tbe_status tbe_cache_attention_workspace_bytes(const tbe_handle* h, const tbe_attention_args* args, size_t* bytes);
 tbe_status tbe_cache_attention(const tbe_handle* h, const tbe_attention_args* args, const tbe_cache* cache, tbe_rows out, float* lse, void* workspace,

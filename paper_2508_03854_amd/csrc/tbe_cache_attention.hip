@@ -2,8 +2,8 @@
 // probabilities are in fp32 anyway; no value of the cache is ever written out.
 //   S^T = C_k Q^T  (a tile: 32 keys x 32 columns)    x = S scale s_k    p = 2^(x - m)    O^T += C_v^T (P s_v)
 // A code has at most eight significant bits, so it is a bfloat16 exactly, and the products run on the matrix cores' bfloat16 form for every type
-// of q: a binary16 or fp32 factor is cut into two or three bfloat16 parts whose products are added (q exactly, probabilities to 2^-16 of
-// themselves or exactly).  bfloat16 probabilities are rounded once.
+// of q: q is cut into one (bfloat16), two (binary16) or three (fp32) bfloat16 parts whose products are added, exactly, probabilities into two parts, to
+// 2^-16 of themselves, for fp32 three, exactly.
 // Bound: long caches by reading the codes once, a few dozen queries each by the vector unit's work on scores and codes (360 instructions a tile of
 // 64 binary16 elements beside 16 matrix products), short caches by a wavefront's trips to memory.  Measured: one query to each of 24 caches of 2000 to
 // 65536 keys, 16 heads over 2 of 128, bfloat16 over e4m3, 0.41 GB: 90 us and 8 for the join, 4.6 TB/s in the former; 61 queries to each of 48 of 100 to
@@ -86,6 +86,11 @@ __device__ __forceinline__ void wait_loads() {
 // How many bfloat16 parts a factor of the type of q has: its significant bits, eight at a time.
 template <typename T>
 constexpr int parts() { return sizeof(T) == 4 ? 3 : (__is_same(T, bf16_t) ? 1 : 2); }
+
+// ... and a probability times its value's scale: sixteen bits even for bfloat16 results, of whose error a probability rounded to eight would make as much
+// as the result's own rounding does (2.4e-3 of the values in the root mean square where this has 1.7e-3).
+template <typename T>
+constexpr int weight_parts() { return sizeof(T) == 4 ? 3 : 2; }
 
 // Eight factors in parts: each part takes the upper eight bits of what is left, as they are; the last one is rounded.
 template <int P>
@@ -198,7 +203,7 @@ constexpr int cache_occupancy(const int D) { return D == 32 ? 3 : 2; }
 
 template <typename T, int D, bool I8, bool BIAS>
 __global__ __launch_bounds__(64 * kCacheWaves, cache_occupancy(D)) void cache_attn_kernel(const CacheAttnArgs a) {
-    constexpr int kWaves = kCacheWaves, kLog = kTileLog2, BK = 1 << kLog, kT = BK / 32, kD = D / 32, kC = D / 16, kP = parts<T>();
+    constexpr int kWaves = kCacheWaves, kLog = kTileLog2, BK = 1 << kLog, kT = BK / 32, kD = D / 32, kC = D / 16, kP = parts<T>(), kW = weight_parts<T>();
     constexpr int kTile = BK * D;
     typedef Mma<bf16_t> M;
     typedef CodeTile<D> Codes;
@@ -475,14 +480,14 @@ __global__ __launch_bounds__(64 * kCacheWaves, cache_occupancy(D)) void cache_at
                     float p[8];
 #pragma unroll
                     for (int r = 0; r < 8; ++r) p[r] = x[k][8 * c + r];
-                    uint4 f[kP];
-                    cut<kP>(p, f);
+                    uint4 f[kW];
+                    cut<kW>(p, f);
 #pragma unroll
                     for (int d = 0; d < kD; ++d) {
                         const uint2 u = Codes::down(vt, 32 * k, c, d, l);
                         const uint4 g = codes_bf16<I8>(u.x, u.y);
 #pragma unroll
-                        for (int n = kP - 1; n >= 0; --n) o[d] = M::mma(g, f[n], o[d]);
+                        for (int n = kW - 1; n >= 0; --n) o[d] = M::mma(g, f[n], o[d]);
                     }
                 }
             settle<bf16_t>();
@@ -688,10 +693,11 @@ __global__ __launch_bounds__(256, many ? 4 : 8) void cache_attn_join_kernel(cons
 //   140;  512 of 128 48 / 70, of 512 131 / 162;  1024 of 256 130 / 177
 // 4 heads of 32: 32 of 512 25 / 23, 256 of 512 27 / 34, of 1024 44 / 42;  61 queries each, 8 heads of 64, binary16 over i8: 8 of 256 23 / 26, 48 of 256 28 / 44, of
 // 1024 74 / 61.
-// Evenly among 512 workgroups, two wavefronts a SIMD (heads of 32: 768); among 256 where the codes' conversions are the cheapest (e4m3 into bfloat16 products of one
-// part), heads have 128 elements and runs are long, since memory then bounds it and fewer streams serve it better: 512 / 256, us, 24 caches of 34,000
-// on average, 16 heads over 2 of 128 bfloat16 101 / 97 (with a bias 122 / 107), 64 of 2250, 32 heads over 8 88 / 81, 128 of 2048 140 / 129;  but over i8 103 / 104,
-// binary16 110 / 110, fp32 136 / 185, heads of 64 61 / 72, 8 of 2048 28 / 33 and 61 queries each to 48 of 2050, 8 heads of 64, 79 / 98.
+// Evenly among 512 workgroups, two wavefronts a SIMD (heads of 32: 768); among 256 where the codes' conversions are the cheapest (e4m3 into bfloat16
+// products), heads have 128 elements and runs are long, since memory then bounds it and fewer streams serve it better: 512 / 256, us, 24 caches of
+// 34,000 on average, 16 heads over 2 of 128 bfloat16 102 / 100 (four queries each 112 / 107, with a bias 127 / 111), 64 of 2250, 32 heads over 8 89 / 86, 128 of 2048
+// 143 / 134;  but over i8 103 / 104, binary16 over i8 104 / 120, fp32 136 / 185, heads of 64 61 / 72, 8 of 2048 28 / 33 and 61 queries each to 48 of 2050, 8 heads of
+// 64, 79 / 98.
 constexpr int64_t kRangeGroups = 512, kRangeGroupsLight = 256, kLongRun = 16;   // kLongRun: tiles
 CacheAttnPlan cache_attn_plan(const AttnShape& sh, const bool light, const int max_pack) {
     CacheAttnPlan p;
