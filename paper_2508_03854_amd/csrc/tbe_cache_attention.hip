@@ -698,6 +698,9 @@ __global__ __launch_bounds__(256, many ? 4 : 8) void cache_attn_join_kernel(cons
 // 34,000 on average, 16 heads over 2 of 128 bfloat16 102 / 100 (four queries each 112 / 107, with a bias 127 / 111), 64 of 2250, 32 heads over 8 89 / 86, 128 of 2048
 // 143 / 134;  but over i8 103 / 104, binary16 over i8 104 / 120, fp32 136 / 185, heads of 64 61 / 72, 8 of 2048 28 / 33 and 61 queries each to 48 of 2050, 8 heads of
 // 64, 79 / 98.
+// Many queries are shared out evenly too (on their own / evenly: 1024 to each of 4 of 4500, 16 heads over 4 of 128, 574 / 277 us; 2048 to one of 8000, 32 heads
+// over 8, 773 / 536; 2048 to each of 8 of 4000, 16 heads over 4 of 64, 832 / 699), as long as the parts' results take no more than some 0.5 GB.
+constexpr int64_t kMostEach = 4096;
 constexpr int64_t kRangeGroups = 512, kRangeGroupsLight = 256, kLongRun = 16;   // kLongRun: tiles
 CacheAttnPlan cache_attn_plan(const AttnShape& sh, const bool light, const int max_pack) {
     CacheAttnPlan p;
@@ -711,13 +714,13 @@ CacheAttnPlan cache_attn_plan(const AttnShape& sh, const bool light, const int m
     p.block = 32 / p.pack;
     const int64_t packs = sh.H / p.pack, units = (sh.q_rows == sh.N ? sh.N : sh.q_rows / p.block + sh.N / 2) * packs;
     p.direct = sh.q_rows == sh.N;
-    p.own = mean_k <= 320 || (units >= 768 && mean_k <= (p.direct ? 1024 : 512));
-    p.ranges = p.qblocks = 1;
+    p.qblocks = (int)std::max<int64_t>(1, (mean_q + p.block - 1) / p.block);
+    const int64_t each = packs * p.qblocks;   // workgroups that go with a run
+    p.own = mean_k <= 320 || (units >= 768 && mean_k <= (p.direct ? 1024 : 512)) || each > kMostEach;
+    p.ranges = 1;
     p.V = p.direct ? sh.N : sh.q_rows / p.block + sh.N;
     p.spans = p.part_ml = p.part_o = 0;
     if (p.own) return p;
-    p.qblocks = (int)std::max<int64_t>(1, (mean_q + p.block - 1) / p.block);
-    const int64_t each = packs * p.qblocks;
     const int64_t tiles = (sh.k_rows >> kTileLog2) + sh.N;
     const bool few = light && p.D == 128 && p.qblocks == 1 && tiles * each >= kLongRun * kRangeGroups * kCacheWaves;
     p.ranges = (int)std::max<int64_t>(1, (few ? kRangeGroupsLight : kRangeGroups * cache_occupancy(p.D) / 2) / each) * kCacheWaves;

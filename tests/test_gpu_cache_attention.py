@@ -130,6 +130,13 @@ def test_many_caches_shared_out_evenly(tbe):
         compare(tbe, s, nq, nk, "even")
 
 
+def test_many_queries_of_many_heads(tbe):
+    """More units of queries of a sequence than workgroups that share its keys; so many that each has all keys to itself."""
+    for nq, nk, H, K, dim in (([700], [1000], 32, 8, 32), ([4200], [600], 32, 32, 32), ([900, 3], [901, 400], 16, 16, 64)):
+        s = build(tbe, gen(27), nq, nk, nk, H, K, dim, torch.bfloat16, E4M3)
+        compare(tbe, s, nq, nk, f"{nq}")
+
+
 def test_largest_tables_of_distances(tbe):
     for H, K, dim, far in ((4, 1, 128, 1024), (8, 2, 32, 700), (3, 3, 64, 1024), (4, 2, 64, 0)):
         for nq, nk in (([1, 1, 1], [3000, 900, 40]), ([33, 2], [1500, 2100])):
