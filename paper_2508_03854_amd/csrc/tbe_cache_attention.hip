@@ -76,6 +76,9 @@ __device__ __forceinline__ uint4 codes_bf16(const uint32_t lo, const uint32_t hi
     }
 }
 
+// All bits where the k-th of four e4m3 codes is not a number, none otherwise.
+__device__ __forceinline__ uint32_t odd_code(const uint32_t four, const int k) { return 0u - (((four >> (8 * k) & 0x7Fu) + 1u) >> 7); }
+
 // Waits until at most N of this wavefront's loads are under way (vmcnt N, the other counters as they are; see loads_done).
 template <int N>
 __device__ __forceinline__ void wait_loads() {
@@ -405,18 +408,29 @@ __global__ __launch_bounds__(64 * kCacheWaves, cache_occupancy(D)) void cache_at
                     x[k][r] *= s.x; x[k][r + 1] *= s.y; x[k][r + 2] *= s.z; x[k][r + 3] *= s.w;
                 }
                 if (BIAS) {
-                    // (a bias of -infinity hides a score that is not finite too)
+                    // A bias of -infinity hides a score that is not finite too.  (The sum as a value that the compiler has to have before it selects: it made
+                    // a branch between the lanes of one of sixteen; see column_row.)
+                    const auto add = [&](float& y, const float b) __attribute__((always_inline)) {
+                        float z = fmaf(y, a.scale2, b);
+                        asm volatile("" : "+v"(z));
+                        y = b == -__builtin_inff() ? b : z;
+                    };
                     const int j = j0 + 32 * k;
                     if (first - (j + 31) >= a.far || wave_last - j <= -a.far) {
                         const float b = first - (j + 31) >= a.far ? beyond : ahead;
 #pragma unroll
-                        for (int r = 0; r < 16; ++r) x[k][r] = b == -__builtin_inff() ? b : fmaf(x[k][r], a.scale2, b);
+                        for (int r = 0; r < 16; ++r) {
+                            float y = x[k][r];
+                            add(y, b);
+                            x[k][r] = y;
+                        }
                     } else {
                         const float* const from = ht + (j + 4 * half - pos + a.far + kTabMargin);
 #pragma unroll
                         for (int r = 0; r < 16; ++r) {
-                            const float b = from[8 * (r / 4) + r % 4];
-                            x[k][r] = b == -__builtin_inff() ? b : fmaf(x[k][r], a.scale2, b);
+                            float y = x[k][r];
+                            add(y, from[8 * (r / 4) + r % 4]);
+                            x[k][r] = y;
                         }
                     }
                 }
@@ -426,8 +440,11 @@ __global__ __launch_bounds__(64 * kCacheWaves, cache_occupancy(D)) void cache_at
 #pragma unroll
                 for (int k = 0; k < kT; ++k)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        if (j0 + 32 * k + 8 * (r / 4) + 4 * half + r % 4 >= upto) x[k][r] = -__builtin_inff();
+                    for (int r = 0; r < 16; ++r) {
+                        float y = x[k][r];
+                        asm volatile("" : "+v"(y));   // (no branch, as above)
+                        x[k][r] = j0 + 32 * k + 8 * (r / 4) + 4 * half + r % 4 >= upto ? -__builtin_inff() : y;
+                    }
             }
             return hides;
         };
@@ -507,6 +524,7 @@ __global__ __launch_bounds__(64 * kCacheWaves, cache_occupancy(D)) void cache_at
                     d = d > a.far ? a.far : (d < -a.far ? -a.far : d);
                     sees = sees && ht[a.far + kTabMargin - d] != -__builtin_inff();
                 }
+                const uint32_t seen = sees ? ~0u : 0u;
 #pragma unroll
                 for (int d = 0; d < kD; ++d)
 #pragma unroll
@@ -514,8 +532,8 @@ __global__ __launch_bounds__(64 * kCacheWaves, cache_occupancy(D)) void cache_at
                         const int e = 32 * d + 8 * n + 4 * half;
                         const uint32_t u = *reinterpret_cast<const uint32_t*>(vt + Codes::place(j, e / 16) + e % 16);
 #pragma unroll
-                        for (int k = 0; k < 4; ++k)
-                            o[d][4 * n + k] = sees && (u >> (8 * k) & 0x7Fu) == 0x7Fu ? __builtin_nanf("") : o[d][4 * n + k];
+                        for (int k = 0; k < 4; ++k)   // (bits, no branches between the lanes)
+                            o[d][4 * n + k] = __uint_as_float(__float_as_uint(o[d][4 * n + k]) | (odd_code(u, k) & seen & 0x7FC00000u));
                     }
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -523,8 +541,7 @@ __global__ __launch_bounds__(64 * kCacheWaves, cache_occupancy(D)) void cache_at
             for (int n = l; n < kTile / 4; n += 64) {
                 uint32_t u = *reinterpret_cast<const uint32_t*>(vt + 4 * n);
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    if ((u >> (8 * k) & 0x7Fu) == 0x7Fu) u &= ~(0xFFu << (8 * k));
+                for (int k = 0; k < 4; ++k) u &= ~(odd_code(u, k) & 0xFFu << (8 * k));
                 *reinterpret_cast<uint32_t*>(vt + 4 * n) = u;
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
