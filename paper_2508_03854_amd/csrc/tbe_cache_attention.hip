@@ -532,8 +532,11 @@ __global__ __launch_bounds__(64 * kCacheWaves, cache_occupancy(D)) void cache_at
                         const int e = 32 * d + 8 * n + 4 * half;
                         const uint32_t u = *reinterpret_cast<const uint32_t*>(vt + Codes::place(j, e / 16) + e % 16);
 #pragma unroll
-                        for (int k = 0; k < 4; ++k)   // (bits, no branches between the lanes)
-                            o[d][4 * n + k] = __uint_as_float(__float_as_uint(o[d][4 * n + k]) | (odd_code(u, k) & seen & 0x7FC00000u));
+                        for (int k = 0; k < 4; ++k) {
+                            uint32_t b = u >> (8 * k) & 0x7Fu & seen;
+                            asm volatile("" : "+v"(b));   // (no branch, as above)
+                            o[d][4 * n + k] = b == 0x7Fu ? __builtin_nanf("") : o[d][4 * n + k];
+                        }
                     }
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
