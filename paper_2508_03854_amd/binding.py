@@ -867,7 +867,7 @@ class TBE:
     def cache_write(self, cache: Cache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, *,
                     stream: Optional[torch.cuda.Stream] = None) -> None:
         """Row r of k and v ([rows, heads, head_dim], float32, float16 or bfloat16; column blocks of one matrix are fine) goes to the cache's row
-        slots[r] (int64 or int32; below 0: nowhere)."""
+        slots[r] (int64 or int32; below 0: nowhere; no two alike otherwise, or that row's contents are not specified)."""
         rows = self._cache_rows(cache, slots)
         if k.dim() != 3 or k.shape != (rows, *cache.k.shape[1:]):
             raise ValueError(f"k must be {(rows, *cache.k.shape[1:])}, got {tuple(k.shape)}")
