@@ -336,8 +336,8 @@ static void turn_blocks(TurnPart& q, TurnPart& k, const int64_t most) {
     k.blocks = some(k);
 }
 // More of them than the chip holds at once: forward 1280 / 2048 / 8192 / 16384 workgroups 361 / 288 / 268 / 270 us (131,071 rows of 20 heads of 128
-// bfloat16); backward 512 / 768 / 1024 / 2048 / 3072 / 4096 284 / 237 / 268 / 224 / 212 / 223 (65,537 rows), where each leaves sums to be added.
-constexpr int64_t kTurnBlocksForward = 8192, kTurnBlocksBackward = 3072;
+// bfloat16); backward 512 / 768 / 1024 / 2048 / 3584 / 4096 284 / 237 / 268 / 224 / 214 / 223 (65,537 rows), where each leaves sums to be added.
+constexpr int64_t kTurnBlocksForward = 8192, kTurnBlocksBackward = 3584;
 
 size_t rotate_workspace(const int dim) {   // (of any element type and layout)
     return (((size_t)kTurnBlocksBackward + 2) * (size_t)dim * sizeof(float) + 255) & ~(size_t)255;
