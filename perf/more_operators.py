@@ -180,7 +180,7 @@ def _plain_codes(x, code):
         exponent = (exponent - torch.where(fraction <= 0.875, 9, 8)).clamp(min=-126)
         exponent = torch.where(top == 0, torch.zeros_like(exponent), exponent)
         return torch.ldexp(x, -exponent[:, :, None]).to(torch.float8_e4m3fn), torch.ldexp(torch.ones_like(top), exponent)
-    scale = torch.where(top == 0, torch.ones_like(top), (top.double() / 127.0).float().clamp(min=2.0 ** -126))  # (the quotient, rounded once)
+    scale = torch.where(top == 0, torch.ones_like(top), (top / 127.0).clamp(min=2.0 ** -126))
     return torch.round(x.double() / scale.double()[:, :, None]).to(torch.int8), scale
 
 
