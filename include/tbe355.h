@@ -324,7 +324,7 @@ tbe_status tbe_layer_norm_backward(const tbe_handle* h, const void* dy, int64_t 
  * Rows of dk and dv that no query saw, or that are a cache's room, become zero.
  *   q, k, v, out and gradients   DEVICE, [rows][heads or kv_heads][head_dim] of dtype: consecutive rows row_stride, consecutive heads
  *             head_stride elements apart, so that they may be column blocks of one matrix.  16-byte aligned, strides multiples of 16
- *             bytes, 0 <= row_stride < 2^22 (a result's strides at least head_dim); head_dim <= 128, a multiple of 8 (4 for TBE_IO_F32).  Results
+ *             bytes, 0 <= row_stride < 2^22 (a result's heads share no byte: TBE_EINVAL); head_dim <= 128, a multiple of 8 (4 for TBE_IO_F32).  Results
  *             share no byte with each other or with what is read
  *   q_offsets, k_offsets   DEVICE, sequences + 1 of index_dtype, ascending from 0 to q_rows resp. k_rows;  k_lengths  DEVICE,
  *             `sequences` of the same type, or NULL.  A sequence whose numbers do not fit, and with
@@ -379,7 +379,7 @@ tbe_status tbe_attention_backward(const tbe_handle* h, const tbe_attention_args*
  * u = dz w:  dx_e = r (u_e - h_e 1/n sum_i u_i h_i),  dw_e = sum over the rows and heads of dz_e h_e (of q for q's weight, of k for k's).
  *   q, k, results and gradients   DEVICE, [rows][q_heads or k_heads][head_dim] of dtype: consecutive rows row_stride, consecutive heads head_stride
  *             elements apart (0 <= strides < 2^40), at any address that is a multiple of the element's size.  A result may be the matrix it is made from, with
- *             equal strides; otherwise results share no byte with each other or with what is read, and neither do their rows and heads
+ *             equal strides; otherwise results share no byte with each other or with what is read, and neither do a result's rows and heads (TBE_EINVAL)
  *   positions   DEVICE, [rows] of index_dtype, any numbers
  *   frequencies DEVICE, [rotary_dim / 2], radians a position, in 64 bits: angles of far positions keep their fraction.  tbe_rotary_frequencies
  *             makes the customary ones.  May be NULL where rotary_dim is 0 (norm alone)
@@ -430,7 +430,8 @@ tbe_status tbe_rotary_frequencies(int32_t rotary_dim, double base, tbe_rotary_sc
  *                  code the whole number nearest to x / scale, ties to even
  * A head with an element that is not finite gets codes 0 and the scale NaN: all of it reads as NaN.
  *   k, v      DEVICE, codes [rows][heads][head_dim]: consecutive rows row_stride, consecutive heads head_stride bytes apart, 16-byte aligned, strides
- *             multiples of 16, row_stride < 2^22, both at least head_dim (they are written); head_dim a multiple of 16, at most 128
+ *             multiples of 16, row_stride < 2^22, both at least head_dim; no two heads share a byte where they are written (TBE_EINVAL); head_dim a
+ *             multiple of 16, at most 128
  *   k_scales, v_scales  DEVICE float [heads][rows] */
 typedef enum { TBE_CODE_E4M3 = 0, TBE_CODE_I8 = 1 } tbe_code;
 typedef struct {

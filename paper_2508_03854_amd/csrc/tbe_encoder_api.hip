@@ -3,6 +3,7 @@
 
 #include "tbe_attention.h"
 #include "tbe_cache.h"
+#include "tbe_overlap.h"
 
 using namespace tbe;
 
@@ -90,7 +91,7 @@ static bool rows_view(const tbe_rows& m, const int64_t rows, const int32_t heads
     if (!m.data && rows > 0) return false;
     if (!multiple_of(m.data, 16) || m.row_stride < 0 || m.row_stride >= 1 << 22 || m.row_stride * e % 16 != 0) return false;
     if (m.head_stride < 0 || m.head_stride >= (int64_t)1 << 40 || m.head_stride * e % 16 != 0) return false;
-    if (result && ((rows > 1 && m.row_stride < a->head_dim) || (rows > 0 && heads > 1 && m.head_stride < a->head_dim))) return false;   // (two writers of one element)
+    if (result && rows > 0 && !runs_apart(HeadRuns{m.data, m.row_stride, m.head_stride, rows, heads, a->head_dim})) return false;
     v.p = static_cast<const char*>(m.data); v.row = m.row_stride * e; v.head = m.head_stride * e;
     return true;
 }
@@ -189,7 +190,7 @@ static bool loose_rows_ok(const tbe_rows& m, const tbe_rotation_args* a, const i
 // ... that is written: no element twice, and as its source where it is that
 static bool loose_result_ok(const tbe_rows& m, const tbe_rotation_args* a, const int32_t heads) {
     if (!loose_rows_ok(m, a, heads)) return false;
-    return heads == 0 || ((a->rows <= 1 || m.row_stride >= a->head_dim) && (heads <= 1 || m.head_stride >= a->head_dim));
+    return heads == 0 || a->rows == 0 || runs_apart(HeadRuns{m.data, m.row_stride, m.head_stride, a->rows, heads, a->head_dim});
 }
 static bool apart_or_same(const tbe_rows& from, const tbe_rows& to, const tbe_rotation_args* a, const int32_t heads) {
     if (from.data != to.data || heads == 0) return true;
@@ -311,6 +312,9 @@ static tbe_status cache_copy(const tbe_handle* h, const tbe_cache* cache, const 
     if (st != TBE_OK) return st;
     if (!io_known(dtype) || (index_dtype != TBE_I64 && index_dtype != TBE_I32)) return TBE_EDTYPE;
     if (rows < 0 || rows >= (int64_t)1 << 31) return TBE_ESHAPE;
+    if (write)
+        for (const CodeRows& r : c.cache)
+            if (!runs_apart(HeadRuns{r.codes.p, r.codes.row, r.codes.head, cache->rows, cache->heads, cache->head_dim})) return TBE_EINVAL;
     tbe_rotation_args as{};   // (the same kind of matrix)
     as.dtype = dtype; as.rows = rows; as.head_dim = cache->head_dim;
     if (write ? !loose_rows_ok(k, &as, cache->heads) || !loose_rows_ok(v, &as, cache->heads)
