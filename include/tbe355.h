@@ -430,9 +430,9 @@ tbe_status tbe_rotary_frequencies(int32_t rotary_dim, double base, tbe_rotary_sc
  *                  code the whole number nearest to x / scale, ties to even
  * A head with an element that is not finite gets codes 0 and the scale NaN: all of it reads as NaN.
  *   k, v      DEVICE, codes [rows][heads][head_dim]: consecutive rows row_stride, consecutive heads head_stride bytes apart, 16-byte aligned, strides
- *             multiples of 16, row_stride < 2^22, both at least head_dim; no two heads share a byte where they are written (TBE_EINVAL); head_dim a
- *             multiple of 16, at most 128
- *   k_scales, v_scales  DEVICE float [heads][rows] */
+ *             multiples of 16, row_stride < 2^22, both at least head_dim; where they are written no two heads share a byte, of k or v or
+ *             of both (TBE_EINVAL); head_dim a multiple of 16, at most 128
+ *   k_scales, v_scales  DEVICE float [heads][rows], apart from each other likewise */
 typedef enum { TBE_CODE_E4M3 = 0, TBE_CODE_I8 = 1 } tbe_code;
 typedef struct {
     int64_t rows;              /* 0 .. 2^31 - 4096 */

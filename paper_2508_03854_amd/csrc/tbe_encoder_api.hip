@@ -192,8 +192,16 @@ static bool loose_result_ok(const tbe_rows& m, const tbe_rotation_args* a, const
     if (!loose_rows_ok(m, a, heads)) return false;
     return heads == 0 || a->rows == 0 || runs_apart(HeadRuns{m.data, m.row_stride, m.head_stride, a->rows, heads, a->head_dim});
 }
+static HeadRuns runs_of(const tbe_rows& m, const tbe_rotation_args* a, const int32_t heads) {
+    const int64_t e = (int64_t)io_size(a->dtype);
+    return HeadRuns{m.data, m.row_stride * e, m.head_stride * e, a->rows, heads, a->head_dim * e};
+}
+static bool apart(const tbe_rows& x, const int32_t x_heads, const tbe_rows& y, const int32_t y_heads, const tbe_rotation_args* a) {
+    return !runs_meet(runs_of(x, a, x_heads), runs_of(y, a, y_heads));
+}
 static bool apart_or_same(const tbe_rows& from, const tbe_rows& to, const tbe_rotation_args* a, const int32_t heads) {
-    if (from.data != to.data || heads == 0) return true;
+    if (heads == 0) return true;
+    if (from.data != to.data) return apart(from, heads, to, heads, a);
     return (a->rows <= 1 || from.row_stride == to.row_stride) && (heads == 1 || from.head_stride == to.head_stride);
 }
 static tbe_status rotation_call(const tbe_handle* h, const tbe_rotation_args* a, RotateCall& r) {
@@ -226,7 +234,9 @@ tbe_status tbe_rotate_heads(const tbe_handle* h, const tbe_rotation_args* args, 
     if (st != TBE_OK) return st;
     if (!loose_rows_ok(q, args, args->q_heads) || !loose_rows_ok(k, args, args->k_heads)) return TBE_EINVAL;
     if (!loose_result_ok(q_out, args, args->q_heads) || !loose_result_ok(k_out, args, args->k_heads)) return TBE_EINVAL;
-    if (!apart_or_same(q, q_out, args, args->q_heads) || !apart_or_same(k, k_out, args, args->k_heads)) return TBE_EINVAL;
+    const int32_t nq = args->q_heads, nk = args->k_heads;
+    if (!apart_or_same(q, q_out, args, nq) || !apart_or_same(k, k_out, args, nk)) return TBE_EINVAL;
+    if (!apart(q_out, nq, k_out, nk, args) || !apart(q_out, nq, k, nk, args) || !apart(k_out, nk, q, nq, args)) return TBE_EINVAL;
     if (args->rows == 0) return TBE_OK;
     r.part[0].x = q; r.part[0].y = q_out;
     r.part[1].x = k; r.part[1].y = k_out;
@@ -249,8 +259,10 @@ tbe_status tbe_rotate_heads_backward(const tbe_handle* h, const tbe_rotation_arg
     const int32_t nq = args->q_heads, nk = args->k_heads;
     if (!loose_rows_ok(dq_out, args, nq) || !loose_rows_ok(dk_out, args, nk) || !loose_result_ok(dq, args, nq) || !loose_result_ok(dk, args, nk)) return TBE_EINVAL;
     if (!apart_or_same(dq_out, dq, args, nq) || !apart_or_same(dk_out, dk, args, nk)) return TBE_EINVAL;
+    if (!apart(dq, nq, dk, nk, args) || !apart(dq, nq, dk_out, nk, args) || !apart(dk, nk, dq_out, nq, args)) return TBE_EINVAL;
     if (r.norm) {
         if (!loose_rows_ok(q, args, nq) || !loose_rows_ok(k, args, nk) || !apart_or_same(q, dq, args, nq) || !apart_or_same(k, dk, args, nk)) return TBE_EINVAL;
+        if (!apart(dq, nq, k, nk, args) || !apart(dk, nk, q, nq, args)) return TBE_EINVAL;
     } else if (dq_weight || dk_weight) {
         return TBE_EINVAL;
     }
@@ -312,13 +324,21 @@ static tbe_status cache_copy(const tbe_handle* h, const tbe_cache* cache, const 
     if (st != TBE_OK) return st;
     if (!io_known(dtype) || (index_dtype != TBE_I64 && index_dtype != TBE_I32)) return TBE_EDTYPE;
     if (rows < 0 || rows >= (int64_t)1 << 31) return TBE_ESHAPE;
-    if (write)
-        for (const CodeRows& r : c.cache)
-            if (!runs_apart(HeadRuns{r.codes.p, r.codes.row, r.codes.head, cache->rows, cache->heads, cache->head_dim})) return TBE_EINVAL;
+    if (write && cache->rows > 0) {
+        HeadRuns m[2];
+        for (int i = 0; i < 2; ++i) {
+            const RowsView& v = c.cache[i].codes;
+            m[i] = HeadRuns{v.p, v.row, v.head, cache->rows, cache->heads, cache->head_dim};
+            if (!runs_apart(m[i])) return TBE_EINVAL;
+        }
+        const int64_t bytes = 4 * cache->rows;   // of a head's scales
+        const HeadRuns ks{cache->k_scales, 0, bytes, 1, cache->heads, bytes}, vs{cache->v_scales, 0, bytes, 1, cache->heads, bytes};
+        if (runs_meet(m[0], m[1]) || runs_meet(ks, vs)) return TBE_EINVAL;
+    }
     tbe_rotation_args as{};   // (the same kind of matrix)
     as.dtype = dtype; as.rows = rows; as.head_dim = cache->head_dim;
     if (write ? !loose_rows_ok(k, &as, cache->heads) || !loose_rows_ok(v, &as, cache->heads)
-              : !loose_result_ok(k, &as, cache->heads) || !loose_result_ok(v, &as, cache->heads)) return TBE_EINVAL;
+              : !loose_result_ok(k, &as, cache->heads) || !loose_result_ok(v, &as, cache->heads) || !apart(k, cache->heads, v, cache->heads, &as)) return TBE_EINVAL;
     if ((!slots && rows > 0) || !multiple_of(slots, index_dtype == TBE_I32 ? 4 : 8)) return TBE_EINVAL;
     if (rows == 0) return TBE_OK;
     c.rows_of[0] = k; c.rows_of[1] = v;

@@ -33,4 +33,18 @@ inline bool runs_apart(const HeadRuns& m) {
     return true;
 }
 
+// A run of a and one of b, of equal length, share a byte.  Exact where they have equal strides, as column blocks of one matrix and shifted views of one
+// matrix have; matrices of unlike strides that lie between each other are taken to be apart.
+inline bool runs_meet(const HeadRuns& a, const HeadRuns& b) {
+    if (a.rows < 1 || b.rows < 1 || a.heads < 1 || b.heads < 1) return false;
+    const auto extent = [](const HeadRuns& m) { return (__int128)(m.rows - 1) * m.row + (m.heads - 1) * m.head + m.len; };
+    const __int128 from_a = (__int128)reinterpret_cast<uintptr_t>(a.at), from_b = (__int128)reinterpret_cast<uintptr_t>(b.at);
+    if (from_a + extent(a) <= from_b || from_b + extent(b) <= from_a) return false;
+    const int64_t rows = a.rows > b.rows ? a.rows : b.rows, row = a.rows > 1 ? a.row : b.row, head = a.heads > 1 ? a.head : b.head;
+    if ((a.rows > 1 && b.rows > 1 && a.row != b.row) || (a.heads > 1 && b.heads > 1 && a.head != b.head)) return false;
+    for (int64_t h = 1 - a.heads; h < b.heads; ++h)
+        if (some_row_meets((int64_t)(from_b - from_a) + h * head, row, rows, a.len)) return true;
+    return false;
+}
+
 }  // namespace tbe
