@@ -386,7 +386,8 @@ tbe_status tbe_attention_backward(const tbe_handle* h, const tbe_attention_args*
  *   q_weight, k_weight   DEVICE, [head_dim] of weight_dtype, or NULL: 1 (without `norm`: not read)
  * 0 <= rows < 2^31, 0 <= q_heads, k_heads <= 1024 and not both 0 (that matrix is then not read or written), 1 <= head_dim <= 256, rotary_dim even,
  * 0 <= rotary_dim <= head_dim; eps finite and >= 0, amplitude finite.  Arithmetic is in fp32, angles in 64 bits; each result is rounded once; the
- * order of all additions is fixed.  Squares beyond fp32's range make a head's norm infinite, and the head 0.  The handle gives the timing record. */
+ * order of all additions is fixed.  With eps below 2^-100 heads may be of any size; otherwise squares beyond fp32's range make a head's norm
+ * infinite, and the head 0.  The handle gives the timing record. */
 typedef struct {
     int32_t q_heads, k_heads, head_dim, rotary_dim;
     int64_t rows;

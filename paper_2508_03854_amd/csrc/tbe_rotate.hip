@@ -76,6 +76,50 @@ __device__ __forceinline__ void move_back(int& from, int& n, int& again, const i
     }
 }
 
+// Below this eps the squares of small heads count, however far below fp32's smallest numbers they lie, and the kernels that take heads of any size run.
+// Among the others (eps is more than all that fp32 loses of such squares) a branch in the heads' loop costs too much: 131,071 rows of 20 heads of 128
+// bfloat16 271 us without / 281 with it, gradients of 65,537 of them 216 / 220, of 60,000 rows of 12 heads of 96, 72 elements turned, 141 / 155.
+constexpr float kEpsAny = 0x1p-100f;
+
+// 1 / sqrt(1/n sum x^2 + eps) of a head that a group of lanes has, each the two runs a and b.  ANY: where the mean of the squares, eps included, leaves
+// fp32's range or comes near its lower end, it is that of the head times a power of two, `by` (otherwise 1), with which the largest magnitude, or
+// eps's root if that is larger, lies next to 1.  All lanes of a wavefront together.
+template <bool ANY, int kN>
+__device__ __forceinline__ float head_rstd(const float (&a)[kN], const float (&b)[kN], const int again_a, const int again_b, const int lanes, const float inv,
+                                           const float eps, const bool here, float& by) {
+    float q = 0.f;
+#pragma unroll
+    for (int j = 0; j < kN; ++j) q = j < again_a ? q : fmaf(a[j], a[j], q);
+#pragma unroll
+    for (int j = 0; j < kN; ++j) q = j < again_b ? q : fmaf(b[j], b[j], q);
+    float m = group_sum(q, lanes) * inv + eps;
+    by = 1.f;
+    if constexpr (!ANY) return 1.f / sqrtf(m);
+    const bool beyond = here && !(m >= kEpsAny && m < __builtin_inff());   // (NaN too)
+    if (__any(beyond)) {
+        uint32_t top = __float_as_uint(sqrtf(eps));
+#pragma unroll
+        for (int j = 0; j < kN; ++j) {
+            top = max(top, __float_as_uint(a[j]) & 0x7FFFFFFFu);
+            top = max(top, __float_as_uint(b[j]) & 0x7FFFFFFFu);
+        }
+        for (int w = 1; w < lanes; w <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, w));
+        int e = (int)(top >> 23) - 127;
+        e = e < -126 ? -126 : (e > 126 ? 126 : e);
+        by = beyond ? __uint_as_float((uint32_t)(127 - e) << 23) : 1.f;
+        q = 0.f;
+#pragma unroll
+        for (int j = 0; j < kN; ++j) {
+            const float x = a[j] * by, y = b[j] * by;
+            q = j < again_a ? q : fmaf(x, x, q);
+            q = j < again_b ? q : fmaf(y, y, q);
+        }
+        q = group_sum(q, lanes) * inv + eps * by * by;   // (eps times `by` twice is at most 4)
+        m = beyond ? q : m;
+    }
+    return 1.f / sqrtf(m);
+}
+
 __device__ __forceinline__ void turn(const bool turned, const float2 cs, float& x, float& y) {
     const float a = x, b = y;
     x = turned ? a * cs.x - b * cs.y : a;
@@ -102,7 +146,8 @@ struct TurnArgs {
 
 constexpr int kTurnThreads = 256;
 
-template <typename T, bool BACK, bool NORM, bool PAIRS>
+constexpr int kNormAny = 2;   // NORM: 0 none, 1 of heads whose squares lie in fp32's range or count for nothing beside eps, kNormAny of all
+template <typename T, bool BACK, int NORM, bool PAIRS>
 __global__ __launch_bounds__(kTurnThreads) void rotate_kernel(const TurnArgs a) {
     constexpr int kN = Frag<T>::kN;
     __shared__ float2 tables[4][64 * kN + kN];   // cosine and sine of the pairs of a wavefront's rows, times the amplitude
@@ -210,16 +255,12 @@ __global__ __launch_bounds__(kTurnThreads) void rotate_kernel(const TurnArgs a) 
                 Frag<T>::unpack(raw[3], xb);
             }
             if constexpr (!BACK && NORM) {
-                float q = 0.f;
-#pragma unroll
-                for (int j = 0; j < kN; ++j) q = j < again_a ? q : fmaf(ua[j], ua[j], q);
-#pragma unroll
-                for (int j = 0; j < kN; ++j) q = j < again_b ? q : fmaf(ub[j], ub[j], q);
-                const float r = 1.f / sqrtf(group_sum(q, lanes) * inv + a.eps);
+                float by;
+                const float r = head_rstd<NORM == kNormAny>(ua, ub, again_a, again_b, lanes, inv, a.eps, here, by);
 #pragma unroll
                 for (int j = 0; j < kN; ++j) {
-                    ua[j] = ua[j] * r * wa[j];
-                    ub[j] = ub[j] * r * wb[j];
+                    ua[j] = ua[j] * by * r * wa[j];
+                    ub[j] = ub[j] * by * r * wb[j];
                 }
             }
             // (elements that are not turned are left as they are: 0 times a neighbour that is not finite is not 0)
@@ -234,27 +275,21 @@ __global__ __launch_bounds__(kTurnThreads) void rotate_kernel(const TurnArgs a) 
                 for (int j = 0; j < kN; ++j) turn(first < a.half, cs[j], ua[j], ub[j]);
             }
             if constexpr (BACK && NORM) {
-                float q = 0.f, m = 0.f;
+                float by, m = 0.f;
+                float r = head_rstd<NORM == kNormAny>(xa, xb, again_a, again_b, lanes, inv, a.eps, here, by);
 #pragma unroll
-                for (int j = 0; j < kN; ++j) {
-                    q = j < again_a ? q : fmaf(xa[j], xa[j], q);
-                    m = j < again_a ? m : fmaf(ua[j] * wa[j], xa[j], m);
-                }
+                for (int j = 0; j < kN; ++j) m = j < again_a ? m : fmaf(ua[j] * wa[j], xa[j] * by, m);
 #pragma unroll
-                for (int j = 0; j < kN; ++j) {
-                    q = j < again_b ? q : fmaf(xb[j], xb[j], q);
-                    m = j < again_b ? m : fmaf(ub[j] * wb[j], xb[j], m);
-                }
-                float r = 1.f / sqrtf(group_sum(q, lanes) * inv + a.eps);
+                for (int j = 0; j < kN; ++j) m = j < again_b ? m : fmaf(ub[j] * wb[j], xb[j] * by, m);
                 r = here ? r : 0.f;
                 m = group_sum(m, lanes) * inv * r;   // the mean of u h
 #pragma unroll
                 for (int j = 0; j < kN; ++j) {
-                    const float ha = xa[j] * r, hb = xb[j] * r;
+                    const float ha = xa[j] * by * r, hb = xb[j] * by * r;
                     dwa[j] = fmaf(ua[j], ha, dwa[j]);
                     dwb[j] = fmaf(ub[j], hb, dwb[j]);
-                    ua[j] = r * (ua[j] * wa[j] - ha * m);
-                    ub[j] = r * (ub[j] * wb[j] - hb * m);
+                    ua[j] = r * (ua[j] * wa[j] - ha * m) * by;
+                    ub[j] = r * (ub[j] * wb[j] - hb * m) * by;
                 }
             }
             T* const to = static_cast<T*>(p.y) + at * p.y_row + (here ? head : 0) * p.y_head;
@@ -343,15 +378,16 @@ size_t rotate_workspace(const int dim) {   // (of any element type and layout)
     return (((size_t)kTurnBlocksBackward + 2) * (size_t)dim * sizeof(float) + 255) & ~(size_t)255;
 }
 
-template <typename T, bool BACK, bool NORM>
+template <typename T, bool BACK, int NORM>
 static void launch_layout(const TurnArgs& a, const bool pairs, const unsigned blocks, hipStream_t s) {
     if (pairs) rotate_kernel<T, BACK, NORM, true><<<blocks, kTurnThreads, 0, s>>>(a);
     else rotate_kernel<T, BACK, NORM, false><<<blocks, kTurnThreads, 0, s>>>(a);
 }
 template <typename T, bool BACK>
 static void launch_norm(const TurnArgs& a, const bool norm, const bool pairs, const unsigned blocks, hipStream_t s) {
-    if (norm) launch_layout<T, BACK, true>(a, pairs, blocks, s);
-    else launch_layout<T, BACK, false>(a, pairs, blocks, s);
+    if (norm && a.eps < kEpsAny) launch_layout<T, BACK, kNormAny>(a, pairs, blocks, s);
+    else if (norm) launch_layout<T, BACK, 1>(a, pairs, blocks, s);
+    else launch_layout<T, BACK, 0>(a, pairs, blocks, s);
 }
 template <typename T>
 static void launch_turn(const TurnArgs& a, const bool back, const bool norm, const bool pairs, const unsigned blocks, hipStream_t s) {
