@@ -339,7 +339,8 @@ tbe_status tbe_layer_norm_backward(const tbe_handle* h, const void* dy, int64_t 
  * v, k, q or dout (fp32: not at all), results once when stored.  With binary16 a dS beyond 65504 thus becomes infinite and one below 2^-25
  * zero: scale the loss, or take bfloat16.  The order of all additions is fixed: results do not depend on timing.  A value that is not
  * finite reaches the results that the formulas lead it to over pairs that see each other; a pair that is hidden (by `causal`, the lengths
- * or a bias of -infinity) is left out, not multiplied by 0.  The handle gives the timing record and the error flag. */
+ * or a bias of -infinity) is left out, not multiplied by 0.  Sums of values are divided by their weights, up to 2^8 a key, at the end: values beyond
+ * 2^120 / keys may make them infinite.  The handle gives the timing record and the error flag. */
 typedef struct {
     void* data;
     int64_t row_stride, head_stride; /* in elements */
@@ -456,8 +457,9 @@ tbe_status tbe_cache_read(const tbe_handle* h, const tbe_cache* cache, const voi
 /* Attention over such a cache: tbe_attention with k = the codes of cache->k times their scales, v likewise, none of which is written out.  args as there, but
  * its k and v are not looked at; kv_heads, head_dim and k_rows are the cache's heads, head_dim and rows (TBE_ESHAPE), so head_dim is a multiple of 16.  dtype
  * is that of q and out.  Products are exact in q and the codes and added in fp32, scales are multiplied in fp32; a probability times its value's scale is
- * rounded to 16 bits, for TBE_IO_F32 not at all; results once when stored.  What is hidden is
- * left out, scales and codes that are not numbers among it; a scale that is infinite may make NaN of what sees it. */
+ * rounded to 16 bits, for TBE_IO_F32 not at all; results once when stored.  Values may be as large
+ * as fp32's numbers; beside such that sums of them leave its range, those below 2^-86 may count as 0.  What is hidden is left out, scales and codes
+ * that are not numbers among it; a scale that is infinite, and a score or its sum of products beyond fp32's range, may make NaN of what sees it. */
 tbe_status tbe_cache_attention_workspace_bytes(const tbe_handle* h, const tbe_attention_args* args, size_t* bytes);
 tbe_status tbe_cache_attention(const tbe_handle* h, const tbe_attention_args* args, const tbe_cache* cache, tbe_rows out, float* lse, void* workspace,
                                size_t workspace_bytes, void* hip_stream);

@@ -365,7 +365,7 @@ __global__ __launch_bounds__(64 * kCacheWaves, cache_occupancy(D)) void cache_at
         }
 
         f32x16_t o[kD];
-        float m, sum;
+        float m, sum, lift = 0.f;   // lift: see below
         auto begin = [&]() __attribute__((always_inline)) {
 #pragma unroll
             for (int d = 0; d < kD; ++d) o[d] = f32x16_t{};
@@ -448,7 +448,7 @@ __global__ __launch_bounds__(64 * kCacheWaves, cache_occupancy(D)) void cache_at
             }
             return hides;
         };
-        auto apply = [&](const char* const vt_, const float* const st_, const bool hides, const int l) __attribute__((always_inline)) {
+        auto apply = [&](const char* const vt_, const float* const st_, const bool hides, const int l, const auto lifted) __attribute__((always_inline)) {
             const int half = l >> 5;
             const char* const vt = vt_ + own;
             const float* const st = st_ + own_scales;
@@ -471,7 +471,8 @@ __global__ __launch_bounds__(64 * kCacheWaves, cache_occupancy(D)) void cache_at
 #pragma unroll
                     for (int r = 0; r < 16; ++r) o[d][r] *= shrink;
             }
-            const float at = m == -__builtin_inff() ? 0.f : m;   // (nothing seen so far: every probability is 2^-inf = 0)
+            float at = m == -__builtin_inff() ? 0.f : m;   // (nothing seen so far: every probability is 2^-inf = 0)
+            if constexpr (decltype(lifted)::value) at += lift;
             // A scale that is not finite must not reach a column that does not see its key.
             const auto weigh = [&](const auto masked) __attribute__((always_inline)) {
 #pragma unroll
@@ -567,7 +568,7 @@ __global__ __launch_bounds__(64 * kCacheWaves, cache_occupancy(D)) void cache_at
             } else {
                 wait_loads<0>();
             }
-            apply(vt, vst, hides, lane);
+            apply(vt, vst, hides, lane, std::false_type{});
             if (after) fetch_values(t + 2, vt, vst, lane);
         };
         begin();
@@ -583,17 +584,34 @@ __global__ __launch_bounds__(64 * kCacheWaves, cache_occupancy(D)) void cache_at
             one(t, keys0, key_scales0, values0, value_scales0);
             if (t + 1 < tiles) one(t + 1, keys1, key_scales1, values1, value_scales1);
         }
-        if (!I8 && (a.causal || BIAS) && __any(is && not_finite(o))) {
-            begin();
+        if (__any(is && not_finite(o))) {
+            // Codes that are not numbers, see above; or, since a probability counts up to 2^8 until it is divided by the sum of all, sums of values near fp32's
+            // largest beyond it.  The columns that are not finite then get a maximum that is greater by `lift`, whose probabilities are that much smaller: no more than
+            // the largest scale here and the number of keys ask for, as small values beside those lose their last bits to it.
+            const int odd = not_finite(o);
+            float top = 0.f;
 #pragma unroll 1
-            for (int t = 0; t < tiles; ++t) {
-                const int l = anew(lane);   // (few registers: nothing of this is kept through the loop above)
-                fetch_keys(t, keys0, key_scales0, l);
-                fetch_values(t, values0, value_scales0, l);
-                loads_done();
-                take_out(t, l);
-                const bool hides = scores(t, keys0, key_scales0, l);
-                apply(values0, value_scales0, hides, l);
+            for (int j = w.lo; j < jend; j += 64) {
+                const int n = j + lane < jend ? j + lane : jend - 1;
+                const float x = fabsf(vs[n]);
+                top = x < __builtin_inff() ? fmaxf(top, x) : top;
+            }
+            const int e = wave_max_i32((int)(__float_as_uint(top) >> 23)) - 126;   // scales are below 2^e, codes below 2^9
+            const int over = uniform(e + 9 + 8 + (32 - __builtin_clz(jend - w.lo)) + 1 - 128);
+            lift = (odd | __shfl_xor(odd, 32)) && over > 0 ? (float)over : 0.f;
+            if (over > 0 || (!I8 && (a.causal || BIAS))) {
+                begin();
+#pragma unroll 1
+                for (int t = 0; t < tiles; ++t) {
+                    const int l = anew(lane);   // (few registers: nothing of this is kept through the loop above)
+                    fetch_keys(t, keys0, key_scales0, l);
+                    fetch_values(t, values0, value_scales0, l);
+                    loads_done();
+                    if (!I8 && (a.causal || BIAS)) take_out(t, l);
+                    const bool hides = scores(t, keys0, key_scales0, l);
+                    apply(values0, value_scales0, hides, l, std::true_type{});
+                }
+                m += lift;
             }
         }
         sum = pair_sum<32>(sum);
@@ -654,8 +672,8 @@ __global__ __launch_bounds__(256, many ? 4 : 8) void cache_attn_join_kernel(cons
     for (int head = head0 + (many ? 0 : wave); head < a.H && head < head0 + heads; head += 4) {
         const int hh = head / a.pack, col = (i - qb * a.block) * a.pack + head - hh * a.pack;
         const int64_t cell0 = ((int64_t)qb * packs + hh) * 32 + col;
-        float m = -__builtin_inff(), sum = 0.f;
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        float m, sum;
+        float4 o;
         const auto add = [&](const float2 c, const float4 x) __attribute__((always_inline)) {
             const float top = fmaxf(m, c.x), at = top == -__builtin_inff() ? 0.f : top;
             const float old = __builtin_amdgcn_exp2f(m - at), by = __builtin_amdgcn_exp2f(c.x - at);
@@ -664,38 +682,56 @@ __global__ __launch_bounds__(256, many ? 4 : 8) void cache_attn_join_kernel(cons
             o.x = fmaf(x.x, by, o.x * old); o.y = fmaf(x.y, by, o.y * old);
             o.z = fmaf(x.z, by, o.z * old); o.w = fmaf(x.w, by, o.w * old);
         };
-        for (int base = group; base < count; base += groups * kAhead) {
-            float2 c[kAhead];
-            float4 x[kAhead];
-#pragma unroll
-            for (int j = 0; j < kAhead; ++j) {
-                const int p = base + j * groups < count ? base + j * groups : base;
-                const int64_t cell = cell0 + (2 * (int64_t)(span.x + p) + (p == 0)) * each;
-                c[j] = *reinterpret_cast<const float2*>(a.part_ml + 2 * cell);
-                x[j] = *reinterpret_cast<const float4*>(a.part_o + cell * D + e0);
-            }
-#pragma unroll
-            for (int j = 0; j < kAhead; ++j)
-                if (base + j * groups < count) add(c[j], x[j]);
-        }
-#pragma unroll
-        for (int w = kLanes; w < 64; w <<= 1) {
-            const float2 c = make_float2(__shfl_xor(m, w), __shfl_xor(sum, w));
-            const float4 x = make_float4(__shfl_xor(o.x, w), __shfl_xor(o.y, w), __shfl_xor(o.z, w), __shfl_xor(o.w, w));
-            add(c, x);
-        }
-        if (many) {
-            if (lane == 0) stats[wave] = make_float2(m, sum);
-            if (lane < kLanes) sums[wave][lane] = o;
-            __syncthreads();
+        const auto join = [&](const auto small) __attribute__((always_inline)) {   // small: of the parts' results times 2^-12
             m = -__builtin_inff();
             sum = 0.f;
             o = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int base = group; base < count; base += groups * kAhead) {
+                float2 c[kAhead];
+                float4 x[kAhead];
 #pragma unroll
-            for (int w = 0; w < 4; ++w) add(stats[w], sums[w][lane % kLanes]);
-            if (wave != 0) return;
+                for (int j = 0; j < kAhead; ++j) {
+                    const int p = base + j * groups < count ? base + j * groups : base;
+                    const int64_t cell = cell0 + (2 * (int64_t)(span.x + p) + (p == 0)) * each;
+                    c[j] = *reinterpret_cast<const float2*>(a.part_ml + 2 * cell);
+                    x[j] = *reinterpret_cast<const float4*>(a.part_o + cell * D + e0);
+                }
+#pragma unroll
+                for (int j = 0; j < kAhead; ++j) {
+                    if constexpr (decltype(small)::value) x[j] = make_float4(x[j].x * 0x1p-12f, x[j].y * 0x1p-12f, x[j].z * 0x1p-12f, x[j].w * 0x1p-12f);
+                    if (base + j * groups < count) add(c[j], x[j]);
+                }
+            }
+#pragma unroll
+            for (int w = kLanes; w < 64; w <<= 1) {
+                const float2 c = make_float2(__shfl_xor(m, w), __shfl_xor(sum, w));
+                const float4 x = make_float4(__shfl_xor(o.x, w), __shfl_xor(o.y, w), __shfl_xor(o.z, w), __shfl_xor(o.w, w));
+                add(c, x);
+            }
+            if (many) {
+                if (lane == 0) stats[wave] = make_float2(m, sum);
+                if (lane < kLanes) sums[wave][lane] = o;
+                __syncthreads();
+                m = -__builtin_inff();
+                sum = 0.f;
+                o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int w = 0; w < 4; ++w) add(stats[w], sums[w][lane % kLanes]);
+            }
+        };
+        join(std::false_type{});
+        // Parts of values near fp32's largest may add up beyond it before they are divided by their weights: fewer than 2^12 parts.  (In a workgroup that has one
+        // head together, all wavefronts find the same here.)
+        float inv = sum == 0.f ? 0.f : 1.f / sum;
+        if (__any(!(fabsf(o.x) < __builtin_inff() && fabsf(o.y) < __builtin_inff() && fabsf(o.z) < __builtin_inff() && fabsf(o.w) < __builtin_inff()))) {
+            const float4 first = o;
+            if (many) __syncthreads();
+            join(std::true_type{});
+            const auto pick = [&](const float x, const float y) { return fabsf(x) < __builtin_inff() ? x * inv : y * inv * 0x1p12f; };
+            o = make_float4(pick(first.x, o.x), pick(first.y, o.y), pick(first.z, o.z), pick(first.w, o.w));
+            inv = 1.f;
         }
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        if (many && wave != 0) return;
         if (lane < kLanes && e0 < a.dim) {
             char* const to = const_cast<char*>(a.o.at(row, head)) + e0 * sizeof(T);
             if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(to) = make_uint2(pack2((const T*)nullptr, o.x * inv, o.y * inv), pack2((const T*)nullptr, o.z * inv, o.w * inv));
