@@ -19,7 +19,7 @@
 namespace tbe {
 
 // Cosine and sine of a number of turns.  What is left after whole and quarter turns are taken off, at most an eighth of a turn, is rounded to
-// fp32 once (2^-25 of its value); the series end where the next term is below 2^-28 (sine) and 2^-32 (cosine).
+// fp32 once (by at most 2^-24 of its value); the series end where the next term is below 2^-28 (sine) and 2^-32 (cosine).
 __device__ __forceinline__ float2 cos_sin(double turns) {
     turns -= __builtin_rint(turns);
     const float quarters = rintf(4.f * (float)turns);
@@ -167,10 +167,9 @@ __global__ __launch_bounds__(kTurnThreads) void rotate_kernel(const TurnArgs a) 
         nb = a.dim - eb;
         na = na < 0 ? 0 : (na < kN ? na : kN);
         nb = nb < 0 ? 0 : (nb < kN ? nb : kN);
-        first = ea / 2;   // (of the first run; of the second: below)
         move_back(ea, na, again_a, 0, kN, true);
         move_back(eb, nb, again_b, 0, kN, true);
-        first = ea / 2;
+        first = ea / 2;   // (of the first run; of the second: below)
     } else {
         const int turning = (a.half + kN - 1) / kN;
         const bool turns = l < turning;
