@@ -430,7 +430,8 @@ tbe_status tbe_rotary_frequencies(int32_t rotary_dim, double base, tbe_rotary_sc
  *                  2^-126; 1 for zeros), and rounds x / scale to the nearest code, ties to even
  *   TBE_CODE_I8    codes are whole numbers -127 .. 127.  The scale is the largest magnitude / 127 rounded to fp32 (at least 2^-126; 1 for zeros), the
  *                  code the whole number nearest to x / scale, ties to even
- * A head with an element that is not finite gets codes 0 and the scale NaN: all of it reads as NaN.
+ * A head with an element that is not finite gets codes 0 and the scale NaN: all of it reads as NaN.  Where code * scale rounds beyond fp32's range, it reads as
+ * infinite: magnitudes from 248 2^120 on with e4m3, fp32's largest number itself with i8.
  *   k, v      DEVICE, codes [rows][heads][head_dim]: consecutive rows row_stride, consecutive heads head_stride bytes apart, 16-byte aligned, strides
  *             multiples of 16, row_stride < 2^22, both at least head_dim; where they are written no two heads share a byte, of k or v or
  *             of both (TBE_EINVAL); head_dim a multiple of 16, at most 128
@@ -458,7 +459,7 @@ tbe_status tbe_cache_read(const tbe_handle* h, const tbe_cache* cache, const voi
  * its k and v are not looked at; kv_heads, head_dim and k_rows are the cache's heads, head_dim and rows (TBE_ESHAPE), so head_dim is a multiple of 16.  dtype
  * is that of q and out.  Products are exact in q and the codes and added in fp32, scales are multiplied in fp32; a probability times its value's scale is
  * rounded to 16 bits, for TBE_IO_F32 not at all; results once when stored.  Values may be as large
- * as fp32's numbers; beside such that sums of them leave its range, those below 2^-86 may count as 0.  What is hidden is left out, scales and codes
+ * as fp32's numbers; beside such that sums of them leave its range, those below 2^-70 may lose their last bits or count as 0.  What is hidden is left out, scales and codes
  * that are not numbers among it; a scale that is infinite, and a score or its sum of products beyond fp32's range, may make NaN of what sees it. */
 tbe_status tbe_cache_attention_workspace_bytes(const tbe_handle* h, const tbe_attention_args* args, size_t* bytes);
 tbe_status tbe_cache_attention(const tbe_handle* h, const tbe_attention_args* args, const tbe_cache* cache, tbe_rows out, float* lse, void* workspace,

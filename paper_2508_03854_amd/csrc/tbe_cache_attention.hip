@@ -6,8 +6,8 @@
 // 2^-16 of themselves, for fp32 three, exactly.
 // Bound: long caches by reading the codes once, a few dozen queries each by the vector unit's work on scores and codes (360 instructions a tile of
 // 64 binary16 elements beside 16 matrix products), short caches by a wavefront's trips to memory.  Measured: one query to each of 24 caches of 2000 to
-// 65536 keys, 16 heads over 2 of 128, bfloat16 over e4m3, 0.41 GB: 90 us and 8 for the join, 4.6 TB/s in the former; 61 queries to each of 48 of 100 to
-// 4000, 8 heads of 64, binary16 over i8: 66 and 15; one to each of 32 of 12 on average, 4 heads of 32 fp32 with a bias: 9.5.
+// 65536 keys, 16 heads over 2 of 128, bfloat16 over e4m3, 0.41 GB: 92 us and 6.7 for the join, 4.5 TB/s in the former; 61 queries to each of 48 of 100 to
+// 4000, 8 heads of 64, binary16 over i8: 62 and 14; one to each of 32 of 12 on average, 4 heads of 32 fp32 with a bias: 10.6.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -201,7 +201,7 @@ struct PartWork {
 };
 
 // Wavefronts of a SIMD that the registers are to leave room for (and the LDS does): heads of 32 2 / 3 / 4, us, 24 caches of 34,000 on average, 16 heads over 2,
-// bfloat16 45 / 43 / 43, fp32 54 / 52 / 54;  of 64 61 / 62 / -, 73 / 81 / - (registers in scratch memory).
+// bfloat16 49 / 46 / 47, fp32 53 / 51 / 57;  of 64 2 / 3 62 / 63, 72 / 81 (registers in scratch memory).
 constexpr int cache_occupancy(const int D) { return D == 32 ? 3 : 2; }
 
 template <typename T, int D, bool I8, bool BIAS>
@@ -751,11 +751,14 @@ __global__ __launch_bounds__(256, many ? 4 : 8) void cache_attn_join_kernel(cons
 // 1024 74 / 61.
 // Evenly among 512 workgroups, two wavefronts a SIMD (heads of 32: 768); among 256 where the codes' conversions are the cheapest (e4m3 into bfloat16
 // products), heads have 128 elements and runs are long, since memory then bounds it and fewer streams serve it better: 512 / 256, us, 24 caches of
-// 34,000 on average, 16 heads over 2 of 128 bfloat16 102 / 100 (four queries each 112 / 107, with a bias 127 / 111), 64 of 2250, 32 heads over 8 89 / 86, 128 of 2048
-// 143 / 134;  but over i8 103 / 104, binary16 over i8 104 / 120, fp32 136 / 185, heads of 64 61 / 72, 8 of 2048 28 / 33 and 61 queries each to 48 of 2050, 8 heads of
-// 64, 79 / 98.
+// 34,000 on average, 16 heads over 2 of 128 bfloat16 102 / 100 (two queries each 104 / 101, four 111 / 105, with a bias 128 / 111), 64 of 2250, 32 heads over 8 93 / 89,
+// 128 of 2048 142 / 133;  but over i8 105 / 111, binary16 over i8 111 / 119, fp32 134 / 158, heads of 64 68 / 75, 8 of 2048 29 / 33 and 61 queries each to 48 of 1024,
+// 8 heads of 64, 54 / 63.
 // Many queries are shared out evenly too (on their own / evenly: 1024 to each of 4 of 4500, 16 heads over 4 of 128, 574 / 277 us; 2048 to one of 8000, 32 heads
 // over 8, 773 / 536; 2048 to each of 8 of 4000, 16 heads over 4 of 64, 832 / 699), as long as the parts' results take no more than some 0.5 GB.
+// What decides is the average, so that one cache that is far longer than the others of a batch of short ones is walked by one wavefront (for every head,
+// or heads side by side). On their own / evenly, us, 1000 of 240 of which one has 3000, 10,000, 60,000, 32 heads of 128 over 8: 165 / 173, 477 / 175, 2770 / 207;
+// 8 heads of 32 over 4: 87 / 49, 269 / 48, 1577 / 58.
 constexpr int64_t kMostEach = 4096;
 constexpr int64_t kRangeGroups = 512, kRangeGroupsLight = 256, kLongRun = 16;   // kLongRun: tiles
 CacheAttnPlan cache_attn_plan(const AttnShape& sh, const bool light, const int max_pack) {

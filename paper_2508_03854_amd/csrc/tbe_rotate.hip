@@ -7,8 +7,8 @@
 // in one lane, in either layout, so that nothing but the sum crosses lanes.  The turns are counted in 64 bits and reduced to an eighth of a turn
 // before they become fp32; a wavefront finds sine and cosine of its rows' pairs together, once for the heads that it has (every lane for its own pairs:
 // 322 us where this takes 288, gradients 365 / 268).  Measured: 131,071 rows of 16 and 4 heads of 128, bfloat16, normed: 270 us, 5.0 TB/s; gradients of 65,537 of
-// them, the weights' among them: 202 and 9 us; 60,001 rows of 16 heads of 80 fp32, 32 elements turned in neighbouring pairs: 137; 40,003 of 24 heads of 64
-// binary16, 24 turned, gradients: 60, 4.1 TB/s.
+// them, the weights' among them: 204 and 9 us; 60,001 rows of 16 heads of 80 fp32, 32 elements turned in neighbouring pairs: 137; 40,003 of 24 heads of 64
+// binary16, 24 turned, gradients: 55, 4.5 TB/s.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

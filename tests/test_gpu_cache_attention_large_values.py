@@ -134,3 +134,22 @@ def test_a_scale_that_is_not_a_number_among_them(tbe):
     got = run(tbe, s)
     assert bool(got[0][1:, :2].isnan().all()) and bool(got[0][0].isfinite().all()) and bool(got[0][1:, 2:].isfinite().all())
     assert bool(got[1].isfinite().all())
+
+
+def test_the_largest_numbers_read_as_infinite(tbe):
+    """A code times its scale beyond fp32: from halfway between 240 and 256 times 2^120 on with e4m3, with i8 for fp32's largest number alone, whose quotient
+    by 127 is rounded up."""
+    top = torch.finfo(torch.float32).max
+    x = torch.zeros(4, 1, 16, device="cuda")
+    x[:, 0, 3] = torch.tensor([top, 248 * 2.0 ** 120, 0.0, 0.0], device="cuda")
+    x[2, 0, 3] = torch.nextafter(x[1, 0, 3], torch.zeros((), device="cuda"))
+    x[3, 0, 3] = torch.nextafter(x[0, 0, 3], torch.zeros((), device="cuda"))
+    for code, want in ((E4M3, [math.inf, math.inf, 240 * 2.0 ** 120, math.inf]), (I8, [math.inf, None, None, None])):
+        c = tbe.alloc_cache(4, 1, 16, code)
+        slots = torch.arange(4, device="cuda")
+        tbe.cache_write(c, x, -x, slots)
+        k, v = tbe.cache_read(c, slots)
+        for i, w in enumerate(want):
+            got = k[i, 0, 3].item()
+            assert v[i, 0, 3].item() == -got and (got == w if w is not None else math.isfinite(got) and abs(got / x[i, 0, 3].item() - 1) < 2.0 ** -22)
+        assert bool((k[:, 0, 4:] == 0).all())
