@@ -458,9 +458,10 @@ tbe_status tbe_cache_read(const tbe_handle* h, const tbe_cache* cache, const voi
 /* Attention over such a cache: tbe_attention with k = the codes of cache->k times their scales, v likewise, none of which is written out.  args as there, but
  * its k and v are not looked at; kv_heads, head_dim and k_rows are the cache's heads, head_dim and rows (TBE_ESHAPE), so head_dim is a multiple of 16.  dtype
  * is that of q and out.  Products are exact in q and the codes and added in fp32, scales are multiplied in fp32; a probability times its value's scale is
- * rounded to 16 bits, for TBE_IO_F32 not at all; results once when stored.  Values may be as large
- * as fp32's numbers; beside such that sums of them leave its range, those below 2^-70 may lose their last bits or count as 0.  What is hidden is left out, scales and codes
- * that are not numbers among it; a scale that is infinite, and a score or its sum of products beyond fp32's range, may make NaN of what sees it. */
+ * rounded to 16 bits, for TBE_IO_F32 not at all; results once when stored.  Values may be as large as fp32's numbers and
+ * keep their accuracy down to 2^-90 (below, a product with a probability becomes a subnormal number); beside such that sums of them leave fp32's range, those below
+ * 2^-70 may lose their last bits or count as 0.  What is hidden is left out, scales and codes that are not numbers among it; a scale that is infinite, and
+ * a score or its sum of products beyond fp32's range, may make NaN of what sees it. */
 tbe_status tbe_cache_attention_workspace_bytes(const tbe_handle* h, const tbe_attention_args* args, size_t* bytes);
 tbe_status tbe_cache_attention(const tbe_handle* h, const tbe_attention_args* args, const tbe_cache* cache, tbe_rows out, float* lse, void* workspace,
                                size_t workspace_bytes, void* hip_stream);

@@ -153,3 +153,15 @@ def test_the_largest_numbers_read_as_infinite(tbe):
             got = k[i, 0, 3].item()
             assert v[i, 0, 3].item() == -got and (got == w if w is not None else math.isfinite(got) and abs(got / x[i, 0, 3].item() - 1) < 2.0 ** -22)
         assert bool((k[:, 0, 4:] == 0).all())
+
+
+@pytest.mark.parametrize("io", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("code", [E4M3, I8])
+def test_small_values_keep_their_accuracy(tbe, io, code):
+    """Values around 2^-90: probabilities of 2^-20 times them still have 24 bits above the last one of bfloat16's subnormal numbers, 2^-133."""
+    for nq, nk, H, K, dim in SHAPES + [([1], [60_000], 2, 1, 32)]:
+        s = build(tbe, gen(dim), nq, nk, nk, H, K, dim, io, code, poison=False)
+        fill(tbe, s, torch.randn(s["cache"].k.shape, generator=gen(1), device="cuda") * 2.0 ** -90)
+        got = run(tbe, s)
+        ref = reference(s["q"], values(s["cache"], "k"), values(s["cache"], "v"), nq, nk, s["k0"], causal=True, scale=dim ** -0.5)
+        check(got, ref, ("out", "lse"), f"{H}/{K} {dim} {nq}")
